@@ -225,7 +225,7 @@ def prepare(case, seed):
             s["opt"] = train.AdamW(s["params"], s["grads"], lr=h["lr"], betas=(h["b1"], h["b2"]), eps=h["eps"],
                                    weight_decay=s["wds"], state=case["state"], copies=s["copies"], seed=h["seed"])
             s["opt"].load_state(s["step"], **{k: s[k] for k in ("m", "v", "m_scale", "v_scale") if k in s})
-            s["opt"].coef.copy_(s["coef"])
+            s["opt"].coef.copy_(s["coef"][0])
     return s
 
 
