@@ -5,4 +5,4 @@ include/rotconv.h; `binding` is the thin ctypes layer over it and `synth` the
 seeded input generators.  Nothing is imported eagerly so that `synth` can be
 used on machines without the HIP runtime.
 """
-__all__ = ["binding", "synth"]
+__all__ = ["binding", "synth", "train"]

@@ -40,6 +40,17 @@ GLUE_EXPORTS = [
 # the bfloat16 twins: every call above except the two workspace-size queries
 GLUE_EXPORTS += [n + "_bf16" for n in GLUE_EXPORTS if not n.endswith("_workspace_bytes")]
 
+# include/unettrain.h
+TRAIN_EXPORTS = [
+    "train_groupnorm_workspace_bytes", "train_groupnorm_fwd", "train_groupnorm_bwd", "train_groupnorm_fwd_bf16",
+    "train_groupnorm_bwd_bf16",
+    "train_list_create", "train_list_destroy", "train_list_elements", "train_list_workspace_bytes",
+    "train_control_init", "train_grad_norm", "train_adamw_step",
+]
+ACTS = {"none": 0, "relu": 1, "silu": 2}
+NCHW, NHWC = 0, 1
+STATES = {"f32": 0, "mx8": 1}
+
 
 class Desc(ctypes.Structure):
     _fields_ = [
@@ -59,6 +70,22 @@ class PlanOptions(ctypes.Structure):
         ("bwd_lut", ctypes.c_int32), ("fwd_base", ctypes.c_int32), ("direct", ctypes.c_int32),
         ("direct_ty", ctypes.c_int32), ("px_fwd", ctypes.c_int32), ("bf16_parts", ctypes.c_int32),
         ("reserved", ctypes.c_int32 * 3),
+    ]
+
+
+class TrainTensor(ctypes.Structure):
+    """train_tensor: one parameter tensor of a list with its gradient."""
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("n", ctypes.c_uint64),
+        ("weight_decay", ctypes.c_float), ("reserved", ctypes.c_int32),
+    ]
+
+
+class TrainAdamW(ctypes.Structure):
+    """train_adamw: what an AdamW step keeps from step to step."""
+    _fields_ = [
+        ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_float), ("state", ctypes.c_int32),
+        ("seed", ctypes.c_uint32), ("reserved", ctypes.c_int32),
     ]
 
 
@@ -134,6 +161,22 @@ def lib():
         for name in GLUE_EXPORTS:
             if name.endswith("_bf16"):
                 getattr(L, name).argtypes = getattr(L, name[:-5]).argtypes
+        fp = ctypes.c_float
+        L.train_groupnorm_workspace_bytes.argtypes = [ci, ci, sz, ci]
+        L.train_groupnorm_workspace_bytes.restype = sz
+        L.train_groupnorm_fwd.argtypes = [vp] * 6 + [ci, ci, sz, ci, fp, ci, ci, vp, sz, vp]
+        L.train_groupnorm_bwd.argtypes = [vp] * 9 + [ci, ci, sz, ci, ci, ci, vp, sz, vp]
+        L.train_groupnorm_fwd_bf16.argtypes = L.train_groupnorm_fwd.argtypes
+        L.train_groupnorm_bwd_bf16.argtypes = L.train_groupnorm_bwd.argtypes
+        L.train_list_create.argtypes = [ctypes.POINTER(TrainTensor), ci, ci, ctypes.POINTER(vp)]
+        L.train_list_destroy.argtypes = [vp]
+        L.train_list_elements.argtypes = [vp]
+        L.train_list_elements.restype = ctypes.c_uint64
+        L.train_list_workspace_bytes.argtypes = [vp]
+        L.train_list_workspace_bytes.restype = sz
+        L.train_control_init.argtypes = [vp, ci, fp, vp]
+        L.train_grad_norm.argtypes = [vp, fp, vp, vp, vp, sz, vp]
+        L.train_adamw_step.argtypes = [vp, ctypes.POINTER(TrainAdamW), vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -442,3 +485,129 @@ def glue_softmax_ce(logits, labels, loss, dlogits, ws):
     P = logits.numel() // (N * K)
     _check(_glue("glue_softmax_ce", logits, dlogits)(_ptr(logits), _ptr(labels), _ptr(loss), _ptr(dlogits), N, K, P, _ptr(ws), _nbytes(ws),
                                  _stream()), "glue_softmax_ce")
+
+
+# ---- training operators (include/unettrain.h) ---------------------------------------------------
+
+def train_groupnorm_workspace_bytes(N, C, P, groups):
+    return int(lib().train_groupnorm_workspace_bytes(N, C, P, groups))
+
+
+def _map_layout(what, *maps):
+    """The order in memory that all maps [N, C, ...] of one call share: NCHW (contiguous), or channels last."""
+    import torch
+
+    if any(m.shape != maps[0].shape for m in maps):
+        raise ValueError(f"{what}: maps must have one shape, got {[tuple(m.shape) for m in maps]}")
+    if maps[0].dim() < 2:
+        raise ValueError(f"{what}: maps are [N, C, ...]")
+    if all(m.is_contiguous() for m in maps):
+        return NCHW
+    if maps[0].dim() == 4 and all(m.is_contiguous(memory_format=torch.channels_last) for m in maps):
+        return NHWC
+    raise ValueError(f"{what}: maps must be all contiguous or all channels last")
+
+
+def _check_f32(what, sizes, **tensors):
+    """Tensors of a call that are fp32 vectors of a known size (None passes)."""
+    import torch
+
+    for name, t in tensors.items():
+        if t is not None and (t.dtype != torch.float32 or t.numel() != sizes[name]):
+            raise ValueError(f"{what}: {name} must be float32 with {sizes[name]} elements")
+
+
+def _groupnorm_args(what, maps, groups, act, ws, **vectors):
+    layout = _map_layout(what, *maps)
+    N, C = maps[0].shape[0], maps[0].shape[1]
+    P = maps[0].numel() // max(1, N * C)
+    per = dict(gamma=C, beta=C, dgamma=C, dbeta=C, mean=N * groups, rstd=N * groups)
+    _check_f32(what, per, **vectors)
+    if act not in ACTS:
+        raise ValueError(f"{what}: act must be one of {sorted(ACTS)}")
+    if ws is None:
+        import torch
+
+        ws = torch.empty(max(256, train_groupnorm_workspace_bytes(N, C, P, groups)), dtype=torch.uint8, device=maps[0].device)
+    return N, C, P, layout, ws
+
+
+def train_groupnorm_fwd(x, gamma, beta, y, mean, rstd, groups, eps=1e-5, act="none", ws=None):
+    """x, y [N, C, ...], both contiguous or both channels last; gamma, beta [C] or None; mean, rstd [N, groups] or None."""
+    N, C, P, layout, ws = _groupnorm_args("train_groupnorm_fwd", (x, y), groups, act, ws, gamma=gamma, beta=beta, mean=mean,
+                                          rstd=rstd)
+    _check(_glue("train_groupnorm_fwd", x, y)(x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), N,
+                                              C, P, groups, eps, ACTS[act], layout, _ptr(ws), _nbytes(ws), _stream()),
+           "train_groupnorm_fwd")
+
+
+def train_groupnorm_bwd(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, groups, act="none", ws=None):
+    """x, dy, dx [N, C, ...] in one order; mean, rstd from the forward call; dgamma, dbeta [C] or None.  dx may be dy."""
+    N, C, P, layout, ws = _groupnorm_args("train_groupnorm_bwd", (x, dy, dx), groups, act, ws, gamma=gamma, beta=beta,
+                                          mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta)
+    _check(_glue("train_groupnorm_bwd", x, dy, dx)(x.data_ptr(), dy.data_ptr(), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd),
+                                                   dx.data_ptr(), _ptr(dgamma), _ptr(dbeta), N, C, P, groups, ACTS[act],
+                                                   layout, _ptr(ws), _nbytes(ws), _stream()), "train_groupnorm_bwd")
+
+
+class TrainList:
+    """Owns a train_list*: parameter tensors (or None, to measure gradients only) with their gradients, optional bf16
+    copies of the parameters and a weight decay for each.  Keeps the tensors alive, as the list holds their addresses."""
+
+    def __init__(self, grads, params=None, copies=None, weight_decay=0.0):
+        import torch
+
+        self._h = ctypes.c_void_p()
+        grads = list(grads)
+        k = len(grads)
+        params = [None] * k if params is None else list(params)
+        copies = [None] * k if copies is None else list(copies)
+        decay = [float(weight_decay)] * k if isinstance(weight_decay, (int, float)) else [float(w) for w in weight_decay]
+        if not (len(params) == len(copies) == len(decay) == k):
+            raise ValueError("TrainList: one parameter, gradient, copy and weight decay for each tensor")
+        kinds = {g.dtype for g in grads}
+        if len(kinds) > 1 or not kinds <= {torch.float32, torch.bfloat16}:
+            raise TypeError(f"TrainList: gradients must be all float32 or all bfloat16, got {sorted(map(str, kinds))}")
+        for p, g, c in zip(params, grads, copies):
+            if p is not None and (p.dtype != torch.float32 or p.shape != g.shape):
+                raise TypeError("TrainList: parameters must be float32 in the shape of their gradients")
+            if c is not None and (c.dtype != torch.bfloat16 or c.shape != g.shape):
+                raise TypeError("TrainList: copies must be bfloat16 in the shape of the gradients")
+        self.tensors = (params, grads, copies)
+        rows = (TrainTensor * max(1, k))(*[TrainTensor(_ptr(p), _ptr(g), _ptr(c), g.numel(), w, 0)
+                                           for p, g, c, w in zip(params, grads, copies, decay)])
+        _check(lib().train_list_create(rows, k, BF16 if kinds == {torch.bfloat16} else F32, ctypes.byref(self._h)),
+               "train_list_create")
+        self.count = k
+        self.elements = int(lib().train_list_elements(self._h))
+        self.workspace_bytes = int(lib().train_list_workspace_bytes(self._h))
+
+    def close(self):
+        if self._h:
+            lib().train_list_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @property
+    def handle(self):
+        return self._h
+
+
+def train_control_init(control, step=0, lr=0.0):
+    """control: 16 int32 on the device (train_control)."""
+    _check(lib().train_control_init(_ptr(control), int(step), float(lr), _stream()), "train_control_init")
+
+
+def train_grad_norm(tensors: TrainList, max_norm, norms, control, ws):
+    _check(lib().train_grad_norm(tensors.handle, max_norm, _ptr(norms), _ptr(control), _ptr(ws), _nbytes(ws), _stream()),
+           "train_grad_norm")
+
+
+def train_adamw_step(tensors: TrainList, options: TrainAdamW, m, v, m_scale, v_scale, control):
+    _check(lib().train_adamw_step(tensors.handle, ctypes.byref(options), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale),
+                                  _ptr(control), _stream()), "train_adamw_step")
