@@ -21,8 +21,8 @@ namespace {
 
 constexpr int kBlock = 32;             // elements that share a scale; a tensor's states start on multiples of it
 constexpr int kThreads = 256;
-constexpr uint32_t kMinChunk = 1024, kMaxChunk = 16384;   // elements of a chunk: one to sixteen per workgroup and lane group
 constexpr int kMaxGrid = 2048;         // workgroups of a launch: eight to a CU, and so few tickets that they cost nothing
+constexpr int kStaged = 4096;          // sums of chunks that the end of the norm holds in LDS
 
 struct Row {
   float* p;
@@ -66,20 +66,24 @@ __device__ __forceinline__ void load_g4(const uint16_t* g, float* v) {
   for (int k = 0; k < 4; ++k) v[k] = bf16_to_f32(a[k]);
 }
 
-// Whether this workgroup is the last of its launch to come here; what the others wrote before is then visible to it.
-// Every workgroup of the grid calls it exactly once.  The ticket is 0 again afterwards.
+// Whether this workgroup is the last of its launch to come here.  Every workgroup of the grid calls it exactly once; the
+// ticket is 0 again afterwards.  No fence: a release at device scope writes back an XCD's whole L2, and 2048 of them held
+// the norm of 31 M gradients at 153 us and their AdamW step at 495 us.  What the last workgroup reads of the others has
+// to go through memory by itself (store_shared, load_shared).
 __device__ __forceinline__ bool last_of_grid(uint32_t* ticket) {
   __shared__ uint32_t mine;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's stores have arrived
   __syncthreads();
   if (threadIdx.x == 0) {
-    __threadfence();
-    mine = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    mine = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (mine == gridDim.x - 1) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __threadfence();
   }
   __syncthreads();
   return mine == gridDim.x - 1;
 }
+// one value through memory, past the caches that XCDs do not share
+__device__ __forceinline__ void store_shared(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ double load_shared(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 __device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
@@ -99,12 +103,14 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 }
 
 // Squares are added in 64 bits: no gradient is so large or so small that its square is lost, and a NaN or an infinity
-// stays one.
+// stays one.  The last workgroup adds the chunks' sums from LDS, sixteen lanes a tensor (a wave a tensor, each sum from
+// memory where another XCD left it: 56 us for 31 M gradients, most of it here).
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_grad_norm(const Row* __restrict__ rows, const Chunk* __restrict__ chunks,
                                                         uint32_t nchunks, uint32_t chunk, int count, float max_norm,
                                                         float* __restrict__ norms, train_control* ctl, double* part) {
   __shared__ double red[kThreads / 64];
+  __shared__ double sums[kStaged];
   for (uint32_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
     const Chunk ch = chunks[c];
     const Row& r = rows[ch.row];
@@ -114,28 +120,44 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const Row* __restrict__ 
     g += at;
     double s = 0;
     const uint32_t nv = r.vec ? n / 4 : 0;
-    for (uint32_t i = threadIdx.x; i < nv; i += kThreads) {
+    uint32_t i = threadIdx.x;
+    for (; i + 7 * kThreads < nv; i += 8 * kThreads) {       // eight loads in flight
+      float v[8][4];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) load_g4(g + 4 * (i + u * kThreads), v[u]);
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s += (double)v[u][k] * v[u][k];
+    }
+    for (; i < nv; i += kThreads) {
       float v[4];
       load_g4(g + 4 * i, v);
 #pragma unroll
       for (int k = 0; k < 4; ++k) s += (double)v[k] * v[k];
     }
-    for (uint32_t i = 4 * nv + threadIdx.x; i < n; i += kThreads) {
+    for (i = 4 * nv + threadIdx.x; i < n; i += kThreads) {
       const double v = Elt<T>::ld(g + i);
       s += v * v;
     }
     s = block_sum(s, red);
-    if (threadIdx.x == 0) part[c] = s;
+    if (threadIdx.x == 0) store_shared(part + c, s);
   }
   if (!last_of_grid(&ctl->ticket[0])) return;
-  // a wave takes a tensor at a time: its lanes the tensor's chunks in turn
+  const bool staged = nchunks <= (uint32_t)kStaged;
+  if (staged) {
+    for (uint32_t c = threadIdx.x; c < nchunks; c += kThreads) sums[c] = load_shared(part + c);
+    __syncthreads();
+  }
   double total = 0;
-  for (int k = threadIdx.x / 64; k < count; k += kThreads / 64) {
+  const int lane = threadIdx.x % 16;
+  for (int k = threadIdx.x / 16; k < count; k += kThreads / 16) {
     const uint32_t c0 = rows[k].first_chunk, nc = rows[k].chunks;
     double s = 0;
-    for (uint32_t c = threadIdx.x % 64; c < nc; c += 64) s += part[c0 + c];
-    s = wave_sum(s);
-    if (threadIdx.x % 64 == 0) {
+    for (uint32_t c = lane; c < nc; c += 16) s += staged ? sums[c0 + c] : load_shared(part + c0 + c);
+#pragma unroll
+    for (int m = 8; m > 0; m >>= 1) s += __shfl_xor(s, m);
+    if (lane == 0) {
       if (norms) norms[k] = (float)sqrt(s);
       total += s;
     }
@@ -356,10 +378,11 @@ int train_list_create(const train_tensor* tensors, int count, int grad_dtype, tr
       return ROTCONV_ERR_UNSUPPORTED;
     total += (t.n + kBlock - 1) / kBlock * kBlock;
   }
-  // chunks so large that a launch's workgroups get one or a few each, from 1024 elements (below, a workgroup has idle
-  // lanes) to 16384 (above, the last ones to end leave CUs idle)
-  uint64_t chunk = kMinChunk;
-  while (chunk < kMaxChunk && total / chunk > (uint64_t)kMaxGrid) chunk *= 2;
+  // A chunk has at least 1024 elements (fewer leave lanes idle).  Beyond one chunk for each workgroup of a full launch it
+  // grows to 16384 (larger ones leave CUs idle at the end), and further only where there would be more than four times
+  // the sums that the end of the norm holds in LDS.
+  uint64_t chunk = 1024;
+  while ((chunk < 16384 && total / chunk > (uint64_t)kMaxGrid) || total / chunk > 4ull * kStaged) chunk *= 2;
   uint64_t nchunks = 0;
   for (int k = 0; k < count; ++k) nchunks += (tensors[k].n + chunk - 1) / chunk;
   if (nchunks > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
