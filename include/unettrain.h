@@ -57,6 +57,11 @@ int train_groupnorm_bwd_bf16(const uint16_t* x, const uint16_t* dy, const float*
                              int C, size_t P, int groups, int act, int layout, void* ws, size_t ws_bytes,
                              void* stream);
 
+/* Workgroups that share a group wait for one another's sums, at most this many ticks of 10 ns (10000 at first) from then
+ * on, and compute what has not arrived themselves: same bits, more reads.  Returns the number before.  For the whole
+ * process; results do not depend on it. */
+int train_diag_groupnorm_wait(int ticks);
+
 /* ---- many tensors at once -----------------------------------------------------------------------
  * A list names parameter tensors with their gradients.  It holds their addresses, not their values: the
  * caller keeps the memory in place for as long as the list is used and creates another list where it moves. */

@@ -43,7 +43,7 @@ GLUE_EXPORTS += [n + "_bf16" for n in GLUE_EXPORTS if not n.endswith("_workspace
 # include/unettrain.h
 TRAIN_EXPORTS = [
     "train_groupnorm_workspace_bytes", "train_groupnorm_fwd", "train_groupnorm_bwd", "train_groupnorm_fwd_bf16",
-    "train_groupnorm_bwd_bf16",
+    "train_groupnorm_bwd_bf16", "train_diag_groupnorm_wait",
     "train_list_create", "train_list_destroy", "train_list_elements", "train_list_workspace_bytes",
     "train_control_init", "train_grad_norm", "train_adamw_step",
 ]
@@ -168,6 +168,7 @@ def lib():
         L.train_groupnorm_bwd.argtypes = [vp] * 9 + [ci, ci, sz, ci, ci, ci, vp, sz, vp]
         L.train_groupnorm_fwd_bf16.argtypes = L.train_groupnorm_fwd.argtypes
         L.train_groupnorm_bwd_bf16.argtypes = L.train_groupnorm_bwd.argtypes
+        L.train_diag_groupnorm_wait.argtypes = [ci]
         L.train_list_create.argtypes = [ctypes.POINTER(TrainTensor), ci, ci, ctypes.POINTER(vp)]
         L.train_list_destroy.argtypes = [vp]
         L.train_list_elements.argtypes = [vp]
@@ -548,6 +549,11 @@ def train_groupnorm_bwd(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, group
     _check(_glue("train_groupnorm_bwd", x, dy, dx)(x.data_ptr(), dy.data_ptr(), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd),
                                                    dx.data_ptr(), _ptr(dgamma), _ptr(dbeta), N, C, P, groups, ACTS[act],
                                                    layout, _ptr(ws), _nbytes(ws), _stream()), "train_groupnorm_bwd")
+
+
+def train_diag_groupnorm_wait(ticks: int) -> int:
+    """Longest wait (in 10 ns) of a group norm's workgroups for one another; returns the one before."""
+    return int(lib().train_diag_groupnorm_wait(int(ticks)))
 
 
 class TrainList:

@@ -22,7 +22,7 @@ namespace {
 constexpr int kBlock = 32;             // elements that share a scale; a tensor's states start on multiples of it
 constexpr int kThreads = 256;
 constexpr int kMaxGrid = 2048;         // workgroups of a launch: eight to a CU, and so few tickets that they cost nothing
-constexpr int kStaged = 4096;          // sums of chunks that the end of the norm holds in LDS
+constexpr int kStaged = 2048;          // sums of chunks that the end of the norm holds in LDS
 
 struct Row {
   float* p;
@@ -379,10 +379,10 @@ int train_list_create(const train_tensor* tensors, int count, int grad_dtype, tr
     total += (t.n + kBlock - 1) / kBlock * kBlock;
   }
   // A chunk has at least 1024 elements (fewer leave lanes idle).  Beyond one chunk for each workgroup of a full launch it
-  // grows to 16384 (larger ones leave CUs idle at the end), and further only where there would be more than four times
+  // grows to 16384 (larger ones leave CUs idle at the end), and further only where there would be more than eight times
   // the sums that the end of the norm holds in LDS.
   uint64_t chunk = 1024;
-  while ((chunk < 16384 && total / chunk > (uint64_t)kMaxGrid) || total / chunk > 4ull * kStaged) chunk *= 2;
+  while ((chunk < 16384 && total / chunk > (uint64_t)kMaxGrid) || total / chunk > 8ull * kStaged) chunk *= 2;
   uint64_t nchunks = 0;
   for (int k = 0; k < count; ++k) nchunks += (tensors[k].n + chunk - 1) / chunk;
   if (nchunks > 0x7fffffffu) return ROTCONV_ERR_SHAPE;

@@ -1,11 +1,20 @@
 // Group normalisation with an activation, forward and backward (see include/unettrain.h).
 //
-// Three launches each way: sums of every channel of every image in pieces, the groups' statistics from them, and the map.
-// A piece's forward sums are its mean and its squared deviations from that mean, joined pairwise-exactly (never as
-// sum x^2 - mean^2, which loses the variance of a map far from zero).
+// A workgroup takes a part of one group's map (NCHW) or of a run of whole groups' channels (channels last) into
+// registers, sums it, and normalises it from there, so that the map is read once and written once: HBM bound.  Where a
+// group needs more than one workgroup, these exchange their sums through memory (one 8-byte slot each) and wait for one
+// another; a group that needs too many for that is done in three launches instead (sums, their join, the map again).
+//
+// The wait is bounded and never needed for the result: a workgroup whose neighbours have not answered in time sums
+// their parts itself, in the same order with the same bits.  So the kernel ends whatever else runs on the device and in
+// whatever order its workgroups start.
+//
+// A part's forward sums are its mean and the squared deviations from it, taken from deviations from the part's first
+// element and joined by the means' distances (never sum x^2 - mean^2, which loses the variance of a map far from zero).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -16,19 +25,75 @@
 namespace rotconv {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512, kWaves = kThreads / 64;
+constexpr int kMaxTeam = kThreads / 4;       // channels that a workgroup holds at once (NCHW), four lanes each at least
+constexpr int kMaxSplit = 256;               // workgroups that wait for one another, at most
+constexpr int kMaxRun = 1024;                // channels of a run (channels last)
+constexpr int kMaxSlots = 2048;              // sums that a workgroup collects (channels last: of every group of its run)
 
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
 
-struct Gn {
-  int N, C, G, cg;
-  size_t P;
-  float eps;
-  int act;
-  int pieces;            // of a channel's pixels
-  size_t step;           // pixels of a piece, the last one's are fewer
+// ---- elements -------------------------------------------------------------------------------------
+typedef uint32_t u4a __attribute__((ext_vector_type(4), aligned(2)));     // global memory takes any alignment
+typedef uint32_t u2a __attribute__((ext_vector_type(2), aligned(2)));
+typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+typedef float fl2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {          // nearest even, NaN stays NaN
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(fl2{a, b}, bf2));
+}
+
+// V neighbouring elements as they lie in memory
+template <typename E, int V> struct Raw;
+template <int V> struct Raw<float, V> {
+  static_assert(V == 4 || V == 1, "");
+  uint32_t w[V];
+  __device__ __forceinline__ void load(const float* p) {
+    if constexpr (V == 4) {
+      const u4a a = *reinterpret_cast<const u4a*>(p);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = a[k];
+    } else {
+      w[0] = __float_as_uint(*p);
+    }
+  }
+  __device__ __forceinline__ float get(int k) const { return __uint_as_float(w[k]); }
+  static __device__ __forceinline__ void store(float* p, const float* v) {
+    if constexpr (V == 4) {
+      *reinterpret_cast<u4a*>(p) = u4a{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+      *p = v[0];
+    }
+  }
+};
+template <int V> struct Raw<uint16_t, V> {
+  static_assert(V == 8 || V == 4 || V == 1, "");
+  uint32_t w[(V + 1) / 2];
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    if constexpr (V == 8) {
+      const u4a a = *reinterpret_cast<const u4a*>(p);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) w[k] = a[k];
+    } else if constexpr (V == 4) {
+      const u2a a = *reinterpret_cast<const u2a*>(p);
+      w[0] = a[0], w[1] = a[1];
+    } else {
+      w[0] = *p;
+    }
+  }
+  __device__ __forceinline__ float get(int k) const { return __uint_as_float(k % 2 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16); }
+  static __device__ __forceinline__ void store(uint16_t* p, const float* v) {
+    if constexpr (V == 8) {
+      *reinterpret_cast<u4a*>(p) = u4a{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+    } else if constexpr (V == 4) {
+      *reinterpret_cast<u2a*>(p) = u2a{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    } else {
+      *p = (uint16_t)pack_bf16(v[0], v[0]);
+    }
+  }
 };
 
+// ---- the formula ----------------------------------------------------------------------------------
 __device__ __forceinline__ float normalised(float x, float mean, float rstd) {
 #pragma clang fp contract(off)
   return (x - mean) * rstd;
@@ -37,76 +102,628 @@ __device__ __forceinline__ float affine(float xh, float gamma, float beta) {
 #pragma clang fp contract(off)
   return xh * gamma + beta;
 }
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 __device__ __forceinline__ float activate(float z, int act) {
   if (act == TRAIN_ACT_RELU) return z <= 0.f ? 0.f : z;
-  if (act == TRAIN_ACT_SILU) return z * (1.f / (1.f + expf(-z)));
+  if (act == TRAIN_ACT_SILU) return z * sigmoid(z);
   return z;
 }
 __device__ __forceinline__ float through(float dy, float z, int act) {      // dy * act'(z)
   if (act == TRAIN_ACT_RELU) return z > 0.f ? dy : 0.f;
   if (act == TRAIN_ACT_SILU) {
-    const float s = 1.f / (1.f + expf(-z));
+    const float s = sigmoid(z);
     return dy * (s * (1.f + z * (1.f - s)));
   }
   return dy;
 }
 
-struct Part {            // of a piece: forward (mean, squared deviations from it); backward (sum dz, sum dz * xh)
+// ---- sums -----------------------------------------------------------------------------------------
+struct Pair {            // forward: mean, squared deviations from it; backward: sum of dz (or t), sum of dz * xh (or t * xh)
   float a, b;
 };
 
+__device__ __forceinline__ float lanes_sum(float v, int width) {      // over aligned runs of `width` lanes, a power of two
+  for (int m = width / 2; m > 0; m >>= 1) v += __shfl_xor(v, m);
+  return v;
+}
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
   return v;
 }
 
-// One wave a piece of one channel of one image; pixels `stride` elements apart.
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_gn_fwd_parts(const T* __restrict__ x, Part* __restrict__ part, Gn q, int nhwc) {
-  const size_t piece = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-  if (piece >= (size_t)q.N * q.C * q.pieces) return;
-  const size_t row = piece / q.pieces, n = row / q.C, c = row % q.C;
-  const size_t p0 = piece % q.pieces * q.step, p1 = min(q.P, p0 + q.step);
-  const size_t stride = nhwc ? q.C : 1;
-  const T* xp = x + (nhwc ? n * q.P * q.C + c : row * q.P);
-  // deviations from the first pixel keep the sums small beside a large mean
-  const float first = Elt<T>::ld(xp + p0 * stride);
-  float s = 0.f, s2 = 0.f;
-  for (size_t p = p0 + threadIdx.x % 64; p < p1; p += 64) {
-    const float d = Elt<T>::ld(xp + p * stride) - first;
-    s += d;
-    s2 += d * d;
+// Mean and squared deviations of `count` parts of size(i) elements, `total` together.  By one wave; the same in all lanes.
+template <typename Get, typename Size>
+__device__ __forceinline__ Pair join(int count, float total, Get get, Size size) {
+  const float ref = get(0).a;
+  float s = 0.f;
+  for (int i = threadIdx.x % 64; i < count; i += 64) s += size(i) * (get(i).a - ref);
+  const float mean = ref + wave_sum(s) / total;
+  s = 0.f;
+  for (int i = threadIdx.x % 64; i < count; i += 64) {
+    const Pair p = get(i);
+    const float d = p.a - mean;
+    s += p.b + size(i) * (d * d);
   }
-  s = wave_sum(s);
-  s2 = wave_sum(s2);
-  const float d = s / (float)(p1 - p0);
-  if (threadIdx.x % 64 == 0) part[piece] = Part{first + d, s2 - s * d};
+  return Pair{mean, wave_sum(s)};
+}
+template <typename Get>
+__device__ __forceinline__ Pair add(int count, Get get) {
+  float a = 0.f, b = 0.f;
+  for (int i = threadIdx.x % 64; i < count; i += 64) {
+    const Pair p = get(i);
+    a += p.a, b += p.b;
+  }
+  return Pair{wave_sum(a), wave_sum(b)};
 }
 
+// ---- exchange -------------------------------------------------------------------------------------
+// A slot is empty (all ones) until its owner writes it; a NaN is written in one fixed form, so that it never looks empty.
+// Who sums a neighbour's part itself looks at its slot again afterwards: still empty, the neighbour had not begun to write
+// its map (which may overwrite the dy that was read); not empty, the slot's value is the one to take.
+constexpr unsigned long long kEmpty = ~0ull;
+__device__ __forceinline__ uint32_t plain_bits(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
+__device__ __forceinline__ void put(unsigned long long* slot, Pair p) {
+  const unsigned long long v = (unsigned long long)plain_bits(p.b) << 32 | plain_bits(p.a);
+  __hip_atomic_store(slot, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // it has arrived before this workgroup writes any of its map
+}
+// The value of a slot, waiting until `deadline` (of the constant clock); false: still empty
+__device__ __forceinline__ bool get(const unsigned long long* slot, long long deadline, Pair* p) {
+  for (;;) {
+    const unsigned long long v = __hip_atomic_load(slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (v != kEmpty) {
+      *p = Pair{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
+      return true;
+    }
+    if ((long long)wall_clock64() >= deadline) return false;
+    __builtin_amdgcn_s_sleep(8);
+  }
+}
+__global__ __launch_bounds__(256) void k_gn_empty(unsigned long long* slots, int n) {
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) slots[i] = kEmpty;
+}
+
+// Makes the compiler forget what it knows of a register: the map then starts from the elements as loaded, instead of from
+// every intermediate value of the sums kept alive across the wait (twice the registers, and spills).
+__device__ __forceinline__ void forget(uint32_t& v) { asm volatile("" : "+v"(v)); }
+template <typename R, int J>
+__device__ __forceinline__ void forget(R (&r)[J]) {
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (unsigned k = 0; k < sizeof(r[j].w) / 4; ++k) forget(r[j].w[k]);
+}
+
+enum Mode { kFused, kSums, kMap };
+
+struct Gn {
+  // the problem
+  int N, C, G, cg;
+  size_t P;
+  float eps;
+  int act;
+  // how it is cut: `split` workgroups for each group (NCHW) or run of channels (channels last)
+  int mode, split, vec, per;           // per: vectors that a lane holds of each map
+  int team, pieces;                    // NCHW: lanes of a channel's piece, pieces of a channel
+  size_t step;                         // NCHW: pixels of a piece (the last may have fewer)
+  int one;                             // channels last: a vector's channels are of one group
+  int run, runs, rows;                 // channels last: channels of a run, runs, pixels that a workgroup holds at once
+  int wait;                            // ticks (10 ns) before a workgroup does without its neighbours
+};
+struct Maps {
+  const void *x, *dy;
+  void* out;                           // y or dx
+  const float *gamma, *beta;
+  float *mean, *rstd;                  // written forward (or NULL), read backward
+  Pair* part;                          // see parts_of
+  unsigned long long* slots;
+  const float2* stat;                  // kMap: mean and rstd forward, the two means of the gradient backward
+};
+
+// ---- NCHW -----------------------------------------------------------------------------------------
+// A team of lanes (4 to 64, or the workgroup) holds one piece of one channel, `per` vectors a lane and the elements
+// beyond the last whole vector one a lane.  Unit u of a group is piece u % pieces of channel u / pieces; workgroup k
+// holds the units from k * (512 / team) on.
+template <typename E, int V, int J, bool BWD>
+struct Nchw {
+  const Gn& q;
+  const Maps& m;
+  size_t group;          // n * G + g
+  int lane, unit0;       // of this lane's team in workgroup 0
+  // what a workgroup holds: the first unit's address (the same for all lanes), a lane's offset from there
+  size_t base = 0;
+  uint32_t off = 0;
+  Raw<E, V> x[J], dy[BWD ? J : 1];
+  float x1 = 0.f, dy1 = 0.f;
+  int c = 0, len = 0;    // len 0: a team without a unit
+
+  __device__ __forceinline__ Nchw(const Gn& q_, const Maps& m_, size_t group_) : q(q_), m(m_), group(group_) {
+    lane = threadIdx.x % q.team;
+    unit0 = threadIdx.x / q.team;
+  }
+  __device__ __forceinline__ int units() const { return q.cg * q.pieces; }
+  __device__ __forceinline__ int teams() const { return kThreads / q.team; }
+  __device__ __forceinline__ bool has(int j) const { return (lane + j * q.team) * V + V <= len; }
+  __device__ __forceinline__ bool has_tail() const { return V > 1 && lane < len % V; }
+  __device__ __forceinline__ uint32_t at(int j) const { return off + (uint32_t)(lane + j * q.team) * V; }
+  __device__ __forceinline__ uint32_t at_tail() const { return off + (uint32_t)(len - len % V + lane); }
+  __device__ __forceinline__ void take(int k) {
+    const int u0 = k * teams(), cl0 = u0 / q.pieces, piece = u0 % q.pieces;      // one piece, or pieces == 1
+    base = (group * q.cg + cl0) * q.P + piece * q.step;
+    const bool active = u0 + unit0 < units();
+    const int cl = active ? unit0 : 0;
+    c = (int)(group % q.G) * q.cg + cl0 + cl;
+    len = active ? (int)min(q.step, q.P - piece * q.step) : 0;
+    off = (uint32_t)cl * (uint32_t)q.P;                                          // less than 512 * per * V
+    const E* xp = static_cast<const E*>(m.x) + base;
+    const E* dp = static_cast<const E*>(m.dy) + base;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (has(j)) {
+        x[j].load(xp + at(j));
+        if (BWD) dy[j].load(dp + at(j));
+      }
+    if (has_tail()) {
+      x1 = Elt<E>::ld(xp + at_tail());
+      if (BWD) dy1 = Elt<E>::ld(dp + at_tail());
+    }
+  }
+  __device__ __forceinline__ float gamma() const { return m.gamma ? m.gamma[c] : 1.f; }
+  __device__ __forceinline__ float beta() const { return m.beta ? m.beta[c] : 0.f; }
+  // elements of workgroup k's part
+  __device__ __forceinline__ float size(int k) const {
+    if (q.pieces > 1) return (float)min(q.step, q.P - (k % q.pieces) * q.step);
+    return (float)min(teams(), units() - k * teams()) * (float)q.P;
+  }
+  // sums of what this workgroup holds, in all lanes.  Ends with a barrier behind every use of `red`.
+  __device__ __forceinline__ Pair sums(Pair* red, int k, bool keep) {
+    float s = 0.f, s2 = 0.f, first = 0.f;
+    if (!BWD) {
+      if (len) first = Elt<E>::ld(static_cast<const E*>(m.x) + base + off);
+      auto one = [&](float xv) {
+        const float d = xv - first;
+        s += d;
+        s2 += d * d;
+      };
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j))
+#pragma unroll
+          for (int e = 0; e < V; ++e) one(x[j].get(e));
+      if (has_tail()) one(x1);
+    } else {
+      const float mu = m.mean[group], r = m.rstd[group], ga = gamma(), be = beta();
+      auto one = [&](float xv, float dv) {
+        const float xh = normalised(xv, mu, r), dz = through(dv, affine(xh, ga, be), q.act);
+        s += dz;
+        s2 += dz * xh;
+      };
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j))
+#pragma unroll
+          for (int e = 0; e < V; ++e) one(x[j].get(e), dy[j].get(e));
+      if (has_tail()) one(x1, dy1);
+    }
+    const int width = min(q.team, 64);
+    s = lanes_sum(s, width);
+    s2 = lanes_sum(s2, width);
+    if (q.team > 64) {                        // one unit: its eight waves' sums belong to the same first element
+      if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = Pair{s, s2};
+      __syncthreads();
+      s = s2 = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) s += red[w].a, s2 += red[w].b;
+      __syncthreads();
+    }
+    Pair p;
+    if (BWD) {
+      if (keep && len && lane == 0) m.part[group * q.cg * q.pieces + k * teams() + unit0] = Pair{s, s2};
+      const float ga = gamma();
+      p = Pair{s * ga, s2 * ga};
+    } else {
+      const float d = s / (float)max(len, 1);
+      p = Pair{first + d, s2 - s * d};
+    }
+    if (q.team > 64) return p;
+    if (len && lane == 0) red[unit0] = p;
+    __syncthreads();
+    const int count = min(teams(), units() - k * teams());
+    if (BWD) {
+      p = add(count, [&](int i) { return red[i]; });
+    } else {
+      const float each = (float)q.P;
+      p = join(count, each * (float)count, [&](int i) { return red[i]; }, [&](int) { return each; });
+    }
+    __syncthreads();
+    return p;
+  }
+  __device__ __forceinline__ void map(float a, float b) {
+    forget(x);
+    if (BWD) forget(dy);
+    E* op = static_cast<E*>(m.out) + base;
+    const float ga = gamma(), be = beta();
+    if (!BWD) {
+      auto one = [&](float xv) { return activate(affine(normalised(xv, a, b), ga, be), q.act); };
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j)) {
+          float v[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = one(x[j].get(e));
+          Raw<E, V>::store(op + at(j), v);
+        }
+      if (has_tail()) Elt<E>::st(op + at_tail(), one(x1));
+    } else {
+      const float mu = m.mean[group], r = m.rstd[group];
+      auto one = [&](float xv, float dv) {
+        const float xh = normalised(xv, mu, r);
+        return r * (through(dv, affine(xh, ga, be), q.act) * ga - a - xh * b);
+      };
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j)) {
+          float v[V];
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = one(x[j].get(e), dy[j].get(e));
+          Raw<E, V>::store(op + at(j), v);
+        }
+      if (has_tail()) Elt<E>::st(op + at_tail(), one(x1, dy1));
+    }
+  }
+};
+
+constexpr uint32_t kMissing = 0xffffffffu;      // in a Pair's first value: put() never writes it
+
+template <typename E, int V, int J, bool BWD>
+__global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m) {
+  __shared__ Pair red[kMaxTeam];
+  __shared__ Pair all[kMaxSplit];
+  __shared__ int missing;
+  const size_t group = blockIdx.x / q.split;
+  const int k = blockIdx.x % q.split;
+  const float M = (float)q.cg * (float)q.P;
+  Nchw<E, V, J, BWD> w(q, m, group);
+  Pair p;
+  // Once, but for a workgroup whose neighbours have not answered in time: that takes their parts, and then its own again.
+  int part = k;
+  for (bool asked = false;;) {
+    w.take(part);
+    if (q.mode == kMap) {
+      p = Pair{m.stat[group].x, m.stat[group].y};
+      break;
+    }
+    p = w.sums(red, part, !asked);
+    if (q.mode == kSums) {
+      if (!BWD && threadIdx.x == 0) m.part[blockIdx.x] = p;
+      return;
+    }
+    if (q.split == 1) break;
+    if (!asked) {
+      asked = true;
+      unsigned long long* slots = m.slots + group * q.split;
+      if (threadIdx.x == 0) {
+        missing = 0;
+        put(slots + k, p);
+      }
+      __syncthreads();
+      const long long deadline = (long long)wall_clock64() + q.wait;
+      for (int i = threadIdx.x; i < q.split; i += kThreads) {
+        Pair o = p;
+        if (i != k && !get(slots + i, deadline, &o)) missing = 1, o.a = __uint_as_float(kMissing);
+        all[i] = o;
+      }
+      __syncthreads();
+      if (!missing) break;
+    } else {
+      if (part == k) break;
+      if (threadIdx.x == 0) {
+        Pair o;
+        all[part] = get(m.slots + group * q.split + part, 0, &o) ? o : p;
+      }
+      __syncthreads();
+    }
+    // the next part that is missing, the same for every lane
+    part = 0;
+    while (part < q.split && __float_as_uint(all[part].a) != kMissing) ++part;
+    if (part == q.split) part = k;
+  }
+  if (q.mode == kFused) {
+    if (q.split > 1) {
+      if (BWD) p = add(q.split, [&](int i) { return all[i]; });
+      else p = join(q.split, M, [&](int i) { return all[i]; }, [&](int i) { return w.size(i); });
+    }
+    if (BWD) {
+      p = Pair{p.a / M, p.b / M};
+    } else {
+      p.b = 1.f / sqrtf(p.b / M + q.eps);
+      if (k == 0 && threadIdx.x == 0) {
+        if (m.mean) m.mean[group] = p.a;
+        if (m.rstd) m.rstd[group] = p.b;
+      }
+    }
+  }
+  w.map(p.a, p.b);
+}
+
+// ---- channels last --------------------------------------------------------------------------------
+// A workgroup holds q.rows * J pixels of a run of channels; a lane the same V channels of each of its J pixels.  ONE: these
+// are of one group, whose statistics a lane then holds once.
+template <typename E, int V, int J, bool ONE, bool BWD>
+struct Nhwc {
+  static constexpr int S = ONE ? 1 : V;
+  const Gn& q;
+  const Maps& m;
+  size_t n;
+  int c0;                // first channel of the run
+  int width;             // channels of the run that exist
+  int c, row;            // this lane's first channel, within the run; its row
+  bool in;
+  // what a workgroup holds: its first pixel's address (the same for all lanes), its pixels
+  size_t base = 0;
+  int left = 0;
+  Raw<E, V> x[J], dy[BWD ? J : 1];
+
+  __device__ __forceinline__ Nhwc(const Gn& q_, const Maps& m_, size_t n_, int run) : q(q_), m(m_), n(n_) {
+    c0 = run * q.run;
+    width = min(q.run, q.C - c0);
+    const int cols = q.run / V;
+    c = (int)(threadIdx.x % cols) * V;
+    row = (int)(threadIdx.x / cols);
+    in = row < q.rows && c < width;
+  }
+  __device__ __forceinline__ bool has(int j) const { return in && j * q.rows + row < left; }
+  __device__ __forceinline__ uint32_t at(int j) const { return (uint32_t)(j * q.rows + row) * (uint32_t)q.C + (uint32_t)c; }
+  __device__ __forceinline__ float count(int k) const {
+    const size_t all = (size_t)q.rows * J;
+    return (float)min(all, q.P - k * all);
+  }
+  __device__ __forceinline__ void take(int k) {
+    const size_t p0 = (size_t)k * q.rows * J;
+    base = (n * q.P + p0) * q.C + c0;
+    left = (int)min((size_t)q.rows * J, q.P - p0);
+    const E* xp = static_cast<const E*>(m.x) + base;
+    const E* dp = static_cast<const E*>(m.dy) + base;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (has(j)) {
+        x[j].load(xp + at(j));
+        if (BWD) dy[j].load(dp + at(j));
+      }
+  }
+  __device__ __forceinline__ size_t group(int e) const { return n * q.G + (c0 + min(c + e, width - 1)) / q.cg; }
+  struct Scale {
+    float ga[V], be[V], mean[S], rstd[S];
+  };
+  __device__ __forceinline__ Scale scale() const {
+    Scale s;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      s.ga[e] = m.gamma && in ? m.gamma[c0 + c + e] : 1.f;
+      s.be[e] = m.beta && in ? m.beta[c0 + c + e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < S; ++e) s.mean[e] = BWD ? m.mean[group(e)] : 0.f, s.rstd[e] = BWD ? m.rstd[group(e)] : 0.f;
+    return s;
+  }
+
+  // Sums of every channel of the run over this workgroup's pixels, left in out[0 .. width).  buf: kThreads * V pairs.
+  __device__ __forceinline__ void sums(Pair* buf, Pair* out, int k) {
+    float s[V], s2[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = s2[e] = 0.f;
+    if (!BWD) {
+      Raw<E, V> first = {};
+      if (in) first.load(static_cast<const E*>(m.x) + base + c);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j))
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float d = x[j].get(e) - first.get(e);
+            s[e] += d;
+            s2[e] += d * d;
+          }
+    } else {
+      const Scale t = scale();
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j))
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float xh = normalised(x[j].get(e), t.mean[ONE ? 0 : e], t.rstd[ONE ? 0 : e]);
+            const float dz = through(dy[j].get(e), affine(xh, t.ga[e], t.be[e]), q.act);
+            s[e] += dz;
+            s2[e] += dz * xh;
+          }
+    }
+    __syncthreads();
+    if (in)
+#pragma unroll
+      for (int e = 0; e < V; ++e) buf[row * q.run + c + e] = Pair{s[e], s2[e]};
+    __syncthreads();
+    // rows together: as many lanes to a channel as there are
+    const int lanes = kThreads / width, ch = threadIdx.x % width, part = threadIdx.x / width;
+    int rows = q.rows;
+    if (lanes > 1) {
+      Pair t = {0.f, 0.f};
+      if (part < lanes)
+        for (int i = part; i < rows; i += lanes) t.a += buf[i * q.run + ch].a, t.b += buf[i * q.run + ch].b;
+      rows = min(lanes, rows);
+      __syncthreads();
+      if (part < rows) buf[part * q.run + ch] = t;
+      __syncthreads();
+    }
+    for (int i = threadIdx.x; i < width; i += kThreads) {
+      Pair t = {0.f, 0.f};
+      for (int j = 0; j < rows; ++j) t.a += buf[j * q.run + i].a, t.b += buf[j * q.run + i].b;
+      if (!BWD) {
+        const float d = t.a / count(k);
+        t = Pair{Elt<E>::ld(static_cast<const E*>(m.x) + base + i) + d, t.b - t.a * d};
+      }
+      out[i] = t;
+    }
+    __syncthreads();
+  }
+  // stat(e): the group of this lane's channel e
+  template <typename Stat>
+  __device__ __forceinline__ void map(Stat stat) {
+    forget(x);
+    if (BWD) forget(dy);
+    E* op = static_cast<E*>(m.out) + base;
+    const Scale t = scale();
+    Pair p[S];
+#pragma unroll
+    for (int e = 0; e < S; ++e) p[e] = stat(e);
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      if (has(j)) {
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int h = ONE ? 0 : e;
+          if (!BWD) {
+            v[e] = activate(affine(normalised(x[j].get(e), p[h].a, p[h].b), t.ga[e], t.be[e]), q.act);
+          } else {
+            const float xh = normalised(x[j].get(e), t.mean[h], t.rstd[h]);
+            v[e] = t.rstd[h] * (through(dy[j].get(e), affine(xh, t.ga[e], t.be[e]), q.act) * t.ga[e] - p[h].a - xh * p[h].b);
+          }
+        }
+        Raw<E, V>::store(op + at(j), v);
+      }
+  }
+};
+
+template <typename E, int V, int J, bool ONE, bool BWD>
+__global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
+  __shared__ Pair buf[kThreads * V];
+  __shared__ Pair all[kMaxSlots];             // [part][group]
+  __shared__ Pair chan[kMaxRun];
+  __shared__ int missing;
+  const size_t cluster = blockIdx.x / q.split;
+  const int k = blockIdx.x % q.split, run = (int)(cluster % q.runs), wave = threadIdx.x / 64;
+  const size_t n = cluster / q.runs;
+  const int groups = q.run / q.cg;            // (kFused)
+  const float M = (float)q.cg * (float)q.P;
+  Nhwc<E, V, J, ONE, BWD> w(q, m, n, run);
+  // a group's sums over its channels, of the part that `chan` holds
+  auto of_group = [&](int g, int part) {
+    const Pair* of = chan + g * q.cg;
+    if (BWD)
+      return add(q.cg, [&](int i) {
+        const float ga = m.gamma ? m.gamma[w.c0 + g * q.cg + i] : 1.f;
+        return Pair{of[i].a * ga, of[i].b * ga};
+      });
+    const float each = w.count(part);
+    return join(q.cg, each * (float)q.cg, [&](int i) { return of[i]; }, [&](int) { return each; });
+  };
+  // Once, but for a workgroup whose neighbours have not answered in time: that takes their parts, and then its own again.
+  int part = k;
+  for (bool asked = false;;) {
+    w.take(part);
+    if (q.mode == kMap) {
+      w.map([&](int e) {
+        const float2 s = m.stat[w.group(e)];
+        return Pair{s.x, s.y};
+      });
+      return;
+    }
+    w.sums(buf, chan, part);
+    if (!asked && (BWD || q.mode == kSums))
+      for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(n * q.split + k) * q.C + w.c0 + i] = chan[i];
+    if (q.mode == kSums) return;
+    for (int g = wave; g < groups; g += kWaves) {
+      const Pair p = of_group(g, part);
+      if (threadIdx.x % 64 == 0) {
+        all[part * groups + g] = p;
+        if (!asked && q.split > 1) put(m.slots + (cluster * q.split + k) * groups + g, p);
+      }
+    }
+    if (q.split == 1) break;
+    if (!asked) {
+      asked = true;
+      if (threadIdx.x == 0) missing = 0;
+      __syncthreads();
+      const unsigned long long* slots = m.slots + cluster * q.split * groups;
+      const long long deadline = (long long)wall_clock64() + q.wait;
+      for (int i = threadIdx.x; i < q.split * groups; i += kThreads) {
+        if (i / groups == k) continue;
+        Pair o;
+        if (!get(slots + i, deadline, &o)) missing = 1, o.a = __uint_as_float(kMissing);
+        all[i] = o;
+      }
+      __syncthreads();
+      if (!missing) break;
+    } else {
+      if (part == k) break;
+      __syncthreads();
+      for (int g = threadIdx.x; g < groups; g += kThreads) {
+        Pair o;
+        if (get(m.slots + (cluster * q.split + part) * groups + g, 0, &o)) all[part * groups + g] = o;
+      }
+      __syncthreads();
+    }
+    // the next part of which a sum is missing, the same for every lane
+    int i = 0;
+    while (i < q.split * groups && __float_as_uint(all[i].a) != kMissing) ++i;
+    part = i < q.split * groups ? i / groups : k;
+    __syncthreads();
+  }
+  __syncthreads();
+  for (int g = wave; g < groups; g += kWaves) {
+    Pair p;
+    if (BWD) p = add(q.split, [&](int i) { return all[i * groups + g]; });
+    else p = join(q.split, M, [&](int i) { return all[i * groups + g]; }, [&](int i) { return w.count(i) * (float)q.cg; });
+    if (BWD) p = Pair{p.a / M, p.b / M};
+    else p.b = 1.f / sqrtf(p.b / M + q.eps);
+    if (threadIdx.x % 64 == 0) {
+      chan[g] = p;
+      const size_t to = n * q.G + (size_t)run * groups + g;
+      if (!BWD && k == 0 && m.mean) m.mean[to] = p.a;
+      if (!BWD && k == 0 && m.rstd) m.rstd[to] = p.b;
+    }
+  }
+  __syncthreads();
+  w.map([&](int e) { return chan[min(w.c + e, w.width - 1) / q.cg]; });
+}
+
+// ---- joins of three-launch runs, and the channels' gradients --------------------------------------
+struct Parts {           // where the sums of part i of channel (NCHW forward: of group) c of image n lie
+  int nhwc, per;
+  size_t C;
+  __device__ __forceinline__ size_t at(size_t n, size_t c, int i) const {
+    return nhwc ? (n * per + i) * C + c : (n * C + c) * per + i;
+  }
+};
+
 // One wave a group of one image
-__global__ __launch_bounds__(kThreads) void k_gn_fwd_join(const Part* __restrict__ part, float* __restrict__ mean,
-                                                          float* __restrict__ rstd, float2* __restrict__ stat, Gn q) {
-  const size_t g = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+__global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ part, float* __restrict__ mean,
+                                                     float* __restrict__ rstd, float2* __restrict__ stat, Gn q, Parts where) {
+  const size_t g = (size_t)blockIdx.x * 4 + threadIdx.x / 64;
   if (g >= (size_t)q.N * q.G) return;
-  const int total = q.cg * q.pieces;
-  const Part* p = part + g * total;
+  const size_t n = g / q.G, c0 = g % q.G * (where.nhwc ? q.cg : 1);
+  const int chans = where.nhwc ? q.cg : 1;
   const double M = (double)q.cg * (double)q.P;
+  auto size = [&](int i) {
+    if (where.nhwc) {
+      const size_t all = (size_t)q.rows * q.per;
+      return (double)min(all, q.P - i * all);
+    }
+    const int teams = kThreads / q.team;
+    return q.pieces > 1 ? (double)min(q.step, q.P - (i % q.pieces) * q.step) : (double)min(teams, q.cg - i * teams) * (double)q.P;
+  };
   double s = 0, s2 = 0;
-  for (int i = threadIdx.x % 64; i < total; i += 64) {
-    const int k = i % q.pieces;
-    s += (double)p[i].a * (double)(min(q.P, (k + 1) * q.step) - k * q.step);
-  }
+  for (int i = threadIdx.x % 64; i < chans * q.split; i += 64) s += size(i / chans) * part[where.at(n, c0 + i % chans, i / chans)].a;
 #pragma unroll
-  for (int m = 32; m > 0; m >>= 1) s += __shfl_xor(s, m);
+  for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
   const double mu = s / M;
-  for (int i = threadIdx.x % 64; i < total; i += 64) {
-    const int k = i % q.pieces;
-    const double d = (double)p[i].a - mu;
-    s2 += (double)p[i].b + d * d * (double)(min(q.P, (k + 1) * q.step) - k * q.step);
+  for (int i = threadIdx.x % 64; i < chans * q.split; i += 64) {
+    const Pair p = part[where.at(n, c0 + i % chans, i / chans)];
+    s2 += p.b + size(i / chans) * (p.a - mu) * (p.a - mu);
   }
 #pragma unroll
-  for (int m = 32; m > 0; m >>= 1) s2 += __shfl_xor(s2, m);
+  for (int d = 32; d > 0; d >>= 1) s2 += __shfl_xor(s2, d);
   if (threadIdx.x % 64) return;
   const float r = (float)(1.0 / sqrt(s2 / M + (double)q.eps));
   stat[g] = make_float2((float)mu, r);
@@ -114,73 +731,34 @@ __global__ __launch_bounds__(kThreads) void k_gn_fwd_join(const Part* __restrict
   if (rstd) rstd[g] = r;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_gn_fwd_map(const T* __restrict__ x, const float* __restrict__ gamma,
-                                                         const float* __restrict__ beta, T* __restrict__ y,
-                                                         const float2* __restrict__ stat, Gn q, int nhwc) {
-  const size_t total = (size_t)q.N * q.C * q.P;
-  for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (size_t)gridDim.x * kThreads) {
-    const size_t n = i / (q.C * q.P);
-    const int c = nhwc ? (int)(i % q.C) : (int)(i / q.P % q.C);
-    const float2 s = stat[n * q.G + c / q.cg];
-    const float z = affine(normalised(Elt<T>::ld(x + i), s.x, s.y), gamma ? gamma[c] : 1.f, beta ? beta[c] : 0.f);
-    Elt<T>::st(y + i, activate(z, q.act));
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_gn_bwd_parts(const T* __restrict__ x, const T* __restrict__ dy,
-                                                           const float* __restrict__ gamma, const float* __restrict__ beta,
-                                                           const float* __restrict__ mean, const float* __restrict__ rstd,
-                                                           Part* __restrict__ part, Gn q, int nhwc) {
-  const size_t piece = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-  if (piece >= (size_t)q.N * q.C * q.pieces) return;
-  const size_t row = piece / q.pieces, n = row / q.C, c = row % q.C;
-  const size_t p0 = piece % q.pieces * q.step, p1 = min(q.P, p0 + q.step);
-  const size_t stride = nhwc ? q.C : 1, at = nhwc ? n * q.P * q.C + c : row * q.P;
-  const float mu = mean[n * q.G + c / q.cg], r = rstd[n * q.G + c / q.cg];
-  const float ga = gamma ? gamma[c] : 1.f, be = beta ? beta[c] : 0.f;
-  float s1 = 0.f, s2 = 0.f;
-  for (size_t p = p0 + threadIdx.x % 64; p < p1; p += 64) {
-    const float xh = normalised(Elt<T>::ld(x + at + p * stride), mu, r);
-    const float dz = through(Elt<T>::ld(dy + at + p * stride), affine(xh, ga, be), q.act);
-    s1 += dz;
-    s2 += dz * xh;
-  }
-  s1 = wave_sum(s1);
-  s2 = wave_sum(s2);
-  if (threadIdx.x % 64 == 0) part[piece] = Part{s1, s2};
-}
-
-// The first N * G waves: a group's two means.  The next C waves: a channel's dbeta and dgamma.
-__global__ __launch_bounds__(kThreads) void k_gn_bwd_join(const Part* __restrict__ part, const float* __restrict__ gamma,
-                                                          float* __restrict__ dgamma, float* __restrict__ dbeta,
-                                                          float2* __restrict__ stat, Gn q) {
-  size_t w = (size_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-  const size_t groups = (size_t)q.N * q.G;
+// The first `groups` waves: a group's two means.  The next C waves: a channel's dbeta and dgamma.
+__global__ __launch_bounds__(256) void k_gn_bwd_join(const Pair* __restrict__ part, const float* __restrict__ gamma,
+                                                     float* __restrict__ dgamma, float* __restrict__ dbeta,
+                                                     float2* __restrict__ stat, Gn q, Parts where, size_t groups) {
+  const size_t w = (size_t)blockIdx.x * 4 + threadIdx.x / 64;
   double s1 = 0, s2 = 0;
   if (w < groups) {
-    const int total = q.cg * q.pieces, c0 = (int)(w % q.G) * q.cg;
-    const Part* p = part + w * total;
-    for (int i = threadIdx.x % 64; i < total; i += 64) {
-      const float ga = gamma ? gamma[c0 + i / q.pieces] : 1.f;
-      s1 += (double)p[i].a * ga;
-      s2 += (double)p[i].b * ga;
+    const size_t c0 = w % q.G * q.cg;
+    for (int i = threadIdx.x % 64; i < q.cg * where.per; i += 64) {
+      const size_t c = where.nhwc ? i % q.cg : i / where.per;
+      const Pair p = part[where.at(w / q.G, c0 + c, where.nhwc ? i / q.cg : i % where.per)];
+      const double ga = gamma ? gamma[c0 + c] : 1.f;
+      s1 += p.a * ga;
+      s2 += p.b * ga;
     }
-  } else {
-    w -= groups;
-    if (w >= (size_t)q.C) return;
-    for (int i = threadIdx.x % 64; i < q.N * q.pieces; i += 64) {
-      const Part p = part[((size_t)(i / q.pieces) * q.C + w) * q.pieces + i % q.pieces];
+  } else if (w - groups < (size_t)q.C) {
+    for (int i = threadIdx.x % 64; i < q.N * where.per; i += 64) {
+      const Pair p = part[where.at(i / where.per, w - groups, i % where.per)];
       s1 += p.a;
       s2 += p.b;
     }
-    w += groups;
+  } else {
+    return;
   }
 #pragma unroll
-  for (int m = 32; m > 0; m >>= 1) {
-    s1 += __shfl_xor(s1, m);
-    s2 += __shfl_xor(s2, m);
+  for (int d = 32; d > 0; d >>= 1) {
+    s1 += __shfl_xor(s1, d);
+    s2 += __shfl_xor(s2, d);
   }
   if (threadIdx.x % 64) return;
   if (w < groups) {
@@ -192,84 +770,188 @@ __global__ __launch_bounds__(kThreads) void k_gn_bwd_join(const Part* __restrict
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void k_gn_bwd_map(const T* __restrict__ x, const T* dy, const float* __restrict__ gamma,
-                                                         const float* __restrict__ beta, const float* __restrict__ mean,
-                                                         const float* __restrict__ rstd, T* dx,
-                                                         const float2* __restrict__ stat, Gn q, int nhwc) {
-  const size_t total = (size_t)q.N * q.C * q.P;
-  for (size_t i = (size_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (size_t)gridDim.x * kThreads) {
-    const size_t n = i / (q.C * q.P);
-    const int c = nhwc ? (int)(i % q.C) : (int)(i / q.P % q.C);
-    const size_t g = n * q.G + c / q.cg;
-    const float ga = gamma ? gamma[c] : 1.f, r = rstd[g];
-    const float xh = normalised(Elt<T>::ld(x + i), mean[g], r);
-    const float t = through(Elt<T>::ld(dy + i), affine(xh, ga, beta ? beta[c] : 0.f), q.act) * ga;
-    Elt<T>::st(dx + i, r * (t - stat[g].x - xh * stat[g].y));
-  }
-}
+// ---- host -----------------------------------------------------------------------------------------
+std::atomic<int> g_wait{10000};        // 100 us
 
 bool shaped(int N, int C, size_t P, int groups) {
-  return N >= 1 && C >= 1 && P >= 1 && groups >= 1 && groups <= C && C % groups == 0 && P < (1ull << 40) &&
+  return N >= 1 && C >= 1 && P >= 1 && groups >= 1 && groups <= C && C % groups == 0 && P < (1ull << 31) && C <= (1 << 20) &&
          (size_t)N * C < (1ull << 31) && (size_t)N * C * P < (1ull << 46);
 }
-Gn pieces_of(int N, int C, size_t P, int groups) {
-  Gn q = {};
-  q.N = N, q.C = C, q.G = groups, q.cg = C / groups, q.P = P;
-  // a few thousand waves where the map has them, at least 1024 pixels each
-  const size_t rows = (size_t)N * C;
-  size_t want = std::max<size_t>(1, (8192 + rows - 1) / rows);
-  want = std::min(want, std::max<size_t>(1, P / 1024));
-  q.step = (P + want - 1) / want;
-  q.pieces = (int)((P + q.step - 1) / q.step);
+
+size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
+
+size_t workgroups(const Gn& q, int layout) { return (size_t)q.N * (layout == TRAIN_NHWC ? q.runs : q.G) * q.split; }
+
+Gn cut_nchw(Gn q, int elem, int per) {
+  const int full = 16 / elem;
+  q.vec = q.P >= (size_t)full ? full : 1;
+  q.per = per;
+  const size_t vectors = std::max<size_t>(1, q.P / q.vec);
+  if (vectors <= 64u * per) {                     // a team of a wave or less holds a channel
+    q.team = 4;
+    while ((size_t)q.team * per < vectors || q.team < q.vec) q.team *= 2;
+    q.pieces = 1;
+    q.step = q.P;
+  } else {
+    q.team = kThreads;
+    q.pieces = (int)ceil_div(vectors, (size_t)kThreads * per);
+    q.step = ceil_div(vectors, q.pieces) * q.vec;
+    if (q.pieces == 1) q.step = q.P;
+  }
+  const size_t split = ceil_div((size_t)q.cg * q.pieces, kThreads / q.team);
+  q.split = (int)split;
   return q;
 }
-size_t parts_bytes(const Gn& q) { return ((size_t)q.N * q.C * q.pieces * sizeof(Part) + 255) / 256 * 256; }
-size_t need(const Gn& q) { return parts_bytes(q) + (size_t)q.N * q.G * sizeof(float2); }
-unsigned waves(size_t n) { return (unsigned)((n + kThreads / 64 - 1) / (kThreads / 64)); }
-unsigned map_blocks(const Gn& q) {
-  return (unsigned)std::min<size_t>(((size_t)q.N * q.C * q.P + kThreads - 1) / kThreads, 1u << 16);
+
+Gn cut_nhwc(Gn q, int elem, int per) {
+  q.vec = 16 / elem;
+  q.one = q.cg % q.vec == 0;
+  if (!q.one) {                // lanes with several groups' statistics: shorter vectors and fewer of them, for the registers
+    q.vec = q.C % 4 == 0 ? 4 : 1;
+    q.one = q.vec == 1;
+    per = std::min(per, q.one ? 8 : 4);
+  }
+  q.per = per;
+  // the shortest run of whole groups that fills a cache line of every pixel
+  const size_t longest = std::min(kMaxRun, kThreads * q.vec);
+  int take = 0;
+  for (int g = 1; g <= q.G && !take; ++g)
+    if (q.G % g == 0 && (size_t)g * q.cg % q.vec == 0 && ((size_t)g * q.cg * elem >= 128 || g == q.G) &&
+        (size_t)g * q.cg <= longest)
+      take = g * q.cg;
+  q.mode = take ? kFused : kSums;
+  q.run = take ? take : (int)std::min<size_t>(q.C, longest);
+  q.runs = (int)ceil_div(q.C, q.run);
+  q.rows = kThreads / (q.run / q.vec);
+  q.split = (int)ceil_div(q.P, (size_t)q.rows * per);
+  return q;
+}
+
+// mode kSums: in three launches
+Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
+  Gn q = {};
+  q.N = N, q.C = C, q.G = groups, q.cg = C / groups, q.P = P;
+  Gn best = {};
+  for (int per : {8, 4, 2}) {
+    best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, bwd ? std::min(per, 4) : per) : cut_nchw(q, elem, per);
+    if (workgroups(best, layout) >= 512) break;       // smaller parts only where they are needed to fill the chip
+  }
+  const size_t slots = (size_t)best.split * (layout == TRAIN_NHWC ? best.run / best.cg : 1);
+  if (best.mode == kFused && (best.split > kMaxSplit || slots > (size_t)kMaxSlots)) best.mode = kSums;
+  return best;
+}
+
+// Room for sums: every channel's pieces or splits (the channels' gradients need them), and what three launches join
+size_t parts_of(const Gn& q, int layout) {
+  if (layout == TRAIN_NHWC) return (size_t)q.N * q.C * q.split;
+  return std::max((size_t)q.N * q.C * q.pieces, (size_t)q.N * q.G * q.split);
+}
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+size_t slots_of(const Gn& q, int layout) {
+  if (q.mode != kFused || q.split == 1) return 0;
+  return workgroups(q, layout) * (layout == TRAIN_NHWC ? q.run / q.cg : 1);
+}
+size_t need(const Gn& q, int layout) {
+  return round256(parts_of(q, layout) * sizeof(Pair)) + round256(slots_of(q, layout) * 8) + round256((size_t)q.N * q.G * sizeof(float2));
 }
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 bool known(int act, int layout) {
   return (act == TRAIN_ACT_NONE || act == TRAIN_ACT_RELU || act == TRAIN_ACT_SILU) && (layout == TRAIN_NCHW || layout == TRAIN_NHWC);
 }
 
-template <typename T>
-int fwd(const T* x, const float* gamma, const float* beta, T* y, float* mean, float* rstd, int N, int C, size_t P, int groups,
+typedef void (*Kernel)(Gn, Maps);
+template <typename E, int V, bool BWD>
+Kernel nchw_kernel(int per) {
+  return per == 8 ? k_gn_nchw<E, V, 8, BWD> : per == 4 ? k_gn_nchw<E, V, 4, BWD> : k_gn_nchw<E, V, 2, BWD>;
+}
+template <typename E, int V, bool BWD>
+Kernel nhwc_kernel(int per) {
+  if constexpr (!BWD)          // two maps of eight vectors do not fit the registers
+    if (per == 8) return k_gn_nhwc<E, V, 8, true, BWD>;
+  return per == 4 ? k_gn_nhwc<E, V, 4, true, BWD> : k_gn_nhwc<E, V, 2, true, BWD>;
+}
+template <typename E, bool BWD>
+Kernel pick(const Gn& q, int layout) {
+  constexpr int full = 16 / sizeof(E);
+  if (layout == TRAIN_NCHW) return q.vec == 1 ? nchw_kernel<E, 1, BWD>(q.per) : nchw_kernel<E, full, BWD>(q.per);
+  if (!q.one) return q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD> : k_gn_nhwc<E, 4, 2, false, BWD>;
+  return q.vec == 1 ? nhwc_kernel<E, 1, BWD>(q.per) : nhwc_kernel<E, full, BWD>(q.per);
+}
+
+// the main kernel once (fused), or as sums and, after `join`, as the map
+template <typename E, bool BWD, typename Join>
+void launch(Gn q, Maps m, int layout, hipStream_t st, Join join) {
+  const Kernel kernel = pick<E, BWD>(q, layout);
+  const unsigned grid = (unsigned)workgroups(q, layout);
+  if (q.mode == kFused) {
+    if (const size_t n = slots_of(q, layout))
+      k_gn_empty<<<(unsigned)std::min<size_t>(ceil_div(n, 256), 256), 256, 0, st>>>(m.slots, (int)n);
+    kernel<<<grid, kThreads, 0, st>>>(q, m);
+    return;
+  }
+  kernel<<<grid, kThreads, 0, st>>>(q, m);
+  join();
+  q.mode = kMap;
+  kernel<<<grid, kThreads, 0, st>>>(q, m);
+}
+
+struct Scratch {
+  Pair* part;
+  unsigned long long* slots;
+  float2* stat;
+  Scratch(const Gn& q, int layout, void* ws) {
+    char* p = static_cast<char*>(ws);
+    part = reinterpret_cast<Pair*>(p);
+    p += round256(parts_of(q, layout) * sizeof(Pair));
+    slots = reinterpret_cast<unsigned long long*>(p);
+    p += round256(slots_of(q, layout) * 8);
+    stat = reinterpret_cast<float2*>(p);
+  }
+};
+
+template <typename E>
+int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, float* rstd, int N, int C, size_t P, int groups,
         float eps, int act, int layout, void* ws, size_t ws_bytes, void* stream) {
   if (!x || !y) return ROTCONV_ERR_NULL;
   if (!shaped(N, C, P, groups)) return ROTCONV_ERR_SHAPE;
-  if (!known(act, layout) || !(eps >= 0.f) || misaligned(x, sizeof(T)) || misaligned(y, sizeof(T))) return ROTCONV_ERR_UNSUPPORTED;
-  Gn q = pieces_of(N, C, P, groups);
-  q.eps = eps, q.act = act;
-  if (!ws || misaligned(ws, 16) || ws_bytes < need(q)) return ROTCONV_ERR_WORKSPACE;
+  if (!known(act, layout) || !(eps >= 0.f) || misaligned(x, sizeof(E)) || misaligned(y, sizeof(E))) return ROTCONV_ERR_UNSUPPORTED;
+  if (P == 1) layout = TRAIN_NHWC;                 // the two are the same
+  Gn q = cut(N, C, P, groups, layout, sizeof(E), false);
+  q.eps = eps, q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
+  if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
+  if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  Part* part = static_cast<Part*>(ws);
-  float2* stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(q));
-  k_gn_fwd_parts<T><<<waves((size_t)N * C * q.pieces), kThreads, 0, st>>>(x, part, q, layout);
-  k_gn_fwd_join<<<waves((size_t)N * groups), kThreads, 0, st>>>(part, mean, rstd, stat, q);
-  k_gn_fwd_map<T><<<map_blocks(q), kThreads, 0, st>>>(x, gamma, beta, y, stat, q, layout);
+  const Scratch s(q, layout, ws);
+  const Maps m{x, nullptr, y, gamma, beta, mean, rstd, s.part, s.slots, s.stat};
+  launch<E, false>(q, m, layout, st, [&] {
+    const Parts where{layout, q.split, (size_t)(layout == TRAIN_NHWC ? C : groups)};
+    k_gn_fwd_join<<<(unsigned)ceil_div((size_t)N * groups, 4), 256, 0, st>>>(s.part, mean, rstd, s.stat, q, where);
+  });
   return finish();
 }
 
-template <typename T>
-int bwd(const T* x, const T* dy, const float* gamma, const float* beta, const float* mean, const float* rstd, T* dx,
+template <typename E>
+int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const float* mean, const float* rstd, E* dx,
         float* dgamma, float* dbeta, int N, int C, size_t P, int groups, int act, int layout, void* ws, size_t ws_bytes,
         void* stream) {
   if (!x || !dy || !mean || !rstd || !dx) return ROTCONV_ERR_NULL;
   if (!shaped(N, C, P, groups)) return ROTCONV_ERR_SHAPE;
-  if (!known(act, layout) || misaligned(x, sizeof(T)) || misaligned(dy, sizeof(T)) || misaligned(dx, sizeof(T)))
+  if (!known(act, layout) || misaligned(x, sizeof(E)) || misaligned(dy, sizeof(E)) || misaligned(dx, sizeof(E)))
     return ROTCONV_ERR_UNSUPPORTED;
-  Gn q = pieces_of(N, C, P, groups);
-  q.act = act;
-  if (!ws || misaligned(ws, 16) || ws_bytes < need(q)) return ROTCONV_ERR_WORKSPACE;
+  if (P == 1) layout = TRAIN_NHWC;
+  Gn q = cut(N, C, P, groups, layout, sizeof(E), true);
+  q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
+  if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
+  if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  Part* part = static_cast<Part*>(ws);
-  float2* stat = reinterpret_cast<float2*>(static_cast<char*>(ws) + parts_bytes(q));
-  k_gn_bwd_parts<T><<<waves((size_t)N * C * q.pieces), kThreads, 0, st>>>(x, dy, gamma, beta, mean, rstd, part, q, layout);
-  k_gn_bwd_join<<<waves((size_t)N * groups + C), kThreads, 0, st>>>(part, gamma, dgamma, dbeta, stat, q);
-  k_gn_bwd_map<T><<<map_blocks(q), kThreads, 0, st>>>(x, dy, gamma, beta, mean, rstd, dx, stat, q, layout);
+  const Scratch s(q, layout, ws);
+  const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), s.part, s.slots, s.stat};
+  const Parts where{layout, layout == TRAIN_NHWC ? q.split : q.pieces, (size_t)C};
+  auto join = [&](size_t g) {
+    k_gn_bwd_join<<<(unsigned)ceil_div(g + C, 4), 256, 0, st>>>(s.part, gamma, dgamma, dbeta, s.stat, q, where, g);
+  };
+  launch<E, true>(q, m, layout, st, [&] { join((size_t)N * groups); });
+  if (q.mode == kFused && (dgamma || dbeta)) join(0);
   return finish();
 }
 
@@ -280,7 +962,11 @@ extern "C" {
 
 size_t train_groupnorm_workspace_bytes(int N, int C, size_t P, int groups) {
   if (!rotconv::shaped(N, C, P, groups)) return 0;
-  return rotconv::need(rotconv::pieces_of(N, C, P, groups));
+  size_t n = 0;
+  for (int layout : {TRAIN_NCHW, TRAIN_NHWC})
+    for (int elem : {4, 2})
+      for (bool bwd : {false, true}) n = std::max(n, rotconv::need(rotconv::cut(N, C, P, groups, layout, elem, bwd), layout));
+  return n;
 }
 int train_groupnorm_fwd(const float* x, const float* gamma, const float* beta, float* y, float* mean, float* rstd, int N, int C,
                         size_t P, int groups, float eps, int act, int layout, void* ws, size_t ws_bytes, void* stream) {
@@ -301,5 +987,6 @@ int train_groupnorm_bwd_bf16(const uint16_t* x, const uint16_t* dy, const float*
                              int act, int layout, void* ws, size_t ws_bytes, void* stream) {
   return rotconv::bwd<uint16_t>(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, N, C, P, groups, act, layout, ws, ws_bytes, stream);
 }
+int train_diag_groupnorm_wait(int ticks) { return rotconv::g_wait.exchange(ticks < 0 ? 0 : ticks, std::memory_order_relaxed); }
 
 }  // extern "C"

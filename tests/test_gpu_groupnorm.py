@@ -315,3 +315,21 @@ def test_offsets_beyond_32_bits(layout):
     rc.train_groupnorm_bwd(x, dy, None, None, mean, rstd, dx, dga, dbe, G)
     assert float(dx[0].float().abs().max()) < 1e-3 and float(dx[N - 1].float().abs().max()) < 1e-3
     assert torch.allclose(dbe, torch.full_like(dbe, float(N * H * W)), rtol=1e-4)
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_workgroups_that_do_not_wait(layout, dtype):
+    """With no time to wait for one another, workgroups that share a group sum its other parts themselves: the same bits."""
+    for shape in ((2, 8, 128, 128, 2), (1, 4, 200, 333, 1), (3, 60, 101, 75, 12), (1, 32, 64, 63, 32)):
+        c = Case(*shape, act="silu", layout=layout, dtype=dtype)
+        a = c.forward()
+        g = c.backward(a[1], a[2])
+        before = rc.train_diag_groupnorm_wait(0)
+        try:
+            b = c.forward()
+            h = c.backward(a[1], a[2])
+            i = c.backward(a[1], a[2], inplace=True)
+        finally:
+            assert rc.train_diag_groupnorm_wait(before) == 0
+        assert all(np.array_equal(p, q) for p, q in zip(a + g + g, b + h + i)), shape
