@@ -58,8 +58,8 @@ int train_groupnorm_bwd_bf16(const uint16_t* x, const uint16_t* dy, const float*
                              void* stream);
 
 /* Workgroups that share a group wait for one another's sums, at most this many ticks of 10 ns (10000 at first) from then
- * on, and compute what has not arrived themselves: same bits, more reads.  Returns the number before.  For the whole
- * process; results do not depend on it. */
+ * on, and leave their part to a second launch where that is too short: same bits, more reads.  Returns the number
+ * before.  For the whole process; results do not depend on it. */
 int train_diag_groupnorm_wait(int ticks);
 
 /* ---- many tensors at once -----------------------------------------------------------------------

@@ -494,61 +494,82 @@ def train_groupnorm_workspace_bytes(N, C, P, groups):
     return int(lib().train_groupnorm_workspace_bytes(N, C, P, groups))
 
 
-def _map_layout(what, *maps):
-    """The order in memory that all maps [N, C, ...] of one call share: NCHW (contiguous), or channels last."""
-    import torch
+_f32 = None      # torch.float32, once torch is needed
 
-    if any(m.shape != maps[0].shape for m in maps):
-        raise ValueError(f"{what}: maps must have one shape, got {[tuple(m.shape) for m in maps]}")
-    if maps[0].dim() < 2:
+
+def _map_layout(what, x, others):
+    """The order in memory that all maps [N, C, ...] of one call share: NCHW (contiguous), or channels last."""
+    shape, kind, plain = x.shape, x.dtype, x.is_contiguous()
+    for m in others:
+        if m.shape != shape:
+            raise ValueError(f"{what}: maps must have one shape, got {tuple(shape)} and {tuple(m.shape)}")
+        if m.dtype is not kind:
+            raise TypeError(f"{what}: tensors must be all float32 or all bfloat16, got {kind} and {m.dtype}")
+        plain = plain and m.is_contiguous()
+    if len(shape) < 2:
         raise ValueError(f"{what}: maps are [N, C, ...]")
-    if all(m.is_contiguous() for m in maps):
+    if plain:
         return NCHW
-    if maps[0].dim() == 4 and all(m.is_contiguous(memory_format=torch.channels_last) for m in maps):
-        return NHWC
+    if len(shape) == 4:
+        import torch
+
+        if all(m.is_contiguous(memory_format=torch.channels_last) for m in (x, *others)):
+            return NHWC
     raise ValueError(f"{what}: maps must be all contiguous or all channels last")
 
 
-def _check_f32(what, sizes, **tensors):
-    """Tensors of a call that are fp32 vectors of a known size (None passes)."""
-    import torch
+def _vec(what, name, t, n):
+    """Address of an fp32 tensor of n elements; None stays NULL."""
+    if t is None:
+        return None
+    if t.dtype is not _f32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what}: {name} must be float32, contiguous, with {n} elements")
+    return t.data_ptr()
 
-    for name, t in tensors.items():
-        if t is not None and (t.dtype != torch.float32 or t.numel() != sizes[name]):
-            raise ValueError(f"{what}: {name} must be float32 with {sizes[name]} elements")
 
+def _groupnorm(what, x, others, groups, act, ws):
+    """What both directions share: entry point, N, C, P, activation, order of the maps, workspace."""
+    global _f32
+    if _f32 is None:
+        import torch
 
-def _groupnorm_args(what, maps, groups, act, ws, **vectors):
-    layout = _map_layout(what, *maps)
-    N, C = maps[0].shape[0], maps[0].shape[1]
-    P = maps[0].numel() // max(1, N * C)
-    per = dict(gamma=C, beta=C, dgamma=C, dbeta=C, mean=N * groups, rstd=N * groups)
-    _check_f32(what, per, **vectors)
+        _f32 = torch.float32
+        lib()
+    layout = _map_layout(what, x, others)
+    shape = x.shape
+    N, C = shape[0], shape[1]
+    P = x.numel() // (N * C) if N * C else 0
     if act not in ACTS:
         raise ValueError(f"{what}: act must be one of {sorted(ACTS)}")
+    fn = getattr(_lib, what) if x.dtype is _f32 else _glue(what, x)
     if ws is None:
         import torch
 
-        ws = torch.empty(max(256, train_groupnorm_workspace_bytes(N, C, P, groups)), dtype=torch.uint8, device=maps[0].device)
-    return N, C, P, layout, ws
+        ws = torch.empty(max(256, train_groupnorm_workspace_bytes(N, C, P, groups)), dtype=torch.uint8, device=x.device)
+    return fn, N, C, P, ACTS[act], layout, ws
 
 
 def train_groupnorm_fwd(x, gamma, beta, y, mean, rstd, groups, eps=1e-5, act="none", ws=None):
     """x, y [N, C, ...], both contiguous or both channels last; gamma, beta [C] or None; mean, rstd [N, groups] or None."""
-    N, C, P, layout, ws = _groupnorm_args("train_groupnorm_fwd", (x, y), groups, act, ws, gamma=gamma, beta=beta, mean=mean,
-                                          rstd=rstd)
-    _check(_glue("train_groupnorm_fwd", x, y)(x.data_ptr(), _ptr(gamma), _ptr(beta), y.data_ptr(), _ptr(mean), _ptr(rstd), N,
-                                              C, P, groups, eps, ACTS[act], layout, _ptr(ws), _nbytes(ws), _stream()),
-           "train_groupnorm_fwd")
+    what = "train_groupnorm_fwd"
+    fn, N, C, P, a, layout, ws = _groupnorm(what, x, (y,), groups, act, ws)
+    status = fn(x.data_ptr(), _vec(what, "gamma", gamma, C), _vec(what, "beta", beta, C), y.data_ptr(),
+                _vec(what, "mean", mean, N * groups), _vec(what, "rstd", rstd, N * groups), N, C, P, groups, eps, a, layout,
+                _ptr(ws), _nbytes(ws), _stream())
+    if status != OK:
+        raise RotconvError(status, what)
 
 
 def train_groupnorm_bwd(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, groups, act="none", ws=None):
     """x, dy, dx [N, C, ...] in one order; mean, rstd from the forward call; dgamma, dbeta [C] or None.  dx may be dy."""
-    N, C, P, layout, ws = _groupnorm_args("train_groupnorm_bwd", (x, dy, dx), groups, act, ws, gamma=gamma, beta=beta,
-                                          mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta)
-    _check(_glue("train_groupnorm_bwd", x, dy, dx)(x.data_ptr(), dy.data_ptr(), _ptr(gamma), _ptr(beta), _ptr(mean), _ptr(rstd),
-                                                   dx.data_ptr(), _ptr(dgamma), _ptr(dbeta), N, C, P, groups, ACTS[act],
-                                                   layout, _ptr(ws), _nbytes(ws), _stream()), "train_groupnorm_bwd")
+    what = "train_groupnorm_bwd"
+    fn, N, C, P, a, layout, ws = _groupnorm(what, x, (dy, dx), groups, act, ws)
+    status = fn(x.data_ptr(), dy.data_ptr(), _vec(what, "gamma", gamma, C), _vec(what, "beta", beta, C),
+                _vec(what, "mean", mean, N * groups), _vec(what, "rstd", rstd, N * groups), dx.data_ptr(),
+                _vec(what, "dgamma", dgamma, C), _vec(what, "dbeta", dbeta, C), N, C, P, groups, a, layout, _ptr(ws),
+                _nbytes(ws), _stream())
+    if status != OK:
+        raise RotconvError(status, what)
 
 
 def train_diag_groupnorm_wait(ticks: int) -> int:

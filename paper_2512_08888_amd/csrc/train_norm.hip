@@ -5,8 +5,8 @@
 // group needs more than one workgroup, these exchange their sums through memory (one 8-byte slot each) and wait for one
 // another; a group that needs too many for that is done in three launches instead (sums, their join, the map again).
 //
-// The wait is bounded and never needed for the result: a workgroup whose neighbours have not answered in time sums
-// their parts itself, in the same order with the same bits.  So the kernel ends whatever else runs on the device and in
+// The wait is bounded and never needed for the result: a workgroup whose neighbours have not answered in time leaves its
+// part to the launch behind, which finds all sums there.  So the kernel ends whatever else runs on the device and in
 // whatever order its workgroups start.
 //
 // A part's forward sums are its mean and the squared deviations from it, taken from deviations from the part's first
@@ -103,18 +103,36 @@ __device__ __forceinline__ float affine(float xh, float gamma, float beta) {
   return xh * gamma + beta;
 }
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == TRAIN_ACT_RELU) return z <= 0.f ? 0.f : z;
-  if (act == TRAIN_ACT_SILU) return z * sigmoid(z);
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if (ACT == TRAIN_ACT_RELU) return z <= 0.f ? 0.f : z;
+  if (ACT == TRAIN_ACT_SILU) return z * sigmoid(z);
   return z;
 }
-__device__ __forceinline__ float through(float dy, float z, int act) {      // dy * act'(z)
-  if (act == TRAIN_ACT_RELU) return z > 0.f ? dy : 0.f;
-  if (act == TRAIN_ACT_SILU) {
+template <int ACT>
+__device__ __forceinline__ float through(float dy, float z) {      // dy * act'(z)
+#pragma clang fp contract(off)
+  if (ACT == TRAIN_ACT_RELU) return z > 0.f ? dy : 0.f;
+  if (ACT == TRAIN_ACT_SILU) {
     const float s = sigmoid(z);
-    return dy * (s * (1.f + z * (1.f - s)));
+    return dy * (s * fmaf(z, 1.f - s, 1.f));
   }
   return dy;
+}
+// What an element adds to the sums of its channel.  Operations are fused or not as written: a part has the same sums
+// whichever workgroup forms them.
+__device__ __forceinline__ void add_fwd(float x, float first, float& s, float& s2) {
+#pragma clang fp contract(off)
+  const float d = x - first;
+  s += d;
+  s2 = fmaf(d, d, s2);
+}
+template <int ACT>
+__device__ __forceinline__ void add_bwd(float x, float dy, float mean, float rstd, float gamma, float beta, float& s, float& s2) {
+#pragma clang fp contract(off)
+  const float xh = normalised(x, mean, rstd), dz = through<ACT>(dy, affine(xh, gamma, beta));
+  s += dz;
+  s2 = fmaf(dz, xh, s2);
 }
 
 // ---- sums -----------------------------------------------------------------------------------------
@@ -159,14 +177,13 @@ __device__ __forceinline__ Pair add(int count, Get get) {
 
 // ---- exchange -------------------------------------------------------------------------------------
 // A slot is empty (all ones) until its owner writes it; a NaN is written in one fixed form, so that it never looks empty.
-// Who sums a neighbour's part itself looks at its slot again afterwards: still empty, the neighbour had not begun to write
-// its map (which may overwrite the dy that was read); not empty, the slot's value is the one to take.
+// A workgroup that has not seen all its slots in time writes nothing but its number into a list; the launch after that
+// finds every slot full and does what is on the list.  late[0]: how many, from late[1] on: which.
 constexpr unsigned long long kEmpty = ~0ull;
 __device__ __forceinline__ uint32_t plain_bits(float v) { return v != v ? 0x7fc00000u : __float_as_uint(v); }
 __device__ __forceinline__ void put(unsigned long long* slot, Pair p) {
   const unsigned long long v = (unsigned long long)plain_bits(p.b) << 32 | plain_bits(p.a);
   __hip_atomic_store(slot, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // it has arrived before this workgroup writes any of its map
 }
 // The value of a slot, waiting until `deadline` (of the constant clock); false: still empty
 __device__ __forceinline__ bool get(const unsigned long long* slot, long long deadline, Pair* p) {
@@ -177,11 +194,12 @@ __device__ __forceinline__ bool get(const unsigned long long* slot, long long de
       return true;
     }
     if ((long long)wall_clock64() >= deadline) return false;
-    __builtin_amdgcn_s_sleep(8);
+    __builtin_amdgcn_s_sleep(2);
   }
 }
-__global__ __launch_bounds__(256) void k_gn_empty(unsigned long long* slots, int n) {
+__global__ __launch_bounds__(256) void k_gn_empty(unsigned long long* slots, int n, uint32_t* late) {
   for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) slots[i] = kEmpty;
+  if (blockIdx.x == 0 && threadIdx.x == 0) late[0] = 0;
 }
 
 // Makes the compiler forget what it knows of a register: the map then starts from the elements as loaded, instead of from
@@ -218,14 +236,16 @@ struct Maps {
   float *mean, *rstd;                  // written forward (or NULL), read backward
   Pair* part;                          // see parts_of
   unsigned long long* slots;
+  uint32_t* late;
   const float2* stat;                  // kMap: mean and rstd forward, the two means of the gradient backward
 };
 
+__device__ __forceinline__ void put_off(const Maps& m) { m.late[1 + atomicAdd(m.late, 1u)] = blockIdx.x; }
 // ---- NCHW -----------------------------------------------------------------------------------------
 // A team of lanes (4 to 64, or the workgroup) holds one piece of one channel, `per` vectors a lane and the elements
 // beyond the last whole vector one a lane.  Unit u of a group is piece u % pieces of channel u / pieces; workgroup k
 // holds the units from k * (512 / team) on.
-template <typename E, int V, int J, bool BWD>
+template <typename E, int V, int J, bool BWD, int ACT>
 struct Nchw {
   const Gn& q;
   const Maps& m;
@@ -235,8 +255,8 @@ struct Nchw {
   size_t base = 0;
   uint32_t off = 0;
   Raw<E, V> x[J], dy[BWD ? J : 1];
-  float x1 = 0.f, dy1 = 0.f;
-  int c = 0, len = 0;    // len 0: a team without a unit
+  float x1 = 0.f, dy1 = 0.f, ga = 1.f, be = 0.f, mu = 0.f, r = 0.f;
+  int len = 0;           // 0: a team without a unit
 
   __device__ __forceinline__ Nchw(const Gn& q_, const Maps& m_, size_t group_) : q(q_), m(m_), group(group_) {
     lane = threadIdx.x % q.team;
@@ -246,66 +266,56 @@ struct Nchw {
   __device__ __forceinline__ int teams() const { return kThreads / q.team; }
   __device__ __forceinline__ bool has(int j) const { return (lane + j * q.team) * V + V <= len; }
   __device__ __forceinline__ bool has_tail() const { return V > 1 && lane < len % V; }
-  __device__ __forceinline__ uint32_t at(int j) const { return off + (uint32_t)(lane + j * q.team) * V; }
+  // a lane's vector j: a scalar step from its first
+  template <typename T>
+  __device__ __forceinline__ T* at(T* p, int j) const { return p + (uint32_t)(j * q.team * V) + (off + (uint32_t)lane * V); }
   __device__ __forceinline__ uint32_t at_tail() const { return off + (uint32_t)(len - len % V + lane); }
-  __device__ __forceinline__ void take(int k) {
+  __device__ __forceinline__ void place(int k) {
     const int u0 = k * teams(), cl0 = u0 / q.pieces, piece = u0 % q.pieces;      // one piece, or pieces == 1
     base = (group * q.cg + cl0) * q.P + piece * q.step;
     const bool active = u0 + unit0 < units();
     const int cl = active ? unit0 : 0;
-    c = (int)(group % q.G) * q.cg + cl0 + cl;
+    const int c = (int)(group % q.G) * q.cg + cl0 + cl;
     len = active ? (int)min(q.step, q.P - piece * q.step) : 0;
     off = (uint32_t)cl * (uint32_t)q.P;                                          // less than 512 * per * V
+    if (m.gamma) ga = m.gamma[c];
+    if (m.beta) be = m.beta[c];
+    if (BWD) mu = m.mean[group], r = m.rstd[group];
+  }
+  __device__ __forceinline__ void take(int k) {
+    place(k);
     const E* xp = static_cast<const E*>(m.x) + base;
     const E* dp = static_cast<const E*>(m.dy) + base;
 #pragma unroll
     for (int j = 0; j < J; ++j)
       if (has(j)) {
-        x[j].load(xp + at(j));
-        if (BWD) dy[j].load(dp + at(j));
+        x[j].load(at(xp, j));
+        if (BWD) dy[j].load(at(dp, j));
       }
     if (has_tail()) {
       x1 = Elt<E>::ld(xp + at_tail());
       if (BWD) dy1 = Elt<E>::ld(dp + at_tail());
     }
   }
-  __device__ __forceinline__ float gamma() const { return m.gamma ? m.gamma[c] : 1.f; }
-  __device__ __forceinline__ float beta() const { return m.beta ? m.beta[c] : 0.f; }
   // elements of workgroup k's part
   __device__ __forceinline__ float size(int k) const {
     if (q.pieces > 1) return (float)min(q.step, q.P - (k % q.pieces) * q.step);
     return (float)min(teams(), units() - k * teams()) * (float)q.P;
   }
-  // sums of what this workgroup holds, in all lanes.  Ends with a barrier behind every use of `red`.
-  __device__ __forceinline__ Pair sums(Pair* red, int k, bool keep) {
+  __device__ __forceinline__ void add_one(float xv, float dv, float first, float& s, float& s2) const {
+    if (BWD) add_bwd<ACT>(xv, dv, mu, r, ga, be, s, s2);
+    else add_fwd(xv, first, s, s2);
+  }
+  // Sums of part k (taken), in all lanes.  Ends with a barrier behind every use of `red`.
+  __device__ __forceinline__ Pair sums(Pair* red, int k) {
     float s = 0.f, s2 = 0.f, first = 0.f;
-    if (!BWD) {
-      if (len) first = Elt<E>::ld(static_cast<const E*>(m.x) + base + off);
-      auto one = [&](float xv) {
-        const float d = xv - first;
-        s += d;
-        s2 += d * d;
-      };
+    if (!BWD && len) first = Elt<E>::ld(static_cast<const E*>(m.x) + base + off);
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (has(j))
+    for (int j = 0; j < J; ++j)
+      if (has(j))
 #pragma unroll
-          for (int e = 0; e < V; ++e) one(x[j].get(e));
-      if (has_tail()) one(x1);
-    } else {
-      const float mu = m.mean[group], r = m.rstd[group], ga = gamma(), be = beta();
-      auto one = [&](float xv, float dv) {
-        const float xh = normalised(xv, mu, r), dz = through(dv, affine(xh, ga, be), q.act);
-        s += dz;
-        s2 += dz * xh;
-      };
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (has(j))
-#pragma unroll
-          for (int e = 0; e < V; ++e) one(x[j].get(e), dy[j].get(e));
-      if (has_tail()) one(x1, dy1);
-    }
+        for (int e = 0; e < V; ++e) add_one(x[j].get(e), BWD ? dy[BWD ? j : 0].get(e) : 0.f, first, s, s2);
+    if (has_tail()) add_one(x1, dy1, first, s, s2);
     const int width = min(q.team, 64);
     s = lanes_sum(s, width);
     s2 = lanes_sum(s2, width);
@@ -319,8 +329,7 @@ struct Nchw {
     }
     Pair p;
     if (BWD) {
-      if (keep && len && lane == 0) m.part[group * q.cg * q.pieces + k * teams() + unit0] = Pair{s, s2};
-      const float ga = gamma();
+      if (len && lane == 0) m.part[group * q.cg * q.pieces + k * teams() + unit0] = Pair{s, s2};
       p = Pair{s * ga, s2 * ga};
     } else {
       const float d = s / (float)max(len, 1);
@@ -339,118 +348,127 @@ struct Nchw {
     __syncthreads();
     return p;
   }
+  __device__ __forceinline__ float one(float xv, float dv, float a, float b) const {
+    if (!BWD) return activate<ACT>(affine(normalised(xv, a, b), ga, be));
+    const float xh = normalised(xv, mu, r);
+    return r * (through<ACT>(dv, affine(xh, ga, be)) * ga - a - xh * b);
+  }
+  __device__ __forceinline__ void vector(E* op, const Raw<E, V>& xr, const Raw<E, V>& dr, int j, float a, float b) const {
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = one(xr.get(e), BWD ? dr.get(e) : 0.f, a, b);
+    Raw<E, V>::store(at(op, j), v);
+  }
   __device__ __forceinline__ void map(float a, float b) {
     forget(x);
     if (BWD) forget(dy);
     E* op = static_cast<E*>(m.out) + base;
-    const float ga = gamma(), be = beta();
-    if (!BWD) {
-      auto one = [&](float xv) { return activate(affine(normalised(xv, a, b), ga, be), q.act); };
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (has(j)) {
-          float v[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = one(x[j].get(e));
-          Raw<E, V>::store(op + at(j), v);
-        }
-      if (has_tail()) Elt<E>::st(op + at_tail(), one(x1));
-    } else {
-      const float mu = m.mean[group], r = m.rstd[group];
-      auto one = [&](float xv, float dv) {
-        const float xh = normalised(xv, mu, r);
-        return r * (through(dv, affine(xh, ga, be), q.act) * ga - a - xh * b);
-      };
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (has(j)) {
-          float v[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[e] = one(x[j].get(e), dy[j].get(e));
-          Raw<E, V>::store(op + at(j), v);
-        }
-      if (has_tail()) Elt<E>::st(op + at_tail(), one(x1, dy1));
-    }
+    for (int j = 0; j < J; ++j)
+      if (has(j)) vector(op, x[j], dy[BWD ? j : 0], j, a, b);
+    if (has_tail()) Elt<E>::st(op + at_tail(), one(x1, dy1, a, b));
+  }
+  // the same of a part that is placed but not held
+  __device__ __forceinline__ void map_from_memory(float a, float b) const {
+    const E* xp = static_cast<const E*>(m.x) + base;
+    const E* dp = static_cast<const E*>(m.dy) + base;
+    E* op = static_cast<E*>(m.out) + base;
+    for (int j = 0; j < q.per; ++j)
+      if (has(j)) {
+        Raw<E, V> xr, dr = {};
+        xr.load(at(xp, j));
+        if (BWD) dr.load(at(dp, j));
+        vector(op, xr, dr, j, a, b);
+      }
+    if (has_tail()) Elt<E>::st(op + at_tail(), one(Elt<E>::ld(xp + at_tail()), BWD ? Elt<E>::ld(dp + at_tail()) : 0.f, a, b));
   }
 };
 
-constexpr uint32_t kMissing = 0xffffffffu;      // in a Pair's first value: put() never writes it
+// A group's statistics (forward), or its gradient's means, from its workgroups' sums
+template <bool BWD, typename Part>
+__device__ __forceinline__ Pair settle(const Part& w, const Pair* all, Pair p, size_t group, bool tell) {
+  const Gn& q = w.q;
+  const float M = (float)q.cg * (float)q.P;
+  if (q.split > 1) {
+    if (BWD) p = add(q.split, [&](int i) { return all[i]; });
+    else p = join(q.split, M, [&](int i) { return all[i]; }, [&](int i) { return w.size(i); });
+  }
+  if (BWD) return Pair{p.a / M, p.b / M};
+  p.b = 1.f / sqrtf(p.b / M + q.eps);
+  if (tell && threadIdx.x == 0) {
+    if (w.m.mean) w.m.mean[group] = p.a;
+    if (w.m.rstd) w.m.rstd[group] = p.b;
+  }
+  return p;
+}
 
-template <typename E, int V, int J, bool BWD>
+// The sums of all parts of a group into `all`; false (in every lane) where the deadline came first.  Starts and ends with
+// a barrier.
+__device__ __forceinline__ bool collect(const unsigned long long* slots, int count, long long deadline, Pair* all, int* missing) {
+  if (threadIdx.x == 0) *missing = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < count; i += kThreads) {
+    Pair o;
+    if (!get(slots + i, deadline, &o)) *missing = 1;
+    all[i] = o;
+  }
+  __syncthreads();
+  return !*missing;
+}
+
+template <typename E, int V, int J, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m) {
   __shared__ Pair red[kMaxTeam];
   __shared__ Pair all[kMaxSplit];
   __shared__ int missing;
   const size_t group = blockIdx.x / q.split;
   const int k = blockIdx.x % q.split;
-  const float M = (float)q.cg * (float)q.P;
-  Nchw<E, V, J, BWD> w(q, m, group);
+  Nchw<E, V, J, BWD, ACT> w(q, m, group);
+  w.take(k);
   Pair p;
-  // Once, but for a workgroup whose neighbours have not answered in time: that takes their parts, and then its own again.
-  int part = k;
-  for (bool asked = false;;) {
-    w.take(part);
-    if (q.mode == kMap) {
-      p = Pair{m.stat[group].x, m.stat[group].y};
-      break;
-    }
-    p = w.sums(red, part, !asked);
+  if (q.mode == kMap) {
+    p = Pair{m.stat[group].x, m.stat[group].y};
+  } else {
+    p = w.sums(red, k);
     if (q.mode == kSums) {
       if (!BWD && threadIdx.x == 0) m.part[blockIdx.x] = p;
       return;
     }
-    if (q.split == 1) break;
-    if (!asked) {
-      asked = true;
-      unsigned long long* slots = m.slots + group * q.split;
-      if (threadIdx.x == 0) {
-        missing = 0;
-        put(slots + k, p);
-      }
-      __syncthreads();
-      const long long deadline = (long long)wall_clock64() + q.wait;
-      for (int i = threadIdx.x; i < q.split; i += kThreads) {
-        Pair o = p;
-        if (i != k && !get(slots + i, deadline, &o)) missing = 1, o.a = __uint_as_float(kMissing);
-        all[i] = o;
-      }
-      __syncthreads();
-      if (!missing) break;
-    } else {
-      if (part == k) break;
-      if (threadIdx.x == 0) {
-        Pair o;
-        all[part] = get(m.slots + group * q.split + part, 0, &o) ? o : p;
-      }
-      __syncthreads();
-    }
-    // the next part that is missing, the same for every lane
-    part = 0;
-    while (part < q.split && __float_as_uint(all[part].a) != kMissing) ++part;
-    if (part == q.split) part = k;
-  }
-  if (q.mode == kFused) {
     if (q.split > 1) {
-      if (BWD) p = add(q.split, [&](int i) { return all[i]; });
-      else p = join(q.split, M, [&](int i) { return all[i]; }, [&](int i) { return w.size(i); });
-    }
-    if (BWD) {
-      p = Pair{p.a / M, p.b / M};
-    } else {
-      p.b = 1.f / sqrtf(p.b / M + q.eps);
-      if (k == 0 && threadIdx.x == 0) {
-        if (m.mean) m.mean[group] = p.a;
-        if (m.rstd) m.rstd[group] = p.b;
+      unsigned long long* slots = m.slots + group * q.split;
+      if (threadIdx.x == 0) put(slots + k, p);
+      if (!collect(slots, q.split, (long long)wall_clock64() + q.wait, all, &missing)) {
+        if (threadIdx.x == 0) put_off(m);
+        return;
       }
     }
+    p = settle<BWD>(w, all, p, group, k == 0);
   }
   w.map(p.a, p.b);
+}
+
+// What the launch before has put off: every slot is full now
+template <typename E, int V, bool BWD, int ACT>
+__global__ __launch_bounds__(kThreads) void k_gn_nchw_late(Gn q, Maps m) {
+  __shared__ Pair all[kMaxSplit];
+  __shared__ int missing;
+  for (uint32_t i = blockIdx.x; i < m.late[0]; i += gridDim.x) {
+    const uint32_t wg = m.late[1 + i];
+    const size_t group = wg / q.split;
+    const int k = wg % q.split;
+    Nchw<E, V, 1, BWD, ACT> w(q, m, group);
+    w.place(k);
+    collect(m.slots + group * q.split, q.split, 0, all, &missing);
+    const Pair p = settle<BWD>(w, all, Pair{}, group, k == 0);
+    w.map_from_memory(p.a, p.b);
+    __syncthreads();
+  }
 }
 
 // ---- channels last --------------------------------------------------------------------------------
 // A workgroup holds q.rows * J pixels of a run of channels; a lane the same V channels of each of its J pixels.  ONE: these
 // are of one group, whose statistics a lane then holds once.
-template <typename E, int V, int J, bool ONE, bool BWD>
+template <typename E, int V, int J, bool ONE, bool BWD, int ACT>
 struct Nhwc {
   static constexpr int S = ONE ? 1 : V;
   const Gn& q;
@@ -474,22 +492,28 @@ struct Nhwc {
     in = row < q.rows && c < width;
   }
   __device__ __forceinline__ bool has(int j) const { return in && j * q.rows + row < left; }
-  __device__ __forceinline__ uint32_t at(int j) const { return (uint32_t)(j * q.rows + row) * (uint32_t)q.C + (uint32_t)c; }
+  template <typename T>
+  __device__ __forceinline__ T* at(T* p, int j) const {
+    return p + (uint32_t)(j * q.rows) * (uint32_t)q.C + ((uint32_t)row * (uint32_t)q.C + (uint32_t)c);
+  }
   __device__ __forceinline__ float count(int k) const {
-    const size_t all = (size_t)q.rows * J;
+    const size_t all = (size_t)q.rows * q.per;
     return (float)min(all, q.P - k * all);
   }
-  __device__ __forceinline__ void take(int k) {
-    const size_t p0 = (size_t)k * q.rows * J;
+  __device__ __forceinline__ void place(int k) {
+    const size_t p0 = (size_t)k * q.rows * q.per;
     base = (n * q.P + p0) * q.C + c0;
-    left = (int)min((size_t)q.rows * J, q.P - p0);
+    left = (int)min((size_t)q.rows * q.per, q.P - p0);
+  }
+  __device__ __forceinline__ void take(int k) {
+    place(k);
     const E* xp = static_cast<const E*>(m.x) + base;
     const E* dp = static_cast<const E*>(m.dy) + base;
 #pragma unroll
     for (int j = 0; j < J; ++j)
       if (has(j)) {
-        x[j].load(xp + at(j));
-        if (BWD) dy[j].load(dp + at(j));
+        x[j].load(at(xp, j));
+        if (BWD) dy[j].load(at(dp, j));
       }
   }
   __device__ __forceinline__ size_t group(int e) const { return n * q.G + (c0 + min(c + e, width - 1)) / q.cg; }
@@ -508,36 +532,24 @@ struct Nhwc {
     return s;
   }
 
-  // Sums of every channel of the run over this workgroup's pixels, left in out[0 .. width).  buf: kThreads * V pairs.
+  // Sums of every channel of the run over part k's pixels (taken), left in out[0 .. width).  buf: kThreads * V pairs.
   __device__ __forceinline__ void sums(Pair* buf, Pair* out, int k) {
     float s[V], s2[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) s[e] = s2[e] = 0.f;
-    if (!BWD) {
-      Raw<E, V> first = {};
-      if (in) first.load(static_cast<const E*>(m.x) + base + c);
+    Scale t;
+    Raw<E, V> first = {};
+    if (BWD) t = scale();
+    else if (in) first.load(static_cast<const E*>(m.x) + base + c);
 #pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (has(j))
+    for (int j = 0; j < J; ++j)
+      if (has(j))
 #pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float d = x[j].get(e) - first.get(e);
-            s[e] += d;
-            s2[e] += d * d;
-          }
-    } else {
-      const Scale t = scale();
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-        if (has(j))
-#pragma unroll
-          for (int e = 0; e < V; ++e) {
-            const float xh = normalised(x[j].get(e), t.mean[ONE ? 0 : e], t.rstd[ONE ? 0 : e]);
-            const float dz = through(dy[j].get(e), affine(xh, t.ga[e], t.be[e]), q.act);
-            s[e] += dz;
-            s2[e] += dz * xh;
-          }
-    }
+        for (int e = 0; e < V; ++e) {
+          const int h = ONE ? 0 : e;
+          if (BWD) add_bwd<ACT>(x[j].get(e), dy[BWD ? j : 0].get(e), t.mean[h], t.rstd[h], t.ga[e], t.be[e], s[e], s2[e]);
+          else add_fwd(x[j].get(e), first.get(e), s[e], s2[e]);
+        }
     __syncthreads();
     if (in)
 #pragma unroll
@@ -567,6 +579,20 @@ struct Nhwc {
     __syncthreads();
   }
   // stat(e): the group of this lane's channel e
+  __device__ __forceinline__ void vector(E* op, const Raw<E, V>& xr, const Raw<E, V>& dr, int j, const Scale& t, const Pair* p) const {
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int h = ONE ? 0 : e;
+      if (!BWD) {
+        v[e] = activate<ACT>(affine(normalised(xr.get(e), p[h].a, p[h].b), t.ga[e], t.be[e]));
+      } else {
+        const float xh = normalised(xr.get(e), t.mean[h], t.rstd[h]);
+        v[e] = t.rstd[h] * (through<ACT>(dr.get(e), affine(xh, t.ga[e], t.be[e])) * t.ga[e] - p[h].a - xh * p[h].b);
+      }
+    }
+    Raw<E, V>::store(at(op, j), v);
+  }
   template <typename Stat>
   __device__ __forceinline__ void map(Stat stat) {
     forget(x);
@@ -578,114 +604,119 @@ struct Nhwc {
     for (int e = 0; e < S; ++e) p[e] = stat(e);
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) {
-        float v[V];
+      if (has(j)) vector(op, x[j], dy[BWD ? j : 0], j, t, p);
+  }
+  // the same of a part that is placed but not held
+  template <typename Stat>
+  __device__ __forceinline__ void map_from_memory(Stat stat) const {
+    const E* xp = static_cast<const E*>(m.x) + base;
+    const E* dp = static_cast<const E*>(m.dy) + base;
+    E* op = static_cast<E*>(m.out) + base;
+    const Scale t = scale();
+    Pair p[S];
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int h = ONE ? 0 : e;
-          if (!BWD) {
-            v[e] = activate(affine(normalised(x[j].get(e), p[h].a, p[h].b), t.ga[e], t.be[e]), q.act);
-          } else {
-            const float xh = normalised(x[j].get(e), t.mean[h], t.rstd[h]);
-            v[e] = t.rstd[h] * (through(dy[j].get(e), affine(xh, t.ga[e], t.be[e]), q.act) * t.ga[e] - p[h].a - xh * p[h].b);
-          }
-        }
-        Raw<E, V>::store(op + at(j), v);
+    for (int e = 0; e < S; ++e) p[e] = stat(e);
+    for (int j = 0; j < q.per; ++j)
+      if (has(j)) {
+        Raw<E, V> xr, dr = {};
+        xr.load(at(xp, j));
+        if (BWD) dr.load(at(dp, j));
+        vector(op, xr, dr, j, t, p);
       }
   }
 };
 
-template <typename E, int V, int J, bool ONE, bool BWD>
-__global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
-  __shared__ Pair buf[kThreads * V];
-  __shared__ Pair all[kMaxSlots];             // [part][group]
-  __shared__ Pair chan[kMaxRun];
-  __shared__ int missing;
-  const size_t cluster = blockIdx.x / q.split;
-  const int k = blockIdx.x % q.split, run = (int)(cluster % q.runs), wave = threadIdx.x / 64;
-  const size_t n = cluster / q.runs;
-  const int groups = q.run / q.cg;            // (kFused)
+// A group's sums over its channels, of the part whose channels' sums `chan` holds.  By one wave.
+template <bool BWD, typename Part>
+__device__ __forceinline__ Pair of_group(const Part& w, const Pair* chan, int g, int part) {
+  const int cg = w.q.cg;
+  chan += g * cg;
+  if (BWD)
+    return add(cg, [&](int i) {
+      const float ga = w.m.gamma ? w.m.gamma[w.c0 + g * cg + i] : 1.f;
+      return Pair{chan[i].a * ga, chan[i].b * ga};
+    });
+  const float each = w.count(part);
+  return join(cg, each * (float)cg, [&](int i) { return chan[i]; }, [&](int) { return each; });
+}
+
+// The statistics of a run's groups (forward), or their gradients' means, from `all` into `stat`; barriers before and after
+template <bool BWD, typename Part>
+__device__ __forceinline__ void settle(const Part& w, const Pair* all, Pair* stat, int run, int groups, bool tell) {
+  const Gn& q = w.q;
   const float M = (float)q.cg * (float)q.P;
-  Nhwc<E, V, J, ONE, BWD> w(q, m, n, run);
-  // a group's sums over its channels, of the part that `chan` holds
-  auto of_group = [&](int g, int part) {
-    const Pair* of = chan + g * q.cg;
-    if (BWD)
-      return add(q.cg, [&](int i) {
-        const float ga = m.gamma ? m.gamma[w.c0 + g * q.cg + i] : 1.f;
-        return Pair{of[i].a * ga, of[i].b * ga};
-      });
-    const float each = w.count(part);
-    return join(q.cg, each * (float)q.cg, [&](int i) { return of[i]; }, [&](int) { return each; });
-  };
-  // Once, but for a workgroup whose neighbours have not answered in time: that takes their parts, and then its own again.
-  int part = k;
-  for (bool asked = false;;) {
-    w.take(part);
-    if (q.mode == kMap) {
-      w.map([&](int e) {
-        const float2 s = m.stat[w.group(e)];
-        return Pair{s.x, s.y};
-      });
-      return;
-    }
-    w.sums(buf, chan, part);
-    if (!asked && (BWD || q.mode == kSums))
-      for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(n * q.split + k) * q.C + w.c0 + i] = chan[i];
-    if (q.mode == kSums) return;
-    for (int g = wave; g < groups; g += kWaves) {
-      const Pair p = of_group(g, part);
-      if (threadIdx.x % 64 == 0) {
-        all[part * groups + g] = p;
-        if (!asked && q.split > 1) put(m.slots + (cluster * q.split + k) * groups + g, p);
-      }
-    }
-    if (q.split == 1) break;
-    if (!asked) {
-      asked = true;
-      if (threadIdx.x == 0) missing = 0;
-      __syncthreads();
-      const unsigned long long* slots = m.slots + cluster * q.split * groups;
-      const long long deadline = (long long)wall_clock64() + q.wait;
-      for (int i = threadIdx.x; i < q.split * groups; i += kThreads) {
-        if (i / groups == k) continue;
-        Pair o;
-        if (!get(slots + i, deadline, &o)) missing = 1, o.a = __uint_as_float(kMissing);
-        all[i] = o;
-      }
-      __syncthreads();
-      if (!missing) break;
-    } else {
-      if (part == k) break;
-      __syncthreads();
-      for (int g = threadIdx.x; g < groups; g += kThreads) {
-        Pair o;
-        if (get(m.slots + (cluster * q.split + part) * groups + g, 0, &o)) all[part * groups + g] = o;
-      }
-      __syncthreads();
-    }
-    // the next part of which a sum is missing, the same for every lane
-    int i = 0;
-    while (i < q.split * groups && __float_as_uint(all[i].a) != kMissing) ++i;
-    part = i < q.split * groups ? i / groups : k;
-    __syncthreads();
-  }
   __syncthreads();
-  for (int g = wave; g < groups; g += kWaves) {
+  for (int g = threadIdx.x / 64; g < groups; g += kWaves) {
     Pair p;
     if (BWD) p = add(q.split, [&](int i) { return all[i * groups + g]; });
     else p = join(q.split, M, [&](int i) { return all[i * groups + g]; }, [&](int i) { return w.count(i) * (float)q.cg; });
     if (BWD) p = Pair{p.a / M, p.b / M};
     else p.b = 1.f / sqrtf(p.b / M + q.eps);
     if (threadIdx.x % 64 == 0) {
-      chan[g] = p;
-      const size_t to = n * q.G + (size_t)run * groups + g;
-      if (!BWD && k == 0 && m.mean) m.mean[to] = p.a;
-      if (!BWD && k == 0 && m.rstd) m.rstd[to] = p.b;
+      stat[g] = p;
+      const size_t to = w.n * q.G + (size_t)run * groups + g;
+      if (!BWD && tell && w.m.mean) w.m.mean[to] = p.a;
+      if (!BWD && tell && w.m.rstd) w.m.rstd[to] = p.b;
     }
   }
   __syncthreads();
-  w.map([&](int e) { return chan[min(w.c + e, w.width - 1) / q.cg]; });
+}
+
+template <typename E, int V, int J, bool ONE, bool BWD, int ACT>
+__global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
+  __shared__ Pair buf[kThreads * V];
+  __shared__ Pair all[kMaxSlots];             // [part][group]
+  __shared__ Pair chan[kMaxRun];
+  __shared__ int missing;
+  const size_t cluster = blockIdx.x / q.split;
+  const int k = blockIdx.x % q.split, run = (int)(cluster % q.runs);
+  const int groups = q.run / q.cg;            // (kFused)
+  Nhwc<E, V, J, ONE, BWD, ACT> w(q, m, cluster / q.runs, run);
+  w.take(k);
+  if (q.mode != kMap) {
+    w.sums(buf, chan, k);
+    if (BWD || q.mode == kSums)
+      for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + k) * q.C + w.c0 + i] = chan[i];
+    if (q.mode == kSums) return;
+    unsigned long long* slots = m.slots + cluster * q.split * groups;
+    for (int g = threadIdx.x / 64; g < groups; g += kWaves) {
+      const Pair p = of_group<BWD>(w, chan, g, k);
+      if (threadIdx.x % 64 == 0) {
+        if (q.split > 1) put(slots + k * groups + g, p);
+        else all[g] = p;
+      }
+    }
+    if (q.split > 1 && !collect(slots, q.split * groups, (long long)wall_clock64() + q.wait, all, &missing)) {
+      if (threadIdx.x == 0) put_off(m);
+      return;
+    }
+    settle<BWD>(w, all, chan, run, groups, k == 0);
+  }
+  w.map([&](int e) {
+    if (q.mode != kMap) return chan[min(w.c + e, w.width - 1) / q.cg];
+    const float2 s = m.stat[w.group(e)];
+    return Pair{s.x, s.y};
+  });
+}
+
+// What the launch before has put off: every slot is full now
+template <typename E, int V, bool ONE, bool BWD, int ACT>
+__global__ __launch_bounds__(kThreads) void k_gn_nhwc_late(Gn q, Maps m) {
+  __shared__ Pair all[kMaxSlots];
+  __shared__ Pair chan[kMaxRun];
+  __shared__ int missing;
+  const int groups = q.run / q.cg;
+  for (uint32_t i = blockIdx.x; i < m.late[0]; i += gridDim.x) {
+    const uint32_t wg = m.late[1 + i];
+    const size_t cluster = wg / q.split;
+    const int k = wg % q.split, run = (int)(cluster % q.runs);
+    Nhwc<E, V, 1, ONE, BWD, ACT> w(q, m, cluster / q.runs, run);
+    w.place(k);
+    collect(m.slots + cluster * q.split * groups, q.split * groups, 0, all, &missing);
+    settle<BWD>(w, all, chan, run, groups, k == 0);
+    w.map_from_memory([&](int e) { return chan[min(w.c + e, w.width - 1) / q.cg]; });
+    __syncthreads();
+  }
 }
 
 // ---- joins of three-launch runs, and the channels' gradients --------------------------------------
@@ -785,7 +816,8 @@ size_t workgroups(const Gn& q, int layout) { return (size_t)q.N * (layout == TRA
 Gn cut_nchw(Gn q, int elem, int per) {
   const int full = 16 / elem;
   q.vec = q.P >= (size_t)full ? full : 1;
-  q.per = per;
+  q.per = q.vec == 1 ? 2 : per;                   // four lanes hold the up to seven pixels
+  per = q.per;
   const size_t vectors = std::max<size_t>(1, q.P / q.vec);
   if (vectors <= 64u * per) {                     // a team of a wave or less holds a channel
     q.team = 4;
@@ -809,7 +841,7 @@ Gn cut_nhwc(Gn q, int elem, int per) {
   if (!q.one) {                // lanes with several groups' statistics: shorter vectors and fewer of them, for the registers
     q.vec = q.C % 4 == 0 ? 4 : 1;
     q.one = q.vec == 1;
-    per = std::min(per, q.one ? 8 : 4);
+    per = q.one ? 4 : std::min(per, 4);
   }
   q.per = per;
   // the shortest run of whole groups that fills a cache line of every pixel
@@ -834,7 +866,7 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
   Gn best = {};
   for (int per : {8, 4, 2}) {
     best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, bwd ? std::min(per, 4) : per) : cut_nchw(q, elem, per);
-    if (workgroups(best, layout) >= 512) break;       // smaller parts only where they are needed to fill the chip
+    if (workgroups(best, layout) >= 256) break;       // smaller parts only where they are needed to fill the chip
   }
   const size_t slots = (size_t)best.split * (layout == TRAIN_NHWC ? best.run / best.cg : 1);
   if (best.mode == kFused && (best.split > kMaxSplit || slots > (size_t)kMaxSlots)) best.mode = kSums;
@@ -851,8 +883,10 @@ size_t slots_of(const Gn& q, int layout) {
   if (q.mode != kFused || q.split == 1) return 0;
   return workgroups(q, layout) * (layout == TRAIN_NHWC ? q.run / q.cg : 1);
 }
+size_t late_bytes(const Gn& q, int layout) { return slots_of(q, layout) ? round256((1 + workgroups(q, layout)) * 4) : 0; }
 size_t need(const Gn& q, int layout) {
-  return round256(parts_of(q, layout) * sizeof(Pair)) + round256(slots_of(q, layout) * 8) + round256((size_t)q.N * q.G * sizeof(float2));
+  return round256(parts_of(q, layout) * sizeof(Pair)) + round256(slots_of(q, layout) * 8) + round256((size_t)q.N * q.G * sizeof(float2)) +
+         late_bytes(q, layout);
 }
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 bool known(int act, int layout) {
@@ -860,44 +894,54 @@ bool known(int act, int layout) {
 }
 
 typedef void (*Kernel)(Gn, Maps);
-template <typename E, int V, bool BWD>
-Kernel nchw_kernel(int per) {
-  return per == 8 ? k_gn_nchw<E, V, 8, BWD> : per == 4 ? k_gn_nchw<E, V, 4, BWD> : k_gn_nchw<E, V, 2, BWD>;
-}
-template <typename E, int V, bool BWD>
-Kernel nhwc_kernel(int per) {
+struct Kernels {
+  Kernel main, late;
+};
+template <typename E, bool BWD, int ACT>
+Kernels pick_of(const Gn& q, int layout) {
+  constexpr int full = 16 / sizeof(E);
+  if (layout == TRAIN_NCHW) {
+    if (q.vec == 1) return {k_gn_nchw<E, 1, 2, BWD, ACT>, k_gn_nchw_late<E, 1, BWD, ACT>};
+    return {q.per == 8 ? k_gn_nchw<E, full, 8, BWD, ACT> : q.per == 4 ? k_gn_nchw<E, full, 4, BWD, ACT> : k_gn_nchw<E, full, 2, BWD, ACT>,
+            k_gn_nchw_late<E, full, BWD, ACT>};
+  }
+  if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_late<E, 1, true, BWD, ACT>};
+  if (!q.one)
+    return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_late<E, 4, false, BWD, ACT>};
+  Kernel main = q.per == 4 ? k_gn_nhwc<E, full, 4, true, BWD, ACT> : k_gn_nhwc<E, full, 2, true, BWD, ACT>;
   if constexpr (!BWD)          // two maps of eight vectors do not fit the registers
-    if (per == 8) return k_gn_nhwc<E, V, 8, true, BWD>;
-  return per == 4 ? k_gn_nhwc<E, V, 4, true, BWD> : k_gn_nhwc<E, V, 2, true, BWD>;
+    if (q.per == 8) main = k_gn_nhwc<E, full, 8, true, BWD, ACT>;
+  return {main, k_gn_nhwc_late<E, full, true, BWD, ACT>};
 }
 template <typename E, bool BWD>
-Kernel pick(const Gn& q, int layout) {
-  constexpr int full = 16 / sizeof(E);
-  if (layout == TRAIN_NCHW) return q.vec == 1 ? nchw_kernel<E, 1, BWD>(q.per) : nchw_kernel<E, full, BWD>(q.per);
-  if (!q.one) return q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD> : k_gn_nhwc<E, 4, 2, false, BWD>;
-  return q.vec == 1 ? nhwc_kernel<E, 1, BWD>(q.per) : nhwc_kernel<E, full, BWD>(q.per);
+Kernels pick(const Gn& q, int layout) {
+  if (q.act == TRAIN_ACT_RELU) return pick_of<E, BWD, TRAIN_ACT_RELU>(q, layout);
+  if (q.act == TRAIN_ACT_SILU) return pick_of<E, BWD, TRAIN_ACT_SILU>(q, layout);
+  return pick_of<E, BWD, TRAIN_ACT_NONE>(q, layout);
 }
 
 // the main kernel once (fused), or as sums and, after `join`, as the map
 template <typename E, bool BWD, typename Join>
 void launch(Gn q, Maps m, int layout, hipStream_t st, Join join) {
-  const Kernel kernel = pick<E, BWD>(q, layout);
+  const Kernels kernel = pick<E, BWD>(q, layout);
   const unsigned grid = (unsigned)workgroups(q, layout);
   if (q.mode == kFused) {
-    if (const size_t n = slots_of(q, layout))
-      k_gn_empty<<<(unsigned)std::min<size_t>(ceil_div(n, 256), 256), 256, 0, st>>>(m.slots, (int)n);
-    kernel<<<grid, kThreads, 0, st>>>(q, m);
+    const size_t n = slots_of(q, layout);
+    if (n) k_gn_empty<<<(unsigned)std::min<size_t>(ceil_div(n, 256), 256), 256, 0, st>>>(m.slots, (int)n, m.late);
+    kernel.main<<<grid, kThreads, 0, st>>>(q, m);
+    if (n) kernel.late<<<std::min(grid, 256u), kThreads, 0, st>>>(q, m);
     return;
   }
-  kernel<<<grid, kThreads, 0, st>>>(q, m);
+  kernel.main<<<grid, kThreads, 0, st>>>(q, m);
   join();
   q.mode = kMap;
-  kernel<<<grid, kThreads, 0, st>>>(q, m);
+  kernel.main<<<grid, kThreads, 0, st>>>(q, m);
 }
 
 struct Scratch {
   Pair* part;
   unsigned long long* slots;
+  uint32_t* late;
   float2* stat;
   Scratch(const Gn& q, int layout, void* ws) {
     char* p = static_cast<char*>(ws);
@@ -905,6 +949,8 @@ struct Scratch {
     p += round256(parts_of(q, layout) * sizeof(Pair));
     slots = reinterpret_cast<unsigned long long*>(p);
     p += round256(slots_of(q, layout) * 8);
+    late = reinterpret_cast<uint32_t*>(p);
+    p += late_bytes(q, layout);
     stat = reinterpret_cast<float2*>(p);
   }
 };
@@ -922,7 +968,7 @@ int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, fl
   if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Scratch s(q, layout, ws);
-  const Maps m{x, nullptr, y, gamma, beta, mean, rstd, s.part, s.slots, s.stat};
+  const Maps m{x, nullptr, y, gamma, beta, mean, rstd, s.part, s.slots, s.late, s.stat};
   launch<E, false>(q, m, layout, st, [&] {
     const Parts where{layout, q.split, (size_t)(layout == TRAIN_NHWC ? C : groups)};
     k_gn_fwd_join<<<(unsigned)ceil_div((size_t)N * groups, 4), 256, 0, st>>>(s.part, mean, rstd, s.stat, q, where);
@@ -945,7 +991,7 @@ int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const fl
   if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Scratch s(q, layout, ws);
-  const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), s.part, s.slots, s.stat};
+  const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), s.part, s.slots, s.late, s.stat};
   const Parts where{layout, layout == TRAIN_NHWC ? q.split : q.pieces, (size_t)C};
   auto join = [&](size_t g) {
     k_gn_bwd_join<<<(unsigned)ceil_div(g + C, 4), 256, 0, st>>>(s.part, gamma, dgamma, dbeta, s.stat, q, where, g);
