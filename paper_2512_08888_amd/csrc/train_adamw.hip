@@ -21,37 +21,46 @@ namespace {
 
 constexpr int kBlock = 32;             // elements that share a scale; a tensor's states start on multiples of it
 constexpr int kThreads = 256;
-constexpr int kMaxGrid = 2048;         // workgroups of a launch: eight to a CU, and so few tickets that they cost nothing
+constexpr uint32_t kStepChunk = 4 * kThreads;          // elements of a step's chunk: four a lane
 constexpr int kStaged = 2048;          // sums of chunks that the end of the norm holds in LDS
+constexpr int kFan = 64;               // ticket counters of a launch, a cache line each
 
-struct Row {
+// The chunks of a list: what a workgroup needs to know, in one read
+struct NormChunk {
+  const void* g;
+  uint32_t n, vec;                     // elements; 1: the gradient can be read four elements at a time
+};
+struct StepChunk {
   float* p;
   const void* g;
   uint16_t* copy;
-  uint64_t n, base;                    // elements; where its states start
-  uint32_t first_chunk, chunks;
+  uint64_t pos;                        // of the states
   float wd;
-  uint32_t vec;                        // 1: param, gradient and copy can be read four elements at a time
+  uint32_t n, vec, reserved;           // vec: of all three
 };
-struct Chunk {
-  uint32_t row, index;
+struct Row {                           // a tensor's chunks in the norm's cut
+  uint32_t first, count;
 };
 
 }  // namespace
 
 struct train_list {
   int device = -1, count = 0, bf16 = 0;
-  uint32_t chunk = 0, nchunks = 0;
   uint64_t elements = 0;
   bool trains = true;                  // every tensor has a param
-  Row* rows = nullptr;                 // device
-  Chunk* chunks = nullptr;             // device
+  void* memory = nullptr;              // device: the tables below
+  uint32_t nnorm = 0, nstep = 0;
+  uint32_t* tickets = nullptr;         // kFan + 1 counters, 32 words apart, 0 between calls
+  StepChunk* step = nullptr;
+  NormChunk* norm = nullptr;
+  Row* rows = nullptr;
 };
 
 namespace rotconv {
 namespace {
 
 typedef uint16_t us4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
 
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
 
@@ -66,20 +75,30 @@ __device__ __forceinline__ void load_g4(const uint16_t* g, float* v) {
   for (int k = 0; k < 4; ++k) v[k] = bf16_to_f32(a[k]);
 }
 
+// A step reads and writes every value once and far more of them than the caches hold: past the caches (nontemporal).
+template <typename T> __device__ __forceinline__ T stream_load(const T* p) { return __builtin_nontemporal_load(p); }
+template <typename T> __device__ __forceinline__ void stream_store(T* p, T v) { __builtin_nontemporal_store(v, p); }
+
 // Whether this workgroup is the last of its launch to come here.  Every workgroup of the grid calls it exactly once; the
-// ticket is 0 again afterwards.  No fence: a release at device scope writes back an XCD's whole L2, and 2048 of them held
-// the norm of 31 M gradients at 153 us and their AdamW step at 495 us.  What the last workgroup reads of the others has
-// to go through memory by itself (store_shared, load_shared).
-__device__ __forceinline__ bool last_of_grid(uint32_t* ticket) {
-  __shared__ uint32_t mine;
+// tickets are 0 again afterwards.  Atomics on one counter take 12 ns each, one after the other (23 us for 1934 workgroups,
+// half of the norm of 31 M gradients), so a workgroup draws from one of 64 counters, and the last of each from a further
+// one.  No fence: a release at device scope writes back an XCD's whole L2 (the same norm: 153 us).  What the last workgroup
+// reads of the others has to go through memory by itself (store_shared, load_shared).
+__device__ __forceinline__ bool draw_last(uint32_t* ticket, uint32_t of) {
+  const bool last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
+  if (last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return last;
+}
+__device__ __forceinline__ bool last_of_grid(uint32_t* tickets) {
+  __shared__ int last;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's stores have arrived
   __syncthreads();
   if (threadIdx.x == 0) {
-    mine = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (mine == gridDim.x - 1) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
+    last = draw_last(tickets + 32 * (1 + mine), of) && draw_last(tickets, min(gridDim.x, (uint32_t)kFan));
   }
   __syncthreads();
-  return mine == gridDim.x - 1;
+  return last;
 }
 // one value through memory, past the caches that XCDs do not share
 __device__ __forceinline__ void store_shared(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -106,18 +125,15 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
 // stays one.  The last workgroup adds the chunks' sums from LDS, sixteen lanes a tensor (a wave a tensor, each sum from
 // memory where another XCD left it: 56 us for 31 M gradients, most of it here).
 template <typename T>
-__global__ __launch_bounds__(kThreads) void k_grad_norm(const Row* __restrict__ rows, const Chunk* __restrict__ chunks,
-                                                        uint32_t nchunks, uint32_t chunk, int count, float max_norm,
-                                                        float* __restrict__ norms, train_control* ctl, double* part) {
+__global__ __launch_bounds__(kThreads) void k_grad_norm(const NormChunk* __restrict__ chunks, const Row* __restrict__ rows, int count,
+                                                        float max_norm, float* __restrict__ norms, train_control* ctl,
+                                                        double* part, uint32_t* tickets) {
   __shared__ double red[kThreads / 64];
   __shared__ double sums[kStaged];
-  for (uint32_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
-    const Chunk ch = chunks[c];
-    const Row& r = rows[ch.row];
+  {
+    const NormChunk r = chunks[blockIdx.x];
     const T* g = static_cast<const T*>(r.g);
-    const uint64_t at = (uint64_t)ch.index * chunk;
-    const uint32_t n = (uint32_t)min((uint64_t)chunk, r.n - at);
-    g += at;
+    const uint32_t n = r.n;
     double s = 0;
     const uint32_t nv = r.vec ? n / 4 : 0;
     uint32_t i = threadIdx.x;
@@ -141,25 +157,40 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const Row* __restrict__ 
       s += v * v;
     }
     s = block_sum(s, red);
-    if (threadIdx.x == 0) store_shared(part + c, s);
+    if (threadIdx.x == 0) store_shared(part + blockIdx.x, s);
   }
-  if (!last_of_grid(&ctl->ticket[0])) return;
+  if (!last_of_grid(tickets)) return;
+  const uint32_t nchunks = gridDim.x;
   const bool staged = nchunks <= (uint32_t)kStaged;
   if (staged) {
-    for (uint32_t c = threadIdx.x; c < nchunks; c += kThreads) sums[c] = load_shared(part + c);
+    constexpr int each = kStaged / kThreads;
+    double v[each];
+#pragma unroll
+    for (int u = 0; u < each; ++u) v[u] = load_shared(part + min(threadIdx.x + u * kThreads, nchunks - 1));
+#pragma unroll
+    for (int u = 0; u < each; ++u) sums[threadIdx.x + u * kThreads] = v[u];
     __syncthreads();
   }
   double total = 0;
   const int lane = threadIdx.x % 16;
-  for (int k = threadIdx.x / 16; k < count; k += kThreads / 16) {
-    const uint32_t c0 = rows[k].first_chunk, nc = rows[k].chunks;
-    double s = 0;
-    for (uint32_t c = lane; c < nc; c += 16) s += staged ? sums[c0 + c] : load_shared(part + c0 + c);
+  constexpr int ahead = 4, apart = kThreads / 16;
+  for (int k0 = threadIdx.x / 16; k0 < count; k0 += ahead * apart) {
+    Row r[ahead];
 #pragma unroll
-    for (int m = 8; m > 0; m >>= 1) s += __shfl_xor(s, m);
-    if (lane == 0) {
-      if (norms) norms[k] = (float)sqrt(s);
-      total += s;
+    for (int u = 0; u < ahead; ++u) r[u] = rows[min(k0 + u * apart, count - 1)];
+#pragma unroll
+    for (int u = 0; u < ahead; ++u) {
+      const int k = k0 + u * apart;
+      if (k >= count) break;
+      double s = 0;
+#pragma unroll 8
+      for (uint32_t c = lane; c < r[u].count; c += 16) s += staged ? sums[r[u].first + c] : load_shared(part + r[u].first + c);
+#pragma unroll
+      for (int m = 8; m > 0; m >>= 1) s += __shfl_xor(s, m);
+      if (lane == 0) {
+        if (norms) norms[k] = (float)sqrt(s);
+        total += s;
+      }
     }
   }
   total = block_sum(total, red);
@@ -191,14 +222,20 @@ __device__ __forceinline__ uint32_t scale_byte(float top, float* inv) {
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? NAN : ldexpf(1.f, (int)byte - 127); }
 
+// A lane's value moved within its row of sixteen lanes
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
 // largest magnitude of the eight lanes that hold a block (32 elements, four a lane), compared as bits: a NaN is above an
 // infinity
 __device__ __forceinline__ float block_top(const float* v) {
   uint32_t t = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) t = max(t, __float_as_uint(v[k]) & 0x7fffffffu);
-#pragma unroll
-  for (int m = 1; m < 8; m <<= 1) t = max(t, (uint32_t)__shfl_xor((int)t, m));
+  t = max(t, moved<0xb1>(t));          // lanes 1 0 3 2
+  t = max(t, moved<0x4e>(t));          // lanes 2 3 0 1
+  t = max(t, moved<0x141>(t));         // lanes 7 6 5 4 3 2 1 0
   return __uint_as_float(t);
 }
 
@@ -215,13 +252,13 @@ __device__ __forceinline__ void from_e4m3_x4(uint32_t w, float scale, float* v) 
   v[3] = __builtin_amdgcn_cvt_f32_fp8(w, 3) * scale;
 }
 
-// 0 <= q <= 448 onto the e4m3 grid, up with the probability of the part cut off (u uniform in [0, 1)), a positive q to no
-// less than the smallest code.  The grid's step is 2^(exponent - 3), 2^-9 below 2^-6.
-__device__ __forceinline__ float round_up_or_down(float q, float u) {
-  const uint32_t e = max(__float_as_uint(q) >> 23, 121u) - 3;
-  const float step = __uint_as_float(e << 23), inv = __uint_as_float((254u - e) << 23);
-  const float n = floorf(q * inv + u);
-  return q > 0.f ? fmaxf(n, 1.f) * step : q;      // 0 and NaN stay
+// 0 <= q <= 448 onto the e4m3 grid, up with the probability of the part cut off, a positive q to no less than the smallest
+// code.  random: 16 bits, times 16.  The twenty bits below e4m3's three of the mantissa take them as a carry; values whose
+// grid has the step 2^-9 (below 2^-6) are moved to [2^-6, 2^-5) for that, where fp32 has the same bits for it.
+__device__ __forceinline__ float round_up_or_down(float q, uint32_t random) {
+  const float shift = q < 0x1p-6f ? 0x1p-6f : 0.f;
+  const float r = __uint_as_float((__float_as_uint(q + shift) + random) & 0xfff00000u) - shift;
+  return q > 0.f ? fmaxf(r, 0x1p-9f) : 0.f;
 }
 
 struct Step {                          // what a step's elements share
@@ -229,6 +266,7 @@ struct Step {                          // what a step's elements share
   float eps, coef, root;               // root: 1 / sqrt(1 - beta2^t)
   float rate, lr;                      // rate: lr / (1 - beta1^t)
   uint32_t key;
+  int t, skip;
 };
 
 __device__ __forceinline__ double power(double b, int t) {
@@ -239,108 +277,139 @@ __device__ __forceinline__ double power(double b, int t) {
 }
 
 // m and v of one element, and its parameter.  Every operation is rounded by itself: a state in 8 bits then takes the
-// same code wherever this formula is evaluated in fp32.
+// same code wherever this formula is evaluated in fp32.  The quotient alone, which no state depends on, is a product with
+// the instruction's reciprocal (2 ulp of the update).
 __device__ __forceinline__ void adamw(const Step& s, float wd, float grad, float& p, float& m, float& v, float& root) {
 #pragma clang fp contract(off)
   const float g = grad * s.coef;
   m = m * s.b1 + g * s.c1;
   v = v * s.b2 + g * g * s.c2;
   root = sqrtf(v);
-  const float update = m / (root * s.root + s.eps);
+  const float update = m * __builtin_amdgcn_rcpf(root * s.root + s.eps);
   p = p - p * (wd * s.lr) - update * s.rate;
 }
 
+template <typename T> struct Grad4;
+template <> struct Grad4<float> {
+  f4 a;
+  __device__ __forceinline__ void load(const float* p) { a = stream_load(reinterpret_cast<const f4*>(p)); }
+  __device__ __forceinline__ void set(int k, float v) { a[k] = v; }
+  __device__ __forceinline__ float get(int k) const { return a[k]; }
+};
+template <> struct Grad4<uint16_t> {
+  us4 a;
+  __device__ __forceinline__ void load(const uint16_t* p) { a = stream_load(reinterpret_cast<const us4*>(p)); }
+  __device__ __forceinline__ void set(int k, uint16_t v) { a[k] = v; }
+  __device__ __forceinline__ float get(int k) const { return bf16_to_f32(a[k]); }
+};
+
+// A workgroup takes a chunk, four elements a lane: all loads first, and while they are under way its first wave works out
+// what the step's elements share.  The chunks are small and the workgroups many, so that what the chip reads and writes at a
+// time lies close together: 31 M parameters with fp32 states take 183 us with 16384 elements to a workgroup (each then walks
+// its own 64 KB of every array), 149 us with 1024.
 template <typename T, bool MX8>
-__global__ __launch_bounds__(kThreads) void k_adamw(const Row* __restrict__ rows, const Chunk* __restrict__ chunks,
-                                                    uint32_t nchunks, uint32_t chunk, train_adamw opt, void* mp, void* vp,
-                                                    uint8_t* msp, uint8_t* vsp, train_control* ctl) {
-  const int t = ctl->step + 1;
-  const bool skip = ctl->nonfinite != 0;
-  if (!skip) {
-    Step s;
-    s.b1 = (float)opt.beta1;
-    s.c1 = (float)(1 - opt.beta1);
-    s.b2 = (float)opt.beta2;
-    s.c2 = (float)(1 - opt.beta2);
-    s.eps = opt.eps;
-    s.coef = ctl->coef;
-    s.lr = ctl->lr;
-    s.root = (float)(1 / sqrt(1 - power(opt.beta2, t)));
-    s.rate = (float)(s.lr / (1 - power(opt.beta1, t)));
-    s.key = opt.seed + (uint32_t)t * 0x9E3779B9u;
-    for (uint32_t c = blockIdx.x; c < nchunks; c += gridDim.x) {
-      const Chunk ch = chunks[c];
-      const Row& r = rows[ch.row];
-      const uint64_t at = (uint64_t)ch.index * chunk;
-      const uint32_t n = (uint32_t)min((uint64_t)chunk, r.n - at);
-      const uint32_t np = (n + kBlock - 1) / kBlock * kBlock;       // whole blocks: the states' padding is there
-      float* p = r.p + at;
-      const T* g = static_cast<const T*>(r.g) + at;
-      uint16_t* copy = r.copy ? r.copy + at : nullptr;
-      const uint64_t pos = r.base + at;
-      // four elements a lane; a block's eight lanes are in or out together
-      for (uint32_t i = 4 * threadIdx.x; i < np; i += 4 * kThreads) {
-        const int have = i < n ? (int)min(4u, n - i) : 0;
-        const bool whole = r.vec && have == 4;
-        float pv[4] = {0, 0, 0, 0}, gv[4] = {0, 0, 0, 0}, m[4], v[4], root[4];
-        if (whole) {
-          load_g4(p + i, pv);
-          load_g4(g + i, gv);
-        } else {
-          for (int k = 0; k < have; ++k) pv[k] = p[i + k], gv[k] = Elt<T>::ld(g + i + k);
-        }
-        const uint64_t at4 = pos + i, blk = at4 / kBlock;
-        if (MX8) {
-          from_e4m3_x4(reinterpret_cast<const uint32_t*>(mp)[at4 / 4], scale_value(msp[blk]), m);
-          from_e4m3_x4(reinterpret_cast<const uint32_t*>(vp)[at4 / 4], scale_value(vsp[blk]), v);
+__global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict__ chunks, train_adamw opt,
+                                                    void* mp, void* vp, uint8_t* msp, uint8_t* vsp, train_control* ctl,
+                                                    uint32_t* tickets) {
+  __shared__ Step shared;
+  const uint32_t i = 4 * threadIdx.x;
+  const StepChunk r = chunks[blockIdx.x];
+  const T* g = static_cast<const T*>(r.g);
+  const int have = i < r.n ? (int)min(4u, r.n - i) : 0;
+  const bool whole = r.vec && have == 4;
+  const bool inside = i < (r.n + kBlock - 1) / kBlock * kBlock;       // whole blocks, that is eight lanes together
+  const uint64_t at = r.pos + i;
+  f4 pv = {0.f, 0.f, 0.f, 0.f}, fm, fv;
+  Grad4<T> gv = {};
+  uint32_t cm, cv, sm, sv;
+  if (whole) {
+    pv = stream_load(reinterpret_cast<const f4*>(r.p + i));
+    gv.load(g + i);
+  } else {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] = v[k] * v[k];
-        } else {
-          load_g4(static_cast<const float*>(mp) + at4, m);
-          load_g4(static_cast<const float*>(vp) + at4, v);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) adamw(s, r.wd, gv[k], pv[k], m[k], v[k], root[k]);
-        if (whole) {
-          *reinterpret_cast<f4*>(p + i) = f4{pv[0], pv[1], pv[2], pv[3]};
-          if (copy) *reinterpret_cast<us4*>(copy + i) = us4{f32_to_bf16(pv[0]), f32_to_bf16(pv[1]), f32_to_bf16(pv[2]), f32_to_bf16(pv[3])};
-        } else {
-          for (int k = 0; k < have; ++k) {
-            p[i + k] = pv[k];
-            if (copy) copy[i + k] = f32_to_bf16(pv[k]);
-          }
-        }
-        if (MX8) {
-          float inv;
-          const uint32_t mb = scale_byte(block_top(m), &inv);
-#pragma unroll
-          for (int k = 0; k < 4; ++k) m[k] = m[k] * inv;
-          reinterpret_cast<uint32_t*>(mp)[at4 / 4] = e4m3_x4(m);
-          const uint32_t vb = scale_byte(block_top(root), &inv);
-#pragma unroll
-          for (int k = 0; k < 4; k += 2) {       // sixteen random bits an element
-            const uint32_t h = mix32((uint32_t)((at4 + k) >> 1) + s.key);
-            root[k] = round_up_or_down(root[k] * inv, (float)(h & 0xffffu) * 0x1p-16f);
-            root[k + 1] = round_up_or_down(root[k + 1] * inv, (float)(h >> 16) * 0x1p-16f);
-          }
-          reinterpret_cast<uint32_t*>(vp)[at4 / 4] = e4m3_x4(root);
-          if (at4 % kBlock == 0) msp[blk] = (uint8_t)mb, vsp[blk] = (uint8_t)vb;
-        } else {
-          *reinterpret_cast<f4*>(static_cast<float*>(mp) + at4) = f4{m[0], m[1], m[2], m[3]};
-          *reinterpret_cast<f4*>(static_cast<float*>(vp) + at4) = f4{v[0], v[1], v[2], v[3]};
-        }
-      }
-    }
+    for (int k = 0; k < 4; ++k)
+      if (k < have) pv[k] = r.p[i + k], gv.set(k, g[i + k]);
   }
-  // the step number and the flag change only when every workgroup has read them
-  if (last_of_grid(&ctl->ticket[1]) && threadIdx.x == 0) {
-    if (skip) {
-      ctl->skipped += 1;
-      ctl->nonfinite = 0;
+  if (inside) {
+    if constexpr (MX8) {
+      cm = stream_load(reinterpret_cast<const uint32_t*>(mp) + at / 4);
+      cv = stream_load(reinterpret_cast<const uint32_t*>(vp) + at / 4);
+      sm = msp[at / kBlock];
+      sv = vsp[at / kBlock];
     } else {
-      ctl->step = t;
+      fm = stream_load(reinterpret_cast<const f4*>(static_cast<const float*>(mp) + at));
+      fv = stream_load(reinterpret_cast<const f4*>(static_cast<const float*>(vp) + at));
     }
   }
+  if (threadIdx.x < 64) {              // even lanes for beta1, odd ones for beta2
+    const int t = ctl->step + 1;
+    const float lr = ctl->lr;
+    const float left = (float)(1 - power(threadIdx.x % 2 ? opt.beta2 : opt.beta1, t));
+    const float scaled = threadIdx.x % 2 ? 1.f / sqrtf(left) : lr / left;
+    const float root = __shfl(scaled, 1);
+    if (threadIdx.x == 0)
+      shared = Step{(float)opt.beta1, (float)(1 - opt.beta1), (float)opt.beta2, (float)(1 - opt.beta2), opt.eps, ctl->coef, root, scaled, lr,
+                    opt.seed + (uint32_t)t * 0x9E3779B9u, t, ctl->nonfinite};
+  }
+  __syncthreads();
+  const Step s = shared;
+  // The first lane alone reads the control block, and has done so: who draws the last ticket knows that nobody will again.
+  auto end = [&] {
+    if (threadIdx.x != 0) return;
+    const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
+    if (!draw_last(tickets + 32 * (1 + mine), of) || !draw_last(tickets, min(gridDim.x, (uint32_t)kFan))) return;
+    if (s.skip) ctl->skipped += 1, ctl->nonfinite = 0;
+    else ctl->step = s.t;
+  };
+  if (s.skip || !inside) {             // (the first lane is inside)
+    end();
+    return;
+  }
+  float p[4], m[4], v[4], root[4];
+  if constexpr (MX8) {
+    from_e4m3_x4(cm, scale_value(sm), m);
+    from_e4m3_x4(cv, scale_value(sv), v);
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    p[k] = pv[k];
+    if constexpr (MX8) v[k] = v[k] * v[k];
+    else m[k] = fm[k], v[k] = fv[k];
+    adamw(s, r.wd, gv.get(k), p[k], m[k], v[k], root[k]);
+  }
+  if (whole) {
+    stream_store(reinterpret_cast<f4*>(r.p + i), f4{p[0], p[1], p[2], p[3]});
+    if (r.copy)
+      stream_store(reinterpret_cast<us4*>(r.copy + i),
+                   __builtin_bit_cast(us4, __builtin_convertvector(f4{p[0], p[1], p[2], p[3]}, bf4)));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (k < have) {
+        r.p[i + k] = p[k];
+        if (r.copy) r.copy[i + k] = f32_to_bf16(p[k]);
+      }
+  }
+  if constexpr (MX8) {
+    float inv;
+    const uint32_t mb = scale_byte(block_top(m), &inv);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = m[k] * inv;
+    stream_store(reinterpret_cast<uint32_t*>(mp) + at / 4, e4m3_x4(m));
+    const uint32_t vb = scale_byte(block_top(root), &inv);
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {       // sixteen random bits an element
+      const uint32_t h = mix32((uint32_t)((at + k) >> 1) + s.key);
+      root[k] = round_up_or_down(root[k] * inv, h << 4 & 0xffff0u);
+      root[k + 1] = round_up_or_down(root[k + 1] * inv, h >> 12 & 0xffff0u);
+    }
+    stream_store(reinterpret_cast<uint32_t*>(vp) + at / 4, e4m3_x4(root));
+    if (at % kBlock == 0) msp[at / kBlock] = (uint8_t)mb, vsp[at / kBlock] = (uint8_t)vb;
+  } else {
+    stream_store(reinterpret_cast<f4*>(static_cast<float*>(mp) + at), f4{m[0], m[1], m[2], m[3]});
+    stream_store(reinterpret_cast<f4*>(static_cast<float*>(vp) + at), f4{v[0], v[1], v[2], v[3]});
+  }
+  end();
 }
 
 __global__ void k_control_init(train_control* ctl, int step, float lr) {
@@ -378,40 +447,58 @@ int train_list_create(const train_tensor* tensors, int count, int grad_dtype, tr
       return ROTCONV_ERR_UNSUPPORTED;
     total += (t.n + kBlock - 1) / kBlock * kBlock;
   }
-  // A chunk has at least 1024 elements (fewer leave lanes idle).  Beyond one chunk for each workgroup of a full launch it
-  // grows to 16384 (larger ones leave CUs idle at the end), and further only where there would be more than eight times
-  // the sums that the end of the norm holds in LDS.
-  uint64_t chunk = 1024;
-  while ((chunk < 16384 && total / chunk > (uint64_t)kMaxGrid) || total / chunk > 8ull * kStaged) chunk *= 2;
-  uint64_t nchunks = 0;
-  for (int k = 0; k < count; ++k) nchunks += (tensors[k].n + chunk - 1) / chunk;
-  if (nchunks > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
+  // The norm's chunks: from 1024 elements (fewer leave lanes idle) to 16384, then larger only where there would be more
+  // sums than eight times what its end holds in LDS.
+  uint64_t size = 1024;
+  while ((size < 16384 && total / size > (uint64_t)kStaged) || total / size > 8ull * kStaged) size *= 2;
+  uint64_t nnorm = 0, nstep = 0;
+  for (int k = 0; k < count; ++k) nnorm += (tensors[k].n + size - 1) / size, nstep += (tensors[k].n + kStepChunk - 1) / kStepChunk;
+  if (nnorm > 0x7fffffffu || nstep > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
   train_list* l = nullptr;
   try {
     std::vector<Row> rows(count);
-    std::vector<Chunk> chunks;
-    chunks.reserve(nchunks);
+    std::vector<NormChunk> norm;
+    std::vector<StepChunk> step;
+    norm.reserve(nnorm);
+    if (tensors[0].param) step.reserve(nstep);
     uint64_t base = 0;
     for (int k = 0; k < count; ++k) {
       const train_tensor& t = tensors[k];
-      Row& r = rows[k];
-      r = Row{t.param, t.grad, t.copy, t.n, base, (uint32_t)chunks.size(), (uint32_t)((t.n + chunk - 1) / chunk), t.weight_decay, 0};
-      r.vec = !misaligned(t.param, 16) && !misaligned(t.grad, 4 * ge) && !misaligned(t.copy, 8);
-      for (uint32_t c = 0; c < r.chunks; ++c) chunks.push_back(Chunk{(uint32_t)k, c});
+      const char* g = static_cast<const char*>(t.grad);
+      rows[k] = Row{(uint32_t)norm.size(), (uint32_t)((t.n + size - 1) / size)};
+      for (uint64_t at = 0; at < t.n; at += size)
+        norm.push_back(NormChunk{g + at * ge, (uint32_t)std::min(size, t.n - at), misaligned(t.grad, 4 * ge) ? 0u : 1u});
+      const uint32_t vec = !misaligned(t.param, 16) && !misaligned(t.grad, 4 * ge) && !misaligned(t.copy, 8);
+      for (uint64_t at = 0; t.param && at < t.n; at += kStepChunk)
+        step.push_back(StepChunk{t.param + at, g + at * ge, t.copy ? t.copy + at : nullptr, base + at, t.weight_decay,
+                                 (uint32_t)std::min<uint64_t>(kStepChunk, t.n - at), vec, 0});
       base += (t.n + kBlock - 1) / kBlock * kBlock;
     }
     l = new train_list;
     l->count = count;
     l->bf16 = grad_dtype == ROTCONV_BF16;
-    l->chunk = (uint32_t)chunk;
-    l->nchunks = (uint32_t)nchunks;
     l->elements = base;
     l->trains = tensors[0].param != nullptr;
-    const bool ok = hipGetDevice(&l->device) == hipSuccess &&
-                    hipMalloc(reinterpret_cast<void**>(&l->rows), rows.size() * sizeof(Row)) == hipSuccess &&
-                    hipMalloc(reinterpret_cast<void**>(&l->chunks), chunks.size() * sizeof(Chunk)) == hipSuccess &&
-                    hipMemcpy(l->rows, rows.data(), rows.size() * sizeof(Row), hipMemcpyHostToDevice) == hipSuccess &&
-                    hipMemcpy(l->chunks, chunks.data(), chunks.size() * sizeof(Chunk), hipMemcpyHostToDevice) == hipSuccess;
+    l->nnorm = (uint32_t)norm.size();
+    l->nstep = (uint32_t)step.size();
+    const std::vector<uint32_t> tickets((kFan + 1) * 32, 0);
+    const size_t ticket_bytes = tickets.size() * sizeof(uint32_t), step_bytes = step.size() * sizeof(StepChunk);
+    const size_t norm_bytes = norm.size() * sizeof(NormChunk), row_bytes = rows.size() * sizeof(Row);
+    bool ok = hipGetDevice(&l->device) == hipSuccess &&
+              hipMalloc(&l->memory, ticket_bytes + step_bytes + norm_bytes + row_bytes) == hipSuccess;
+    if (ok) {
+      char* p = static_cast<char*>(l->memory);
+      auto put = [&](const void* from, size_t bytes) {
+        void* to = p;
+        ok = ok && (bytes == 0 || hipMemcpy(to, from, bytes, hipMemcpyHostToDevice) == hipSuccess);
+        p += bytes;
+        return to;
+      };
+      l->tickets = static_cast<uint32_t*>(put(tickets.data(), ticket_bytes));
+      l->step = static_cast<StepChunk*>(put(step.data(), step_bytes));
+      l->norm = static_cast<NormChunk*>(put(norm.data(), norm_bytes));
+      l->rows = static_cast<Row*>(put(rows.data(), row_bytes));
+    }
     if (!ok) {
       (void)hipGetLastError();
       train_list_destroy(l);
@@ -427,14 +514,13 @@ int train_list_create(const train_tensor* tensors, int count, int grad_dtype, tr
 
 int train_list_destroy(train_list* l) {
   if (!l) return ROTCONV_OK;
-  if (l->rows) (void)hipFree(l->rows);
-  if (l->chunks) (void)hipFree(l->chunks);
+  if (l->memory) (void)hipFree(l->memory);
   delete l;
   return ROTCONV_OK;
 }
 
 uint64_t train_list_elements(const train_list* l) { return l ? l->elements : 0; }
-size_t train_list_workspace_bytes(const train_list* l) { return l ? (size_t)l->nchunks * sizeof(double) : 0; }
+size_t train_list_workspace_bytes(const train_list* l) { return l ? (size_t)l->nnorm * sizeof(double) : 0; }
 
 int train_control_init(train_control* control, int step, float lr, void* stream) {
   if (!control) return ROTCONV_ERR_NULL;
@@ -449,10 +535,9 @@ int train_grad_norm(const train_list* l, float max_norm, float* norms, train_con
   if (!l || !control) return ROTCONV_ERR_NULL;
   if (!(max_norm > 0.f) || !on_its_device(l) || misaligned(control, 4) || misaligned(norms, 4)) return ROTCONV_ERR_UNSUPPORTED;
   if (!ws || misaligned(ws, 8) || ws_bytes < train_list_workspace_bytes(l)) return ROTCONV_ERR_WORKSPACE;
-  const unsigned grid = std::min<uint32_t>(l->nchunks, kMaxGrid);
   auto kernel = l->bf16 ? k_grad_norm<uint16_t> : k_grad_norm<float>;
-  kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(l->rows, l->chunks, l->nchunks, l->chunk, l->count, max_norm,
-                                                                  norms, control, static_cast<double*>(ws));
+  kernel<<<l->nnorm, kThreads, 0, static_cast<hipStream_t>(stream)>>>(l->norm, l->rows, l->count, max_norm, norms, control,
+                                                                      static_cast<double*>(ws), l->tickets);
   return finish();
 }
 
@@ -464,11 +549,12 @@ int train_adamw_step(const train_list* l, const train_adamw* o, void* m, void* v
   if (!l->trains || !on_its_device(l) || (!mx8 && o->state != TRAIN_STATE_F32) || o->reserved != 0) return ROTCONV_ERR_UNSUPPORTED;
   if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1) || !(o->eps > 0.f)) return ROTCONV_ERR_UNSUPPORTED;
   if (misaligned(m, mx8 ? 4 : 16) || misaligned(v, mx8 ? 4 : 16) || misaligned(control, 4)) return ROTCONV_ERR_UNSUPPORTED;
-  const unsigned grid = std::min<uint32_t>(l->nchunks, kMaxGrid);
-  auto kernel = mx8 ? (l->bf16 ? k_adamw<uint16_t, true> : k_adamw<float, true>)
-                    : (l->bf16 ? k_adamw<uint16_t, false> : k_adamw<float, false>);
-  kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(l->rows, l->chunks, l->nchunks, l->chunk, *o, m, v, m_scale,
-                                                                  v_scale, control);
+  // LDS that nobody uses keeps five workgroups on a CU where eight would fit: with fp32 states their streams then get in one
+  // another's way less (31 M parameters: 163 us with eight, 149 us with five or four); 8-bit states need all eight to keep
+  // enough bytes under way (89 us with eight, 112 us with five).
+  const size_t lds = mx8 ? 0 : 32000;
+  auto kernel = mx8 ? (l->bf16 ? k_adamw<uint16_t, true> : k_adamw<float, true>) : (l->bf16 ? k_adamw<uint16_t, false> : k_adamw<float, false>);
+  kernel<<<l->nstep, kThreads, lds, static_cast<hipStream_t>(stream)>>>(l->step, *o, m, v, m_scale, v_scale, control, l->tickets);
   return finish();
 }
 

@@ -860,14 +860,22 @@ Gn cut_nhwc(Gn q, int elem, int per) {
 }
 
 // mode kSums: in three launches
-Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
+Gn cut(int N, int C, size_t P, int groups, int layout, int elem) {
   Gn q = {};
   q.N = N, q.C = C, q.G = groups, q.cg = C / groups, q.P = P;
   Gn best = {};
-  for (int per : {8, 4, 2}) {
-    best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, bwd ? std::min(per, 4) : per) : cut_nchw(q, elem, per);
-    if (workgroups(best, layout) >= 256) break;       // smaller parts only where they are needed to fill the chip
+  auto with = [&](int per) { return layout == TRAIN_NHWC ? cut_nhwc(q, elem, per) : cut_nchw(q, elem, per); };
+  // A group (or run) in one workgroup needs no exchange and one launch: with as many lanes as that leaves.  Else the largest
+  // parts that still give every CU a workgroup.
+  for (int per : {2, 4, 8}) {
+    best = with(per);
+    if (best.split == 1) break;
   }
+  if (best.split > 1)
+    for (int per : {8, 4, 2}) {
+      best = with(per);
+      if (workgroups(best, layout) >= 256) break;
+    }
   const size_t slots = (size_t)best.split * (layout == TRAIN_NHWC ? best.run / best.cg : 1);
   if (best.mode == kFused && (best.split > kMaxSplit || slots > (size_t)kMaxSlots)) best.mode = kSums;
   return best;
@@ -908,10 +916,10 @@ Kernels pick_of(const Gn& q, int layout) {
   if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_late<E, 1, true, BWD, ACT>};
   if (!q.one)
     return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_late<E, 4, false, BWD, ACT>};
-  Kernel main = q.per == 4 ? k_gn_nhwc<E, full, 4, true, BWD, ACT> : k_gn_nhwc<E, full, 2, true, BWD, ACT>;
-  if constexpr (!BWD)          // two maps of eight vectors do not fit the registers
-    if (q.per == 8) main = k_gn_nhwc<E, full, 8, true, BWD, ACT>;
-  return {main, k_gn_nhwc_late<E, full, true, BWD, ACT>};
+  return {q.per == 8   ? k_gn_nhwc<E, full, 8, true, BWD, ACT>
+          : q.per == 4 ? k_gn_nhwc<E, full, 4, true, BWD, ACT>
+                       : k_gn_nhwc<E, full, 2, true, BWD, ACT>,
+          k_gn_nhwc_late<E, full, true, BWD, ACT>};
 }
 template <typename E, bool BWD>
 Kernels pick(const Gn& q, int layout) {
@@ -929,7 +937,7 @@ void launch(Gn q, Maps m, int layout, hipStream_t st, Join join) {
     const size_t n = slots_of(q, layout);
     if (n) k_gn_empty<<<(unsigned)std::min<size_t>(ceil_div(n, 256), 256), 256, 0, st>>>(m.slots, (int)n, m.late);
     kernel.main<<<grid, kThreads, 0, st>>>(q, m);
-    if (n) kernel.late<<<std::min(grid, 256u), kThreads, 0, st>>>(q, m);
+    if (n) kernel.late<<<std::min(grid, 64u), kThreads, 0, st>>>(q, m);
     return;
   }
   kernel.main<<<grid, kThreads, 0, st>>>(q, m);
@@ -962,7 +970,7 @@ int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, fl
   if (!shaped(N, C, P, groups)) return ROTCONV_ERR_SHAPE;
   if (!known(act, layout) || !(eps >= 0.f) || misaligned(x, sizeof(E)) || misaligned(y, sizeof(E))) return ROTCONV_ERR_UNSUPPORTED;
   if (P == 1) layout = TRAIN_NHWC;                 // the two are the same
-  Gn q = cut(N, C, P, groups, layout, sizeof(E), false);
+  Gn q = cut(N, C, P, groups, layout, sizeof(E));
   q.eps = eps, q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
   if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
   if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
@@ -985,7 +993,7 @@ int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const fl
   if (!known(act, layout) || misaligned(x, sizeof(E)) || misaligned(dy, sizeof(E)) || misaligned(dx, sizeof(E)))
     return ROTCONV_ERR_UNSUPPORTED;
   if (P == 1) layout = TRAIN_NHWC;
-  Gn q = cut(N, C, P, groups, layout, sizeof(E), true);
+  Gn q = cut(N, C, P, groups, layout, sizeof(E));
   q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
   if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
   if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
@@ -1010,8 +1018,7 @@ size_t train_groupnorm_workspace_bytes(int N, int C, size_t P, int groups) {
   if (!rotconv::shaped(N, C, P, groups)) return 0;
   size_t n = 0;
   for (int layout : {TRAIN_NCHW, TRAIN_NHWC})
-    for (int elem : {4, 2})
-      for (bool bwd : {false, true}) n = std::max(n, rotconv::need(rotconv::cut(N, C, P, groups, layout, elem, bwd), layout));
+    for (int elem : {4, 2}) n = std::max(n, rotconv::need(rotconv::cut(N, C, P, groups, layout, elem), layout));
   return n;
 }
 int train_groupnorm_fwd(const float* x, const float* gamma, const float* beta, float* y, float* mean, float* rstd, int N, int C,
