@@ -104,10 +104,31 @@ __device__ __forceinline__ bool last_of_grid(uint32_t* tickets) {
 __device__ __forceinline__ void store_shared(double* p, double v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ double load_shared(const double* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
+// A lane's value moved within its row of sixteen lanes, and sums over rows and waves: the same in all their lanes
+template <int CTRL>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140;     // lanes 1 0 3 2; 2 3 0 1; 7 .. 0; 15 .. 0
+template <int CTRL>
+__device__ __forceinline__ double moved(double v) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)moved<CTRL>((uint32_t)(w >> 32)) << 32 | moved<CTRL>((uint32_t)w));
+}
+__device__ __forceinline__ double row_sum(double v) {
+  v += moved<kSwap1>(v);
+  v += moved<kSwap2>(v);
+  v += moved<kMirror8>(v);
+  return v + moved<kMirror16>(v);
+}
+__device__ __forceinline__ double lane_of(double v, int lane) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(w >> 32), lane) << 32 |
+                                        (uint32_t)__builtin_amdgcn_readlane((int)w, lane));
+}
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+  v = row_sum(v);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 // sum over the workgroup, in every thread; red: one double a wave
 __device__ __forceinline__ double block_sum(double v, double* red) {
@@ -183,10 +204,14 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const NormChunk* __restr
       const int k = k0 + u * apart;
       if (k >= count) break;
       double s = 0;
+      if (staged) {
 #pragma unroll 8
-      for (uint32_t c = lane; c < r[u].count; c += 16) s += staged ? sums[r[u].first + c] : load_shared(part + r[u].first + c);
-#pragma unroll
-      for (int m = 8; m > 0; m >>= 1) s += __shfl_xor(s, m);
+        for (uint32_t c = lane; c < r[u].count; c += 16) s += sums[r[u].first + c];
+      } else {
+#pragma unroll 8
+        for (uint32_t c = lane; c < r[u].count; c += 16) s += load_shared(part + r[u].first + c);
+      }
+      s = row_sum(s);
       if (lane == 0) {
         if (norms) norms[k] = (float)sqrt(s);
         total += s;
@@ -222,20 +247,15 @@ __device__ __forceinline__ uint32_t scale_byte(float top, float* inv) {
 }
 __device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? NAN : ldexpf(1.f, (int)byte - 127); }
 
-// A lane's value moved within its row of sixteen lanes
-template <int CTRL>
-__device__ __forceinline__ uint32_t moved(uint32_t v) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
-}
 // largest magnitude of the eight lanes that hold a block (32 elements, four a lane), compared as bits: a NaN is above an
 // infinity
 __device__ __forceinline__ float block_top(const float* v) {
   uint32_t t = 0;
 #pragma unroll
   for (int k = 0; k < 4; ++k) t = max(t, __float_as_uint(v[k]) & 0x7fffffffu);
-  t = max(t, moved<0xb1>(t));          // lanes 1 0 3 2
-  t = max(t, moved<0x4e>(t));          // lanes 2 3 0 1
-  t = max(t, moved<0x141>(t));         // lanes 7 6 5 4 3 2 1 0
+  t = max(t, moved<kSwap1>(t));
+  t = max(t, moved<kSwap2>(t));
+  t = max(t, moved<kMirror8>(t));
   return __uint_as_float(t);
 }
 

@@ -43,6 +43,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {          // ne
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(fl2{a, b}, bf2));
 }
 
+// A map is read once: past the caches (nontemporal; backward of 4x64x512x512 bf16: 88 us without, 78 us with it)
+template <typename T, typename E>
+__device__ __forceinline__ T get_vector(const E* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+}
+
 // V neighbouring elements as they lie in memory
 template <typename E, int V> struct Raw;
 template <int V> struct Raw<float, V> {
@@ -50,7 +56,7 @@ template <int V> struct Raw<float, V> {
   uint32_t w[V];
   __device__ __forceinline__ void load(const float* p) {
     if constexpr (V == 4) {
-      const u4a a = *reinterpret_cast<const u4a*>(p);
+      const u4a a = get_vector<u4a>(p);
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = a[k];
     } else {
@@ -58,6 +64,7 @@ template <int V> struct Raw<float, V> {
     }
   }
   __device__ __forceinline__ float get(int k) const { return __uint_as_float(w[k]); }
+  __device__ __forceinline__ void set(int k, float v) { w[k] = __float_as_uint(v); }
   static __device__ __forceinline__ void store(float* p, const float* v) {
     if constexpr (V == 4) {
       *reinterpret_cast<u4a*>(p) = u4a{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
@@ -71,11 +78,11 @@ template <int V> struct Raw<uint16_t, V> {
   uint32_t w[(V + 1) / 2];
   __device__ __forceinline__ void load(const uint16_t* p) {
     if constexpr (V == 8) {
-      const u4a a = *reinterpret_cast<const u4a*>(p);
+      const u4a a = get_vector<u4a>(p);
 #pragma unroll
       for (int k = 0; k < 4; ++k) w[k] = a[k];
     } else if constexpr (V == 4) {
-      const u2a a = *reinterpret_cast<const u2a*>(p);
+      const u2a a = get_vector<u2a>(p);
       w[0] = a[0], w[1] = a[1];
     } else {
       w[0] = *p;
@@ -127,10 +134,8 @@ __device__ __forceinline__ void add_fwd(float x, float first, float& s, float& s
   s += d;
   s2 = fmaf(d, d, s2);
 }
-template <int ACT>
-__device__ __forceinline__ void add_bwd(float x, float dy, float mean, float rstd, float gamma, float beta, float& s, float& s2) {
+__device__ __forceinline__ void add_bwd(float xh, float dz, float& s, float& s2) {
 #pragma clang fp contract(off)
-  const float xh = normalised(x, mean, rstd), dz = through<ACT>(dy, affine(xh, gamma, beta));
   s += dz;
   s2 = fmaf(dz, xh, s2);
 }
@@ -140,15 +145,26 @@ struct Pair {            // forward: mean, squared deviations from it; backward:
   float a, b;
 };
 
-__device__ __forceinline__ float lanes_sum(float v, int width) {      // over aligned runs of `width` lanes, a power of two
-  for (int m = width / 2; m > 0; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+// A lane's value moved within its row of sixteen lanes
+template <int CTRL>
+__device__ __forceinline__ float moved(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e, kMirror8 = 0x141, kMirror16 = 0x140;     // lanes 1 0 3 2; 2 3 0 1; 7 .. 0; 15 .. 0
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+// over aligned runs of `width` lanes (4, 8, 16, 32 or 64; the same for the whole wave), in all of them
+__device__ __forceinline__ float lanes_sum(float v, int width) {
+  v += moved<kSwap1>(v);
+  v += moved<kSwap2>(v);
+  if (width == 4) return v;
+  v += moved<kMirror8>(v);
+  if (width == 8) return v;
+  v += moved<kMirror16>(v);
+  if (width == 16) return v;
+  if (width == 32) return v + __shfl_xor(v, 16);
+  return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
+__device__ __forceinline__ float wave_sum(float v) { return lanes_sum(v, 64); }
 
 // Mean and squared deviations of `count` parts of size(i) elements, `total` together.  By one wave; the same in all lanes.
 template <typename Get, typename Size>
@@ -205,15 +221,18 @@ __global__ __launch_bounds__(256) void k_gn_empty(unsigned long long* slots, int
 // Makes the compiler forget what it knows of a register: the map then starts from the elements as loaded, instead of from
 // every intermediate value of the sums kept alive across the wait (twice the registers, and spills).
 __device__ __forceinline__ void forget(uint32_t& v) { asm volatile("" : "+v"(v)); }
+template <typename R>
+__device__ __forceinline__ void forget_vector(R& r) {
+#pragma unroll
+  for (unsigned k = 0; k < sizeof(r.w) / 4; ++k) forget(r.w[k]);
+}
 template <typename R, int J>
 __device__ __forceinline__ void forget(R (&r)[J]) {
 #pragma unroll
-  for (int j = 0; j < J; ++j)
-#pragma unroll
-    for (unsigned k = 0; k < sizeof(r[j].w) / 4; ++k) forget(r[j].w[k]);
+  for (int j = 0; j < J; ++j) forget_vector(r[j]);
 }
 
-enum Mode { kFused, kSums, kMap };
+enum Mode { kFused, kSums };            // in one launch; in three: sums, join, map
 
 struct Gn {
   // the problem
@@ -223,8 +242,12 @@ struct Gn {
   int act;
   // how it is cut: `split` workgroups for each group (NCHW) or run of channels (channels last)
   int mode, split, vec, per;           // per: vectors that a lane holds of each map
-  int team, pieces;                    // NCHW: lanes of a channel's piece, pieces of a channel
+  int team_log, pieces;                // NCHW: lanes of a channel's piece (their logarithm), pieces of a channel
   size_t step;                         // NCHW: pixels of a piece (the last may have fewer)
+  // Elements (NCHW) or pixels (channels last) of a workgroup's part: every period-th has `size_last`, the others `size`.
+  // (For a split of at most 256: x / period == x * over >> 16.)
+  int period, over;
+  float size, size_last;
   int one;                             // channels last: a vector's channels are of one group
   int run, runs, rows;                 // channels last: channels of a run, runs, pixels that a workgroup holds at once
   int wait;                            // ticks (10 ns) before a workgroup does without its neighbours
@@ -237,10 +260,12 @@ struct Maps {
   Pair* part;                          // see parts_of
   unsigned long long* slots;
   uint32_t* late;
-  const float2* stat;                  // kMap: mean and rstd forward, the two means of the gradient backward
+  const float2* stat;                  // in three launches: mean and rstd forward, the two means of the gradient backward
 };
 
-__device__ __forceinline__ void put_off(const Maps& m) { m.late[1 + atomicAdd(m.late, 1u)] = blockIdx.x; }
+__device__ __forceinline__ void put_off(const Maps& m) {
+  m.late[1 + atomicAdd(m.late, 1u)] = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+}
 // ---- NCHW -----------------------------------------------------------------------------------------
 // A team of lanes (4 to 64, or the workgroup) holds one piece of one channel, `per` vectors a lane and the elements
 // beyond the last whole vector one a lane.  Unit u of a group is piece u % pieces of channel u / pieces; workgroup k
@@ -250,32 +275,36 @@ struct Nchw {
   const Gn& q;
   const Maps& m;
   size_t group;          // n * G + g
-  int lane, unit0;       // of this lane's team in workgroup 0
+  int g, lane, unit0;    // unit0: of this lane's team in workgroup 0
   // what a workgroup holds: the first unit's address (the same for all lanes), a lane's offset from there
   size_t base = 0;
   uint32_t off = 0;
-  Raw<E, V> x[J], dy[BWD ? J : 1];
+  Raw<E, V> x[J], dy[J];               // (dy: backward)
   float x1 = 0.f, dy1 = 0.f, ga = 1.f, be = 0.f, mu = 0.f, r = 0.f;
   int len = 0;           // 0: a team without a unit
 
-  __device__ __forceinline__ Nchw(const Gn& q_, const Maps& m_, size_t group_) : q(q_), m(m_), group(group_) {
-    lane = threadIdx.x % q.team;
-    unit0 = threadIdx.x / q.team;
+  __device__ __forceinline__ Nchw(const Gn& q_, const Maps& m_, size_t n, int g_) : q(q_), m(m_), g(g_) {
+    group = n * q.G + g;
+    lane = threadIdx.x & (team() - 1);
+    unit0 = threadIdx.x >> q.team_log;
   }
+  __device__ __forceinline__ int team() const { return 1 << q.team_log; }
   __device__ __forceinline__ int units() const { return q.cg * q.pieces; }
-  __device__ __forceinline__ int teams() const { return kThreads / q.team; }
-  __device__ __forceinline__ bool has(int j) const { return (lane + j * q.team) * V + V <= len; }
+  __device__ __forceinline__ int teams() const { return kThreads >> q.team_log; }
+  __device__ __forceinline__ bool has(int j) const { return (lane + (j << q.team_log)) * V + V <= len; }
   __device__ __forceinline__ bool has_tail() const { return V > 1 && lane < len % V; }
   // a lane's vector j: a scalar step from its first
   template <typename T>
-  __device__ __forceinline__ T* at(T* p, int j) const { return p + (uint32_t)(j * q.team * V) + (off + (uint32_t)lane * V); }
+  __device__ __forceinline__ T* at(T* p, int j) const { return p + (uint32_t)((j << q.team_log) * V) + (off + (uint32_t)lane * V); }
   __device__ __forceinline__ uint32_t at_tail() const { return off + (uint32_t)(len - len % V + lane); }
   __device__ __forceinline__ void place(int k) {
-    const int u0 = k * teams(), cl0 = u0 / q.pieces, piece = u0 % q.pieces;      // one piece, or pieces == 1
+    const int u0 = k * teams();                   // one piece, or pieces == 1
+    const int cl0 = q.pieces == 1 ? u0 : q.split <= kMaxSplit ? k * q.over >> 16 : k / q.pieces;
+    const int piece = q.pieces == 1 ? 0 : k - cl0 * q.pieces;
     base = (group * q.cg + cl0) * q.P + piece * q.step;
     const bool active = u0 + unit0 < units();
     const int cl = active ? unit0 : 0;
-    const int c = (int)(group % q.G) * q.cg + cl0 + cl;
+    const int c = g * q.cg + cl0 + cl;
     len = active ? (int)min(q.step, q.P - piece * q.step) : 0;
     off = (uint32_t)cl * (uint32_t)q.P;                                          // less than 512 * per * V
     if (m.gamma) ga = m.gamma[c];
@@ -297,29 +326,44 @@ struct Nchw {
       if (BWD) dy1 = Elt<E>::ld(dp + at_tail());
     }
   }
-  // elements of workgroup k's part
-  __device__ __forceinline__ float size(int k) const {
-    if (q.pieces > 1) return (float)min(q.step, q.P - (k % q.pieces) * q.step);
-    return (float)min(teams(), units() - k * teams()) * (float)q.P;
-  }
-  __device__ __forceinline__ void add_one(float xv, float dv, float first, float& s, float& s2) const {
-    if (BWD) add_bwd<ACT>(xv, dv, mu, r, ga, be, s, s2);
-    else add_fwd(xv, first, s, s2);
+  // What the map needs of an element: in fp32 the sums leave xh and dz in the registers of x and dy.
+  static constexpr bool FORM = BWD && sizeof(E) == 4;
+  __device__ __forceinline__ void form(float& xv, float& dv) const {
+    xv = normalised(xv, mu, r);
+    dv = through<ACT>(dv, affine(xv, ga, be));
   }
   // Sums of part k (taken), in all lanes.  Ends with a barrier behind every use of `red`.
   __device__ __forceinline__ Pair sums(Pair* red, int k) {
     float s = 0.f, s2 = 0.f, first = 0.f;
     if (!BWD && len) first = Elt<E>::ld(static_cast<const E*>(m.x) + base + off);
+    auto add_one = [&](float& xv, float& dv) {
+      if (BWD) {
+        form(xv, dv);
+        add_bwd(xv, dv, s, s2);
+      } else {
+        add_fwd(xv, first, s, s2);
+      }
+    };
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j))
+      if (has(j)) {
+        if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
 #pragma unroll
-        for (int e = 0; e < V; ++e) add_one(x[j].get(e), BWD ? dy[BWD ? j : 0].get(e) : 0.f, first, s, s2);
-    if (has_tail()) add_one(x1, dy1, first, s, s2);
-    const int width = min(q.team, 64);
-    s = lanes_sum(s, width);
-    s2 = lanes_sum(s2, width);
-    if (q.team > 64) {                        // one unit: its eight waves' sums belong to the same first element
+        for (int e = 0; e < V; ++e) {
+          float xv = x[j].get(e), dv = BWD ? dy[j].get(e) : 0.f;
+          add_one(xv, dv);
+          if constexpr (FORM) x[j].set(e, xv), dy[j].set(e, dv);
+        }
+        if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
+      }
+    if (has_tail()) {
+      float xv = x1, dv = dy1;
+      add_one(xv, dv);
+      if constexpr (FORM) x1 = xv, dy1 = dv;
+    }
+    s = lanes_sum(s, min(team(), 64));
+    s2 = lanes_sum(s2, min(team(), 64));
+    if (team() > 64) {                        // one unit: its eight waves' sums belong to the same first element
       if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = Pair{s, s2};
       __syncthreads();
       s = s2 = 0.f;
@@ -335,7 +379,7 @@ struct Nchw {
       const float d = s / (float)max(len, 1);
       p = Pair{first + d, s2 - s * d};
     }
-    if (q.team > 64) return p;
+    if (team() > 64) return p;
     if (len && lane == 0) red[unit0] = p;
     __syncthreads();
     const int count = min(teams(), units() - k * teams());
@@ -348,15 +392,17 @@ struct Nchw {
     __syncthreads();
     return p;
   }
+  template <bool FORMED>
   __device__ __forceinline__ float one(float xv, float dv, float a, float b) const {
     if (!BWD) return activate<ACT>(affine(normalised(xv, a, b), ga, be));
-    const float xh = normalised(xv, mu, r);
-    return r * (through<ACT>(dv, affine(xh, ga, be)) * ga - a - xh * b);
+    if (!FORMED) form(xv, dv);
+    return r * (dv * ga - a - xv * b);
   }
+  template <bool FORMED>
   __device__ __forceinline__ void vector(E* op, const Raw<E, V>& xr, const Raw<E, V>& dr, int j, float a, float b) const {
     float v[V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = one(xr.get(e), BWD ? dr.get(e) : 0.f, a, b);
+    for (int e = 0; e < V; ++e) v[e] = one<FORMED>(xr.get(e), BWD ? dr.get(e) : 0.f, a, b);
     Raw<E, V>::store(at(op, j), v);
   }
   __device__ __forceinline__ void map(float a, float b) {
@@ -365,8 +411,8 @@ struct Nchw {
     E* op = static_cast<E*>(m.out) + base;
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) vector(op, x[j], dy[BWD ? j : 0], j, a, b);
-    if (has_tail()) Elt<E>::st(op + at_tail(), one(x1, dy1, a, b));
+      if (has(j)) vector<FORM>(op, x[j], dy[j], j, a, b);
+    if (has_tail()) Elt<E>::st(op + at_tail(), one<FORM>(x1, dy1, a, b));
   }
   // the same of a part that is placed but not held
   __device__ __forceinline__ void map_from_memory(float a, float b) const {
@@ -378,11 +424,15 @@ struct Nchw {
         Raw<E, V> xr, dr = {};
         xr.load(at(xp, j));
         if (BWD) dr.load(at(dp, j));
-        vector(op, xr, dr, j, a, b);
+        vector<false>(op, xr, dr, j, a, b);
       }
-    if (has_tail()) Elt<E>::st(op + at_tail(), one(Elt<E>::ld(xp + at_tail()), BWD ? Elt<E>::ld(dp + at_tail()) : 0.f, a, b));
+    if (has_tail()) Elt<E>::st(op + at_tail(), one<false>(Elt<E>::ld(xp + at_tail()), BWD ? Elt<E>::ld(dp + at_tail()) : 0.f, a, b));
   }
 };
+
+__device__ __forceinline__ float size_of(const Gn& q, int part) {
+  return part - (part * q.over >> 16) * q.period == q.period - 1 ? q.size_last : q.size;
+}
 
 // A group's statistics (forward), or its gradient's means, from its workgroups' sums
 template <bool BWD, typename Part>
@@ -391,7 +441,7 @@ __device__ __forceinline__ Pair settle(const Part& w, const Pair* all, Pair p, s
   const float M = (float)q.cg * (float)q.P;
   if (q.split > 1) {
     if (BWD) p = add(q.split, [&](int i) { return all[i]; });
-    else p = join(q.split, M, [&](int i) { return all[i]; }, [&](int i) { return w.size(i); });
+    else p = join(q.split, M, [&](int i) { return all[i]; }, [&](int i) { return size_of(q, i); });
   }
   if (BWD) return Pair{p.a / M, p.b / M};
   p.b = 1.f / sqrtf(p.b / M + q.eps);
@@ -421,44 +471,46 @@ __global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m)
   __shared__ Pair red[kMaxTeam];
   __shared__ Pair all[kMaxSplit];
   __shared__ int missing;
-  const size_t group = blockIdx.x / q.split;
-  const int k = blockIdx.x % q.split;
-  Nchw<E, V, J, BWD, ACT> w(q, m, group);
+  const int k = blockIdx.x;
+  Nchw<E, V, J, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
   w.take(k);
-  Pair p;
-  if (q.mode == kMap) {
-    p = Pair{m.stat[group].x, m.stat[group].y};
-  } else {
-    p = w.sums(red, k);
-    if (q.mode == kSums) {
-      if (!BWD && threadIdx.x == 0) m.part[blockIdx.x] = p;
+  Pair p = w.sums(red, k);
+  if (q.mode == kSums) {
+    if (!BWD && threadIdx.x == 0) m.part[w.group * q.split + k] = p;
+    return;
+  }
+  if (q.split > 1) {
+    unsigned long long* slots = m.slots + w.group * q.split;
+    if (threadIdx.x == 0) put(slots + k, p);
+    if (!collect(slots, q.split, (long long)wall_clock64() + q.wait, all, &missing)) {
+      if (threadIdx.x == 0) put_off(m);
       return;
     }
-    if (q.split > 1) {
-      unsigned long long* slots = m.slots + group * q.split;
-      if (threadIdx.x == 0) put(slots + k, p);
-      if (!collect(slots, q.split, (long long)wall_clock64() + q.wait, all, &missing)) {
-        if (threadIdx.x == 0) put_off(m);
-        return;
-      }
-    }
-    p = settle<BWD>(w, all, p, group, k == 0);
   }
+  p = settle<BWD>(w, all, p, w.group, k == 0);
   w.map(p.a, p.b);
 }
 
-// What the launch before has put off: every slot is full now
+// The map of parts that nobody holds: of those that the launch before has put off (every slot is full now), or, in three
+// launches, of all
 template <typename E, int V, bool BWD, int ACT>
-__global__ __launch_bounds__(kThreads) void k_gn_nchw_late(Gn q, Maps m) {
+__global__ __launch_bounds__(kThreads) void k_gn_nchw_map(Gn q, Maps m) {
   __shared__ Pair all[kMaxSplit];
   __shared__ int missing;
+  if (q.mode == kSums) {
+    Nchw<E, V, 1, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
+    w.place(blockIdx.x);
+    const float2 p = m.stat[w.group];
+    w.map_from_memory(p.x, p.y);
+    return;
+  }
   for (uint32_t i = blockIdx.x; i < m.late[0]; i += gridDim.x) {
     const uint32_t wg = m.late[1 + i];
-    const size_t group = wg / q.split;
+    const uint32_t group = wg / q.split;
     const int k = wg % q.split;
-    Nchw<E, V, 1, BWD, ACT> w(q, m, group);
+    Nchw<E, V, 1, BWD, ACT> w(q, m, group / q.G, group % q.G);
     w.place(k);
-    collect(m.slots + group * q.split, q.split, 0, all, &missing);
+    collect(m.slots + (size_t)group * q.split, q.split, 0, all, &missing);
     const Pair p = settle<BWD>(w, all, Pair{}, group, k == 0);
     w.map_from_memory(p.a, p.b);
     __syncthreads();
@@ -481,7 +533,7 @@ struct Nhwc {
   // what a workgroup holds: its first pixel's address (the same for all lanes), its pixels
   size_t base = 0;
   int left = 0;
-  Raw<E, V> x[J], dy[BWD ? J : 1];
+  Raw<E, V> x[J], dy[J];               // (dy: backward)
 
   __device__ __forceinline__ Nhwc(const Gn& q_, const Maps& m_, size_t n_, int run) : q(q_), m(m_), n(n_) {
     c0 = run * q.run;
@@ -495,10 +547,6 @@ struct Nhwc {
   template <typename T>
   __device__ __forceinline__ T* at(T* p, int j) const {
     return p + (uint32_t)(j * q.rows) * (uint32_t)q.C + ((uint32_t)row * (uint32_t)q.C + (uint32_t)c);
-  }
-  __device__ __forceinline__ float count(int k) const {
-    const size_t all = (size_t)q.rows * q.per;
-    return (float)min(all, q.P - k * all);
   }
   __device__ __forceinline__ void place(int k) {
     const size_t p0 = (size_t)k * q.rows * q.per;
@@ -520,6 +568,13 @@ struct Nhwc {
   struct Scale {
     float ga[V], be[V], mean[S], rstd[S];
   };
+  // What the map needs of an element: in fp32 the sums leave xh and dz in the registers of x and dy.
+  static constexpr bool FORM = BWD && sizeof(E) == 4;
+  __device__ __forceinline__ void form(float& xv, float& dv, const Scale& t, int e) const {
+    const int h = ONE ? 0 : e;
+    xv = normalised(xv, t.mean[h], t.rstd[h]);
+    dv = through<ACT>(dv, affine(xv, t.ga[e], t.be[e]));
+  }
   __device__ __forceinline__ Scale scale() const {
     Scale s;
 #pragma unroll
@@ -543,13 +598,21 @@ struct Nhwc {
     else if (in) first.load(static_cast<const E*>(m.x) + base + c);
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j))
+      if (has(j)) {
+        if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-          const int h = ONE ? 0 : e;
-          if (BWD) add_bwd<ACT>(x[j].get(e), dy[BWD ? j : 0].get(e), t.mean[h], t.rstd[h], t.ga[e], t.be[e], s[e], s2[e]);
-          else add_fwd(x[j].get(e), first.get(e), s[e], s2[e]);
+          float xv = x[j].get(e), dv = BWD ? dy[j].get(e) : 0.f;
+          if (BWD) {
+            form(xv, dv, t, e);
+            add_bwd(xv, dv, s[e], s2[e]);
+            if constexpr (FORM) x[j].set(e, xv), dy[j].set(e, dv);
+          } else {
+            add_fwd(xv, first.get(e), s[e], s2[e]);
+          }
         }
+        if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
+      }
     __syncthreads();
     if (in)
 #pragma unroll
@@ -571,7 +634,7 @@ struct Nhwc {
       Pair t = {0.f, 0.f};
       for (int j = 0; j < rows; ++j) t.a += buf[j * q.run + i].a, t.b += buf[j * q.run + i].b;
       if (!BWD) {
-        const float d = t.a / count(k);
+        const float d = t.a / size_of(q, k);
         t = Pair{Elt<E>::ld(static_cast<const E*>(m.x) + base + i) + d, t.b - t.a * d};
       }
       out[i] = t;
@@ -579,16 +642,18 @@ struct Nhwc {
     __syncthreads();
   }
   // stat(e): the group of this lane's channel e
+  template <bool FORMED>
   __device__ __forceinline__ void vector(E* op, const Raw<E, V>& xr, const Raw<E, V>& dr, int j, const Scale& t, const Pair* p) const {
     float v[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
       const int h = ONE ? 0 : e;
+      float xv = xr.get(e), dv = BWD ? dr.get(e) : 0.f;
       if (!BWD) {
-        v[e] = activate<ACT>(affine(normalised(xr.get(e), p[h].a, p[h].b), t.ga[e], t.be[e]));
+        v[e] = activate<ACT>(affine(normalised(xv, p[h].a, p[h].b), t.ga[e], t.be[e]));
       } else {
-        const float xh = normalised(xr.get(e), t.mean[h], t.rstd[h]);
-        v[e] = t.rstd[h] * (through<ACT>(dr.get(e), affine(xh, t.ga[e], t.be[e])) * t.ga[e] - p[h].a - xh * p[h].b);
+        if (!FORMED) form(xv, dv, t, e);
+        v[e] = t.rstd[h] * (dv * t.ga[e] - p[h].a - xv * p[h].b);
       }
     }
     Raw<E, V>::store(at(op, j), v);
@@ -604,7 +669,7 @@ struct Nhwc {
     for (int e = 0; e < S; ++e) p[e] = stat(e);
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) vector(op, x[j], dy[BWD ? j : 0], j, t, p);
+      if (has(j)) vector<FORM>(op, x[j], dy[j], j, t, p);
   }
   // the same of a part that is placed but not held
   template <typename Stat>
@@ -621,7 +686,7 @@ struct Nhwc {
         Raw<E, V> xr, dr = {};
         xr.load(at(xp, j));
         if (BWD) dr.load(at(dp, j));
-        vector(op, xr, dr, j, t, p);
+        vector<false>(op, xr, dr, j, t, p);
       }
   }
 };
@@ -636,7 +701,7 @@ __device__ __forceinline__ Pair of_group(const Part& w, const Pair* chan, int g,
       const float ga = w.m.gamma ? w.m.gamma[w.c0 + g * cg + i] : 1.f;
       return Pair{chan[i].a * ga, chan[i].b * ga};
     });
-  const float each = w.count(part);
+  const float each = size_of(w.q, part);
   return join(cg, each * (float)cg, [&](int i) { return chan[i]; }, [&](int) { return each; });
 }
 
@@ -649,7 +714,7 @@ __device__ __forceinline__ void settle(const Part& w, const Pair* all, Pair* sta
   for (int g = threadIdx.x / 64; g < groups; g += kWaves) {
     Pair p;
     if (BWD) p = add(q.split, [&](int i) { return all[i * groups + g]; });
-    else p = join(q.split, M, [&](int i) { return all[i * groups + g]; }, [&](int i) { return w.count(i) * (float)q.cg; });
+    else p = join(q.split, M, [&](int i) { return all[i * groups + g]; }, [&](int i) { return size_of(q, i) * (float)q.cg; });
     if (BWD) p = Pair{p.a / M, p.b / M};
     else p.b = 1.f / sqrtf(p.b / M + q.eps);
     if (threadIdx.x % 64 == 0) {
@@ -668,43 +733,45 @@ __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
   __shared__ Pair all[kMaxSlots];             // [part][group]
   __shared__ Pair chan[kMaxRun];
   __shared__ int missing;
-  const size_t cluster = blockIdx.x / q.split;
-  const int k = blockIdx.x % q.split, run = (int)(cluster % q.runs);
+  const int k = blockIdx.x, run = blockIdx.y;
   const int groups = q.run / q.cg;            // (kFused)
-  Nhwc<E, V, J, ONE, BWD, ACT> w(q, m, cluster / q.runs, run);
+  Nhwc<E, V, J, ONE, BWD, ACT> w(q, m, blockIdx.z, run);
   w.take(k);
-  if (q.mode != kMap) {
-    w.sums(buf, chan, k);
-    if (BWD || q.mode == kSums)
-      for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + k) * q.C + w.c0 + i] = chan[i];
-    if (q.mode == kSums) return;
-    unsigned long long* slots = m.slots + cluster * q.split * groups;
-    for (int g = threadIdx.x / 64; g < groups; g += kWaves) {
-      const Pair p = of_group<BWD>(w, chan, g, k);
-      if (threadIdx.x % 64 == 0) {
-        if (q.split > 1) put(slots + k * groups + g, p);
-        else all[g] = p;
-      }
+  w.sums(buf, chan, k);
+  if (BWD || q.mode == kSums)
+    for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + k) * q.C + w.c0 + i] = chan[i];
+  if (q.mode == kSums) return;
+  unsigned long long* slots = m.slots + ((size_t)blockIdx.z * q.runs + run) * q.split * groups;
+  for (int g = threadIdx.x / 64; g < groups; g += kWaves) {
+    const Pair p = of_group<BWD>(w, chan, g, k);
+    if (threadIdx.x % 64 == 0) {
+      if (q.split > 1) put(slots + k * groups + g, p);
+      else all[g] = p;
     }
-    if (q.split > 1 && !collect(slots, q.split * groups, (long long)wall_clock64() + q.wait, all, &missing)) {
-      if (threadIdx.x == 0) put_off(m);
-      return;
-    }
-    settle<BWD>(w, all, chan, run, groups, k == 0);
   }
-  w.map([&](int e) {
-    if (q.mode != kMap) return chan[min(w.c + e, w.width - 1) / q.cg];
-    const float2 s = m.stat[w.group(e)];
-    return Pair{s.x, s.y};
-  });
+  if (q.split > 1 && !collect(slots, q.split * groups, (long long)wall_clock64() + q.wait, all, &missing)) {
+    if (threadIdx.x == 0) put_off(m);
+    return;
+  }
+  settle<BWD>(w, all, chan, run, groups, k == 0);
+  w.map([&](int e) { return chan[min(w.c + e, w.width - 1) / q.cg]; });
 }
 
-// What the launch before has put off: every slot is full now
+// As k_gn_nchw_map
 template <typename E, int V, bool ONE, bool BWD, int ACT>
-__global__ __launch_bounds__(kThreads) void k_gn_nhwc_late(Gn q, Maps m) {
+__global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
   __shared__ Pair all[kMaxSlots];
   __shared__ Pair chan[kMaxRun];
   __shared__ int missing;
+  if (q.mode == kSums) {
+    Nhwc<E, V, 1, ONE, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
+    w.place(blockIdx.x);
+    w.map_from_memory([&](int e) {
+      const float2 s = m.stat[w.group(e)];
+      return Pair{s.x, s.y};
+    });
+    return;
+  }
   const int groups = q.run / q.cg;
   for (uint32_t i = blockIdx.x; i < m.late[0]; i += gridDim.x) {
     const uint32_t wg = m.late[1 + i];
@@ -741,7 +808,7 @@ __global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ pa
       const size_t all = (size_t)q.rows * q.per;
       return (double)min(all, q.P - i * all);
     }
-    const int teams = kThreads / q.team;
+    const int teams = kThreads >> q.team_log;
     return q.pieces > 1 ? (double)min(q.step, q.P - (i % q.pieces) * q.step) : (double)min(teams, q.cg - i * teams) * (double)q.P;
   };
   double s = 0, s2 = 0;
@@ -805,7 +872,7 @@ __global__ __launch_bounds__(256) void k_gn_bwd_join(const Pair* __restrict__ pa
 std::atomic<int> g_wait{10000};        // 100 us
 
 bool shaped(int N, int C, size_t P, int groups) {
-  return N >= 1 && C >= 1 && P >= 1 && groups >= 1 && groups <= C && C % groups == 0 && P < (1ull << 31) && C <= (1 << 20) &&
+  return N >= 1 && C >= 1 && P >= 1 && groups >= 1 && groups <= C && C % groups == 0 && P < (1ull << 31) && N < 65536 && groups < 65536 && C <= (1 << 20) &&
          (size_t)N * C < (1ull << 31) && (size_t)N * C * P < (1ull << 46);
 }
 
@@ -820,18 +887,22 @@ Gn cut_nchw(Gn q, int elem, int per) {
   per = q.per;
   const size_t vectors = std::max<size_t>(1, q.P / q.vec);
   if (vectors <= 64u * per) {                     // a team of a wave or less holds a channel
-    q.team = 4;
-    while ((size_t)q.team * per < vectors || q.team < q.vec) q.team *= 2;
+    q.team_log = 2;
+    while (((size_t)per << q.team_log) < vectors || 1 << q.team_log < q.vec) ++q.team_log;
     q.pieces = 1;
     q.step = q.P;
   } else {
-    q.team = kThreads;
+    q.team_log = 9;
+    static_assert(kThreads == 1 << 9, "");
     q.pieces = (int)ceil_div(vectors, (size_t)kThreads * per);
     q.step = ceil_div(vectors, q.pieces) * q.vec;
     if (q.pieces == 1) q.step = q.P;
   }
-  const size_t split = ceil_div((size_t)q.cg * q.pieces, kThreads / q.team);
-  q.split = (int)split;
+  const int teams = kThreads >> q.team_log;
+  q.split = (int)ceil_div((size_t)q.cg * q.pieces, teams);
+  q.period = q.pieces > 1 ? q.pieces : q.split;
+  q.size = q.pieces > 1 ? (float)q.step : (float)teams * (float)q.P;
+  q.size_last = q.pieces > 1 ? (float)(q.P - (q.pieces - 1) * q.step) : (float)(q.cg - (q.split - 1) * teams) * (float)q.P;
   return q;
 }
 
@@ -856,6 +927,9 @@ Gn cut_nhwc(Gn q, int elem, int per) {
   q.runs = (int)ceil_div(q.C, q.run);
   q.rows = kThreads / (q.run / q.vec);
   q.split = (int)ceil_div(q.P, (size_t)q.rows * per);
+  q.period = q.split;
+  q.size = (float)(q.rows * per);
+  q.size_last = (float)(q.P - (size_t)(q.split - 1) * q.rows * per);
   return q;
 }
 
@@ -878,6 +952,7 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem) {
     }
   const size_t slots = (size_t)best.split * (layout == TRAIN_NHWC ? best.run / best.cg : 1);
   if (best.mode == kFused && (best.split > kMaxSplit || slots > (size_t)kMaxSlots)) best.mode = kSums;
+  best.over = 65536 / best.period + 1;
   return best;
 }
 
@@ -903,23 +978,23 @@ bool known(int act, int layout) {
 
 typedef void (*Kernel)(Gn, Maps);
 struct Kernels {
-  Kernel main, late;
+  Kernel main, map;
 };
 template <typename E, bool BWD, int ACT>
 Kernels pick_of(const Gn& q, int layout) {
   constexpr int full = 16 / sizeof(E);
   if (layout == TRAIN_NCHW) {
-    if (q.vec == 1) return {k_gn_nchw<E, 1, 2, BWD, ACT>, k_gn_nchw_late<E, 1, BWD, ACT>};
+    if (q.vec == 1) return {k_gn_nchw<E, 1, 2, BWD, ACT>, k_gn_nchw_map<E, 1, BWD, ACT>};
     return {q.per == 8 ? k_gn_nchw<E, full, 8, BWD, ACT> : q.per == 4 ? k_gn_nchw<E, full, 4, BWD, ACT> : k_gn_nchw<E, full, 2, BWD, ACT>,
-            k_gn_nchw_late<E, full, BWD, ACT>};
+            k_gn_nchw_map<E, full, BWD, ACT>};
   }
-  if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_late<E, 1, true, BWD, ACT>};
+  if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_map<E, 1, true, BWD, ACT>};
   if (!q.one)
-    return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_late<E, 4, false, BWD, ACT>};
+    return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 4, false, BWD, ACT>};
   return {q.per == 8   ? k_gn_nhwc<E, full, 8, true, BWD, ACT>
           : q.per == 4 ? k_gn_nhwc<E, full, 4, true, BWD, ACT>
                        : k_gn_nhwc<E, full, 2, true, BWD, ACT>,
-          k_gn_nhwc_late<E, full, true, BWD, ACT>};
+          k_gn_nhwc_map<E, full, true, BWD, ACT>};
 }
 template <typename E, bool BWD>
 Kernels pick(const Gn& q, int layout) {
@@ -932,18 +1007,17 @@ Kernels pick(const Gn& q, int layout) {
 template <typename E, bool BWD, typename Join>
 void launch(Gn q, Maps m, int layout, hipStream_t st, Join join) {
   const Kernels kernel = pick<E, BWD>(q, layout);
-  const unsigned grid = (unsigned)workgroups(q, layout);
+  const dim3 grid(q.split, layout == TRAIN_NHWC ? q.runs : q.G, q.N);
   if (q.mode == kFused) {
     const size_t n = slots_of(q, layout);
     if (n) k_gn_empty<<<(unsigned)std::min<size_t>(ceil_div(n, 256), 256), 256, 0, st>>>(m.slots, (int)n, m.late);
     kernel.main<<<grid, kThreads, 0, st>>>(q, m);
-    if (n) kernel.late<<<std::min(grid, 64u), kThreads, 0, st>>>(q, m);
+    if (n) kernel.map<<<(unsigned)std::min<size_t>(workgroups(q, layout), 64), kThreads, 0, st>>>(q, m);
     return;
   }
   kernel.main<<<grid, kThreads, 0, st>>>(q, m);
   join();
-  q.mode = kMap;
-  kernel.main<<<grid, kThreads, 0, st>>>(q, m);
+  kernel.map<<<grid, kThreads, 0, st>>>(q, m);
 }
 
 struct Scratch {
@@ -973,7 +1047,7 @@ int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, fl
   Gn q = cut(N, C, P, groups, layout, sizeof(E));
   q.eps = eps, q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
   if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
-  if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
+  if (q.split >= 1 << 22) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Scratch s(q, layout, ws);
   const Maps m{x, nullptr, y, gamma, beta, mean, rstd, s.part, s.slots, s.late, s.stat};
@@ -996,7 +1070,7 @@ int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const fl
   Gn q = cut(N, C, P, groups, layout, sizeof(E));
   q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
   if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
-  if (workgroups(q, layout) > 0x7fffffffu || slots_of(q, layout) > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
+  if (q.split >= 1 << 22) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Scratch s(q, layout, ws);
   const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), s.part, s.slots, s.late, s.stat};
