@@ -257,6 +257,7 @@ struct Maps {
   void* out;                           // y or dx
   const float *gamma, *beta;
   float *mean, *rstd;                  // written forward (or NULL), read backward
+  float *dgamma, *dbeta;               // backward, or NULL
   Pair* part;                          // see parts_of
   unsigned long long* slots;
   uint32_t* late;
@@ -266,6 +267,34 @@ struct Maps {
 __device__ __forceinline__ void put_off(const Maps& m) {
   m.late[1 + atomicAdd(m.late, 1u)] = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
 }
+struct Parts {           // where the sums of part i of channel (NCHW forward: of group) c of image n lie
+  int nhwc, per;
+  size_t C;
+  __device__ __forceinline__ size_t at(size_t n, size_t c, int i) const {
+    return nhwc ? (n * per + i) * C + c : (n * C + c) * per + i;
+  }
+};
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+// dbeta and dgamma of channel c, by one wave
+__device__ __forceinline__ void channel_gradient(const Gn& q, const Maps& m, const Parts& where, size_t c) {
+  double s1 = 0, s2 = 0;
+  for (int i = threadIdx.x % 64; i < q.N * where.per; i += 64) {
+    const Pair p = m.part[where.at(i / where.per, c, i % where.per)];
+    s1 += p.a;
+    s2 += p.b;
+  }
+  s1 = wave_sum(s1);
+  s2 = wave_sum(s2);
+  if (threadIdx.x % 64) return;
+  if (m.dbeta) m.dbeta[c] = (float)s1;
+  if (m.dgamma) m.dgamma[c] = (float)s2;
+}
+
 // ---- NCHW -----------------------------------------------------------------------------------------
 // A team of lanes (4 to 64, or the workgroup) holds one piece of one channel, `per` vectors a lane and the elements
 // beyond the last whole vector one a lane.  Unit u of a group is piece u % pieces of channel u / pieces; workgroup k
@@ -492,7 +521,7 @@ __global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m)
 }
 
 // The map of parts that nobody holds: of those that the launch before has put off (every slot is full now), or, in three
-// launches, of all
+// launches, of all.  Behind one launch also the channels' gradients, which need every part's sums.
 template <typename E, int V, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads) void k_gn_nchw_map(Gn q, Maps m) {
   __shared__ Pair all[kMaxSplit];
@@ -504,7 +533,11 @@ __global__ __launch_bounds__(kThreads) void k_gn_nchw_map(Gn q, Maps m) {
     w.map_from_memory(p.x, p.y);
     return;
   }
-  for (uint32_t i = blockIdx.x; i < m.late[0]; i += gridDim.x) {
+  if (BWD && (m.dgamma || m.dbeta))
+    for (size_t c = blockIdx.x * kWaves + threadIdx.x / 64; c < (size_t)q.C; c += gridDim.x * kWaves)
+      channel_gradient(q, m, Parts{0, q.pieces, (size_t)q.C}, c);
+  const uint32_t count = q.split > 1 ? m.late[0] : 0;
+  for (uint32_t i = blockIdx.x; i < count; i += gridDim.x) {
     const uint32_t wg = m.late[1 + i];
     const uint32_t group = wg / q.split;
     const int k = wg % q.split;
@@ -772,8 +805,12 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
     });
     return;
   }
+  if (BWD && (m.dgamma || m.dbeta))
+    for (size_t c = blockIdx.x * kWaves + threadIdx.x / 64; c < (size_t)q.C; c += gridDim.x * kWaves)
+      channel_gradient(q, m, Parts{1, q.split, (size_t)q.C}, c);
   const int groups = q.run / q.cg;
-  for (uint32_t i = blockIdx.x; i < m.late[0]; i += gridDim.x) {
+  const uint32_t count = q.split > 1 ? m.late[0] : 0;
+  for (uint32_t i = blockIdx.x; i < count; i += gridDim.x) {
     const uint32_t wg = m.late[1 + i];
     const size_t cluster = wg / q.split;
     const int k = wg % q.split, run = (int)(cluster % q.runs);
@@ -787,14 +824,6 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
 }
 
 // ---- joins of three-launch runs, and the channels' gradients --------------------------------------
-struct Parts {           // where the sums of part i of channel (NCHW forward: of group) c of image n lie
-  int nhwc, per;
-  size_t C;
-  __device__ __forceinline__ size_t at(size_t n, size_t c, int i) const {
-    return nhwc ? (n * per + i) * C + c : (n * C + c) * per + i;
-  }
-};
-
 // One wave a group of one image
 __global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ part, float* __restrict__ mean,
                                                      float* __restrict__ rstd, float2* __restrict__ stat, Gn q, Parts where) {
@@ -813,15 +842,12 @@ __global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ pa
   };
   double s = 0, s2 = 0;
   for (int i = threadIdx.x % 64; i < chans * q.split; i += 64) s += size(i / chans) * part[where.at(n, c0 + i % chans, i / chans)].a;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d);
-  const double mu = s / M;
+  const double mu = wave_sum(s) / M;
   for (int i = threadIdx.x % 64; i < chans * q.split; i += 64) {
     const Pair p = part[where.at(n, c0 + i % chans, i / chans)];
     s2 += p.b + size(i / chans) * (p.a - mu) * (p.a - mu);
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) s2 += __shfl_xor(s2, d);
+  s2 = wave_sum(s2);
   if (threadIdx.x % 64) return;
   const float r = (float)(1.0 / sqrt(s2 / M + (double)q.eps));
   stat[g] = make_float2((float)mu, r);
@@ -829,43 +855,26 @@ __global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ pa
   if (rstd) rstd[g] = r;
 }
 
-// The first `groups` waves: a group's two means.  The next C waves: a channel's dbeta and dgamma.
-__global__ __launch_bounds__(256) void k_gn_bwd_join(const Pair* __restrict__ part, const float* __restrict__ gamma,
-                                                     float* __restrict__ dgamma, float* __restrict__ dbeta,
-                                                     float2* __restrict__ stat, Gn q, Parts where, size_t groups) {
-  const size_t w = (size_t)blockIdx.x * 4 + threadIdx.x / 64;
-  double s1 = 0, s2 = 0;
-  if (w < groups) {
-    const size_t c0 = w % q.G * q.cg;
-    for (int i = threadIdx.x % 64; i < q.cg * where.per; i += 64) {
-      const size_t c = where.nhwc ? i % q.cg : i / where.per;
-      const Pair p = part[where.at(w / q.G, c0 + c, where.nhwc ? i / q.cg : i % where.per)];
-      const double ga = gamma ? gamma[c0 + c] : 1.f;
-      s1 += p.a * ga;
-      s2 += p.b * ga;
-    }
-  } else if (w - groups < (size_t)q.C) {
-    for (int i = threadIdx.x % 64; i < q.N * where.per; i += 64) {
-      const Pair p = part[where.at(i / where.per, w - groups, i % where.per)];
-      s1 += p.a;
-      s2 += p.b;
-    }
-  } else {
+// The first N * G waves: a group's two means.  The next C waves: a channel's dbeta and dgamma.
+__global__ __launch_bounds__(256) void k_gn_bwd_join(Gn q, Maps m, Parts where, float2* __restrict__ stat) {
+  const size_t w = (size_t)blockIdx.x * 4 + threadIdx.x / 64, groups = (size_t)q.N * q.G;
+  if (w >= groups) {
+    if (w - groups < (size_t)q.C) channel_gradient(q, m, where, w - groups);
     return;
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    s1 += __shfl_xor(s1, d);
-    s2 += __shfl_xor(s2, d);
+  double s1 = 0, s2 = 0;
+  const size_t c0 = w % q.G * q.cg;
+  for (int i = threadIdx.x % 64; i < q.cg * where.per; i += 64) {
+    const size_t c = where.nhwc ? i % q.cg : i / where.per;
+    const Pair p = m.part[where.at(w / q.G, c0 + c, where.nhwc ? i / q.cg : i % where.per)];
+    const double ga = m.gamma ? m.gamma[c0 + c] : 1.f;
+    s1 += p.a * ga;
+    s2 += p.b * ga;
   }
-  if (threadIdx.x % 64) return;
-  if (w < groups) {
-    const double M = (double)q.cg * (double)q.P;
-    stat[w] = make_float2((float)(s1 / M), (float)(s2 / M));
-  } else {
-    if (dbeta) dbeta[w - groups] = (float)s1;
-    if (dgamma) dgamma[w - groups] = (float)s2;
-  }
+  s1 = wave_sum(s1);
+  s2 = wave_sum(s2);
+  const double M = (double)q.cg * (double)q.P;
+  if (threadIdx.x % 64 == 0) stat[w] = make_float2((float)(s1 / M), (float)(s2 / M));
 }
 
 // ---- host -----------------------------------------------------------------------------------------
@@ -1012,7 +1021,7 @@ void launch(Gn q, Maps m, int layout, hipStream_t st, Join join) {
     const size_t n = slots_of(q, layout);
     if (n) k_gn_empty<<<(unsigned)std::min<size_t>(ceil_div(n, 256), 256), 256, 0, st>>>(m.slots, (int)n, m.late);
     kernel.main<<<grid, kThreads, 0, st>>>(q, m);
-    if (n) kernel.map<<<(unsigned)std::min<size_t>(workgroups(q, layout), 64), kThreads, 0, st>>>(q, m);
+    if (n || (BWD && (m.dgamma || m.dbeta))) kernel.map<<<64, kThreads, 0, st>>>(q, m);
     return;
   }
   kernel.main<<<grid, kThreads, 0, st>>>(q, m);
@@ -1050,7 +1059,7 @@ int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, fl
   if (q.split >= 1 << 22) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Scratch s(q, layout, ws);
-  const Maps m{x, nullptr, y, gamma, beta, mean, rstd, s.part, s.slots, s.late, s.stat};
+  const Maps m{x, nullptr, y, gamma, beta, mean, rstd, nullptr, nullptr, s.part, s.slots, s.late, s.stat};
   launch<E, false>(q, m, layout, st, [&] {
     const Parts where{layout, q.split, (size_t)(layout == TRAIN_NHWC ? C : groups)};
     k_gn_fwd_join<<<(unsigned)ceil_div((size_t)N * groups, 4), 256, 0, st>>>(s.part, mean, rstd, s.stat, q, where);
@@ -1073,13 +1082,11 @@ int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const fl
   if (q.split >= 1 << 22) return ROTCONV_ERR_SHAPE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const Scratch s(q, layout, ws);
-  const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), s.part, s.slots, s.late, s.stat};
-  const Parts where{layout, layout == TRAIN_NHWC ? q.split : q.pieces, (size_t)C};
-  auto join = [&](size_t g) {
-    k_gn_bwd_join<<<(unsigned)ceil_div(g + C, 4), 256, 0, st>>>(s.part, gamma, dgamma, dbeta, s.stat, q, where, g);
-  };
-  launch<E, true>(q, m, layout, st, [&] { join((size_t)N * groups); });
-  if (q.mode == kFused && (dgamma || dbeta)) join(0);
+  const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), dgamma, dbeta, s.part, s.slots, s.late, s.stat};
+  launch<E, true>(q, m, layout, st, [&] {
+    const Parts where{layout, layout == TRAIN_NHWC ? q.split : q.pieces, (size_t)C};
+    k_gn_bwd_join<<<(unsigned)ceil_div((size_t)N * groups + C, 4), 256, 0, st>>>(q, m, where, s.stat);
+  });
   return finish();
 }
 
