@@ -1,6 +1,10 @@
 """The optimiser's side of a training step: the norm and clip factor of all gradients, and AdamW over all parameters,
 through the C-ABI library (include/unettrain.h).  This module only owns the device buffers (torch tensors as plain
 memory) and the order of the calls; no arithmetic of the method happens here.
+
+    python -m paper_2512_08888_amd.train [--steps 60] [--dtype bf16] [--state mx8] [--graph]
+
+trains a small stack with group norms (paper_2512_08888_amd/unet.py) on one synthetic batch and prints its loss.
 """
 from __future__ import annotations
 
@@ -95,3 +99,42 @@ class AdamW(_Control):
                 raise ValueError(f"load_state: {name} must be {mine[name].dtype} with {mine[name].numel()} elements")
             mine[name].view(torch.uint8).copy_(t.reshape(-1).view(torch.uint8))
         self.step_count.fill_(int(step))
+
+
+def main(argv=None):
+    """A stack of two levels learns to tell the quadrants of its images apart (labels by pixel position and brightness):
+    group norm, clipping and AdamW as a training program uses them.  Returns the losses."""
+    import argparse
+
+    import numpy as np
+    import torch
+
+    from . import unet
+
+    ap = argparse.ArgumentParser(description=main.__doc__)
+    ap.add_argument("--steps", type=int, default=60)
+    ap.add_argument("--dtype", choices=("f32", "bf16"), default="f32")
+    ap.add_argument("--state", choices=sorted(rc.STATES), default="f32")
+    ap.add_argument("--lr", type=float, default=3e-3)
+    ap.add_argument("--graph", action="store_true", help="record the step into a HIP graph and replay it")
+    a = ap.parse_args(argv)
+    cfg = unet.UNetConfig("train", 2, 3, 64, 64, (16, 32, 64), 4, R=4, norm_groups=8, seed=11)
+    net = unet.UNet(cfg, unet.make_params(cfg), dtype=a.dtype)
+    images, _ = unet.make_batch(cfg)
+    labels = (images.mean(1) > 0.5).astype(np.int32) + 2 * (np.arange(cfg.W) >= cfg.W // 2).astype(np.int32)
+    net.load_batch(images, labels)
+    opt = net.optimizer(lr=a.lr, weight_decay=0.01, state=a.state)
+    if a.graph:
+        net.capture(opt, max_norm=1.0)
+    losses = []
+    for k in range(a.steps):
+        loss = net.replay() if a.graph else net.train_step(opt, max_norm=1.0)
+        if k % 10 == 0 or k == a.steps - 1:
+            losses.append(float(loss.cpu()[0]))
+            print(f"step {k:4d}  loss {losses[-1]:.4f}  gradient norm {opt.norm.item():.4f}  clipped by {opt.coef.item():.3f}", flush=True)
+    torch.cuda.synchronize()
+    return losses
+
+
+if __name__ == "__main__":
+    main()

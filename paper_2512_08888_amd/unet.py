@@ -4,10 +4,12 @@ entirely through the C-ABI library: this module only owns the device buffers (to
 plain memory), the per-layer plans and the order of the calls.
 
     Block(a->b) = rotconv_pool(a->b) + ReLU, rotconv_pool(b->b) + ReLU        (3x3, pad 1)
+                  with norm_groups: group norm + ReLU behind each rotation convolution
     encoder: Block, 2x2 max-pool per level; bottleneck Block; decoder per level: 2x2 stride-2
     transposed convolution, concat [skip, up], Block; 1x1 head; mean soft-max cross-entropy.
 
-No arithmetic happens here and nothing falls back to torch ops.
+UNet.optimizer() and UNet.train_step() close the step: the gradients' norm, clipping and AdamW over all parameters
+(paper_2512_08888_amd/train.py).  No arithmetic happens here and nothing falls back to torch ops.
 """
 from __future__ import annotations
 
@@ -38,6 +40,11 @@ class UNetConfig:
     # pooling over the 4 quarter turns of each first-quadrant angle (R/4 features per filter, so
     # width / (R/4) filters), the second a standard convolution (R = 1 through the same library).
     block: str = "rot_rot"
+    # 0: none, as in the paper.  Else every rotation convolution is followed by a group norm of this many groups with a
+    # learned scale and shift for each channel, and the ReLU comes behind that.  (Normalising pooled responses keeps the
+    # stack's rotation invariance: a turn permutes a channel's pixels.)
+    norm_groups: int = 0
+    norm_eps: float = 1e-5
 
     @property
     def depth(self):
@@ -102,13 +109,23 @@ def param_shapes(cfg: UNetConfig) -> Dict[str, Tuple[int, ...]]:
     for lvl in range(cfg.depth):
         shapes[f"up{lvl}"] = (cfg.widths[lvl + 1], cfg.widths[lvl], 2, 2)
     shapes["head"] = (cfg.classes, cfg.widths[0])
+    if cfg.norm_groups:
+        for sp in layer_specs(cfg):
+            shapes[sp["name"] + ".gamma"] = shapes[sp["name"] + ".beta"] = (sp["width"],)
     return shapes
 
 
+def _is_norm(name):
+    return name.endswith((".gamma", ".beta"))
+
+
 def make_params(cfg: UNetConfig) -> Dict[str, np.ndarray]:
-    """He-normal parameters sqrt(2 / fan_in) from the counter-based generator (fp32 values)."""
+    """He-normal parameters sqrt(2 / fan_in) from the counter-based generator (fp32 values); group norms' scales 1, shifts 0."""
     out = {}
-    for i, (name, shp) in enumerate(sorted(param_shapes(cfg).items())):
+    shapes = param_shapes(cfg)
+    for name in filter(_is_norm, sorted(shapes)):
+        out[name] = np.full(shapes[name], 1.0 if name.endswith(".gamma") else 0.0, dtype=np.float32)
+    for i, (name, shp) in enumerate(sorted((n, s) for n, s in shapes.items() if not _is_norm(n))):
         fan_in = shp[1] if name == "head" else shp[0] if name.startswith("up") else shp[2] * 9
         n = int(np.prod(shp))
         v = synth.normal01(cfg.seed * 1000 + i, n) * np.sqrt(2.0 / fan_in)
@@ -144,7 +161,8 @@ class UNet:
         if dtype not in ("f32", "bf16"):
             raise ValueError("dtype must be 'f32' or 'bf16'")
         self.dtype = dtype
-        self.fuse_relu = bool(fuse_relu)
+        self.norm = cfg.norm_groups
+        self.fuse_relu = bool(fuse_relu) and not self.norm      # with a norm, the ReLU is the norm's activation
         f32, u8 = torch.float32, torch.uint8
         adt = torch.bfloat16 if dtype == "bf16" else f32      # storage type of activations and parameters
         self.adt = adt
@@ -169,6 +187,13 @@ class UNet:
             ws_bytes = max(ws_bytes, p.workspace_bytes)
             self.act[name] = dict(y=buf(N, p.Cpooled, h, w), idx=buf(N, p.Cpooled, h, w, dtype=u8),
                                   g=buf(N, p.Cpooled, h, w))
+            if self.norm:
+                # pooled responses before the norm, their gradient, and the statistics that the backward pass needs
+                self.act[name].update(pre=buf(N, p.Cpooled, h, w), gpre=buf(N, p.Cpooled, h, w),
+                                      mean=buf(N, self.norm, dtype=f32), rstd=buf(N, self.norm, dtype=f32))
+                if sp["width"] % self.norm:
+                    raise ValueError(f"{name}: norm_groups must divide the layer width {sp['width']}")
+                ws_bytes = max(ws_bytes, rc.train_groupnorm_workspace_bytes(N, sp["width"], h * w, self.norm))
             if p.Cpooled != sp["width"]:
                 raise ValueError(f"{name}: pooled channel count {p.Cpooled} differs from the layer width {sp['width']}")
         h, w = cfg.H, cfg.W
@@ -190,7 +215,9 @@ class UNet:
         self._where = ""
         self.images = buf(N, cfg.Cin, cfg.H, cfg.W)
         self.labels = buf(N, cfg.H, cfg.W, dtype=torch.int32)
-        self.params = {n: buf(*s) for n, s in param_shapes(cfg).items()}
+        # a norm's scale and shift are fp32 whatever the storage type
+        self.params = {n: buf(*s, dtype=f32 if _is_norm(n) else adt) for n, s in param_shapes(cfg).items()}
+        self.masters = self.params          # what an optimizer updates: see optimizer()
         self.grads = {n: buf(*s, dtype=f32) for n, s in param_shapes(cfg).items()}
         if params is not None:
             self.load_params(params)
@@ -212,7 +239,10 @@ class UNet:
     # ---- host <-> device plumbing -------------------------------------------------------------
     def load_params(self, params):
         for n, t in self.params.items():
-            t.copy_(self.torch.from_numpy(np.ascontiguousarray(params[n], dtype=np.float32)))   # rounds if bf16
+            v = self.torch.from_numpy(np.ascontiguousarray(params[n], dtype=np.float32))
+            t.copy_(v)                      # rounds if bf16
+            if self.masters[n] is not t:
+                self.masters[n].copy_(v)
 
     def load_batch(self, images, labels):
         self.images.copy_(self.torch.from_numpy(np.ascontiguousarray(images, dtype=np.float32)))
@@ -236,9 +266,13 @@ class UNet:
         self._where = name
         a = self.act[name]
         a["x"] = x
-        self._c("rotconv_pool_fwd", rc.rotconv_pool_fwd, self.plans[name], x, self.params[name], a["y"], a["idx"],
-                self.ws)
-        if not self.fuse_relu:
+        self._c("rotconv_pool_fwd", rc.rotconv_pool_fwd, self.plans[name], x, self.params[name], a["pre" if self.norm else "y"],
+                a["idx"], self.ws)
+        if self.norm:
+            self._c("train_groupnorm_fwd", rc.train_groupnorm_fwd, a["pre"], self.params[name + ".gamma"],
+                    self.params[name + ".beta"], a["y"], a["mean"], a["rstd"], self.norm, eps=self.cfg.norm_eps, act="relu",
+                    ws=self.ws)
+        elif not self.fuse_relu:
             self._c("glue_relu_fwd", rc.glue_relu_fwd, a["y"], a["y"])
         return a["y"]
 
@@ -246,12 +280,18 @@ class UNet:
         """a['g'] holds dL/d(ReLU output); returns nothing: dL/dx lands in the producer's 'g' slot."""
         self._where = name
         a = self.act[name]
-        if not self.fuse_relu:      # fused: idx = 255 at dead elements already keeps their gradient out
+        g = a["g"]
+        if self.norm:
+            g = a["gpre"]
+            self._c("train_groupnorm_bwd", rc.train_groupnorm_bwd, a["pre"], a["g"], self.params[name + ".gamma"],
+                    self.params[name + ".beta"], a["mean"], a["rstd"], g, self.grads[name + ".gamma"],
+                    self.grads[name + ".beta"], self.norm, act="relu", ws=self.ws)
+        elif not self.fuse_relu:    # fused: idx = 255 at dead elements already keeps their gradient out
             self._c("glue_relu_bwd", rc.glue_relu_bwd, a["y"], a["g"], a["g"])
-        self._c("rotconv_pool_bwd_weight", rc.rotconv_pool_bwd_weight, self.plans[name], a["x"], a["g"], a["idx"],
+        self._c("rotconv_pool_bwd_weight", rc.rotconv_pool_bwd_weight, self.plans[name], a["x"], g, a["idx"],
                 self.grads[name], self.ws)
         if need_dx:
-            self._c("rotconv_pool_bwd_data", rc.rotconv_pool_bwd_data, self.plans[name], a["g"], a["idx"],
+            self._c("rotconv_pool_bwd_data", rc.rotconv_pool_bwd_data, self.plans[name], g, a["idx"],
                     self.params[name], a["gx"], self.ws)
 
     def forward(self):
@@ -323,17 +363,46 @@ class UNet:
         self.backward()
         return self.loss
 
-    def capture(self):
+    # ---- training -----------------------------------------------------------------------------
+    def optimizer(self, weight_decay=0.0, **options):
+        """train.AdamW over all parameters and this network's gradient buffers; options: lr, betas, eps, state, seed.
+        Filters decay, a norm's scale and shift do not.  dtype "bf16": the optimizer updates fp32 copies (kept from the
+        parameters loaded from now on, or the rounded ones held now), and every step rounds them into the network's own."""
+        from . import train
+
+        names = list(self.params)
+        half = [n for n in names if self.params[n].dtype == self.torch.bfloat16]
+        if half and self.masters is self.params:
+            self.masters = {n: self.params[n].float() if n in half else self.params[n] for n in names}
+        return train.AdamW([self.masters[n] for n in names], [self.grads[n] for n in names],
+                           weight_decay=[0.0 if _is_norm(n) else weight_decay for n in names],
+                           copies=[self.params[n] if n in half else None for n in names], **options)
+
+    def train_step(self, optimizer, max_norm=None):
+        """Forward, backward, with max_norm the gradients' norm (clipping, and no update where it is not finite), update."""
+        self.step()
+        if max_norm is not None:
+            self._where = "clip"
+            self._c("train_grad_norm", optimizer.clip, max_norm)
+        self._where = "optimizer"
+        self._c("train_adamw_step", optimizer.step)
+        return self.loss
+
+    def capture(self, optimizer=None, max_norm=None):
         """Records one step (after at least one eager step: the plans upload their tables on first use) into a HIP
         graph on the current device; `replay()` then runs the whole step with one launch from the host.  Every
         library call enqueues kernels only and every buffer of the step is preallocated, so the recorded step is
-        the eager step."""
+        the eager step.  With an optimizer the recorded step is train_step(optimizer, max_norm); its step number and
+        learning rate live on the device."""
         assert self.trace is None
         self.step()
         self.torch.cuda.synchronize()
         self._graph = self.torch.cuda.CUDAGraph()
         with self.torch.cuda.graph(self._graph):
-            self.step()
+            if optimizer is None:
+                self.step()
+            else:
+                self.train_step(optimizer, max_norm)
         return self._graph
 
     def replay(self):
