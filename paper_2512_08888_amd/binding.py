@@ -201,9 +201,14 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream() -> Optional[int]:
+    """The current stream's handle (None: the null stream).  torch.cuda.current_stream() builds a Python object for it,
+    3 us on the host, as long as a launch; the raw getter takes 0.1 us where this torch has it."""
     import torch
 
-    return torch.cuda.current_stream().cuda_stream or None
+    try:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
+    except AttributeError:
+        return torch.cuda.current_stream().cuda_stream or None
 
 
 class Plan:

@@ -27,8 +27,10 @@ namespace {
 
 constexpr int kThreads = 512, kWaves = kThreads / 64;
 constexpr int kMaxTeam = kThreads / 4;       // channels that a workgroup holds at once (NCHW), four lanes each at least
+constexpr int kBatch = 4;                    // vectors under way at a time where a map is read without being held
 constexpr int kMaxSplit = 256;               // workgroups that wait for one another, at most
 constexpr int kMaxRun = 1024;                // channels of a run (channels last)
+constexpr size_t kTwoBytes = 8u << 20;       // of a map, up to which a shared group takes two launches
 constexpr int kMaxSlots = 2048;              // sums that a workgroup collects (channels last: of every group of its run)
 
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
@@ -232,7 +234,9 @@ __device__ __forceinline__ void forget(R (&r)[J]) {
   for (int j = 0; j < J; ++j) forget_vector(r[j]);
 }
 
-enum Mode { kFused, kSums };            // in one launch; in three: sums, join, map
+// One launch (and one behind it for what was put off); two: sums, map, each workgroup of which joins its group's sums;
+// three: sums, join, map
+enum Mode { kFused, kTwo, kSums };
 
 struct Gn {
   // the problem
@@ -340,19 +344,22 @@ struct Nchw {
     if (m.beta) be = m.beta[c];
     if (BWD) mu = m.mean[group], r = m.rstd[group];
   }
-  __device__ __forceinline__ void take(int k) {
-    place(k);
+  // vectors first .. first + J of each lane
+  __device__ __forceinline__ bool has(int first, int j) const { return (first == 0 || first + j < q.per) && has(first + j); }
+  __device__ __forceinline__ void load(int first) {
     const E* xp = static_cast<const E*>(m.x) + base;
     const E* dp = static_cast<const E*>(m.dy) + base;
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) {
-        x[j].load(at(xp, j));
-        if (BWD) dy[j].load(at(dp, j));
+      if (has(first, j)) {
+        x[j].load(at(xp, first + j));
+        if (BWD) dy[j].load(at(dp, first + j));
       }
+  }
+  __device__ __forceinline__ void load_tail() {
     if (has_tail()) {
-      x1 = Elt<E>::ld(xp + at_tail());
-      if (BWD) dy1 = Elt<E>::ld(dp + at_tail());
+      x1 = Elt<E>::ld(static_cast<const E*>(m.x) + base + at_tail());
+      if (BWD) dy1 = Elt<E>::ld(static_cast<const E*>(m.dy) + base + at_tail());
     }
   }
   // What the map needs of an element: in fp32 the sums leave xh and dz in the registers of x and dy.
@@ -361,35 +368,40 @@ struct Nchw {
     xv = normalised(xv, mu, r);
     dv = through<ACT>(dv, affine(xv, ga, be));
   }
-  // Sums of part k (taken), in all lanes.  Ends with a barrier behind every use of `red`.
-  __device__ __forceinline__ Pair sums(Pair* red, int k) {
-    float s = 0.f, s2 = 0.f, first = 0.f;
-    if (!BWD && len) first = Elt<E>::ld(static_cast<const E*>(m.x) + base + off);
-    auto add_one = [&](float& xv, float& dv) {
-      if (BWD) {
-        form(xv, dv);
-        add_bwd(xv, dv, s, s2);
-      } else {
-        add_fwd(xv, first, s, s2);
-      }
-    };
+  __device__ __forceinline__ float first_value() const { return !BWD && len ? Elt<E>::ld(static_cast<const E*>(m.x) + base + off) : 0.f; }
+  __device__ __forceinline__ void add_one(float& xv, float& dv, float ref, Pair& s) const {
+    if (BWD) {
+      form(xv, dv);
+      add_bwd(xv, dv, s.a, s.b);
+    } else {
+      add_fwd(xv, ref, s.a, s.b);
+    }
+  }
+  __device__ __forceinline__ void add_loaded(int first, float ref, Pair& s) {
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) {
+      if (has(first, j)) {
         if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           float xv = x[j].get(e), dv = BWD ? dy[j].get(e) : 0.f;
-          add_one(xv, dv);
+          add_one(xv, dv, ref, s);
           if constexpr (FORM) x[j].set(e, xv), dy[j].set(e, dv);
         }
         if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
       }
+  }
+  __device__ __forceinline__ void add_tail(float ref, Pair& s) {
     if (has_tail()) {
       float xv = x1, dv = dy1;
-      add_one(xv, dv);
+      add_one(xv, dv, ref, s);
       if constexpr (FORM) x1 = xv, dy1 = dv;
     }
+  }
+  // Part k's sums, in all lanes, from every lane's own (of deviations from `first`).  Ends with a barrier behind every use
+  // of `red`.
+  __device__ __forceinline__ Pair sums(Pair* red, int k, float first, Pair own) {
+    float s = own.a, s2 = own.b;
     s = lanes_sum(s, min(team(), 64));
     s2 = lanes_sum(s2, min(team(), 64));
     if (team() > 64) {                        // one unit: its eight waves' sums belong to the same first element
@@ -444,18 +456,16 @@ struct Nchw {
     if (has_tail()) Elt<E>::st(op + at_tail(), one<FORM>(x1, dy1, a, b));
   }
   // the same of a part that is placed but not held
-  __device__ __forceinline__ void map_from_memory(float a, float b) const {
-    const E* xp = static_cast<const E*>(m.x) + base;
-    const E* dp = static_cast<const E*>(m.dy) + base;
+  __device__ __forceinline__ void map_from_memory(float a, float b) {
     E* op = static_cast<E*>(m.out) + base;
-    for (int j = 0; j < q.per; ++j)
-      if (has(j)) {
-        Raw<E, V> xr, dr = {};
-        xr.load(at(xp, j));
-        if (BWD) dr.load(at(dp, j));
-        vector<false>(op, xr, dr, j, a, b);
-      }
-    if (has_tail()) Elt<E>::st(op + at_tail(), one<false>(Elt<E>::ld(xp + at_tail()), BWD ? Elt<E>::ld(dp + at_tail()) : 0.f, a, b));
+    for (int first = 0; first < q.per; first += J) {
+      load(first);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(first, j)) vector<false>(op, x[j], dy[j], first + j, a, b);
+    }
+    load_tail();
+    if (has_tail()) Elt<E>::st(op + at_tail(), one<false>(x1, dy1, a, b));
   }
 };
 
@@ -502,15 +512,18 @@ __global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m)
   __shared__ int missing;
   const int k = blockIdx.x;
   Nchw<E, V, J, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
-  w.take(k);
-  Pair p = w.sums(red, k);
-  if (q.mode == kSums) {
-    if (!BWD && threadIdx.x == 0) m.part[w.group * q.split + k] = p;
-    return;
-  }
+  w.place(k);
+  w.load(0);
+  w.load_tail();
+  const float first = w.first_value();
+  Pair p = {0.f, 0.f};
+  w.add_loaded(0, first, p);
+  w.add_tail(first, p);
+  p = w.sums(red, k, first, p);
   if (q.split > 1) {
     unsigned long long* slots = m.slots + w.group * q.split;
     if (threadIdx.x == 0) put(slots + k, p);
+    if (q.mode == kTwo) return;
     if (!collect(slots, q.split, (long long)wall_clock64() + q.wait, all, &missing)) {
       if (threadIdx.x == 0) put_off(m);
       return;
@@ -520,14 +533,34 @@ __global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m)
   w.map(p.a, p.b);
 }
 
-// The map of parts that nobody holds: of those that the launch before has put off (every slot is full now), or, in three
-// launches, of all.  Behind one launch also the channels' gradients, which need every part's sums.
+// The sums alone, of parts that need not fit the registers
+template <typename E, int V, bool BWD, int ACT>
+__global__ __launch_bounds__(kThreads) void k_gn_nchw_sums(Gn q, Maps m) {
+  __shared__ Pair red[kMaxTeam];
+  Nchw<E, V, kBatch, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
+  w.place(blockIdx.x);
+  const float ref = w.first_value();
+  Pair p = {0.f, 0.f};
+  for (int first = 0; first < q.per; first += kBatch) {
+    Pair some = {0.f, 0.f};
+    w.load(first);
+    w.add_loaded(first, ref, some);
+    p.a += some.a, p.b += some.b;
+  }
+  w.load_tail();
+  w.add_tail(ref, p);
+  p = w.sums(red, blockIdx.x, ref, p);
+  if (!BWD && threadIdx.x == 0) m.part[w.group * q.split + blockIdx.x] = p;
+}
+
+// The map of parts that nobody holds: of those that the launch before has put off, or, in two or three launches, of all.
+// Every slot is full now.  But in three launches also the channels' gradients, which need every part's sums.
 template <typename E, int V, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads) void k_gn_nchw_map(Gn q, Maps m) {
   __shared__ Pair all[kMaxSplit];
   __shared__ int missing;
   if (q.mode == kSums) {
-    Nchw<E, V, 1, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
+    Nchw<E, V, kBatch, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
     w.place(blockIdx.x);
     const float2 p = m.stat[w.group];
     w.map_from_memory(p.x, p.y);
@@ -536,12 +569,12 @@ __global__ __launch_bounds__(kThreads) void k_gn_nchw_map(Gn q, Maps m) {
   if (BWD && (m.dgamma || m.dbeta))
     for (size_t c = blockIdx.x * kWaves + threadIdx.x / 64; c < (size_t)q.C; c += gridDim.x * kWaves)
       channel_gradient(q, m, Parts{0, q.pieces, (size_t)q.C}, c);
-  const uint32_t count = q.split > 1 ? m.late[0] : 0;
+  const uint32_t count = q.mode == kTwo ? gridDim.x : q.split > 1 ? m.late[0] : 0;
   for (uint32_t i = blockIdx.x; i < count; i += gridDim.x) {
-    const uint32_t wg = m.late[1 + i];
+    const uint32_t wg = q.mode == kTwo ? i : m.late[1 + i];
     const uint32_t group = wg / q.split;
     const int k = wg % q.split;
-    Nchw<E, V, 1, BWD, ACT> w(q, m, group / q.G, group % q.G);
+    Nchw<E, V, kBatch, BWD, ACT> w(q, m, group / q.G, group % q.G);
     w.place(k);
     collect(m.slots + (size_t)group * q.split, q.split, 0, all, &missing);
     const Pair p = settle<BWD>(w, all, Pair{}, group, k == 0);
@@ -579,22 +612,23 @@ struct Nhwc {
   __device__ __forceinline__ bool has(int j) const { return in && j * q.rows + row < left; }
   template <typename T>
   __device__ __forceinline__ T* at(T* p, int j) const {
-    return p + (uint32_t)(j * q.rows) * (uint32_t)q.C + ((uint32_t)row * (uint32_t)q.C + (uint32_t)c);
+    return p + (size_t)(j * q.rows) * q.C + ((uint32_t)row * (uint32_t)q.C + (uint32_t)c);
   }
   __device__ __forceinline__ void place(int k) {
     const size_t p0 = (size_t)k * q.rows * q.per;
     base = (n * q.P + p0) * q.C + c0;
     left = (int)min((size_t)q.rows * q.per, q.P - p0);
   }
-  __device__ __forceinline__ void take(int k) {
-    place(k);
+  // pixels first .. first + J of each lane
+  __device__ __forceinline__ bool has(int first, int j) const { return (first == 0 || first + j < q.per) && has(first + j); }
+  __device__ __forceinline__ void load(int first) {
     const E* xp = static_cast<const E*>(m.x) + base;
     const E* dp = static_cast<const E*>(m.dy) + base;
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) {
-        x[j].load(at(xp, j));
-        if (BWD) dy[j].load(at(dp, j));
+      if (has(first, j)) {
+        x[j].load(at(xp, first + j));
+        if (BWD) dy[j].load(at(dp, first + j));
       }
   }
   __device__ __forceinline__ size_t group(int e) const { return n * q.G + (c0 + min(c + e, width - 1)) / q.cg; }
@@ -620,18 +654,15 @@ struct Nhwc {
     return s;
   }
 
-  // Sums of every channel of the run over part k's pixels (taken), left in out[0 .. width).  buf: kThreads * V pairs.
-  __device__ __forceinline__ void sums(Pair* buf, Pair* out, int k) {
-    float s[V], s2[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[e] = s2[e] = 0.f;
-    Scale t;
-    Raw<E, V> first = {};
-    if (BWD) t = scale();
-    else if (in) first.load(static_cast<const E*>(m.x) + base + c);
+  __device__ __forceinline__ Raw<E, V> first_values() const {
+    Raw<E, V> f = {};
+    if (!BWD && in) f.load(static_cast<const E*>(m.x) + base + c);
+    return f;
+  }
+  __device__ __forceinline__ void add_loaded(int first, const Raw<E, V>& ref, const Scale& t, float* s, float* s2) {
 #pragma unroll
     for (int j = 0; j < J; ++j)
-      if (has(j)) {
+      if (has(first, j)) {
         if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
 #pragma unroll
         for (int e = 0; e < V; ++e) {
@@ -641,11 +672,15 @@ struct Nhwc {
             add_bwd(xv, dv, s[e], s2[e]);
             if constexpr (FORM) x[j].set(e, xv), dy[j].set(e, dv);
           } else {
-            add_fwd(xv, first.get(e), s[e], s2[e]);
+            add_fwd(xv, ref.get(e), s[e], s2[e]);
           }
         }
         if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
       }
+  }
+  // Sums of every channel of the run over this part's pixels, left in out[0 .. width), from every lane's own (of deviations
+  // from the part's first pixel).  buf: kThreads * V pairs.
+  __device__ __forceinline__ void sums(Pair* buf, Pair* out, const float* s, const float* s2) {
     __syncthreads();
     if (in)
 #pragma unroll
@@ -667,7 +702,7 @@ struct Nhwc {
       Pair t = {0.f, 0.f};
       for (int j = 0; j < rows; ++j) t.a += buf[j * q.run + i].a, t.b += buf[j * q.run + i].b;
       if (!BWD) {
-        const float d = t.a / size_of(q, k);
+        const float d = t.a / (float)left;
         t = Pair{Elt<E>::ld(static_cast<const E*>(m.x) + base + i) + d, t.b - t.a * d};
       }
       out[i] = t;
@@ -706,21 +741,18 @@ struct Nhwc {
   }
   // the same of a part that is placed but not held
   template <typename Stat>
-  __device__ __forceinline__ void map_from_memory(Stat stat) const {
-    const E* xp = static_cast<const E*>(m.x) + base;
-    const E* dp = static_cast<const E*>(m.dy) + base;
+  __device__ __forceinline__ void map_from_memory(Stat stat) {
     E* op = static_cast<E*>(m.out) + base;
     const Scale t = scale();
     Pair p[S];
 #pragma unroll
     for (int e = 0; e < S; ++e) p[e] = stat(e);
-    for (int j = 0; j < q.per; ++j)
-      if (has(j)) {
-        Raw<E, V> xr, dr = {};
-        xr.load(at(xp, j));
-        if (BWD) dr.load(at(dp, j));
-        vector<false>(op, xr, dr, j, t, p);
-      }
+    for (int first = 0; first < q.per; first += J) {
+      load(first);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(first, j)) vector<false>(op, x[j], dy[j], first + j, t, p);
+    }
   }
 };
 
@@ -767,13 +799,18 @@ __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
   __shared__ Pair chan[kMaxRun];
   __shared__ int missing;
   const int k = blockIdx.x, run = blockIdx.y;
-  const int groups = q.run / q.cg;            // (kFused)
+  const int groups = q.run / q.cg;
   Nhwc<E, V, J, ONE, BWD, ACT> w(q, m, blockIdx.z, run);
-  w.take(k);
-  w.sums(buf, chan, k);
-  if (BWD || q.mode == kSums)
+  w.place(k);
+  w.load(0);
+  {
+    float s[V] = {}, s2[V] = {};
+    if (BWD) w.add_loaded(0, {}, w.scale(), s, s2);
+    else w.add_loaded(0, w.first_values(), {}, s, s2);
+    w.sums(buf, chan, s, s2);
+  }
+  if (BWD)
     for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + k) * q.C + w.c0 + i] = chan[i];
-  if (q.mode == kSums) return;
   unsigned long long* slots = m.slots + ((size_t)blockIdx.z * q.runs + run) * q.split * groups;
   for (int g = threadIdx.x / 64; g < groups; g += kWaves) {
     const Pair p = of_group<BWD>(w, chan, g, k);
@@ -782,12 +819,35 @@ __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
       else all[g] = p;
     }
   }
+  if (q.mode == kTwo) return;
   if (q.split > 1 && !collect(slots, q.split * groups, (long long)wall_clock64() + q.wait, all, &missing)) {
     if (threadIdx.x == 0) put_off(m);
     return;
   }
   settle<BWD>(w, all, chan, run, groups, k == 0);
   w.map([&](int e) { return chan[min(w.c + e, w.width - 1) / q.cg]; });
+}
+
+// The sums alone, of runs that need not be of whole groups and parts that need not fit the registers
+template <typename E, int V, bool ONE, bool BWD, int ACT>
+__global__ __launch_bounds__(kThreads) void k_gn_nhwc_sums(Gn q, Maps m) {
+  __shared__ Pair buf[kThreads * V];
+  __shared__ Pair chan[kMaxRun];
+  Nhwc<E, V, kBatch, ONE, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
+  w.place(blockIdx.x);
+  float s[V] = {}, s2[V] = {};
+  typename Nhwc<E, V, kBatch, ONE, BWD, ACT>::Scale t = {};
+  if (BWD) t = w.scale();
+  const Raw<E, V> ref = w.first_values();
+  for (int first = 0; first < q.per; first += kBatch) {
+    float some[V] = {}, some2[V] = {};
+    w.load(first);
+    w.add_loaded(first, ref, t, some, some2);
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] += some[e], s2[e] += some2[e];
+  }
+  w.sums(buf, chan, s, s2);
+  for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + blockIdx.x) * q.C + w.c0 + i] = chan[i];
 }
 
 // As k_gn_nchw_map
@@ -797,7 +857,7 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
   __shared__ Pair chan[kMaxRun];
   __shared__ int missing;
   if (q.mode == kSums) {
-    Nhwc<E, V, 1, ONE, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
+    Nhwc<E, V, kBatch, ONE, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
     w.place(blockIdx.x);
     w.map_from_memory([&](int e) {
       const float2 s = m.stat[w.group(e)];
@@ -809,12 +869,12 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
     for (size_t c = blockIdx.x * kWaves + threadIdx.x / 64; c < (size_t)q.C; c += gridDim.x * kWaves)
       channel_gradient(q, m, Parts{1, q.split, (size_t)q.C}, c);
   const int groups = q.run / q.cg;
-  const uint32_t count = q.split > 1 ? m.late[0] : 0;
+  const uint32_t count = q.mode == kTwo ? gridDim.x : q.split > 1 ? m.late[0] : 0;
   for (uint32_t i = blockIdx.x; i < count; i += gridDim.x) {
-    const uint32_t wg = m.late[1 + i];
+    const uint32_t wg = q.mode == kTwo ? i : m.late[1 + i];
     const size_t cluster = wg / q.split;
     const int k = wg % q.split, run = (int)(cluster % q.runs);
-    Nhwc<E, V, 1, ONE, BWD, ACT> w(q, m, cluster / q.runs, run);
+    Nhwc<E, V, kBatch, ONE, BWD, ACT> w(q, m, cluster / q.runs, run);
     w.place(k);
     collect(m.slots + cluster * q.split * groups, q.split * groups, 0, all, &missing);
     settle<BWD>(w, all, chan, run, groups, k == 0);
@@ -889,10 +949,10 @@ size_t ceil_div(size_t a, size_t b) { return (a + b - 1) / b; }
 
 size_t workgroups(const Gn& q, int layout) { return (size_t)q.N * (layout == TRAIN_NHWC ? q.runs : q.G) * q.split; }
 
-Gn cut_nchw(Gn q, int elem, int per) {
+Gn cut_nchw(Gn q, int elem, int per, bool held) {
   const int full = 16 / elem;
   q.vec = q.P >= (size_t)full ? full : 1;
-  q.per = q.vec == 1 ? 2 : per;                   // four lanes hold the up to seven pixels
+  q.per = q.vec == 1 && held ? 2 : per;           // four lanes hold the up to seven pixels
   per = q.per;
   const size_t vectors = std::max<size_t>(1, q.P / q.vec);
   if (vectors <= 64u * per) {                     // a team of a wave or less holds a channel
@@ -915,13 +975,14 @@ Gn cut_nchw(Gn q, int elem, int per) {
   return q;
 }
 
-Gn cut_nhwc(Gn q, int elem, int per) {
+// held: a workgroup's vectors stay in registers
+Gn cut_nhwc(Gn q, int elem, int per, bool held) {
   q.vec = 16 / elem;
   q.one = q.cg % q.vec == 0;
   if (!q.one) {                // lanes with several groups' statistics: shorter vectors and fewer of them, for the registers
     q.vec = q.C % 4 == 0 ? 4 : 1;
     q.one = q.vec == 1;
-    per = q.one ? 4 : std::min(per, 4);
+    if (held) per = q.one ? 4 : std::min(per, 4);
   }
   q.per = per;
   // the shortest run of whole groups that fills a cache line of every pixel
@@ -947,7 +1008,7 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem) {
   Gn q = {};
   q.N = N, q.C = C, q.G = groups, q.cg = C / groups, q.P = P;
   Gn best = {};
-  auto with = [&](int per) { return layout == TRAIN_NHWC ? cut_nhwc(q, elem, per) : cut_nchw(q, elem, per); };
+  auto with = [&](int per) { return layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, true) : cut_nchw(q, elem, per, true); };
   // A group (or run) in one workgroup needs no exchange and one launch: with as many lanes as that leaves.  Else the largest
   // parts that still give every CU a workgroup.
   for (int per : {2, 4, 8}) {
@@ -960,7 +1021,15 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem) {
       if (workgroups(best, layout) >= 256) break;
     }
   const size_t slots = (size_t)best.split * (layout == TRAIN_NHWC ? best.run / best.cg : 1);
-  if (best.mode == kFused && (best.split > kMaxSplit || slots > (size_t)kMaxSlots)) best.mode = kSums;
+  if (best.mode == kSums || best.split > kMaxSplit || slots > (size_t)kMaxSlots) {
+    // parts of any size, a few for each CU
+    for (int per = 8;; per *= 2) {
+      best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, false) : cut_nchw(q, elem, per, false);
+      if (workgroups(best, layout) <= 4096 || per == 256) break;
+    }
+    best.mode = kSums;
+  }
+  if (best.mode == kFused && best.split > 1 && (size_t)N * C * P * elem <= kTwoBytes) best.mode = kTwo;
   best.over = 65536 / best.period + 1;
   return best;
 }
@@ -972,7 +1041,7 @@ size_t parts_of(const Gn& q, int layout) {
 }
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 size_t slots_of(const Gn& q, int layout) {
-  if (q.mode != kFused || q.split == 1) return 0;
+  if (q.mode == kSums || q.split == 1) return 0;
   return workgroups(q, layout) * (layout == TRAIN_NHWC ? q.run / q.cg : 1);
 }
 size_t late_bytes(const Gn& q, int layout) { return slots_of(q, layout) ? round256((1 + workgroups(q, layout)) * 4) : 0; }
@@ -987,23 +1056,25 @@ bool known(int act, int layout) {
 
 typedef void (*Kernel)(Gn, Maps);
 struct Kernels {
-  Kernel main, map;
+  Kernel main, map, sums;          // held in registers; read for the map, for the sums
 };
 template <typename E, bool BWD, int ACT>
 Kernels pick_of(const Gn& q, int layout) {
   constexpr int full = 16 / sizeof(E);
+  constexpr int SUM = BWD ? ACT : TRAIN_ACT_NONE;        // forward sums know no activation
   if (layout == TRAIN_NCHW) {
-    if (q.vec == 1) return {k_gn_nchw<E, 1, 2, BWD, ACT>, k_gn_nchw_map<E, 1, BWD, ACT>};
+    if (q.vec == 1) return {k_gn_nchw<E, 1, 2, BWD, ACT>, k_gn_nchw_map<E, 1, BWD, ACT>, k_gn_nchw_sums<E, 1, BWD, SUM>};
     return {q.per == 8 ? k_gn_nchw<E, full, 8, BWD, ACT> : q.per == 4 ? k_gn_nchw<E, full, 4, BWD, ACT> : k_gn_nchw<E, full, 2, BWD, ACT>,
-            k_gn_nchw_map<E, full, BWD, ACT>};
+            k_gn_nchw_map<E, full, BWD, ACT>, k_gn_nchw_sums<E, full, BWD, SUM>};
   }
-  if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_map<E, 1, true, BWD, ACT>};
+  if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_map<E, 1, true, BWD, ACT>, k_gn_nhwc_sums<E, 1, true, BWD, SUM>};
   if (!q.one)
-    return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 4, false, BWD, ACT>};
+    return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 4, false, BWD, ACT>,
+            k_gn_nhwc_sums<E, 4, false, BWD, SUM>};
   return {q.per == 8   ? k_gn_nhwc<E, full, 8, true, BWD, ACT>
           : q.per == 4 ? k_gn_nhwc<E, full, 4, true, BWD, ACT>
                        : k_gn_nhwc<E, full, 2, true, BWD, ACT>,
-          k_gn_nhwc_map<E, full, true, BWD, ACT>};
+          k_gn_nhwc_map<E, full, true, BWD, ACT>, k_gn_nhwc_sums<E, full, true, BWD, SUM>};
 }
 template <typename E, bool BWD>
 Kernels pick(const Gn& q, int layout) {
@@ -1024,7 +1095,12 @@ void launch(Gn q, Maps m, int layout, hipStream_t st, Join join) {
     if (n || (BWD && (m.dgamma || m.dbeta))) kernel.map<<<64, kThreads, 0, st>>>(q, m);
     return;
   }
-  kernel.main<<<grid, kThreads, 0, st>>>(q, m);
+  if (q.mode == kTwo) {
+    kernel.main<<<grid, kThreads, 0, st>>>(q, m);
+    kernel.map<<<(unsigned)workgroups(q, layout), kThreads, 0, st>>>(q, m);
+    return;
+  }
+  kernel.sums<<<grid, kThreads, 0, st>>>(q, m);
   join();
   kernel.map<<<grid, kThreads, 0, st>>>(q, m);
 }
