@@ -284,6 +284,15 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int d = 32; d > 0; d >>= 1) v += __shfl_xor(v, d);
   return v;
 }
+// over a workgroup of 256
+__device__ __forceinline__ double block_sum(double v) {
+  __shared__ double red[4];
+  v = wave_sum(v);
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
 // dbeta and dgamma of channel c, by one wave
 __device__ __forceinline__ void channel_gradient(const Gn& q, const Maps& m, const Parts& where, size_t c) {
   double s1 = 0, s2 = 0;
@@ -681,18 +690,30 @@ struct Nhwc {
   // Sums of every channel of the run over this part's pixels, left in out[0 .. width), from every lane's own (of deviations
   // from the part's first pixel).  buf: kThreads * V pairs.
   __device__ __forceinline__ void sums(Pair* buf, Pair* out, const float* s, const float* s2) {
+    // A lane's V pairs lie together, two at a time at places that turn with the lane (64 bytes apart, the same two of eight
+    // lanes would share their banks).
+    auto place_of = [](int l, int e) { return V < 8 ? l * V + e : l * V + (((e >> 1) ^ ((l >> 2) & 3)) << 1 | (e & 1)); };
     __syncthreads();
-    if (in)
+    if (in) {
+      if constexpr (V == 1) {
+        buf[threadIdx.x] = Pair{s[0], s2[0]};
+      } else {
 #pragma unroll
-      for (int e = 0; e < V; ++e) buf[row * q.run + c + e] = Pair{s[e], s2[e]};
+        for (int e = 0; e < V; e += 2)
+          *reinterpret_cast<f4*>(buf + place_of(threadIdx.x, e)) = f4{s[e], s2[e], s[e + 1], s2[e + 1]};
+      }
+    }
     __syncthreads();
     // rows together: as many lanes to a channel as there are
-    const int lanes = kThreads / width, ch = threadIdx.x % width, part = threadIdx.x / width;
+    const int lanes = kThreads / width, ch = threadIdx.x % width, part = threadIdx.x / width, cols = q.run / V;
     int rows = q.rows;
     if (lanes > 1) {
       Pair t = {0.f, 0.f};
       if (part < lanes)
-        for (int i = part; i < rows; i += lanes) t.a += buf[i * q.run + ch].a, t.b += buf[i * q.run + ch].b;
+        for (int i = part; i < rows; i += lanes) {
+          const Pair o = buf[place_of(i * cols + ch / V, ch % V)];
+          t.a += o.a, t.b += o.b;
+        }
       rows = min(lanes, rows);
       __syncthreads();
       if (part < rows) buf[part * q.run + ch] = t;
@@ -700,7 +721,10 @@ struct Nhwc {
     }
     for (int i = threadIdx.x; i < width; i += kThreads) {
       Pair t = {0.f, 0.f};
-      for (int j = 0; j < rows; ++j) t.a += buf[j * q.run + i].a, t.b += buf[j * q.run + i].b;
+      for (int j = 0; j < rows; ++j) {
+        const Pair o = buf[lanes > 1 ? j * q.run + i : place_of(j * cols + i / V, i % V)];
+        t.a += o.a, t.b += o.b;
+      }
       if (!BWD) {
         const float d = t.a / (float)left;
         t = Pair{Elt<E>::ld(static_cast<const E*>(m.x) + base + i) + d, t.b - t.a * d};
@@ -794,10 +818,12 @@ __device__ __forceinline__ void settle(const Part& w, const Pair* all, Pair* sta
 
 template <typename E, int V, int J, bool ONE, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
-  __shared__ Pair buf[kThreads * V];
-  __shared__ Pair all[kMaxSlots];             // [part][group]
+  // 40 KB at most, four workgroups to a CU: what is collected takes the room of the lanes' sums
+  constexpr int room = kThreads * V > kMaxSlots + 1 ? kThreads * V : kMaxSlots + 1;
+  __shared__ __attribute__((aligned(16))) Pair buf[room];
   __shared__ Pair chan[kMaxRun];
-  __shared__ int missing;
+  Pair* const all = buf;                      // [part][group]
+  int* const missing = reinterpret_cast<int*>(buf + kMaxSlots);
   const int k = blockIdx.x, run = blockIdx.y;
   const int groups = q.run / q.cg;
   Nhwc<E, V, J, ONE, BWD, ACT> w(q, m, blockIdx.z, run);
@@ -820,7 +846,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
     }
   }
   if (q.mode == kTwo) return;
-  if (q.split > 1 && !collect(slots, q.split * groups, (long long)wall_clock64() + q.wait, all, &missing)) {
+  if (q.split > 1 && !collect(slots, q.split * groups, (long long)wall_clock64() + q.wait, all, missing)) {
     if (threadIdx.x == 0) put_off(m);
     return;
   }
@@ -831,7 +857,7 @@ __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
 // The sums alone, of runs that need not be of whole groups and parts that need not fit the registers
 template <typename E, int V, bool ONE, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads) void k_gn_nhwc_sums(Gn q, Maps m) {
-  __shared__ Pair buf[kThreads * V];
+  __shared__ __attribute__((aligned(16))) Pair buf[kThreads * V];
   __shared__ Pair chan[kMaxRun];
   Nhwc<E, V, kBatch, ONE, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
   w.place(blockIdx.x);
@@ -884,13 +910,11 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
 }
 
 // ---- joins of three-launch runs, and the channels' gradients --------------------------------------
-// One wave a group of one image
+// One workgroup a group of one image
 __global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ part, float* __restrict__ mean,
                                                      float* __restrict__ rstd, float2* __restrict__ stat, Gn q, Parts where) {
-  const size_t g = (size_t)blockIdx.x * 4 + threadIdx.x / 64;
-  if (g >= (size_t)q.N * q.G) return;
-  const size_t n = g / q.G, c0 = g % q.G * (where.nhwc ? q.cg : 1);
-  const int chans = where.nhwc ? q.cg : 1;
+  const size_t g = blockIdx.x, n = g / q.G, c0 = g % q.G * (where.nhwc ? q.cg : 1);
+  const int chans = where.nhwc ? q.cg : 1, count = chans * q.split;
   const double M = (double)q.cg * (double)q.P;
   auto size = [&](int i) {
     if (where.nhwc) {
@@ -900,41 +924,55 @@ __global__ __launch_bounds__(256) void k_gn_fwd_join(const Pair* __restrict__ pa
     const int teams = kThreads >> q.team_log;
     return q.pieces > 1 ? (double)min(q.step, q.P - (i % q.pieces) * q.step) : (double)min(teams, q.cg - i * teams) * (double)q.P;
   };
+  auto get = [&](int i) { return part[where.at(n, c0 + i % chans, i / chans)]; };
   double s = 0, s2 = 0;
-  for (int i = threadIdx.x % 64; i < chans * q.split; i += 64) s += size(i / chans) * part[where.at(n, c0 + i % chans, i / chans)].a;
-  const double mu = wave_sum(s) / M;
-  for (int i = threadIdx.x % 64; i < chans * q.split; i += 64) {
-    const Pair p = part[where.at(n, c0 + i % chans, i / chans)];
+#pragma unroll 4
+  for (int i = threadIdx.x; i < count; i += 256) s += size(i / chans) * get(i).a;
+  const double mu = block_sum(s) / M;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < count; i += 256) {
+    const Pair p = get(i);
     s2 += p.b + size(i / chans) * (p.a - mu) * (p.a - mu);
   }
-  s2 = wave_sum(s2);
-  if (threadIdx.x % 64) return;
+  s2 = block_sum(s2);
+  if (threadIdx.x) return;
   const float r = (float)(1.0 / sqrt(s2 / M + (double)q.eps));
   stat[g] = make_float2((float)mu, r);
   if (mean) mean[g] = (float)mu;
   if (rstd) rstd[g] = r;
 }
 
-// The first N * G waves: a group's two means.  The next C waves: a channel's dbeta and dgamma.
+// The first N * G workgroups: a group's two means.  The next C: a channel's dbeta and dgamma.
 __global__ __launch_bounds__(256) void k_gn_bwd_join(Gn q, Maps m, Parts where, float2* __restrict__ stat) {
-  const size_t w = (size_t)blockIdx.x * 4 + threadIdx.x / 64, groups = (size_t)q.N * q.G;
+  const size_t w = blockIdx.x, groups = (size_t)q.N * q.G;
+  double s1 = 0, s2 = 0;
   if (w >= groups) {
-    if (w - groups < (size_t)q.C) channel_gradient(q, m, where, w - groups);
+    const size_t c = w - groups;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < q.N * where.per; i += 256) {
+      const Pair p = m.part[where.at(i / where.per, c, i % where.per)];
+      s1 += p.a;
+      s2 += p.b;
+    }
+    s1 = block_sum(s1);
+    s2 = block_sum(s2);
+    if (threadIdx.x == 0 && m.dbeta) m.dbeta[c] = (float)s1;
+    if (threadIdx.x == 0 && m.dgamma) m.dgamma[c] = (float)s2;
     return;
   }
-  double s1 = 0, s2 = 0;
   const size_t c0 = w % q.G * q.cg;
-  for (int i = threadIdx.x % 64; i < q.cg * where.per; i += 64) {
+#pragma unroll 4
+  for (int i = threadIdx.x; i < q.cg * where.per; i += 256) {
     const size_t c = where.nhwc ? i % q.cg : i / where.per;
     const Pair p = m.part[where.at(w / q.G, c0 + c, where.nhwc ? i / q.cg : i % where.per)];
     const double ga = m.gamma ? m.gamma[c0 + c] : 1.f;
     s1 += p.a * ga;
     s2 += p.b * ga;
   }
-  s1 = wave_sum(s1);
-  s2 = wave_sum(s2);
+  s1 = block_sum(s1);
+  s2 = block_sum(s2);
   const double M = (double)q.cg * (double)q.P;
-  if (threadIdx.x % 64 == 0) stat[w] = make_float2((float)(s1 / M), (float)(s2 / M));
+  if (threadIdx.x == 0) stat[w] = make_float2((float)(s1 / M), (float)(s2 / M));
 }
 
 // ---- host -----------------------------------------------------------------------------------------
@@ -976,11 +1014,12 @@ Gn cut_nchw(Gn q, int elem, int per, bool held) {
 }
 
 // held: a workgroup's vectors stay in registers
-Gn cut_nhwc(Gn q, int elem, int per, bool held) {
+Gn cut_nhwc(Gn q, int elem, int per, bool held, bool bwd) {
   q.vec = 16 / elem;
   q.one = q.cg % q.vec == 0;
-  if (!q.one) {                // lanes with several groups' statistics: shorter vectors and fewer of them, for the registers
-    q.vec = q.C % 4 == 0 ? 4 : 1;
+  if (!q.one) {
+    // several groups' statistics in a lane: fewer vectors, and backward shorter ones, for the registers
+    if (q.C % q.vec || bwd) q.vec = q.C % 4 == 0 ? 4 : 1;
     q.one = q.vec == 1;
     if (held) per = q.one ? 4 : std::min(per, 4);
   }
@@ -1004,11 +1043,11 @@ Gn cut_nhwc(Gn q, int elem, int per, bool held) {
 }
 
 // mode kSums: in three launches
-Gn cut(int N, int C, size_t P, int groups, int layout, int elem) {
+Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
   Gn q = {};
   q.N = N, q.C = C, q.G = groups, q.cg = C / groups, q.P = P;
   Gn best = {};
-  auto with = [&](int per) { return layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, true) : cut_nchw(q, elem, per, true); };
+  auto with = [&](int per) { return layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, true, bwd) : cut_nchw(q, elem, per, true); };
   // A group (or run) in one workgroup needs no exchange and one launch: with as many lanes as that leaves.  Else the largest
   // parts that still give every CU a workgroup.
   for (int per : {2, 4, 8}) {
@@ -1024,7 +1063,7 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem) {
   if (best.mode == kSums || best.split > kMaxSplit || slots > (size_t)kMaxSlots) {
     // parts of any size, a few for each CU
     for (int per = 8;; per *= 2) {
-      best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, false) : cut_nchw(q, elem, per, false);
+      best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, false, bwd) : cut_nchw(q, elem, per, false);
       if (workgroups(best, layout) <= 4096 || per == 256) break;
     }
     best.mode = kSums;
@@ -1068,6 +1107,10 @@ Kernels pick_of(const Gn& q, int layout) {
             k_gn_nchw_map<E, full, BWD, ACT>, k_gn_nchw_sums<E, full, BWD, SUM>};
   }
   if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_map<E, 1, true, BWD, ACT>, k_gn_nhwc_sums<E, 1, true, BWD, SUM>};
+  if constexpr (!BWD && full == 8)
+    if (!q.one && q.vec == 8)
+      return {q.per == 4 ? k_gn_nhwc<E, 8, 4, false, BWD, ACT> : k_gn_nhwc<E, 8, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 8, false, BWD, ACT>,
+              k_gn_nhwc_sums<E, 8, false, BWD, SUM>};
   if (!q.one)
     return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 4, false, BWD, ACT>,
             k_gn_nhwc_sums<E, 4, false, BWD, SUM>};
@@ -1129,7 +1172,7 @@ int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, fl
   if (!shaped(N, C, P, groups)) return ROTCONV_ERR_SHAPE;
   if (!known(act, layout) || !(eps >= 0.f) || misaligned(x, sizeof(E)) || misaligned(y, sizeof(E))) return ROTCONV_ERR_UNSUPPORTED;
   if (P == 1) layout = TRAIN_NHWC;                 // the two are the same
-  Gn q = cut(N, C, P, groups, layout, sizeof(E));
+  Gn q = cut(N, C, P, groups, layout, sizeof(E), false);
   q.eps = eps, q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
   if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
   if (q.split >= 1 << 22) return ROTCONV_ERR_SHAPE;
@@ -1138,7 +1181,7 @@ int fwd(const E* x, const float* gamma, const float* beta, E* y, float* mean, fl
   const Maps m{x, nullptr, y, gamma, beta, mean, rstd, nullptr, nullptr, s.part, s.slots, s.late, s.stat};
   launch<E, false>(q, m, layout, st, [&] {
     const Parts where{layout, q.split, (size_t)(layout == TRAIN_NHWC ? C : groups)};
-    k_gn_fwd_join<<<(unsigned)ceil_div((size_t)N * groups, 4), 256, 0, st>>>(s.part, mean, rstd, s.stat, q, where);
+    k_gn_fwd_join<<<(unsigned)((size_t)N * groups), 256, 0, st>>>(s.part, mean, rstd, s.stat, q, where);
   });
   return finish();
 }
@@ -1152,7 +1195,7 @@ int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const fl
   if (!known(act, layout) || misaligned(x, sizeof(E)) || misaligned(dy, sizeof(E)) || misaligned(dx, sizeof(E)))
     return ROTCONV_ERR_UNSUPPORTED;
   if (P == 1) layout = TRAIN_NHWC;
-  Gn q = cut(N, C, P, groups, layout, sizeof(E));
+  Gn q = cut(N, C, P, groups, layout, sizeof(E), true);
   q.act = act, q.wait = g_wait.load(std::memory_order_relaxed);
   if (!ws || misaligned(ws, 16) || ws_bytes < need(q, layout)) return ROTCONV_ERR_WORKSPACE;
   if (q.split >= 1 << 22) return ROTCONV_ERR_SHAPE;
@@ -1161,7 +1204,7 @@ int bwd(const E* x, const E* dy, const float* gamma, const float* beta, const fl
   const Maps m{x, dy, dx, gamma, beta, const_cast<float*>(mean), const_cast<float*>(rstd), dgamma, dbeta, s.part, s.slots, s.late, s.stat};
   launch<E, true>(q, m, layout, st, [&] {
     const Parts where{layout, layout == TRAIN_NHWC ? q.split : q.pieces, (size_t)C};
-    k_gn_bwd_join<<<(unsigned)ceil_div((size_t)N * groups + C, 4), 256, 0, st>>>(q, m, where, s.stat);
+    k_gn_bwd_join<<<(unsigned)((size_t)N * groups + C), 256, 0, st>>>(q, m, where, s.stat);
   });
   return finish();
 }
@@ -1175,7 +1218,8 @@ size_t train_groupnorm_workspace_bytes(int N, int C, size_t P, int groups) {
   if (!rotconv::shaped(N, C, P, groups)) return 0;
   size_t n = 0;
   for (int layout : {TRAIN_NCHW, TRAIN_NHWC})
-    for (int elem : {4, 2}) n = std::max(n, rotconv::need(rotconv::cut(N, C, P, groups, layout, elem), layout));
+    for (int elem : {4, 2})
+      for (bool bwd : {false, true}) n = std::max(n, rotconv::need(rotconv::cut(N, C, P, groups, layout, elem, bwd), layout));
   return n;
 }
 int train_groupnorm_fwd(const float* x, const float* gamma, const float* beta, float* y, float* mean, float* rstd, int N, int C,
