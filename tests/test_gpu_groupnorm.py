@@ -333,3 +333,76 @@ def test_workgroups_that_do_not_wait(layout, dtype):
         finally:
             assert rc.train_diag_groupnorm_wait(before) == 0
         assert all(np.array_equal(p, q) for p, q in zip(a + g + g, b + h + i)), shape
+
+
+def test_pieces_that_divide_a_channel_but_for_its_end():
+    """A channel's whole vectors divide evenly over its pieces and a few pixels are left."""
+    for P, dtype in ((8 * 2520 + 3, "f32"), (20480 + 1, "f32"), (4 * 8 * 512 + 3, "f32"), (16 * 1031 + 7, "bf16"), (8 * 512 * 2 + 5, "bf16"),
+                     (8 * 4096 + 7, "bf16"), (16 * 4096 + 1, "bf16")):
+        c = Case(2, 3, 1, P, 1, act="relu", dtype=dtype)
+        mean, rstd = c.check_forward()
+        c.check_backward(mean, rstd)
+
+
+# Maps of more than 8 MiB, whose workgroups exchange their groups' sums within the launch: odd numbers of pixels, a channel
+# in several pieces, several channels to a workgroup's part, vectors across groups, channels that fill no vector
+SHARED = {"nchw": [(4, 64, 133, 131, 4), (9, 24, 141, 143, 1)], "nhwc": [(4, 64, 133, 131, 4), (5, 56, 131, 127, 14), (10, 33, 120, 123, 3)]}
+# Groups of more parts than wait for one another, or of more sums than a workgroup collects; groups wider than a run of
+# channels, and runs that are not of whole groups
+THREE = {"nchw": [(1, 6, 1201, 1200, 1)],
+         "nhwc": [(2, 521, 5, 7, 521), (1, 2060, 3, 3, 2), (1, 2064, 4, 3, 2), (2, 2056, 3, 7, 2), (1, 64, 130, 130, 64), (2, 33, 190, 199, 11)]}
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("which", ["shared", "three"])
+def test_large_groups_against_the_oracle(which, layout, dtype):
+    for k, shape in enumerate((SHARED if which == "shared" else THREE)[layout]):
+        c = Case(*shape, act=("silu", "relu", "none")[k % 3], layout=layout, dtype=dtype, shift=k % 2)
+        print(shape, flush=True)
+        mean, rstd = c.check_forward()
+        c.check_backward(mean, rstd)
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_groups_have_the_same_bits_however_they_wait(layout, dtype):
+    """With no time to wait, every part is left to the launch behind; also in place, and without what may be left out."""
+    for shape in SHARED[layout] + THREE[layout]:
+        c = Case(*shape, act="silu", layout=layout, dtype=dtype)
+        print(shape, flush=True)
+        a = c.forward()
+        g = c.backward(a[1], a[2])
+        before = rc.train_diag_groupnorm_wait(0)
+        try:
+            b, n = c.forward(), c.forward(stats=False)
+            h, i = c.backward(a[1], a[2]), c.backward(a[1], a[2], inplace=True)
+            v = c.backward(a[1], a[2], vectors=False)
+        finally:
+            assert rc.train_diag_groupnorm_wait(before) == 0
+        j = c.backward(a[1], a[2], inplace=True)
+        assert all(np.array_equal(p, q) for p, q in zip(a + g + g + g, b + h + i + j)), shape
+        assert np.array_equal(n[0], a[0]) and np.array_equal(v[0], g[0])
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+def test_large_groups_far_from_zero(layout):
+    for shape in (SHARED[layout][0], THREE[layout][-2 if layout == "nhwc" else 0]):
+        c = Case(*shape, act="none", layout=layout, offset=4096.0)
+        mean, rstd = c.check_forward()
+        c.check_backward(mean, rstd)
+
+
+def test_more_groups_than_a_launch_has_workgroups_for():
+    """20 million groups of one element, in runs of channels that hold no whole number of vectors: x - mean is 0."""
+    N, C = 300, 65521
+    x = torch.randn(N, C, 1, 1, device="cuda")
+    y, mean, rstd = torch.empty_like(x), torch.empty(N, C, device="cuda"), torch.empty(N, C, device="cuda")
+    rc.train_groupnorm_fwd(x, None, None, y, mean, rstd, C)
+    assert torch.equal(mean, x[:, :, 0, 0]) and bool((y == 0).all())
+    assert float((rstd * (1e-5 ** 0.5) - 1).abs().max()) <= 4 * U
+    dy, dga, dbe = torch.randn_like(x), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")
+    dx = torch.empty_like(x)
+    rc.train_groupnorm_bwd(x, dy, None, None, mean, rstd, dx, dga, dbe, C)
+    assert bool((dx == 0).all()) and bool((dga == 0).all())
+    assert bool(((dbe.double() - dy[:, :, 0, 0].double().sum(0)).abs() <= 2 * U * dy.double().abs().sum((0, 2, 3))).all())
