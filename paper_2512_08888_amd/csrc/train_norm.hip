@@ -515,7 +515,7 @@ __device__ __forceinline__ bool collect(const unsigned long long* slots, int cou
 }
 
 template <typename E, int V, int J, bool BWD, int ACT>
-__global__ __launch_bounds__(kThreads, BWD ? 4 : 6) void k_gn_nchw(Gn q, Maps m) {
+__global__ __launch_bounds__(kThreads, BWD || J == 16 ? 4 : 6) void k_gn_nchw(Gn q, Maps m) {
   __shared__ Pair red[kMaxTeam];
   __shared__ Pair all[kMaxSplit];
   __shared__ int missing;
@@ -1030,7 +1030,7 @@ Gn cut_nhwc(Gn q, int elem, int per, bool held, bool bwd) {
     // several groups' statistics in a lane: fewer vectors, and backward shorter ones, for the registers
     if (q.C % q.vec || bwd) q.vec = q.C % 4 == 0 ? 4 : 1;
     q.one = q.vec == 1;
-    if (held) per = q.one ? 4 : std::min(per, 4);
+    if (held) per = q.one ? 4 : std::min(per, 8);
   }
   q.per = per;
   // the shortest run of whole groups that fills a cache line of every pixel
@@ -1056,13 +1056,16 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
   Gn best = {};
   auto with = [&](int per) { return layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, true, bwd) : cut_nchw(q, elem, per, true); };
   // A group (or run) in one workgroup needs no exchange and one launch: with as many lanes as that leaves.  Else the largest
-  // parts that still give every CU a workgroup.
+  // parts that still give every CU a workgroup, so that fewer wait for one another: forward sixteen vectors a lane, backward
+  // eight of each map.  (Forward by eight and by sixteen: bf16 4x128x256x256 channels last in 8 groups 41 and 31 us, NCHW in
+  // 32 groups 26.2 and 24.6; fp32 4x64x256x256 NCHW in 2 groups 31 and 24.  Backward, the same two: 55 and 62 us, 39 and 43.)
   for (int per : {2, 4, 8}) {
     best = with(per);
     if (best.split == 1) break;
   }
   if (best.split > 1)
-    for (int per : {8, 4, 2}) {
+    for (int per : {16, 8, 4, 2}) {
+      if (per == 16 && bwd) continue;
       best = with(per);
       if (workgroups(best, layout) >= 256) break;
     }
@@ -1110,17 +1113,28 @@ Kernels pick_of(const Gn& q, int layout) {
   constexpr int SUM = BWD ? ACT : TRAIN_ACT_NONE;        // forward sums know no activation
   if (layout == TRAIN_NCHW) {
     if (q.vec == 1) return {k_gn_nchw<E, 1, 2, BWD, ACT>, k_gn_nchw_map<E, 1, BWD, ACT>, k_gn_nchw_sums<E, 1, BWD, SUM>};
+    if constexpr (!BWD)
+      if (q.per == 16) return {k_gn_nchw<E, full, 16, BWD, ACT>, k_gn_nchw_map<E, full, BWD, ACT>, k_gn_nchw_sums<E, full, BWD, SUM>};
     return {q.per == 8 ? k_gn_nchw<E, full, 8, BWD, ACT> : q.per == 4 ? k_gn_nchw<E, full, 4, BWD, ACT> : k_gn_nchw<E, full, 2, BWD, ACT>,
             k_gn_nchw_map<E, full, BWD, ACT>, k_gn_nchw_sums<E, full, BWD, SUM>};
   }
   if (q.vec == 1) return {k_gn_nhwc<E, 1, 4, true, BWD, ACT>, k_gn_nhwc_map<E, 1, true, BWD, ACT>, k_gn_nhwc_sums<E, 1, true, BWD, SUM>};
   if constexpr (!BWD && full == 8)
     if (!q.one && q.vec == 8)
-      return {q.per == 4 ? k_gn_nhwc<E, 8, 4, false, BWD, ACT> : k_gn_nhwc<E, 8, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 8, false, BWD, ACT>,
+      return {q.per == 8   ? k_gn_nhwc<E, 8, 8, false, BWD, ACT>
+              : q.per == 4 ? k_gn_nhwc<E, 8, 4, false, BWD, ACT>
+                           : k_gn_nhwc<E, 8, 2, false, BWD, ACT>,
+              k_gn_nhwc_map<E, 8, false, BWD, ACT>,
               k_gn_nhwc_sums<E, 8, false, BWD, SUM>};
   if (!q.one)
-    return {q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT> : k_gn_nhwc<E, 4, 2, false, BWD, ACT>, k_gn_nhwc_map<E, 4, false, BWD, ACT>,
+    return {q.per == 8   ? k_gn_nhwc<E, 4, 8, false, BWD, ACT>
+            : q.per == 4 ? k_gn_nhwc<E, 4, 4, false, BWD, ACT>
+                         : k_gn_nhwc<E, 4, 2, false, BWD, ACT>,
+            k_gn_nhwc_map<E, 4, false, BWD, ACT>,
             k_gn_nhwc_sums<E, 4, false, BWD, SUM>};
+  if constexpr (!BWD)
+    if (q.per == 16)
+      return {k_gn_nhwc<E, full, 16, true, BWD, ACT>, k_gn_nhwc_map<E, full, true, BWD, ACT>, k_gn_nhwc_sums<E, full, true, BWD, SUM>};
   return {q.per == 8   ? k_gn_nhwc<E, full, 8, true, BWD, ACT>
           : q.per == 4 ? k_gn_nhwc<E, full, 4, true, BWD, ACT>
                        : k_gn_nhwc<E, full, 2, true, BWD, ACT>,
