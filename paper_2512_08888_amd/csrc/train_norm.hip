@@ -1063,14 +1063,18 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
     best = with(per);
     if (best.split == 1) break;
   }
+  // Where two launches make it, every workgroup of the map joins the sums of its run's groups for itself: half as many
+  // workgroups do where the parts would else leave more than 1024 sums (channels last bf16 3x60x101x75 in 12 groups, 672 sums
+  // and 1344: 11.5 and 13.2 us; 4x256x32x32 fp32 in 32 groups, 128 and 256: 10.7 and 10.0).
+  const bool two = (size_t)N * C * P * elem <= kTwoBytes;
+  auto sums_of = [&](const Gn& g) { return (size_t)g.split * (layout == TRAIN_NHWC ? g.run / g.cg : 1); };
   if (best.split > 1)
     for (int per : {16, 8, 4, 2}) {
       if (per == 16 && bwd) continue;
       best = with(per);
-      if (workgroups(best, layout) >= 256) break;
+      if (workgroups(best, layout) >= (two && sums_of(best) > 512 ? 128 : 256)) break;
     }
-  const size_t slots = (size_t)best.split * (layout == TRAIN_NHWC ? best.run / best.cg : 1);
-  if (best.mode == kSums || best.split > kMaxSplit || slots > (size_t)kMaxSlots) {
+  if (best.mode == kSums || best.split > kMaxSplit || sums_of(best) > (size_t)kMaxSlots) {
     // parts of any size, a few for each CU
     for (int per = 8;; per *= 2) {
       best = layout == TRAIN_NHWC ? cut_nhwc(q, elem, per, false, bwd) : cut_nchw(q, elem, per, false);
@@ -1078,7 +1082,7 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
     }
     best.mode = kSums;
   }
-  if (best.mode == kFused && best.split > 1 && (size_t)N * C * P * elem <= kTwoBytes) best.mode = kTwo;
+  if (best.mode == kFused && best.split > 1 && two) best.mode = kTwo;
   best.over = 65536 / best.period + 1;
   return best;
 }
