@@ -28,7 +28,8 @@ extern "C" {
  * backward pass sees every element on the side of a ReLU's kink on which the forward pass left it.
  * gamma / beta: fp32 [C], or NULL for ones / zeros.  mean, rstd: fp32 [N, groups].
  * A NaN or an infinity makes its group's results NaN and touches no other group; an activation
- * passes a NaN on. */
+ * passes a NaN on.
+ * Refused (ROTCONV_ERR_SHAPE): N or groups of 65536 or more, C above 2^20, P of 2^31 or more, N * C of 2^31 or more. */
 typedef enum { TRAIN_ACT_NONE = 0, TRAIN_ACT_RELU = 1, TRAIN_ACT_SILU = 2 } train_act;
 /* order of x, y, dy and dx in memory: [N][C][P] or, channels last, [N][P][C] */
 typedef enum { TRAIN_NCHW = 0, TRAIN_NHWC = 1 } train_layout;
@@ -64,7 +65,8 @@ int train_diag_groupnorm_wait(int ticks);
 
 /* ---- many tensors at once -----------------------------------------------------------------------
  * A list names parameter tensors with their gradients.  It holds their addresses, not their values: the
- * caller keeps the memory in place for as long as the list is used and creates another list where it moves. */
+ * caller keeps the memory in place for as long as the list is used and creates another list where it moves.  The list
+ * holds the counters by which a launch's workgroups find the last of them: one list serves one stream at a time. */
 typedef struct {
   float* param;            /* fp32; NULL in lists that are only measured */
   const void* grad;        /* of the list's gradient type */
@@ -93,8 +95,7 @@ typedef struct {
   float norm;              /* norm of all gradients, of the last train_grad_norm() */
   int32_t nonfinite;       /* 1: that norm was not finite; the next step then changes nothing but `skipped` */
   int32_t skipped;         /* steps skipped so */
-  uint32_t ticket[2];      /* 0 between calls */
-  int32_t reserved[8];
+  int32_t reserved[10];    /* 0 */
 } train_control;
 
 /* step as given, lr as given, coef 1, everything else 0 */
@@ -120,7 +121,7 @@ int train_grad_norm(const train_list* list, float max_norm, float* norms, train_
 typedef enum { TRAIN_STATE_F32 = 0, TRAIN_STATE_MX8 = 1 } train_state;
 typedef struct {
   double beta1, beta2;     /* 0 <= beta < 1 */
-  float eps;               /* > 0 */
+  float eps;               /* a normal number > 0 */
   int32_t state;           /* a train_state */
   uint32_t seed;
   int32_t reserved;        /* 0 */

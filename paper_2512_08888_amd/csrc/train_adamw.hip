@@ -1,13 +1,16 @@
 // Operators over many parameter tensors at once (see include/unettrain.h): the norm of all gradients with the factor
 // that clips it, and the AdamW step with states in 32 or in 8 bits.
 //
-// A list is cut into chunks of one tensor each; a table in device memory names every chunk's tensor, so one launch
-// covers tensors of any number and size.  The workgroups of a launch walk the chunks in steps of the grid and the last
-// one to end (an atomic ticket in the control block) finishes the call: it adds the chunks' sums in a fixed order, or
-// advances the step number.  Both kernels are HBM bound.
+// A list is cut into chunks of one tensor each; a table in device memory says of every chunk what a workgroup needs to know,
+// so one launch covers tensors of any number and size, a chunk to a workgroup.  The last workgroup to end (atomic tickets
+// that the list holds) finishes the call: it adds the chunks' sums in a fixed order, or advances the step number.
+// Both are HBM bound: a few operations an element.  31 M parameters (the 59 tensors of a UNet of widths 64 to 1024, fp32 gradients): the
+// norm reads 124 MB in 27 us (22.7 of them the reading, 1.4 the tickets, 3.4 the end), the step reads and writes 0.93 GB with
+// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 83 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -569,7 +572,7 @@ int train_adamw_step(const train_list* l, const train_adamw* o, void* m, void* v
   const bool mx8 = o->state == TRAIN_STATE_MX8;
   if (mx8 ? (!m_scale || !v_scale) : (m_scale || v_scale)) return ROTCONV_ERR_NULL;
   if (!l->trains || !on_its_device(l) || (!mx8 && o->state != TRAIN_STATE_F32) || o->reserved != 0) return ROTCONV_ERR_UNSUPPORTED;
-  if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1) || !(o->eps > 0.f)) return ROTCONV_ERR_UNSUPPORTED;
+  if (!(o->beta1 >= 0 && o->beta1 < 1 && o->beta2 >= 0 && o->beta2 < 1) || !(o->eps >= FLT_MIN)) return ROTCONV_ERR_UNSUPPORTED;
   if (misaligned(m, mx8 ? 4 : 16) || misaligned(v, mx8 ? 4 : 16) || misaligned(control, 4)) return ROTCONV_ERR_UNSUPPORTED;
   // LDS that nobody uses keeps five workgroups on a CU where eight would fit: with fp32 states their streams then get in one
   // another's way less (31 M parameters: 163 us with eight, 149 us with five or four); 8-bit states need all eight to keep

@@ -349,7 +349,7 @@ def test_pieces_that_divide_a_channel_but_for_its_end():
 SHARED = {"nchw": [(4, 64, 133, 131, 4), (9, 24, 141, 143, 1)], "nhwc": [(4, 64, 133, 131, 4), (5, 56, 131, 127, 14), (10, 33, 120, 123, 3)]}
 # Groups of more parts than wait for one another, or of more sums than a workgroup collects; groups wider than a run of
 # channels, and runs that are not of whole groups
-THREE = {"nchw": [(1, 6, 1201, 1200, 1), (1, 12, 1201, 1200, 1)],
+THREE = {"nchw": [(1, 6, 1201, 1200, 1), (1, 12, 1201, 1200, 1), (1, 65700, 1, 7, 1), (1, 33000, 8, 8, 1)],
          "nhwc": [(2, 521, 5, 7, 521), (1, 2060, 3, 3, 2), (1, 2064, 4, 3, 2), (2, 2056, 3, 7, 2), (1, 64, 130, 130, 64), (2, 33, 190, 199, 11)]}
 
 
