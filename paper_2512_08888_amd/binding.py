@@ -393,7 +393,7 @@ def rotconv_steerable_reg(w, lambda_mag, lambda_orth, eps, losses, dw=None, accu
 # ---- network glue (include/unetglue.h): same names, argument marshalling only -------------------
 
 def _nbytes(t):
-    return 0 if t is None else t.numel() * t.element_size()
+    return 0 if t is None else t.nbytes
 
 
 def _glue(name, *tensors):
@@ -504,15 +504,18 @@ _f32 = None      # torch.float32, once torch is needed
 
 def _map_layout(what, x, others):
     """The order in memory that all maps [N, C, ...] of one call share: NCHW (contiguous), or channels last."""
-    shape, kind, plain = x.shape, x.dtype, x.is_contiguous()
+    shape, kind, plain, resident = x.shape, x.dtype, x.is_contiguous(), x.is_cuda
     for m in others:
         if m.shape != shape:
             raise ValueError(f"{what}: maps must have one shape, got {tuple(shape)} and {tuple(m.shape)}")
         if m.dtype is not kind:
             raise TypeError(f"{what}: tensors must be all float32 or all bfloat16, got {kind} and {m.dtype}")
         plain = plain and m.is_contiguous()
+        resident = resident and m.is_cuda
     if len(shape) < 2:
         raise ValueError(f"{what}: maps are [N, C, ...]")
+    if not resident:
+        raise ValueError(f"{what}: maps must be on the GPU")
     if plain:
         return NCHW
     if len(shape) == 4:
@@ -527,8 +530,8 @@ def _vec(what, name, t, n):
     """Address of an fp32 tensor of n elements; None stays NULL."""
     if t is None:
         return None
-    if t.dtype is not _f32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{what}: {name} must be float32, contiguous, with {n} elements")
+    if t.dtype is not _f32 or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: {name} must be float32, contiguous, on the GPU, with {n} elements")
     return t.data_ptr()
 
 
@@ -541,6 +544,8 @@ def _groupnorm(what, x, others, groups, act, ws):
         _f32 = torch.float32
         lib()
     layout = _map_layout(what, x, others)
+    if ws is not None and not ws.is_cuda:
+        raise ValueError(f"{what}: the workspace must be on the GPU")
     shape = x.shape
     N, C = shape[0], shape[1]
     P = x.numel() // (N * C) if N * C else 0
@@ -605,6 +610,9 @@ class TrainList:
                 raise TypeError("TrainList: parameters must be float32 in the shape of their gradients")
             if c is not None and (c.dtype != torch.bfloat16 or c.shape != g.shape):
                 raise TypeError("TrainList: copies must be bfloat16 in the shape of the gradients")
+        devices = {t.device for ts in (params, grads, copies) for t in ts if t is not None}
+        if len(devices) > 1 or any(d.type != "cuda" for d in devices):
+            raise ValueError(f"TrainList: tensors must be on one GPU, got {sorted(map(str, devices))}")
         self.tensors = (params, grads, copies)
         rows = (TrainTensor * max(1, k))(*[TrainTensor(_ptr(p), _ptr(g), _ptr(c), g.numel(), w, 0)
                                            for p, g, c, w in zip(params, grads, copies, decay)])
@@ -630,16 +638,38 @@ class TrainList:
         return self._h
 
 
+def _room(what, name, t, nbytes, align=1):
+    """Address of a device buffer of at least nbytes; None stays NULL, and an address off `align` is the library's to refuse."""
+    if t is None:
+        return None
+    p = t.data_ptr()
+    if not t.is_contiguous() or not t.is_cuda or (t.nbytes < nbytes and p % align == 0):
+        raise ValueError(f"{what}: {name} must be contiguous, with {nbytes} bytes on the GPU")
+    return p
+
+
+CONTROL_BYTES = 64
+
+
 def train_control_init(control, step=0, lr=0.0):
     """control: 16 int32 on the device (train_control)."""
-    _check(lib().train_control_init(_ptr(control), int(step), float(lr), _stream()), "train_control_init")
+    what = "train_control_init"
+    _check(lib().train_control_init(_room(what, "control", control, CONTROL_BYTES), int(step), float(lr), _stream()), what)
 
 
 def train_grad_norm(tensors: TrainList, max_norm, norms, control, ws):
-    _check(lib().train_grad_norm(tensors.handle, max_norm, _ptr(norms), _ptr(control), _ptr(ws), _nbytes(ws), _stream()),
-           "train_grad_norm")
+    """norms: fp32 [count] or None; control: 16 int32; ws: tensors.workspace_bytes."""
+    what = "train_grad_norm"
+    _check(lib().train_grad_norm(tensors.handle, max_norm, _room(what, "norms", norms, 4 * tensors.count),
+                                 _room(what, "control", control, CONTROL_BYTES), _room(what, "ws", ws, 0), _nbytes(ws),
+                                 _stream()), what)
 
 
 def train_adamw_step(tensors: TrainList, options: TrainAdamW, m, v, m_scale, v_scale, control):
-    _check(lib().train_adamw_step(tensors.handle, ctypes.byref(options), _ptr(m), _ptr(v), _ptr(m_scale), _ptr(v_scale),
-                                  _ptr(control), _stream()), "train_adamw_step")
+    """m, v: tensors.elements values each, fp32 or (8-bit states) bytes; the scales: a byte for each 32 of them, or None."""
+    what, n = "train_adamw_step", tensors.elements
+    size, align = (1, 4) if options.state == STATES["mx8"] else (4, 16)
+    _check(lib().train_adamw_step(tensors.handle, ctypes.byref(options), _room(what, "m", m, n * size, align),
+                                  _room(what, "v", v, n * size, align), _room(what, "m_scale", m_scale, n // 32),
+                                  _room(what, "v_scale", v_scale, n // 32), _room(what, "control", control, CONTROL_BYTES),
+                                  _stream()), what)

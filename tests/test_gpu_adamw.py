@@ -355,6 +355,37 @@ def test_refusals_on_the_device():
     assert opt.step_count.item() == 0
 
 
+@pytest.mark.parametrize("state", ["f32", "mx8"])
+def test_buffers_that_are_too_small_or_elsewhere(state):
+    net = Net([100, 7])
+    opt = train.AdamW(net.params, net.grads, state=state)
+    n = opt.list.elements
+    assert n == 160
+
+    def step(**kw):
+        a = dict(m=opt.m, v=opt.v, m_scale=opt.m_scale, v_scale=opt.v_scale, control=opt.control)
+        a.update(kw)
+        rc.train_adamw_step(opt.list, opt.options, *a.values())
+
+    bad = [dict(m=opt.m[:n - 4]), dict(v=opt.v[:n - 4]), dict(m=opt.m.cpu()), dict(control=opt.control[:8])]
+    if state == "mx8":
+        bad += [dict(m_scale=opt.m_scale[:4]), dict(v_scale=opt.v_scale[1:])]
+    for kw in bad:
+        with pytest.raises(ValueError):
+            step(**kw)
+    for norms, control in ((opt.norms[:1], opt.control), (opt.norms, opt.control[:15]), (opt.norms.cpu(), opt.control)):
+        with pytest.raises(ValueError):
+            rc.train_grad_norm(opt.list, 1.0, norms, control, opt.ws)
+    with pytest.raises(ValueError):
+        rc.train_control_init(opt.control[:15])
+    with pytest.raises(ValueError):
+        rc.TrainList([net.grads[0], net.grads[1].cpu()])
+    with pytest.raises(rc.RotconvError):                               # an eps whose reciprocal is not finite
+        rc.train_adamw_step(opt.list, rc.TrainAdamW(0.9, 0.999, 1e-40, rc.STATES[state], 0, 0), opt.m, opt.v, opt.m_scale, opt.v_scale, opt.control)
+    torch.cuda.synchronize()
+    assert opt.step_count.item() == 0
+
+
 def test_offsets_beyond_32_bits():
     """One tensor of more than 2^32 elements, states in 8 bits: its first and last elements against the formula."""
     n = (1 << 32) + 100

@@ -118,6 +118,20 @@ def test_binding_refusals():
         rc.TrainList([torch.zeros(4, 4).t()])
 
 
+def test_binding_refuses_host_memory():
+    import torch
+
+    x, v, s = torch.zeros(2, 6, 3, 5), torch.ones(6), torch.zeros(2, 3)
+    with pytest.raises(ValueError, match="GPU"):
+        rc.train_groupnorm_fwd(x, v, v, torch.zeros_like(x), s, s, 3)
+    with pytest.raises(ValueError, match="GPU"):
+        rc.train_groupnorm_bwd(x, x, v, v, s, s, torch.zeros_like(x), v, v, 3)
+    with pytest.raises(ValueError, match="GPU"):
+        rc.TrainList([torch.zeros(3)], [torch.zeros(3)])
+    with pytest.raises(ValueError, match="GPU"):
+        rc.train_control_init(torch.zeros(16, dtype=torch.int32))
+
+
 @pytest.mark.parametrize("act", ["none", "silu"])
 @pytest.mark.parametrize("shape,groups", [((2, 6, 5), 3), ((1, 4, 1), 1), ((3, 4, 7), 4)])
 def test_oracle_gradients_against_differences(act, shape, groups):
