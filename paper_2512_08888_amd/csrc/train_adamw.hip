@@ -279,10 +279,15 @@ __device__ __forceinline__ void from_e4m3_x4(uint32_t w, float scale, float* v) 
 
 // 0 <= q <= 448 onto the e4m3 grid, up with the probability of the part cut off, a positive q to no less than the smallest
 // code.  random: 16 bits, times 16.  The twenty bits below e4m3's three of the mantissa take them as a carry; values whose
-// grid has the step 2^-9 (below 2^-6) are moved to [2^-6, 2^-5) for that, where fp32 has the same bits for it.
-__device__ __forceinline__ float round_up_or_down(float q, uint32_t random) {
+// grid has the step 2^-9 (below 2^-6) are moved to [2^-6, 2^-5) for that, where fp32 has the same bits for it.  rest: has the
+// sign of what q lacks of the value that it was rounded from.  Where the bits end exactly on a code, that says whether the
+// value reaches it: the code is then the one that arithmetic without rounding gives (of 31 M elements some 15 were not).
+__device__ __forceinline__ float round_up_or_down(float q, uint32_t random, float rest) {
   const float shift = q < 0x1p-6f ? 0x1p-6f : 0.f;
-  const float r = __uint_as_float((__float_as_uint(q + shift) + random) & 0xfff00000u) - shift;
+  const float placed = q + shift, lacks = q - (placed - shift);
+  const uint32_t sum = __float_as_uint(placed) + random;
+  const bool short_of = (sum & 0xfffffu) == 0 && (lacks < 0.f || (lacks == 0.f && rest < 0.f));
+  const float r = __uint_as_float((sum - short_of) & 0xfff00000u) - shift;
   return q > 0.f ? fmaxf(r, 0x1p-9f) : 0.f;
 }
 
@@ -301,15 +306,25 @@ __device__ __forceinline__ double power(double b, int t) {
   return r;
 }
 
-// m and v of one element, and its parameter.  Every operation is rounded by itself: a state in 8 bits then takes the
-// same code wherever this formula is evaluated in fp32.  The quotient alone, which no state depends on, is a product with
-// the instruction's reciprocal (2 ulp of the update).
-__device__ __forceinline__ void adamw(const Step& s, float wd, float grad, float& p, float& m, float& v, float& root) {
+// m and v of one element, and its parameter.  In 32 bits every operation is rounded by itself.  In 8 bits v holds sqrt(v);
+// its square is formed and decayed in 64 bits, which this chip does as fast as unpacked fp32, and rest tells the root's
+// rounding (see round_up_or_down).  The quotient alone, which no state depends on, is a product with the instruction's
+// reciprocal (2 ulp of the update).
+template <bool MX8>
+__device__ __forceinline__ void adamw(const Step& s, const train_adamw& opt, float wd, float grad, float& p, float& m, float& v,
+                                      float& root, float& rest) {
 #pragma clang fp contract(off)
   const float g = grad * s.coef;
   m = m * s.b1 + g * s.c1;
-  v = v * s.b2 + g * g * s.c2;
-  root = sqrtf(v);
+  if constexpr (MX8) {
+    const double exact = (double)grad * s.coef;
+    const double square = fma(opt.beta2, (double)v * v, (1 - opt.beta2) * (exact * exact));
+    root = sqrtf((float)square);
+    rest = (float)fma(-(double)root, (double)root, square);
+  } else {
+    v = v * s.b2 + g * g * s.c2;
+    root = sqrtf(v);
+  }
   const float update = m * __builtin_amdgcn_rcpf(root * s.root + s.eps);
   p = p - p * (wd * s.lr) - update * s.rate;
 }
@@ -390,7 +405,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
     end();
     return;
   }
-  float p[4], m[4], v[4], root[4];
+  float p[4], m[4], v[4], root[4], rest[4];
   if constexpr (MX8) {
     from_e4m3_x4(cm, scale_value(sm), m);
     from_e4m3_x4(cv, scale_value(sv), v);
@@ -398,9 +413,8 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     p[k] = pv[k];
-    if constexpr (MX8) v[k] = v[k] * v[k];
-    else m[k] = fm[k], v[k] = fv[k];
-    adamw(s, r.wd, gv.get(k), p[k], m[k], v[k], root[k]);
+    if constexpr (!MX8) m[k] = fm[k], v[k] = fv[k];
+    adamw<MX8>(s, opt, r.wd, gv.get(k), p[k], m[k], v[k], root[k], rest[k]);
   }
   if (whole) {
     stream_store(reinterpret_cast<f4*>(r.p + i), f4{p[0], p[1], p[2], p[3]});
@@ -425,8 +439,8 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
 #pragma unroll
     for (int k = 0; k < 4; k += 2) {       // sixteen random bits an element
       const uint32_t h = mix32((uint32_t)((at + k) >> 1) + s.key);
-      root[k] = round_up_or_down(root[k] * inv, h << 4 & 0xffff0u);
-      root[k + 1] = round_up_or_down(root[k + 1] * inv, h >> 12 & 0xffff0u);
+      root[k] = round_up_or_down(root[k] * inv, h << 4 & 0xffff0u, rest[k]);
+      root[k + 1] = round_up_or_down(root[k + 1] * inv, h >> 12 & 0xffff0u, rest[k + 1]);
     }
     stream_store(reinterpret_cast<uint32_t*>(vp) + at / 4, e4m3_x4(root));
     if (at % kBlock == 0) msp[at / kBlock] = (uint8_t)mb, vsp[at / kBlock] = (uint8_t)vb;
