@@ -6,7 +6,7 @@
 // that the list holds) finishes the call: it adds the chunks' sums in a fixed order, or advances the step number.
 // Both are HBM bound: a few operations an element.  31 M parameters (the 59 tensors of a UNet of widths 64 to 1024, fp32 gradients): the
 // norm reads 124 MB in 27 us (22.7 of them the reading, 1.4 the tickets, 3.4 the end), the step reads and writes 0.93 GB with
-// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 83 us.
+// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 85 us (5.9).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -307,8 +307,8 @@ __device__ __forceinline__ double power(double b, int t) {
 }
 
 // m and v of one element, and its parameter.  In 32 bits every operation is rounded by itself.  In 8 bits v holds sqrt(v);
-// its square is formed and decayed in 64 bits, which this chip does as fast as unpacked fp32, and rest tells the root's
-// rounding (see round_up_or_down).  The quotient alone, which no state depends on, is a product with the instruction's
+// its square is formed and decayed in 64 bits, and rest tells the root's rounding (see round_up_or_down): 85 us for 31 M
+// parameters, 82.7 in 32 bits, and as long where only elements that end close to a code are done again in 64.  The quotient alone, which no state depends on, is a product with the instruction's
 // reciprocal (2 ulp of the update).
 template <bool MX8>
 __device__ __forceinline__ void adamw(const Step& s, const train_adamw& opt, float wd, float grad, float& p, float& m, float& v,
@@ -590,7 +590,7 @@ int train_adamw_step(const train_list* l, const train_adamw* o, void* m, void* v
   if (misaligned(m, mx8 ? 4 : 16) || misaligned(v, mx8 ? 4 : 16) || misaligned(control, 4)) return ROTCONV_ERR_UNSUPPORTED;
   // LDS that nobody uses keeps five workgroups on a CU where eight would fit: with fp32 states their streams then get in one
   // another's way less (31 M parameters: 163 us with eight, 149 us with five or four); 8-bit states need all eight to keep
-  // enough bytes under way (89 us with eight, 112 us with five).
+  // enough bytes under way (89 us with eight, 112 us with five, when the whole took that long).
   const size_t lds = mx8 ? 0 : 32000;
   auto kernel = mx8 ? (l->bf16 ? k_adamw<uint16_t, true> : k_adamw<float, true>) : (l->bf16 ? k_adamw<uint16_t, false> : k_adamw<float, false>);
   kernel<<<l->nstep, kThreads, lds, static_cast<hipStream_t>(stream)>>>(l->step, *o, m, v, m_scale, v_scale, control, l->tickets);
