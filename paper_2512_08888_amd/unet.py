@@ -393,17 +393,19 @@ class UNet:
         graph on the current device; `replay()` then runs the whole step with one launch from the host.  Every
         library call enqueues kernels only and every buffer of the step is preallocated, so the recorded step is
         the eager step.  With an optimizer the recorded step is train_step(optimizer, max_norm); its step number and
-        learning rate live on the device."""
+        learning rate live on the device, and the network keeps the optimizer until the next recording, since the
+        graph holds addresses of its memory.  (A graph that outlives the network needs both kept.)"""
         assert self.trace is None
         self.step()
         self.torch.cuda.synchronize()
-        self._graph = self.torch.cuda.CUDAGraph()
-        with self.torch.cuda.graph(self._graph):
+        graph = self.torch.cuda.CUDAGraph()
+        with self.torch.cuda.graph(graph):
             if optimizer is None:
                 self.step()
             else:
                 self.train_step(optimizer, max_norm)
-        return self._graph
+        self._graph, self._graph_optimizer = graph, optimizer
+        return graph
 
     def replay(self):
         self._graph.replay()
