@@ -6,7 +6,7 @@
 // that the list holds) finishes the call: it adds the chunks' sums in a fixed order, or advances the step number.
 // Both are HBM bound: a few operations an element.  31 M parameters (the 59 tensors of a UNet of widths 64 to 1024, fp32 gradients): the
 // norm reads 124 MB in 27 us (22.7 of them the reading, 1.4 the tickets, 3.4 the end), the step reads and writes 0.93 GB with
-// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 85 us (5.9).
+// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 84 us (5.9).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -246,10 +246,11 @@ __device__ __forceinline__ uint32_t scale_byte(float top, float* inv) {
   const uint32_t bits = __float_as_uint(top);
   const int e = (int)(bits >> 23) - 135 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0);
   const uint32_t byte = bits >= 0x7f800000u ? 255u : (uint32_t)(max(e, -127) + 127);
-  // 2^(127 - byte) as fp32; the smallest are denormal
+  // 2^(127 - byte): 2^-120 to 2^127, since no finite top needs a byte above 247
   *inv = byte == 255u ? NAN : ldexpf(1.f, 127 - (int)byte);
   return byte;
 }
+// 2^-127 (denormal in fp32) to 2^127
 __device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? NAN : ldexpf(1.f, (int)byte - 127); }
 
 // largest magnitude of the eight lanes that hold a block (32 elements, four a lane), compared as bits: a NaN is above an
@@ -277,18 +278,33 @@ __device__ __forceinline__ void from_e4m3_x4(uint32_t w, float scale, float* v) 
   v[3] = __builtin_amdgcn_cvt_f32_fp8(w, 3) * scale;
 }
 
-// 0 <= q <= 448 onto the e4m3 grid, up with the probability of the part cut off, a positive q to no less than the smallest
-// code.  random: 16 bits, times 16.  The twenty bits below e4m3's three of the mantissa take them as a carry; values whose
-// grid has the step 2^-9 (below 2^-6) are moved to [2^-6, 2^-5) for that, where fp32 has the same bits for it.  rest: has the
-// sign of what q lacks of the value that it was rounded from.  Where the bits end exactly on a code, that says whether the
-// value reaches it: the code is then the one that arithmetic without rounding gives (of 31 M elements some 15 were not).
-__device__ __forceinline__ float round_up_or_down(float q, uint32_t random, float rest) {
-  const float shift = q < 0x1p-6f ? 0x1p-6f : 0.f;
-  const float placed = q + shift, lacks = q - (placed - shift);
-  const uint32_t sum = __float_as_uint(placed) + random;
-  const bool short_of = (sum & 0xfffffu) == 0 && (lacks < 0.f || (lacks == 0.f && rest < 0.f));
-  const float r = __uint_as_float((sum - short_of) & 0xfff00000u) - shift;
-  return q > 0.f ? fmaxf(r, 0x1p-9f) : 0.f;
+// Four 0 <= q <= 448 onto the e4m3 grid, up with the probability of the part cut off, a positive value (q itself may be too small
+// for fp32) to no less than the smallest code.  random: 16 bits, times 16.  The twenty bits below e4m3's three of the mantissa
+// take them as a carry; values whose grid has the step 2^-9 (below 2^-6) are moved to [2^-6, 2^-5) for that, where fp32 has the
+// same bits for it.  rest: has the sign of what q lacks of the value that it was rounded from.  Where the bits end exactly on a
+// code, that says whether the value reaches it: the code is then the one that arithmetic without rounding gives (of 31 M elements
+// some 15 were not).
+__device__ __forceinline__ void round_up_or_down(float* q, const uint32_t* random, const float* rest, const bool* positive) {
+  uint32_t sum[4], least = ~0u;
+  float shift[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    shift[k] = q[k] < 0x1p-6f ? 0x1p-6f : 0.f;
+    sum[k] = __float_as_uint(q[k] + shift[k]) + random[k];
+    least = min(least, sum[k] & 0xfffffu);
+  }
+  if (least == 0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float lacks = q[k] - (q[k] + shift[k] - shift[k]);
+      sum[k] -= (sum[k] & 0xfffffu) == 0 && (lacks < 0.f || (lacks == 0.f && rest[k] < 0.f));
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float r = __uint_as_float(sum[k] & 0xfff00000u) - shift[k];
+    q[k] = positive[k] ? fmaxf(r, 0x1p-9f) : 0.f;
+  }
 }
 
 struct Step {                          // what a step's elements share
@@ -306,26 +322,42 @@ __device__ __forceinline__ double power(double b, int t) {
   return r;
 }
 
-// m and v of one element, and its parameter.  In 32 bits every operation is rounded by itself.  In 8 bits v holds sqrt(v);
-// its square is formed and decayed in 64 bits, and rest tells the root's rounding (see round_up_or_down): 85 us for 31 M
-// parameters, 82.7 in 32 bits, and as long where only elements that end close to a code are done again in 64.  The quotient alone, which no state depends on, is a product with the instruction's
-// reciprocal (2 ulp of the update).
-template <bool MX8>
-__device__ __forceinline__ void adamw(const Step& s, const train_adamw& opt, float wd, float grad, float& p, float& m, float& v,
-                                      float& root, float& rest) {
+// m and v of one element, and its parameter: every operation is rounded by itself.
+__device__ __forceinline__ void adamw(const Step& s, float wd, float grad, float& p, float& m, float& v) {
 #pragma clang fp contract(off)
   const float g = grad * s.coef;
   m = m * s.b1 + g * s.c1;
-  if constexpr (MX8) {
-    const double exact = (double)grad * s.coef;
-    const double square = fma(opt.beta2, (double)v * v, (1 - opt.beta2) * (exact * exact));
-    root = sqrtf((float)square);
-    rest = (float)fma(-(double)root, (double)root, square);
+  v = v * s.b2 + g * g * s.c2;
+  p = p - p * (wd * s.lr) - m * __builtin_amdgcn_rcpf(sqrtf(v) * s.root + s.eps) * s.rate;
+}
+// The same in 8 bits.  v holds sqrt(v); its square is formed and decayed in 64 bits, and rest tells the root's rounding (see
+// round_up_or_down).  The quotient, which no state depends on, is a product with the instruction's reciprocal (2 ulp of the update).
+// Bound by instructions as much as by memory (31 M parameters: 84.4 us, 85.4 with sqrtf()).  So the square is narrowed for a first
+// root that one step of Newton's makes good to its last bit, with v and the gradient 2^32 times as large for room below.
+// FAR: for any square, by a root in 64 bits; else for blocks whose largest sqrt(v) is from 2^-48 to 2^30, and an eps from 2^-64:
+// what is too small for fp32 there has the smallest code, and does not show beside eps.
+constexpr float kLift = 0x1p32f;
+template <bool FAR>
+__device__ __forceinline__ void adamw_mx8(const Step& s, const train_adamw& opt, float wd, float grad, float& p, float& m, float& v,
+                                          float& rest, bool& positive) {
+#pragma clang fp contract(off)
+  const float g = grad * s.coef;
+  m = m * s.b1 + g * s.c1;
+  const double exact = (double)grad * (FAR ? (double)s.coef : (double)s.coef * kLift);
+  const double square = fma(opt.beta2, (double)v * v, (1 - opt.beta2) * (exact * exact));
+  positive = square > 0;
+  float update;
+  if constexpr (FAR) {
+    const double root = sqrt(square);
+    v = (float)root;
+    rest = root > v ? 1.f : root < v ? -1.f : 0.f;
+    update = m / (v * s.root + s.eps);
   } else {
-    v = v * s.b2 + g * g * s.c2;
-    root = sqrtf(v);
+    const float x = (float)square, y = __builtin_amdgcn_rsqf(fmaxf(x, FLT_MIN)), first = x * y;
+    v = fmaf(fmaf(-first, first, x), 0.5f * y, first);                  // sqrt(x) to half of the last bit, and a little
+    rest = (float)fma(-(double)v, (double)v, square);
+    update = m * __builtin_amdgcn_rcpf(v * (s.root / kLift) + s.eps);
   }
-  const float update = m * __builtin_amdgcn_rcpf(root * s.root + s.eps);
   p = p - p * (wd * s.lr) - update * s.rate;
 }
 
@@ -405,16 +437,57 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
     end();
     return;
   }
-  float p[4], m[4], v[4], root[4], rest[4];
+  float p[4];
   if constexpr (MX8) {
+    float m[4], v[4], rest[4], inv;
+    bool positive[4];
     from_e4m3_x4(cm, scale_value(sm), m);
-    from_e4m3_x4(cv, scale_value(sv), v);
-  }
+    from_e4m3_x4(cv, scale_value(sv) * kLift, v);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    p[k] = pv[k];
-    if constexpr (!MX8) m[k] = fm[k], v[k] = fv[k];
-    adamw<MX8>(s, opt, r.wd, gv.get(k), p[k], m[k], v[k], root[k], rest[k]);
+    for (int k = 0; k < 4; ++k) {
+      p[k] = pv[k];
+      adamw_mx8<false>(s, opt, r.wd, gv.get(k), p[k], m[k], v[k], rest[k], positive[k]);
+    }
+    float top = block_top(v);
+    float lower = 1.f / kLift;
+    if (!(top >= 0x1p-48f * kLift && top <= 0x1p30f * kLift) || s.eps < 0x1p-64f) {       // the lanes of a block go together
+      lower = 1.f;
+      from_e4m3_x4(cm, scale_value(sm), m);
+      from_e4m3_x4(cv, scale_value(sv), v);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        p[k] = pv[k];
+        adamw_mx8<true>(s, opt, r.wd, gv.get(k), p[k], m[k], v[k], rest[k], positive[k]);
+      }
+      top = block_top(v);
+    }
+    const uint32_t vb = scale_byte(top * lower, &inv);
+    inv *= lower;
+    uint32_t random[4];                    // sixteen random bits an element
+#pragma unroll
+    for (int k = 0; k < 4; k += 2) {
+      const uint32_t h = mix32((uint32_t)((at + k) >> 1) + s.key);
+      random[k] = h << 4 & 0xffff0u, random[k + 1] = h >> 12 & 0xffff0u;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = v[k] * inv;
+    round_up_or_down(v, random, rest, positive);
+    stream_store(reinterpret_cast<uint32_t*>(vp) + at / 4, e4m3_x4(v));
+    const uint32_t mb = scale_byte(block_top(m), &inv);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) m[k] = m[k] * inv;
+    stream_store(reinterpret_cast<uint32_t*>(mp) + at / 4, e4m3_x4(m));
+    if (at % kBlock == 0) msp[at / kBlock] = (uint8_t)mb, vsp[at / kBlock] = (uint8_t)vb;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float m = fm[k], v = fv[k];
+      p[k] = pv[k];
+      adamw(s, r.wd, gv.get(k), p[k], m, v);
+      fm[k] = m, fv[k] = v;
+    }
+    stream_store(reinterpret_cast<f4*>(static_cast<float*>(mp) + at), fm);
+    stream_store(reinterpret_cast<f4*>(static_cast<float*>(vp) + at), fv);
   }
   if (whole) {
     stream_store(reinterpret_cast<f4*>(r.p + i), f4{p[0], p[1], p[2], p[3]});
@@ -428,25 +501,6 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
         r.p[i + k] = p[k];
         if (r.copy) r.copy[i + k] = f32_to_bf16(p[k]);
       }
-  }
-  if constexpr (MX8) {
-    float inv;
-    const uint32_t mb = scale_byte(block_top(m), &inv);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) m[k] = m[k] * inv;
-    stream_store(reinterpret_cast<uint32_t*>(mp) + at / 4, e4m3_x4(m));
-    const uint32_t vb = scale_byte(block_top(root), &inv);
-#pragma unroll
-    for (int k = 0; k < 4; k += 2) {       // sixteen random bits an element
-      const uint32_t h = mix32((uint32_t)((at + k) >> 1) + s.key);
-      root[k] = round_up_or_down(root[k] * inv, h << 4 & 0xffff0u, rest[k]);
-      root[k + 1] = round_up_or_down(root[k + 1] * inv, h >> 12 & 0xffff0u, rest[k + 1]);
-    }
-    stream_store(reinterpret_cast<uint32_t*>(vp) + at / 4, e4m3_x4(root));
-    if (at % kBlock == 0) msp[at / kBlock] = (uint8_t)mb, vsp[at / kBlock] = (uint8_t)vb;
-  } else {
-    stream_store(reinterpret_cast<f4*>(static_cast<float*>(mp) + at), f4{m[0], m[1], m[2], m[3]});
-    stream_store(reinterpret_cast<f4*>(static_cast<float*>(vp) + at), f4{v[0], v[1], v[2], v[3]});
   }
   end();
 }

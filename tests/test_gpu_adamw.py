@@ -406,3 +406,59 @@ def test_offsets_beyond_32_bits():
         unit = 2.0 ** (int(opt.m_scale.view(torch.uint8)[blk]) - 127)
         assert np.all(np.abs(opt.m[at].float().cpu().numpy() * unit - m) <= np.abs(m) / 16)
     assert int(opt.m[5:64].view(torch.uint8).any()) == 0 and float(p[5:n - 5].abs().max()) == 0
+
+
+# sqrt(v) far from 1: its square is below or above what fp32 holds, sqrt(v) itself is not.
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-8])
+@pytest.mark.parametrize("size", [1e-24, 1e-22, 3e-21, 1e-20, 1e-18, 1e-14, 1e-11, 1.0, 1e9, 1e12, 1e18, 1e21, 1e24, 1e30, 1e37])
+def test_8_bit_states_far_from_one(size, eps):
+    """Codes and scales of sqrt(v) are those of 64 bits wherever fp32 holds sqrt(v) as a normal number, no finite gradient marks its
+    block, no positive sqrt(v) becomes 0, and the parameters move by the formula.  Blocks of one size, of sizes up to 2^20 apart,
+    and with a few elements at 0."""
+    n, seed, lr = 4096, 17, 1e-3
+    rng = np.random.default_rng(3)
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+    opt = train.AdamW([p], [g], lr=lr, betas=(0.9, 0.999), eps=eps, state="mx8", seed=seed)
+    lr, eps = opt.lr.item(), float(np.float32(eps))
+    for t in range(1, 5):
+        spread = np.where(np.arange(n) < n // 2, 1.0, 2.0 ** -rng.integers(0, 21, n))
+        g.copy_(torch.from_numpy((size * spread * (0.5 + rng.random(n)) * rng.choice([-1.0, 1.0], n)).astype(np.float32)))
+        g[5::97] = 0.0
+        g64 = g.double().cpu().numpy()
+        m0, s0 = decode(opt.m, opt.m_scale)[0], decode(opt.v, opt.v_scale)[0]
+        before = p.double().cpu().numpy()
+        opt.step()
+        ref, m, v = to.adamw(before, g64, m0, s0 ** 2, t, lr, 0.9, 0.999, eps, 0.0)
+        s = np.sqrt(v)
+        fs, cs, es = decode(opt.v, opt.v_scale)
+        assert np.array_equal(es, to.block_exponents(s)) and np.all(cs[s > 0] > 0) and np.all(cs[s == 0] == 0)
+        unit = np.repeat(2.0 ** es, 32)
+        q = s / unit
+        step = to.grid_step(q)
+        at = q / step + to.random16(np.arange(n), t, seed)
+        want = np.where(q > 0, np.maximum(np.floor(at), 1), 0) * step * unit
+        assert np.all((fs == want) | (np.abs(at - np.round(at)) < 2.0 ** -44))
+        # the update is lr times a quotient of at most sqrt(1 / (1 - beta2)): 64 u of it with m's terms as magnitudes
+        move = to.adamw(np.zeros(n), np.abs(g64), np.abs(m0), s0 ** 2, t, lr, 0.9, 0.999, eps, 0.0)[0]
+        assert np.all(np.abs(p.double().cpu().numpy() - ref) <= 4 * U * (np.abs(before) + np.abs(ref)) + 64 * U * np.abs(move))
+
+
+def test_8_bit_states_at_the_ends_of_the_range():
+    """The smallest gradient and the largest: no code of 0 beside a positive sqrt(v), and nothing that is not finite."""
+    for size in (2.0 ** -149, 2.0 ** -126, 3.3e38):
+        p, g = torch.zeros(64, device="cuda"), torch.full((64,), size, device="cuda")
+        opt = train.AdamW([p], [g], lr=1e-3, betas=(0.9, 0.999), eps=2.0 ** -126, state="mx8")
+        for _ in range(3):
+            opt.step()
+            fs, cs, _ = decode(opt.v, opt.v_scale)
+            assert np.all(cs > 0) and bool(torch.isfinite(p).all()) and np.isfinite(decode(opt.m, opt.m_scale)[0]).all()
+
+
+def test_elements_that_vanish_beside_their_block():
+    """A positive sqrt(v) 2^-200 times its block's largest: the smallest code."""
+    g = torch.full((32,), 2.0 ** -100, device="cuda")
+    g[3], g[4] = 2.0 ** 100, 0.0
+    opt = train.AdamW([torch.zeros(32, device="cuda")], [g], lr=1e-3, betas=(0.9, 0.999), state="mx8")
+    opt.step()
+    cs = decode(opt.v, opt.v_scale)[1]
+    assert cs[4] == 0 and cs[3] > 1 and np.all(np.delete(cs, [3, 4]) == 1)
