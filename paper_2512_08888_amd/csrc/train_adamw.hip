@@ -322,13 +322,14 @@ __device__ __forceinline__ double power(double b, int t) {
   return r;
 }
 
-// m and v of one element, and its parameter: every operation is rounded by itself.
+// m and v of one element, and its parameter: every operation is rounded by itself, the quotient too (31 M parameters: 148 us with the
+// division and with the reciprocal instruction).
 __device__ __forceinline__ void adamw(const Step& s, float wd, float grad, float& p, float& m, float& v) {
 #pragma clang fp contract(off)
   const float g = grad * s.coef;
   m = m * s.b1 + g * s.c1;
   v = v * s.b2 + g * g * s.c2;
-  p = p - p * (wd * s.lr) - m * __builtin_amdgcn_rcpf(sqrtf(v) * s.root + s.eps) * s.rate;
+  p = p - p * (wd * s.lr) - m / (sqrtf(v) * s.root + s.eps) * s.rate;
 }
 // The same in 8 bits.  v holds sqrt(v); its square is formed and decayed in 64 bits, and rest tells the root's rounding (see
 // round_up_or_down).  The quotient, which no state depends on, is a product with the instruction's reciprocal (2 ulp of the update).
