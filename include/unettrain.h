@@ -91,11 +91,16 @@ size_t train_list_workspace_bytes(const train_list* list);
 typedef struct {
   int32_t step;            /* steps taken */
   float lr;                /* learning rate of the next step */
-  float coef;              /* factor of every gradient in the next step; train_grad_norm() sets it */
+  float coef;              /* factor of every gradient in the next step: train_grad_norm()'s serves that step alone and can be
+                            * read until the next (in further steps it counts as 1, and a skipped step sets it to 1); one that
+                            * the caller writes serves until another is written */
   float norm;              /* norm of all gradients, of the last train_grad_norm() */
-  int32_t nonfinite;       /* 1: that norm was not finite; the next step then changes nothing but `skipped` */
+  int32_t nonfinite;       /* 1: that norm was not finite; the next step then changes nothing here but `skipped`, coef and this */
   int32_t skipped;         /* steps skipped so */
-  int32_t reserved[10];    /* 0 */
+  int32_t reserved[2];     /* 0 */
+  int32_t clip;            /* 1: coef is train_grad_norm()'s and waits for its step; 2: spent is one that a step has used */
+  float spent;             /* coef is that one as long as the two have the same bits */
+  int32_t reserved2[6];    /* 0 */
 } train_control;
 
 /* step as given, lr as given, coef 1, everything else 0 */
@@ -109,7 +114,7 @@ int train_grad_norm(const train_list* list, float max_norm, float* norms, train_
 /* One AdamW step of every tensor.  With t = control->step + 1 and g = control->coef * grad:
  *     m = beta1 * m + (1 - beta1) * g          v = beta2 * v + (1 - beta2) * g^2
  *     param -= lr * weight_decay * param + lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * then control->step = t.  With control->nonfinite set it changes nothing but control->skipped and clears the flag.
+ * then control->step = t.  With control->nonfinite set it changes nothing but the control block: one more skipped, the flag cleared.
  * States, train_list_elements() elements each and zero before the first step:
  *   TRAIN_STATE_F32: m, v fp32; the scales are NULL.
  *   TRAIN_STATE_MX8: m and s = sqrt(v) (in v's place) in OCP e4m3, with one power-of-two scale (e8m0: 2^(byte - 127)) for

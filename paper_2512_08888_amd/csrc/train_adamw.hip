@@ -6,7 +6,7 @@
 // that the list holds) finishes the call: it adds the chunks' sums in a fixed order, or advances the step number.
 // Both are HBM bound: a few operations an element.  31 M parameters (the 59 tensors of a UNet of widths 64 to 1024, fp32 gradients): the
 // norm reads 124 MB in 27 us (22.7 of them the reading, 1.4 the tickets, 3.4 the end), the step reads and writes 0.93 GB with
-// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 84 us (5.9).
+// fp32 states in 148 us (6.3 TB/s) and 0.50 GB with 8-bit states in 85 us (5.9).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -228,6 +228,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const NormChunk* __restr
     const double norm = sqrt(total), r = max_norm / norm;
     ctl->norm = (float)norm;
     ctl->coef = r >= 1 ? 1.f : (float)r;
+    ctl->clip = 1;
     ctl->nonfinite = !(norm < (double)INFINITY);
   }
 }
@@ -307,6 +308,11 @@ __device__ __forceinline__ void round_up_or_down(float* q, const uint32_t* rando
   }
 }
 
+// The factor of a step's gradients: a clip factor that a step has used, and that nobody has written over, counts no more.
+__device__ __forceinline__ float factor(const train_control& c) {
+  return c.clip == 2 && __float_as_uint(c.coef) == __float_as_uint(c.spent) ? 1.f : c.coef;
+}
+
 struct Step {                          // what a step's elements share
   float b1, c1, b2, c2;                // beta, 1 - beta
   float eps, coef, root;               // root: 1 / sqrt(1 - beta2^t)
@@ -333,7 +339,7 @@ __device__ __forceinline__ void adamw(const Step& s, float wd, float grad, float
 }
 // The same in 8 bits.  v holds sqrt(v); its square is formed and decayed in 64 bits, and rest tells the root's rounding (see
 // round_up_or_down).  The quotient, which no state depends on, is a product with the instruction's reciprocal (2 ulp of the update).
-// Bound by instructions as much as by memory (31 M parameters: 84.4 us, 85.4 with sqrtf()).  So the square is narrowed for a first
+// Bound by instructions as much as by memory (31 M parameters: 85 us, 86 with sqrtf()).  So the square is narrowed for a first
 // root that one step of Newton's makes good to its last bit, with v and the gradient 2^32 times as large for room below.
 // FAR: for any square, by a root in 64 bits; else for blocks whose largest sqrt(v) is from 2^-48 to 2^30, and an eps from 2^-64:
 // what is too small for fp32 there has the smallest code, and does not show beside eps.
@@ -421,7 +427,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
     const float scaled = threadIdx.x % 2 ? 1.f / sqrtf(left) : lr / left;
     const float root = __shfl(scaled, 1);
     if (threadIdx.x == 0)
-      shared = Step{(float)opt.beta1, (float)(1 - opt.beta1), (float)opt.beta2, (float)(1 - opt.beta2), opt.eps, ctl->coef, root, scaled, lr,
+      shared = Step{(float)opt.beta1, (float)(1 - opt.beta1), (float)opt.beta2, (float)(1 - opt.beta2), opt.eps, factor(*ctl), root, scaled, lr,
                     opt.seed + (uint32_t)t * 0x9E3779B9u, t, ctl->nonfinite};
   }
   __syncthreads();
@@ -431,8 +437,13 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
     if (threadIdx.x != 0) return;
     const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
     if (!draw_last(tickets + 32 * (1 + mine), of) || !draw_last(tickets, min(gridDim.x, (uint32_t)kFan))) return;
-    if (s.skip) ctl->skipped += 1, ctl->nonfinite = 0;
-    else ctl->step = s.t;
+    if (s.skip) {
+      ctl->skipped += 1, ctl->nonfinite = 0;
+      ctl->coef = 1.f, ctl->clip = 0;                  // of a norm that was not finite
+      return;
+    }
+    ctl->step = s.t;
+    if (ctl->clip == 1) ctl->clip = 2, ctl->spent = ctl->coef;
   };
   if (s.skip || !inside) {             // (the first lane is inside)
     end();

@@ -76,7 +76,8 @@ class AdamW(_Control):
         rc.train_control_init(self.control, 0, lr)
 
     def clip(self, max_norm):
-        """Measures the gradients; the next step multiplies them with `coef`, or is skipped where `nonfinite` is set."""
+        """Measures the gradients; the next step, and no other, multiplies them with `coef`, or is skipped where
+        `nonfinite` is set.  (A factor written into `coef` by hand serves every step until another is written.)"""
         rc.train_grad_norm(self.list, max_norm, self.norms, self.control, self.ws)
 
     def step(self):

@@ -462,3 +462,74 @@ def test_elements_that_vanish_beside_their_block():
     opt.step()
     cs = decode(opt.v, opt.v_scale)[1]
     assert cs[4] == 0 and cs[3] > 1 and np.all(np.delete(cs, [3, 4]) == 1)
+
+
+@pytest.mark.parametrize("state", ["f32", "mx8"])
+def test_a_clip_factor_serves_one_step(state):
+    """Steps without a clip behind a clipped one, or behind a skipped one, take their gradients as they are; a factor that the
+    caller writes stays until another is written.  A second optimizer that never clips takes the same steps."""
+    nets = [Net([100, 2000, 33], seed=5) for _ in range(2)]
+    a, b = (train.AdamW(n.params, n.grads, state=state, seed=2, **HYPER) for n in nets)
+    same = lambda: torch.equal(nets[0].p_buf, nets[1].p_buf) and all(  # noqa: E731
+        torch.equal(p.view(torch.uint8), q.view(torch.uint8)) for p, q in zip(a.state().values(), b.state().values()))
+    a.clip(0.01)
+    coef = a.coef.item()
+    assert coef < 0.1
+    b.coef.fill_(coef)
+    a.step()
+    b.step()
+    assert same() and a.coef.item() == coef          # still there to be read
+    b.coef.fill_(1.0)
+    for _ in range(2):
+        a.step()
+        b.step()
+        assert same()
+    for bad in (math.nan, math.inf):
+        good = nets[0].grads[1][7].clone()
+        nets[0].grads[1][7] = bad
+        a.clip(0.01)
+        a.step()
+        nets[0].grads[1][7] = good
+        assert a.skipped.item() == (1 if math.isnan(bad) else 2) and same()
+        a.step()
+        b.step()
+        assert same() and a.step_count.item() == b.step_count.item()
+    a.clip(math.inf)                                 # measured, not clipped: nothing to take back
+    a.step()
+    b.step()
+    for o in (a, b):
+        o.coef.fill_(0.25)
+    for _ in range(2):
+        a.step()
+        b.step()
+    assert same() and a.coef.item() == 0.25
+
+
+def test_a_clip_factor_serves_one_replay():
+    """The same where the step alone is recorded and the clip comes from outside, now and then."""
+    nets = [Net([100, 2000, 33], seed=5) for _ in range(2)]
+    a, b = (train.AdamW(n.params, n.grads, **HYPER) for n in nets)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a.step()
+    for k in range(6):
+        if k % 3 == 1:
+            a.clip(0.01)
+        b.coef.fill_(a.coef.item() if k % 3 == 1 else 1.0)
+        graph.replay()
+        b.step()
+        torch.cuda.synchronize()
+        assert torch.equal(nets[0].p_buf, nets[1].p_buf) and torch.equal(a.v, b.v), k
+
+
+def test_saved_states_in_32_bits_continue():
+    nets = [Net([500, 33], seed=4) for _ in range(2)]
+    a, b = (train.AdamW(n.params, n.grads, **HYPER) for n in nets)
+    a.step()
+    for p, q in zip(nets[0].params, nets[1].params):
+        q.copy_(p)
+    b.load_state(a.step_count.item(), **{k: t.cpu() for k, t in a.state().items()})
+    a.step()
+    b.step()
+    assert torch.equal(nets[0].p_buf, nets[1].p_buf) and torch.equal(a.m, b.m) and torch.equal(a.v, b.v)

@@ -121,3 +121,27 @@ def test_a_step_without_norms_is_what_it_was():
 def test_the_command_learns(args):
     losses = train.main(["--steps", "41", *args])
     assert losses[-1] < 0.6 * losses[0]
+
+
+@pytest.mark.parametrize("bad", [None, float("nan"), float("inf")])
+def test_a_step_without_clipping_behind_a_clipped_or_skipped_one(bad):
+    """train_step(opt) takes the gradients as they are, whatever the step before did to its own."""
+    nets = [make(CFG)[0] for _ in range(2)]
+    a, b = (n.optimizer(lr=1e-2) for n in nets)
+    if bad is None:
+        nets[0].train_step(a, max_norm=1e-3)
+        b.coef.copy_(a.coef)
+        nets[1].train_step(b)
+        b.coef.fill_(1.0)
+    else:
+        keep = nets[0].images.clone()
+        nets[0].images[0, 0, 3, 3] = bad
+        nets[0].train_step(a, max_norm=1.0)
+        assert a.skipped.item() == 1 and a.step_count.item() == 0
+        nets[0].images.copy_(keep)
+    for _ in range(2):
+        nets[0].train_step(a)
+        nets[1].train_step(b)
+    torch.cuda.synchronize()
+    assert all(torch.equal(nets[0].params[n], nets[1].params[n]) for n in nets[0].params)
+    assert all(bool(torch.isfinite(t).all()) for t in nets[0].params.values())
