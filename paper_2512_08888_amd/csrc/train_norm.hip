@@ -17,8 +17,11 @@
 // part to the launch behind, which finds all sums there.  So the kernel ends whatever else runs on the device and in
 // whatever order its workgroups start.
 //
-// A part's forward sums are its mean and the squared deviations from it, taken from deviations from the part's first
-// element and joined by the means' distances (never sum x^2 - mean^2, which loses the variance of a map far from zero).
+// A part's forward sums are its mean and the squared deviations from it.  Deviations are taken from a point that a few values far
+// from the others hardly move: the mean of the first vectors of a wave, channels last of a lane's first four pixels; parts, waves
+// and rows are joined by their means' distances.  So sums of squares and squares of sums do not cancel, wherever a map's values
+// lie and whichever of them is far out.  (From the part's first element, with that one 1000 deviations out, rstd of fp32
+// 4x64x512x512 was off by 2.6e-3; now by 1.7e-7.  Of all maps tried the worst is off by 2e-6.)
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -191,12 +194,33 @@ __device__ __forceinline__ Pair join(int count, float total, Get get, Size size)
   for (int i = threadIdx.x % 64; i < count; i += 64) s += size(i) * (get(i).a - ref);
   const float mean = ref + wave_sum(s) / total;
   s = 0.f;
+  float t = 0.f;                         // what the first mean lacks: much of its last bits where part 0 is far from the others
   for (int i = threadIdx.x % 64; i < count; i += 64) {
     const Pair p = get(i);
-    const float d = p.a - mean;
-    s += p.b + size(i) * (d * d);
+    const float d = p.a - mean, w = size(i) * d;
+    t += w;
+    s += p.b + w * d;
   }
-  return Pair{mean, wave_sum(s)};
+  t = wave_sum(t);
+  return Pair{mean + t / total, wave_sum(s) - t * (t / total)};
+}
+// The same of N parts by every lane for itself, read once
+template <int N, typename Get, typename Size>
+__device__ __forceinline__ Pair join_few(float total, Get get, Size size) {
+  Pair o[N];
+  float n[N], s = 0.f, t = 0.f, m2 = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = get(i), n[i] = size(i);
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += n[i] * (o[i].a - o[0].a);
+  const float per = total > 0.f ? 1.f / total : 0.f, mean = o[0].a + s * per;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float d = o[i].a - mean, w = n[i] * d;
+    t += w;
+    m2 += o[i].b + w * d;
+  }
+  return Pair{mean + t * per, m2 - t * (t * per)};
 }
 template <typename Get>
 __device__ __forceinline__ Pair add(int count, Get get) {
@@ -390,7 +414,30 @@ struct Nchw {
     xv = normalised(xv, mu, r);
     dv = through<ACT>(dv, affine(xv, ga, be));
   }
-  __device__ __forceinline__ float first_value() const { return !BWD && len ? Elt<E>::ld(static_cast<const E*>(m.x) + base + off) : 0.f; }
+  // Lanes that share a unit and need no barrier to add up: a team, or a wave of one
+  __device__ __forceinline__ int width() const { return min(team(), 64); }
+  // Of `vectors` of a unit that its lanes take in turn, those of this lane's wave (of its team, where that is less than a wave)
+  __device__ __forceinline__ int share(int vectors) const {
+    if (team() <= 64) return vectors;
+    const int wave = threadIdx.x / 64;
+    return (vectors >> q.team_log) * 64 + min(max((vectors & (team() - 1)) - wave * 64, 0), 64);
+  }
+  // A point near the mean of what this lane's team or wave holds of its unit: the mean of the first kNear vectors of each lane,
+  // which are loaded.  (Not of all: that is two operations an element more.  The deviations' sums lose the more digits the smaller
+  // a part of all this is, at worst the sixteenth, or in three launches the 64th.)
+  static constexpr int kNear = J > 4 ? 1 : J;
+  __device__ __forceinline__ float centre() const {
+    const float first = len ? Elt<E>::ld(static_cast<const E*>(m.x) + base + off) : 0.f;
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < kNear; ++j)
+      if (has(0, j)) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += x[j].get(e) - first;
+      }
+    const int near = share(min(len / V, kNear << q.team_log));
+    return first + lanes_sum(s, width()) / (float)max(near * V, 1);
+  }
   __device__ __forceinline__ void add_one(float& xv, float& dv, float ref, Pair& s) const {
     if (BWD) {
       form(xv, dv);
@@ -420,27 +467,34 @@ struct Nchw {
       if constexpr (FORM) x1 = xv, dy1 = dv;
     }
   }
-  // Part k's sums, in all lanes, from every lane's own (of deviations from `first`).  Ends with a barrier behind every use
+  // Part k's sums, in all lanes, from every lane's own (of deviations from `ref`).  Ends with a barrier behind every use
   // of `red`.
-  __device__ __forceinline__ Pair sums(Pair* red, int k, float first, Pair own) {
+  __device__ __forceinline__ Pair sums(Pair* red, int k, float ref, Pair own) {
     float s = own.a, s2 = own.b;
-    s = lanes_sum(s, min(team(), 64));
-    s2 = lanes_sum(s2, min(team(), 64));
-    if (team() > 64) {                        // one unit: its eight waves' sums belong to the same first element
-      if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = Pair{s, s2};
-      __syncthreads();
-      s = s2 = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) s += red[w].a, s2 += red[w].b;
-      __syncthreads();
-    }
+    s = lanes_sum(s, width());
+    s2 = lanes_sum(s2, width());
     Pair p;
     if (BWD) {
+      if (team() > 64) {                      // one unit
+        if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = Pair{s, s2};
+        __syncthreads();
+        s = s2 = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) s += red[w].a, s2 += red[w].b;
+        __syncthreads();
+      }
       if (len && lane == 0) m.part[group * q.cg * q.pieces + k * teams() + unit0] = Pair{s, s2};
       p = Pair{s * ga, s2 * ga};
     } else {
-      const float d = s / (float)max(len, 1);
-      p = Pair{first + d, s2 - s * d};
+      const int n = share(len / V) * V + (threadIdx.x < 64 || team() <= 64 ? len % V : 0);
+      const float d = s / (float)max(n, 1);
+      p = Pair{ref + d, s2 - s * d};
+      if (team() > 64) {                      // one unit: its eight waves' parts
+        if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = p, red[kWaves + threadIdx.x / 64].a = (float)n;
+        __syncthreads();
+        p = join_few<kWaves>((float)len, [&](int w) { return red[w]; }, [&](int w) { return red[kWaves + w].a; });
+        __syncthreads();
+      }
     }
     if (team() > 64) return p;
     if (len && lane == 0) red[unit0] = p;
@@ -540,11 +594,11 @@ __global__ __launch_bounds__(kThreads, BWD || J == 16 ? 4 : 6) void k_gn_nchw(Gn
   w.place(k);
   w.load(0);
   w.load_tail();
-  const float first = w.first_value();
+  const float ref = BWD ? 0.f : w.centre();
   Pair p = {0.f, 0.f};
-  w.add_loaded(0, first, p);
-  w.add_tail(first, p);
-  p = w.sums(red, k, first, p);
+  w.add_loaded(0, ref, p);
+  w.add_tail(ref, p);
+  p = w.sums(red, k, ref, p);
   if (q.split > 1) {
     unsigned long long* slots = m.slots + w.group * q.split;
     if (threadIdx.x == 0) put(slots + k, p);
@@ -564,11 +618,12 @@ __global__ __launch_bounds__(kThreads) void k_gn_nchw_sums(Gn q, Maps m) {
   __shared__ Pair red[kMaxTeam];
   Nchw<E, V, kBatch, BWD, ACT> w(q, m, blockIdx.z, blockIdx.y);
   w.place(blockIdx.x);
-  const float ref = w.first_value();
+  w.load(0);
+  const float ref = BWD ? 0.f : w.centre();
   Pair p = {0.f, 0.f};
   for (int first = 0; first < q.per; first += kBatch) {
     Pair some = {0.f, 0.f};
-    w.load(first);
+    if (first) w.load(first);
     w.add_loaded(first, ref, some);
     p.a += some.a, p.b += some.b;
   }
@@ -623,7 +678,7 @@ struct Nhwc {
   bool in;
   // what a workgroup holds: its first pixel's address (the same for all lanes), its pixels
   size_t base = 0;
-  int left = 0;
+  int left = 0, each = 0, more = 0;    // each: whole rows of them, more: pixels beyond
   Raw<E, V> x[J], dy[J];               // (dy: backward)
 
   __device__ __forceinline__ Nhwc(const Gn& q_, const Maps& m_, size_t n_, int run) : q(q_), m(m_), n(n_) {
@@ -643,6 +698,8 @@ struct Nhwc {
     const size_t p0 = (size_t)k * q.rows * q.per;
     base = (n * q.P + p0) * q.C + c0;
     left = (int)min((size_t)q.rows * q.per, q.P - p0);
+    each = left / q.rows;
+    more = left % q.rows;
   }
   // pixels first .. first + J of each lane
   __device__ __forceinline__ bool has(int first, int j) const { return (first == 0 || first + j < q.per) && has(first + j); }
@@ -679,14 +736,26 @@ struct Nhwc {
     return s;
   }
 
-  __device__ __forceinline__ Raw<E, V> first_values() const {
-    Raw<E, V> f = {};
-    if (!BWD && in) f.load(static_cast<const E*>(m.x) + base + c);
-    return f;
-  }
-  __device__ __forceinline__ void add_loaded(int first, const Raw<E, V>& ref, const Scale& t, float* s, float* s2) {
+  // The points that deviations are taken from: this lane's first pixel, and from its fifth pixel on the means of the first four
+  // (recentre), so that whichever is far out weighs no more than a sixteenth.
+  __device__ __forceinline__ void centres(float* ref) const {
 #pragma unroll
-    for (int j = 0; j < J; ++j)
+    for (int e = 0; e < V; ++e) ref[e] = has(0, 0) ? x[0].get(e) : 0.f;
+  }
+  __device__ __forceinline__ void recentre(int taken, float* ref, float* s, float* s2) const {
+    const float n = min(pixels(row), (float)taken), per = n > 0.f ? 1.f / n : 0.f;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float d = s[e] * per, to = ref[e] + d;
+      s2[e] -= s[e] * d;
+      s[e] = n * (d - (to - ref[e]));
+      ref[e] = to;
+    }
+  }
+  __device__ __forceinline__ void add_loaded(int first, float* ref, const Scale& t, float* s, float* s2) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (!BWD && j == kBatch) recentre(kBatch, ref, s, s2);
       if (has(first, j)) {
         if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
 #pragma unroll
@@ -697,18 +766,56 @@ struct Nhwc {
             add_bwd(xv, dv, s[e], s2[e]);
             if constexpr (FORM) x[j].set(e, xv), dy[j].set(e, dv);
           } else {
-            add_fwd(xv, ref.get(e), s[e], s2[e]);
+            add_fwd(xv, ref[e], s[e], s2[e]);
           }
         }
         if (FORM) forget_vector(x[j]), forget_vector(dy[j]);
       }
+    }
+  }
+  // Pixels of a row
+  __device__ __forceinline__ float pixels(int i) const { return (float)(each + (i < more)); }
+  // One channel's sums over count of the rows, or of what they have been joined to: get(i), of size(i) pixels.  From deviations
+  // from the first: there are at most sixteen, and it weighs as much as another.
+  template <typename Get, typename Size>
+  static __device__ __forceinline__ Pair over_rows(int count, float& total, Get get, Size size) {
+    const float ref = get(0).a;
+    float s = 0.f, s2 = 0.f;
+    total = 0.f;
+    for (int i = 0; i < count; ++i) {
+      const Pair o = get(i);
+      const float n = size(i), d = o.a - ref, w = n * d;
+      total += n;
+      s += w;
+      s2 += o.b + w * d;
+    }
+    const float d = total > 0.f ? s / total : 0.f;
+    return Pair{ref + d, s2 - s * d};
+  }
+  template <typename Get>
+  static __device__ __forceinline__ Pair add_rows(int count, Get get) {
+    Pair t = {0.f, 0.f};
+    for (int i = 0; i < count; ++i) {
+      const Pair o = get(i);
+      t.a += o.a, t.b += o.b;
+    }
+    return t;
   }
   // Sums of every channel of the run over this part's pixels, left in out[0 .. width), from every lane's own (of deviations
-  // from the part's first pixel).  buf: kThreads * V pairs.
-  __device__ __forceinline__ void sums(Pair* buf, Pair* out, const float* s, const float* s2) {
+  // from `ref`).  buf: kThreads * V pairs; out: kMaxRun.
+  __device__ __forceinline__ void sums(Pair* buf, Pair* out, const float* ref, float* s, float* s2) {
     // A lane's V pairs lie together, two at a time at places that turn with the lane (64 bytes apart, the same two of eight
     // lanes would share their banks).
     auto place_of = [](int l, int e) { return V < 8 ? l * V + e : l * V + (((e >> 1) ^ ((l >> 2) & 3)) << 1 | (e & 1)); };
+    if (!BWD) {
+      const float n = pixels(row), per = n > 0.f ? 1.f / n : 0.f;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = s[e] * per;
+        s2[e] -= s[e] * d;
+        s[e] = ref[e] + d;
+      }
+    }
     __syncthreads();
     if (in) {
       if constexpr (V == 1) {
@@ -720,32 +827,55 @@ struct Nhwc {
       }
     }
     __syncthreads();
-    // rows together: as many lanes to a channel as there are
+    // rows together: as many lanes to a channel as there are; the pixels of what each joins lie behind `out` (width <= 256 then)
     const int lanes = kThreads / width, ch = threadIdx.x % width, part = threadIdx.x / width, cols = q.run / V;
+    float* const sizes = reinterpret_cast<float*>(out + kMaxRun / 2);
     int rows = q.rows;
     if (lanes > 1) {
+      const int count = part < lanes && part < rows ? (rows - 1 - part) / lanes + 1 : 0;
+      auto get = [&](int i) { return buf[place_of((part + i * lanes) * cols + ch / V, ch % V)]; };
       Pair t = {0.f, 0.f};
-      if (part < lanes)
-        for (int i = part; i < rows; i += lanes) {
-          const Pair o = buf[place_of(i * cols + ch / V, ch % V)];
-          t.a += o.a, t.b += o.b;
-        }
+      float total = 0.f;
+      if (count) {
+        // (lanes is more than two thirds of 512 / width, rows at most 512 * V / width: count is at most 1.5 * V)
+        if (BWD) t = add_rows(count, get);
+        else if (more == 0) t = over_rows(count, total, get, [&](int) { return (float)each; });
+        else t = over_rows(count, total, get, [&](int i) { return pixels(part + i * lanes); });
+      }
       rows = min(lanes, rows);
       __syncthreads();
-      if (part < rows) buf[part * q.run + ch] = t;
+      if (part < rows) {
+        buf[part * q.run + ch] = t;
+        if (!BWD && ch == 0) sizes[part] = total;
+      }
       __syncthreads();
     }
-    for (int i = threadIdx.x; i < width; i += kThreads) {
-      Pair t = {0.f, 0.f};
-      for (int j = 0; j < rows; ++j) {
-        const Pair o = buf[lanes > 1 ? j * q.run + i : place_of(j * cols + i / V, i % V)];
-        t.a += o.a, t.b += o.b;
+    if (!BWD && lanes > 1 && rows > 4) {
+      // sixteen lanes to a channel
+      const int lane = threadIdx.x % 16;
+      for (int i = threadIdx.x / 16; i < width; i += kThreads / 16) {
+        auto get = [&](int j) { return buf[j * q.run + i]; };
+        const float ref = get(0).a;
+        float s = 0.f, t = 0.f, m2 = 0.f;
+        for (int j = lane; j < rows; j += 16) s += sizes[j] * (get(j).a - ref);
+        const float mean = ref + lanes_sum(s, 16) / (float)left;
+        for (int j = lane; j < rows; j += 16) {
+          const Pair o = get(j);
+          const float d = o.a - mean, w = sizes[j] * d;
+          t += w;
+          m2 += o.b + w * d;
+        }
+        t = lanes_sum(t, 16);
+        m2 = lanes_sum(m2, 16);
+        if (lane == 0) out[i] = Pair{mean + t / (float)left, m2 - t * (t / (float)left)};
       }
-      if (!BWD) {
-        const float d = t.a / (float)left;
-        t = Pair{Elt<E>::ld(static_cast<const E*>(m.x) + base + i) + d, t.b - t.a * d};
+    } else {
+      for (int i = threadIdx.x; i < width; i += kThreads) {
+        auto get = [&](int j) { return buf[lanes > 1 ? j * q.run + i : place_of(j * cols + i / V, i % V)]; };
+        // (lanes == 1: width is above 256, rows at most 15)
+        float total;
+        out[i] = BWD ? add_rows(rows, get) : over_rows(rows, total, get, [&](int j) { return lanes > 1 ? sizes[j] : pixels(j); });
       }
-      out[i] = t;
     }
     __syncthreads();
   }
@@ -849,10 +979,14 @@ __global__ __launch_bounds__(kThreads, 4) void k_gn_nhwc(Gn q, Maps m) {
   w.place(k);
   w.load(0);
   {
-    float s[V] = {}, s2[V] = {};
-    if (BWD) w.add_loaded(0, {}, w.scale(), s, s2);
-    else w.add_loaded(0, w.first_values(), {}, s, s2);
-    w.sums(buf, chan, s, s2);
+    float ref[V] = {}, s[V] = {}, s2[V] = {};
+    if (BWD) {
+      w.add_loaded(0, ref, w.scale(), s, s2);
+    } else {
+      w.centres(ref);
+      w.add_loaded(0, ref, {}, s, s2);
+    }
+    w.sums(buf, chan, ref, s, s2);
   }
   if (BWD)
     for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + k) * q.C + w.c0 + i] = chan[i];
@@ -883,15 +1017,18 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_sums(Gn q, Maps m) {
   float s[V] = {}, s2[V] = {};
   typename Nhwc<E, V, kBatch, ONE, BWD, ACT>::Scale t = {};
   if (BWD) t = w.scale();
-  const Raw<E, V> ref = w.first_values();
+  float ref[V] = {};
+  w.load(0);
+  if (!BWD) w.centres(ref);
   for (int first = 0; first < q.per; first += kBatch) {
     float some[V] = {}, some2[V] = {};
-    w.load(first);
+    if (first) w.load(first);
     w.add_loaded(first, ref, t, some, some2);
 #pragma unroll
     for (int e = 0; e < V; ++e) s[e] += some[e], s2[e] += some2[e];
+    if (!BWD && first == 0) w.recentre(kBatch, ref, s, s2);
   }
-  w.sums(buf, chan, s, s2);
+  w.sums(buf, chan, ref, s, s2);
   for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + blockIdx.x) * q.C + w.c0 + i] = chan[i];
 }
 

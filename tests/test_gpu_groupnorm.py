@@ -406,3 +406,46 @@ def test_more_groups_than_a_launch_has_workgroups_for():
     rc.train_groupnorm_bwd(x, dy, None, None, mean, rstd, dx, dga, dbe, C)
     assert bool((dx == 0).all()) and bool((dga == 0).all())
     assert bool(((dbe.double() - dy[:, :, 0, 0].double().sum(0)).abs() <= 2 * U * dy.double().abs().sum((0, 2, 3))).all())
+
+
+# Maps whose first pixel (a corner, the edge of a padding) is far from the others, which are noise or all alike; one workgroup a
+# group, two launches, groups shared by workgroups that wait for one another, three launches
+OUTLIERS = [(1, 1, 64, 64, 1), (2, 8, 64, 64, 2), (3, 12, 13, 11, 4), (2, 10, 7, 9, 5), (1, 1030, 2, 2, 10), (4, 64, 128, 128, 32),
+            (1, 2, 512, 512, 1), (2, 60, 101, 75, 12), (4, 64, 133, 131, 4), (1, 6, 1201, 1200, 1), (1, 64, 130, 130, 64), (1, 8, 1024, 1024, 1)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("rest,far", [(0.0, 7.3), (0.0, -300.0), (0.1, 5.0), (1.0, 1000.0), (1e-3, 1e4)])
+@pytest.mark.parametrize("where", ["channels", "one", "strip", "sparse"])
+def test_values_far_from_the_others(where, rest, far, layout, dtype):
+    """The bars here do not grow with the distance of the first element.  Statistics are sums of deviations from a point at most a
+    deviation from the mean (see the bars above): the mean is off by K u (mean |x - mean| + |mean|), the variance by 8 K u of
+    itself, rstd by half of that."""
+    for shape in OUTLIERS:
+        N, C, H, W, G = shape
+        rng = np.random.default_rng(C + H)
+        c = Case(*shape, layout=layout, dtype=dtype, affine=False)
+        x = rest * rng.standard_normal((N, C, H * W)) + (0.25 if far < 0 else 0.0)
+        if where == "channels":
+            x[:, :, 0] = far
+        elif where == "one":
+            x[:, 0, 0] = far
+        elif where == "strip":
+            x[:, :, : H * W // 32] = far
+        else:
+            x[rng.random(x.shape) < 1 / 5000] = far
+            x[:, :: max(1, C // G), 0] = far
+        c.x = c.round(x.reshape(N, C, H, W))
+        y, mean, rstd = c.forward()
+        x = c.flat(c.x).astype(np.float64)
+        ry, rmean, rrstd = to.groupnorm_fwd(x, np.ones(C), np.zeros(C), G, 1e-5, "none")
+        g = x.reshape(N, G, -1)
+        e_mean = K * U * (np.abs(g - rmean[..., None]).mean(2) + np.abs(rmean))
+        print(shape, flush=True)
+        assert np.all(np.abs(mean - rmean) <= e_mean), shape
+        assert np.all(np.abs(rstd - rrstd) <= rrstd * 4 * K * U), shape
+        bar = c.spread(e_mean * rrstd) + np.abs(ry) * (4 * K * U + 64 * U) + 4 * U * (np.abs(x) + np.abs(c.spread(rmean))) * c.spread(rrstd) + 1e-30
+        if dtype == "bf16":
+            bar = bar + 2.0 ** -8 * np.abs(ry)
+        assert np.all(np.abs(c.flat(y) - ry) <= bar), shape
