@@ -28,7 +28,8 @@ extern "C" {
  * backward pass sees every element on the side of a ReLU's kink on which the forward pass left it.
  * gamma / beta: fp32 [C], or NULL for ones / zeros.  mean, rstd: fp32 [N, groups].
  * A NaN or an infinity makes its group's results NaN and touches no other group; an activation
- * passes a NaN on.
+ * passes a NaN on, backward too: dgamma and dbeta of the group's channels are NaN (dbeta without an activation is the sum of
+ * dy whatever x holds).
  * Refused (ROTCONV_ERR_SHAPE): N or groups of 65536 or more, C above 2^20, P of 2^31 or more, N * C of 2^31 or more. */
 typedef enum { TRAIN_ACT_NONE = 0, TRAIN_ACT_RELU = 1, TRAIN_ACT_SILU = 2 } train_act;
 /* order of x, y, dy and dx in memory: [N][C][P] or, channels last, [N][P][C] */

@@ -47,7 +47,7 @@ def groupnorm_bwd(x, dy, gamma, beta, mean, rstd, groups, act):
     if act == "relu":
         z32 = (x.astype(F32) - mu.astype(F32)) * r.astype(F32) * ga.astype(F32) + be.astype(F32)
         assert z32.dtype == F32
-        dz = np.where(z32 > 0, dz, 0.0)
+        dz = np.where(z32 > 0, dz, np.where(z32 <= 0, 0.0, np.nan))
     elif act == "silu":
         s = _sigmoid(z)
         dz = dz * s * (1 + z * (1 - s))

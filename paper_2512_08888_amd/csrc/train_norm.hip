@@ -160,6 +160,13 @@ __device__ __forceinline__ void add_bwd(float xh, float dz, float& s, float& s2)
   s2 = fmaf(dz, xh, s2);
 }
 
+// The sum of dz over a part of a channel.  A ReLU's comparison leaves out an element whose z is NaN as if it were dead; where x, the
+// statistics, gamma or beta make it so, the sum is NaN: xh is then too, and the sum of dz * xh with it, or gamma or beta themselves.
+template <int ACT>
+__device__ __forceinline__ float with_nan(float s, float s2, float gamma, float beta) {
+  return ACT == TRAIN_ACT_RELU && (s2 != s2 || gamma != gamma || beta != beta) ? NAN : s;
+}
+
 // ---- sums -----------------------------------------------------------------------------------------
 struct Pair {            // forward: mean, squared deviations from it; backward: sum of dz (or t), sum of dz * xh (or t * xh)
   float a, b;
@@ -483,6 +490,7 @@ struct Nchw {
         for (int w = 0; w < kWaves; ++w) s += red[w].a, s2 += red[w].b;
         __syncthreads();
       }
+      s = with_nan<ACT>(s, s2, ga, be);
       if (len && lane == 0) m.part[group * q.cg * q.pieces + k * teams() + unit0] = Pair{s, s2};
       p = Pair{s * ga, s2 * ga};
     } else {
@@ -874,7 +882,9 @@ struct Nhwc {
         auto get = [&](int j) { return buf[lanes > 1 ? j * q.run + i : place_of(j * cols + i / V, i % V)]; };
         // (lanes == 1: width is above 256, rows at most 15)
         float total;
-        out[i] = BWD ? add_rows(rows, get) : over_rows(rows, total, get, [&](int j) { return lanes > 1 ? sizes[j] : pixels(j); });
+        Pair t = BWD ? add_rows(rows, get) : over_rows(rows, total, get, [&](int j) { return lanes > 1 ? sizes[j] : pixels(j); });
+        if (BWD && ACT == TRAIN_ACT_RELU) t.a = with_nan<ACT>(t.a, t.b, m.gamma ? m.gamma[c0 + i] : 1.f, m.beta ? m.beta[c0 + i] : 0.f);
+        out[i] = t;
       }
     }
     __syncthreads();

@@ -449,3 +449,38 @@ def test_values_far_from_the_others(where, rest, far, layout, dtype):
         if dtype == "bf16":
             bar = bar + 2.0 ** -8 * np.abs(ry)
         assert np.all(np.abs(c.flat(y) - ry) <= bar), shape
+
+
+@pytest.mark.parametrize("layout", ["nchw", "nhwc"])
+@pytest.mark.parametrize("act", ["none", "relu", "silu"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sums_over_the_images_pass_a_nan_on(dtype, act, layout):
+    """A group whose results are NaN makes its channels' gradients NaN, the shift's too (where there is an activation: without
+    one it is the sum of dy alone), and no others: a ReLU does not take its elements for dead ones.  One workgroup a group, groups shared by several, three launches."""
+    for shape in ((2, 12, 9, 7, 4), (2, 4, 96, 90, 2), (2, 64, 133, 131, 4), (1, 6, 1201, 1200, 2), (2, 521, 5, 7, 521)):
+        N, C, H, W, G = shape
+        cg = C // G
+        for bad in (float("nan"), float("inf")):
+            c, ref = Case(*shape, act=act, layout=layout, dtype=dtype), Case(*shape, act=act, layout=layout, dtype=dtype)
+            c.x[N - 1, cg, H // 2, W // 2] = bad
+            _, mean, rstd = c.forward()
+            _, rmean, rrstd = ref.forward()
+            _, dga, dbe = c.backward(mean, rstd)
+            _, rdga, rdbe = ref.backward(rmean, rrstd)
+            inside = np.arange(C) // cg == 1
+            assert np.isnan(dga[inside]).all(), shape
+            assert np.array_equal(dbe[inside], rdbe[inside]) if act == "none" else np.isnan(dbe[inside]).all(), shape
+            assert np.array_equal(dga[~inside], rdga[~inside]) and np.array_equal(dbe[~inside], rdbe[~inside]), shape
+
+
+def test_a_shift_or_scale_that_is_nan():
+    """The channel's own gradients are NaN, and its group's maps."""
+    for layout in ("nchw", "nhwc"):
+        for which in ("gamma", "beta"):
+            c = Case(2, 12, 9, 7, 4, act="relu", layout=layout)
+            _, mean, rstd = c.forward()
+            getattr(c, which)[4] = np.nan
+            dx, dga, dbe = c.backward(mean, rstd)
+            group = np.arange(12) // 3 == 1
+            assert np.isnan(dx[:, group]).all() and np.isfinite(dx[:, ~group]).all()
+            assert np.isnan(dbe[4]) and np.isfinite(np.delete(dbe, 4)).all() and np.isfinite(np.delete(dga, 4)).all()
