@@ -79,7 +79,8 @@ typedef struct {
 
 typedef struct train_list train_list;
 
-/* grad_dtype: ROTCONV_F32 or ROTCONV_BF16.  The list belongs to the device that is current here. */
+/* grad_dtype: ROTCONV_F32 or ROTCONV_BF16.  The list belongs to the device that is current here.  Refused (ROTCONV_ERR_SHAPE):
+ * tensors of more than 2^40 elements, and lists whose norm would take 2^24 workgroups or more (16 million tensors). */
 int train_list_create(const train_tensor* tensors, int count, int grad_dtype, train_list** out);
 int train_list_destroy(train_list* list);
 /* Elements that the states of a list span: tensor k's start at the sum of the sizes before it, each size rounded

@@ -27,6 +27,7 @@ constexpr int kThreads = 256;
 constexpr uint32_t kStepChunk = 4 * kThreads;          // elements of a step's chunk: four a lane
 constexpr int kStaged = 2048;          // sums of chunks that the end of the norm holds in LDS
 constexpr int kFan = 64;               // ticket counters of a launch, a cache line each
+constexpr uint32_t kMostWorkgroups = (1u << 24) - 1;   // of a launch: fewer than 2^32 threads
 
 // The chunks of a list: what a workgroup needs to know, in one read
 struct NormChunk {
@@ -389,7 +390,7 @@ template <> struct Grad4<uint16_t> {
 template <typename T, bool MX8>
 __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict__ chunks, train_adamw opt,
                                                     void* mp, void* vp, uint8_t* msp, uint8_t* vsp, train_control* ctl,
-                                                    uint32_t* tickets) {
+                                                    uint32_t* tickets, int ends) {
   __shared__ Step shared;
   const uint32_t i = 4 * threadIdx.x;
   const StepChunk r = chunks[blockIdx.x];
@@ -434,7 +435,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
   const Step s = shared;
   // The first lane alone reads the control block, and has done so: who draws the last ticket knows that nobody will again.
   auto end = [&] {
-    if (threadIdx.x != 0) return;
+    if (!ends || threadIdx.x != 0) return;             // (more launches of this step follow)
     const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
     if (!draw_last(tickets + 32 * (1 + mine), of) || !draw_last(tickets, min(gridDim.x, (uint32_t)kFan))) return;
     if (s.skip) {
@@ -558,7 +559,8 @@ int train_list_create(const train_tensor* tensors, int count, int grad_dtype, tr
   while ((size < 16384 && total / size > (uint64_t)kStaged) || total / size > 8ull * kStaged) size *= 2;
   uint64_t nnorm = 0, nstep = 0;
   for (int k = 0; k < count; ++k) nnorm += (tensors[k].n + size - 1) / size, nstep += (tensors[k].n + kStepChunk - 1) / kStepChunk;
-  if (nnorm > 0x7fffffffu || nstep > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
+  // The norm is one launch, at least a workgroup a tensor; a step may be several.
+  if (nnorm > kMostWorkgroups || nstep > 0x7fffffffu) return ROTCONV_ERR_SHAPE;
   train_list* l = nullptr;
   try {
     std::vector<Row> rows(count);
@@ -659,7 +661,12 @@ int train_adamw_step(const train_list* l, const train_adamw* o, void* m, void* v
   // enough bytes under way (89 us with eight, 112 us with five, when the whole took that long).
   const size_t lds = mx8 ? 0 : 32000;
   auto kernel = mx8 ? (l->bf16 ? k_adamw<uint16_t, true> : k_adamw<float, true>) : (l->bf16 ? k_adamw<uint16_t, false> : k_adamw<float, false>);
-  kernel<<<l->nstep, kThreads, lds, static_cast<hipStream_t>(stream)>>>(l->step, *o, m, v, m_scale, v_scale, control, l->tickets);
+  for (uint32_t done = 0; done < l->nstep;) {
+    const uint32_t now = std::min(l->nstep - done, kMostWorkgroups);
+    kernel<<<now, kThreads, lds, static_cast<hipStream_t>(stream)>>>(l->step + done, *o, m, v, m_scale, v_scale, control, l->tickets,
+                                                                     done + now == l->nstep);
+    done += now;
+  }
   return finish();
 }
 

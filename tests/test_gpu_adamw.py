@@ -533,3 +533,31 @@ def test_saved_states_in_32_bits_continue():
     a.step()
     b.step()
     assert torch.equal(nets[0].p_buf, nets[1].p_buf) and torch.equal(a.m, b.m) and torch.equal(a.v, b.v)
+
+
+def test_more_elements_than_a_launch_has_threads_for():
+    """2^34 elements and two small tensors, states in 8 bits (140 GB): a step of more than 2^24 workgroups.  Both ends, the middle and
+    the small tensors against the formula; the step counts once, a skipped one too."""
+    n = (1 << 34) + 77
+    p = torch.zeros(n, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    small = [torch.zeros(5, device="cuda") for _ in range(2)]
+    grads = [torch.full((5,), 0.5, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    opt = train.AdamW([small[0], p, small[1]], [grads[0], g, grads[1]], state="mx8", **HYPER)
+    spots = [0, (1 << 33) + 5, (1 << 34) - 2048, n - 5]
+    for at in spots:
+        g[at:at + 5] = 0.5
+    opt.clip(math.inf)
+    assert abs(opt.norm.item() - math.sqrt(0.25 * 5 * 6)) < 1e-6
+    opt.step()
+    lr = opt.lr.item()
+    ref, _, _ = to.adamw(np.zeros(5), np.full(5, 0.5), np.zeros(5), np.zeros(5), 1, lr, 0.9, 0.99, 1e-8, 0.0)
+    for t in (*small, *(p[at:at + 5] for at in spots)):
+        assert np.allclose(t.cpu().numpy(), ref, rtol=1e-6, atol=0)
+    assert opt.step_count.item() == 1 and opt.skipped.item() == 0
+    g[n - 1] = math.inf
+    opt.clip(1.0)
+    opt.step()
+    assert opt.step_count.item() == 1 and opt.skipped.item() == 1 and np.allclose(small[1].cpu().numpy(), ref, rtol=1e-6, atol=0)
+    del p, g, small, grads, opt, t
+    torch.cuda.empty_cache()

@@ -179,3 +179,14 @@ def test_random_bits_are_uniform():
         hist = np.bincount((u * 64).astype(int), minlength=64)
         assert ((hist - n / 64) ** 2 / (n / 64)).sum() < 150
     assert abs(np.corrcoef(a, b)[0, 1]) < 5 / np.sqrt(n)
+
+
+def test_lists_of_more_tensors_than_a_launch_has_workgroups_are_refused():
+    """2^24 tensors of one element: refused before anything is copied to a device."""
+    row = np.zeros(1, dtype=[("param", "u8"), ("grad", "u8"), ("copy", "u8"), ("n", "u8"), ("weight_decay", "f4"), ("reserved", "i4")])
+    assert row.itemsize == ctypes.sizeof(rc.TrainTensor)
+    row["grad"], row["n"] = 64, 1
+    rows = np.broadcast_to(row, 1 << 24).copy()
+    h = ctypes.c_void_p()
+    at = ctypes.cast(rows.ctypes.data, ctypes.POINTER(rc.TrainTensor))
+    assert rc.lib().train_list_create(at, rows.size, 0, ctypes.byref(h)) == rc.ERR_SHAPE and not h
