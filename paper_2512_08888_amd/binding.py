@@ -495,7 +495,18 @@ def glue_softmax_ce(logits, labels, loss, dlogits, ws):
 
 # ---- training operators (include/unettrain.h) ---------------------------------------------------
 
+_INT_MAX = 2**31 - 1
+
+
+def _ints(what, *values):
+    """Refuses what a C int would hold another number for."""
+    for v in values:
+        if not -_INT_MAX <= v <= _INT_MAX:
+            raise RotconvError(ERR_SHAPE, what)
+
+
 def train_groupnorm_workspace_bytes(N, C, P, groups):
+    _ints("train_groupnorm_workspace_bytes", N, C, groups)
     return int(lib().train_groupnorm_workspace_bytes(N, C, P, groups))
 
 
@@ -548,6 +559,7 @@ def _groupnorm(what, x, others, groups, act, ws):
         raise ValueError(f"{what}: the workspace must be on the GPU")
     shape = x.shape
     N, C = shape[0], shape[1]
+    _ints(what, N, C, groups)
     P = x.numel() // (N * C) if N * C else 0
     if act not in ACTS:
         raise ValueError(f"{what}: act must be one of {sorted(ACTS)}")
@@ -654,6 +666,7 @@ CONTROL_BYTES = 64
 def train_control_init(control, step=0, lr=0.0):
     """control: 16 int32 on the device (train_control)."""
     what = "train_control_init"
+    _ints(what, step)
     _check(lib().train_control_init(_room(what, "control", control, CONTROL_BYTES), int(step), float(lr), _stream()), what)
 
 

@@ -484,3 +484,20 @@ def test_a_shift_or_scale_that_is_nan():
             group = np.arange(12) // 3 == 1
             assert np.isnan(dx[:, group]).all() and np.isfinite(dx[:, ~group]).all()
             assert np.isnan(dbe[4]) and np.isfinite(np.delete(dbe, 4)).all() and np.isfinite(np.delete(dga, 4)).all()
+
+
+def test_extents_beyond_32_bits_are_refused():
+    """2^32 + 2 groups are not two, and a map of 2^32 + 4 images is not one of four."""
+    x = torch.randn(2, 4, 3, 3, device="cuda")
+    y, keep = torch.zeros_like(x), torch.zeros_like(x)
+    for groups in ((1 << 32) + 2, -(1 << 32) + 2):
+        with pytest.raises(rc.RotconvError) as e:
+            rc.train_groupnorm_fwd(x, None, None, y, None, None, groups)
+        assert e.value.status == rc.ERR_SHAPE
+    x = torch.ones((1 << 32) + 4, 1, dtype=torch.bfloat16, device="cuda")
+    out = torch.zeros_like(x)
+    with pytest.raises(rc.RotconvError) as e:
+        rc.train_groupnorm_fwd(x, None, None, out, None, None, 1)
+    assert e.value.status == rc.ERR_SHAPE and torch.equal(y, keep) and not bool(out[:4].any())
+    del x, out
+    torch.cuda.empty_cache()

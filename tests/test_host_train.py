@@ -190,3 +190,11 @@ def test_lists_of_more_tensors_than_a_launch_has_workgroups_are_refused():
     h = ctypes.c_void_p()
     at = ctypes.cast(rows.ctypes.data, ctypes.POINTER(rc.TrainTensor))
     assert rc.lib().train_list_create(at, rows.size, 0, ctypes.byref(h)) == rc.ERR_SHAPE and not h
+
+
+def test_numbers_that_no_c_int_holds_are_refused():
+    for call in (lambda: rc.train_groupnorm_workspace_bytes((1 << 32) + 1, 4, 4, 2), lambda: rc.train_groupnorm_workspace_bytes(1, 4, 4, (1 << 32) + 2),
+                 lambda: rc.train_control_init(None, 1 << 32)):
+        with pytest.raises(rc.RotconvError) as e:
+            call()
+        assert e.value.status == rc.ERR_SHAPE
