@@ -89,17 +89,21 @@ class AdamW(_Control):
         return s if self.kind == "f32" else {**s, "m_scale": self.m_scale, "v_scale": self.v_scale}
 
     def load_state(self, step, **state):
-        """Continues from a saved step number and state(), taken from a list of the same sizes in the same order."""
+        """Continues from a saved step number and state(), taken from a list of the same sizes in the same order.  A state
+        that does not fit is refused as a whole."""
         import torch
 
-        mine = self.state()
+        mine, step = self.state(), int(step)
+        if not 0 <= step < 2**31 - 1:
+            raise ValueError(f"load_state: a step number is from 0 to 2^31 - 2, got {step}")
         if set(state) != set(mine):
             raise ValueError(f"load_state: expected {sorted(mine)}, got {sorted(state)}")
         for name, t in state.items():
             if t.dtype != mine[name].dtype or t.numel() != mine[name].numel():
                 raise ValueError(f"load_state: {name} must be {mine[name].dtype} with {mine[name].numel()} elements")
+        for name, t in state.items():
             mine[name].view(torch.uint8).copy_(t.reshape(-1).view(torch.uint8))
-        self.step_count.fill_(int(step))
+        self.step_count.fill_(step)
 
 
 def main(argv=None):

@@ -561,3 +561,19 @@ def test_more_elements_than_a_launch_has_threads_for():
     assert opt.step_count.item() == 1 and opt.skipped.item() == 1 and np.allclose(small[1].cpu().numpy(), ref, rtol=1e-6, atol=0)
     del p, g, small, grads, opt, t
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("state", ["f32", "mx8"])
+def test_a_state_that_is_refused_changes_nothing(state):
+    net = Net([100, 2000])
+    opt = train.AdamW(net.params, net.grads, state=state, **HYPER)
+    opt.step()
+    opt.step()
+    good = {k: t.clone() for k, t in opt.state().items()}
+    other = {k: torch.zeros_like(t.view(torch.uint8)).view(t.dtype) for k, t in good.items()}
+    last = list(other)[-1]
+    for step, s in ((7, {**other, last: other[last][:-1]}), (-1, other), (1 << 31, other), (7, {**other, "more": other[last]})):
+        with pytest.raises(ValueError):
+            opt.load_state(step, **s)
+        assert all(torch.equal(good[k].view(torch.uint8), t.view(torch.uint8)) for k, t in opt.state().items())
+        assert opt.step_count.item() == 2
