@@ -129,6 +129,10 @@ __device__ __forceinline__ float affine(float xh, float gamma, float beta) {
 #pragma clang fp contract(off)
   return xh * gamma + beta;
 }
+// The exponential's argument is rounded once, which makes it off by |z| / 2 of its last bit; where z is so negative that this is much,
+// z * sigmoid(z) and its slope are so small that it stays below 2^-24 of 1.  With the argument in two parts SiLU takes 3 % longer in
+// fp32 (4x64x512x512 forward 105.6 us instead of 102.2) and 9 to 16 % in bf16, whose results lose it anyway.  The reciprocal
+// instruction is off by one of its last bits.
 __device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
