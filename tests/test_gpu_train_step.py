@@ -145,3 +145,30 @@ def test_a_step_without_clipping_behind_a_clipped_or_skipped_one(bad):
     torch.cuda.synchronize()
     assert all(torch.equal(nets[0].params[n], nets[1].params[n]) for n in nets[0].params)
     assert all(bool(torch.isfinite(t).all()) for t in nets[0].params.values())
+
+
+STD = un.UNetConfig("norm_std", 2, 3, 16, 24, (8, 16), 3, R=8, mode="bilinear", block="rot_std", norm_groups=4, seed=33)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_layers_of_a_step_with_standard_convolutions(dtype):
+    """Norms behind rotation convolutions and behind the standard convolutions of the other kind of block."""
+    test_layers_of_a_step(STD, dtype)
+
+
+def test_an_optimizer_that_only_the_graph_needs():
+    """Replays of a step recorded with an optimizer that nobody else holds, with memory allocated and freed in between."""
+    import gc
+
+    nets = [make(CFG)[0] for _ in range(2)]
+    opt = nets[0].optimizer(lr=3e-3)
+    nets[1].capture(nets[1].optimizer(lr=3e-3), max_norm=1.0)
+    gc.collect()
+    for k in range(3):
+        junk = [torch.full((n,), float("nan"), device="cuda") for n in (16, 4096, 100_000, 1 << 22)]
+        a = nets[0].train_step(opt, max_norm=1.0)
+        torch.cuda.synchronize()
+        b = nets[1].replay()
+        torch.cuda.synchronize()
+        del junk
+        assert torch.equal(a, b) and all(torch.equal(nets[0].params[n], nets[1].params[n]) for n in nets[0].params), k
