@@ -105,7 +105,7 @@ typedef struct {
   int32_t reserved2[6];    /* 0 */
 } train_control;
 
-/* step as given, lr as given, coef 1, everything else 0 */
+/* step (0 to 2^31 - 2) as given, lr as given, coef 1, everything else 0 */
 int train_control_init(train_control* control, int step, float lr, void* stream);
 
 /* norms[k] = sqrt(sum of grad_k^2) (fp32 [count], or NULL), control->norm = sqrt(sum of all squares), summed in 64 bits;

@@ -631,7 +631,7 @@ size_t train_list_workspace_bytes(const train_list* l) { return l ? (size_t)l->n
 
 int train_control_init(train_control* control, int step, float lr, void* stream) {
   if (!control) return ROTCONV_ERR_NULL;
-  if (step < 0) return ROTCONV_ERR_SHAPE;
+  if (step < 0 || step == INT32_MAX) return ROTCONV_ERR_SHAPE;         // (the next step's number is an int32_t too)
   if (misaligned(control, 4)) return ROTCONV_ERR_UNSUPPORTED;
   k_control_init<<<1, 1, 0, static_cast<hipStream_t>(stream)>>>(control, step, lr);
   return finish();

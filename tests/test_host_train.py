@@ -198,3 +198,7 @@ def test_numbers_that_no_c_int_holds_are_refused():
         with pytest.raises(rc.RotconvError) as e:
             call()
         assert e.value.status == rc.ERR_SHAPE
+
+
+def test_a_step_number_without_a_successor_is_refused():
+    assert rc.lib().train_control_init(64, 2**31 - 1, 0.1, None) == rc.ERR_SHAPE
