@@ -109,7 +109,8 @@ typedef struct {
 int train_control_init(train_control* control, int step, float lr, void* stream);
 
 /* norms[k] = sqrt(sum of grad_k^2) (fp32 [count], or NULL), control->norm = sqrt(sum of all squares), summed in 64 bits;
- * control->coef = min(1, max_norm / norm), 1 for a norm of 0; control->nonfinite.  max_norm > 0, infinity: no clipping. */
+ * control->coef = min(1, max_norm / norm), 1 for a norm of 0; control->nonfinite (judged in 64 bits: a norm above fp32's range is
+ * finite, and norm then shows an infinity).  max_norm > 0, infinity: no clipping. */
 int train_grad_norm(const train_list* list, float max_norm, float* norms, train_control* control, void* ws,
                     size_t ws_bytes, void* stream);
 

@@ -9,9 +9,9 @@
 //   three, where a group has more parts than wait for one another: sums, their join, the map again (kSums).
 // Backward, the last of these launches forms dgamma and dbeta, from the sums of every part of every channel.
 //
-// Measured, of a copy's 5.7 TB/s: forward bf16 4x128x256x256 in 32 groups 26 us (5.1 TB/s), fp32 4x64x512x512 100 us (5.35);
-// backward bf16 4x64x512x512 84 us (4.8), channels last fp32 4x256x128x128 48 us (4.2); small maps by their launches: fp32
-// 64x16x16 4 us, bf16 3x60x101x75 channels last 11 us.
+// Measured, of a copy's 5.7 TB/s: forward bf16 4x128x256x256 in 32 groups 27 us (5.0 TB/s), fp32 4x64x512x512 101 us (5.3);
+// backward bf16 4x64x512x512 83 us (4.8), fp32 143 us (5.6), channels last fp32 4x256x128x128 48 us (4.2); small maps by their
+// launches: fp32 64x16x16 4 us, bf16 3x60x101x75 channels last 12 us.
 //
 // The wait is bounded and never needed for the result: a workgroup whose neighbours have not answered in time leaves its
 // part to the launch behind, which finds all sums there.  So the kernel ends whatever else runs on the device and in
@@ -47,7 +47,9 @@ constexpr int kOver = 18;                     // (kMaxSplit - 1) * kMaxSplit < 2
 constexpr int kMaxRun = 1024;                // channels of a run (channels last)
 // Of a map, up to which a shared group takes two launches.  (Two, and one that waits between two small ones: fp32 64x128x128
 // in 4 groups, 4 MB, 9.2 and 11.7 us forward, 10.3 and 13.2 backward; bf16 channels last 4x64x128x128 in 8, 8 MB, 13.5 and
-// 15.5, 19.2 and 20.8; fp32 4x64x128x128 in 4, 17 MB, 16.2 and 13.0, 20.4 and 15.6.)
+// 15.5, 19.2 and 20.8; fp32 4x64x128x128 in 4, 17 MB, 16.2 and 13.0, 20.4 and 15.6.  Of thirteen other maps, the six of 2 to 8 MB
+// gain 0.6 to 3.3 us by two, one of 10.5 MB 1.4 forward and 0.5 backward; the six of 12 to 19 MB lose 0.8 to 6.0 but for one direction
+// of two of them, 1.4 and 1.3.)
 constexpr size_t kTwoBytes = 8u << 20;
 constexpr int kMaxSlots = 2048;              // sums that a workgroup collects (channels last: of every group of its run)
 
@@ -594,7 +596,7 @@ __device__ __forceinline__ bool collect(const unsigned long long* slots, int cou
 }
 
 // Sums, exchange and map of a part that stays in registers; in two launches the sums alone.  HBM bound: bf16 4x128x256x256 in
-// 32 groups forward 24 us (5.5 TB/s), 4x64x512x512 backward 83 us (4.9).  512 threads: a group of the deep levels fits one
+// 32 groups forward 25 us (5.4 TB/s), 4x64x512x512 backward 80 us (5.0).  512 threads: a group of the deep levels fits one
 // workgroup, and two of sixteen vectors a lane (backward eight of each map) fill a CU's registers.
 template <typename E, int V, int J, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads, BWD || J == 16 ? 4 : 6) void k_gn_nchw(Gn q, Maps m) {
@@ -1046,7 +1048,7 @@ __global__ __launch_bounds__(kThreads) void k_gn_nhwc_sums(Gn q, Maps m) {
   for (int i = threadIdx.x; i < w.width; i += kThreads) m.part[(w.n * q.split + blockIdx.x) * q.C + w.c0 + i] = chan[i];
 }
 
-// As k_gn_nchw_map, and bound as it is: bf16 4x64x512x512 in 16 groups, in three launches, 96 us forward and 141 backward.
+// As k_gn_nchw_map, and bound as it is: bf16 4x64x512x512 in 16 groups, in three launches, 97 us forward and 140 backward.
 template <typename E, int V, bool ONE, bool BWD, int ACT>
 __global__ __launch_bounds__(kThreads) void k_gn_nhwc_map(Gn q, Maps m) {
   __shared__ Pair all[kMaxSlots];
@@ -1235,7 +1237,9 @@ Gn cut(int N, int C, size_t P, int groups, int layout, int elem, bool bwd) {
   }
   // Where two launches make it, every workgroup of the map joins the sums of its run's groups for itself: half as many
   // workgroups do where the parts would else leave more than 1024 sums (channels last bf16 3x60x101x75 in 12 groups, 672 sums
-  // and 1344: 11.5 and 13.2 us; 4x256x32x32 fp32 in 32 groups, 128 and 256: 10.7 and 10.0).
+  // and 1344: 11.5 and 13.2 us; 4x256x32x32 fp32 in 32 groups, 128 and 256: 10.7 and 10.0; bf16 1x128x128x128 in 64, 2048 and
+  // 4096, which three launches would join: forward 17.4 and 19.1, backward 22.2 and 20.0; of eight maps of 4 to 8 MB with fewer sums
+  // all but one lose 0.3 to 4.5 us with half as many).
   const bool two = (size_t)N * C * P * elem <= kTwoBytes;
   auto sums_of = [&](const Gn& g) { return (size_t)g.split * (layout == TRAIN_NHWC ? g.run / g.cg : 1); };
   if (best.split > 1)
