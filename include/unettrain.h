@@ -122,7 +122,8 @@ int train_grad_norm(const train_list* list, float max_norm, float* norms, train_
  *   TRAIN_STATE_F32: m, v fp32; the scales are NULL.
  *   TRAIN_STATE_MX8: m and s = sqrt(v) (in v's place) in OCP e4m3, with one power-of-two scale (e8m0: 2^(byte - 127)) for
  *     each block of 32 elements in m_scale / v_scale [elements / 32].  A block's scale is the smallest with every value
- *     at most 448 times it.  param is updated from the unrounded m and v.  m is rounded to nearest even.  s is rounded
+ *     at most 448 times it.  param is updated from the unrounded m and v.  m is formed in fp32 and rounded to
+ *     nearest even.  s is rounded
  *     stochastically, so that a change far smaller than the step between two codes still moves it on average: up with the
  *     probability of the part cut off, from 16 bits of a hash of (seed, t, position), and a positive s to no less than
  *     the smallest code, so that no denominator vanishes beside an m.  A NaN or an infinity makes its block NaN. */
