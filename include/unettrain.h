@@ -1,11 +1,12 @@
 /*
  * unettrain.h - C ABI of the training operators around the stack: group normalisation with an
- * activation (forward and backward), the norm of many gradients at once, and the AdamW step over
- * many parameter tensors at once.
+ * activation (forward and backward), log-probabilities of labels (forward and backward) and the
+ * clipped policy loss with its gradient, the norm of many gradients at once, the AdamW step over
+ * many parameter tensors at once, and Muon's step over many matrices at once.
  *
  * Same conventions as rotconv.h and unetglue.h: plain C; every tensor pointer is DEVICE memory owned
  * by the caller; `stream` is a hipStream_t passed as void*; calls only enqueue (train_list_create
- * excepted: it uploads a table and returns when the table is there); results are bitwise
+ * and train_matrices_create excepted: they upload tables and return when these are there); results are bitwise
  * reproducible.  Return value: a rotconv_status (ROTCONV_ERR_NULL, ROTCONV_ERR_SHAPE,
  * ROTCONV_ERR_UNSUPPORTED, ROTCONV_ERR_WORKSPACE, ROTCONV_ERR_LAUNCH).
  */
@@ -63,6 +64,62 @@ int train_groupnorm_bwd_bf16(const uint16_t* x, const uint16_t* dy, const float*
  * on, and leave their part to a second launch where that is too short: same bits, more reads.  Returns the number
  * before.  For the whole process; results do not depend on it. */
 int train_diag_groupnorm_wait(int ticks);
+
+/* ---- log-probabilities of labels, and the clipped policy loss ----------------------------------------
+ * logits z hold N images of K classes of P pixels (TRAIN_NCHW: [N][K][P]; TRAIN_NHWC: [N][P][K]; tokens are images of one
+ * pixel); labels int32 [N, P].  A row is a pixel's K logits.  With t the largest of a row and l = ln sum_j exp(z_j - t):
+ *     logp = z_label - t - l      p_j = exp(z_j - t - l)      entropy = l - sum_j p_j (z_j - t)
+ * Logits of -infinity are classes that cannot be taken: p_j = 0, and p_j ln p_j counts as 0.  A row is left out (its outputs 0,
+ * its logits' gradient 0, nothing in any sum, whatever it holds) where its label lies outside 0..K-1; the notes at the calls
+ * name the further ones.  A NaN or a +infinity makes its own row's results NaN.
+ * Refused (ROTCONV_ERR_SHAPE): N or K below 1, P of 0, K above 2^24, N * P of 2^31 or more. */
+
+/* scratch that train_logp_fwd and train_policy_loss need, whatever the layout and storage type; 0 for extents that are refused */
+size_t train_logp_workspace_bytes(int N, int K, size_t P);
+/* logp, entropy: fp32 [N, P]; stat: fp32 [N, P, 2], t and l, which the backward call reads.  entropy and stat may be NULL.
+ * Left out beside those without a label: rows whose logits are all -infinity (their t is kept as it is, -infinity). */
+int train_logp_fwd(const float* logits, const int32_t* labels, float* logp, float* entropy, float* stat, int N, int K,
+                   size_t P, int layout, void* ws, size_t ws_bytes, void* stream);
+/* dlogits_j = dlogp (1[j = label] - p_j) - dentropy p_j (ln p_j + entropy)
+ * stat, entropy: what the forward call wrote.  dentropy may be NULL (none), and entropy is read only beside it.
+ * dlogits may be the logits themselves (same address), but overlap nothing else.  Left out too: rows whose t is -infinity, and
+ * rows whose dlogp and dentropy are 0. */
+int train_logp_bwd(const float* logits, const int32_t* labels, const float* stat, const float* entropy,
+                   const float* dlogp, const float* dentropy, float* dlogits, int N, int K, size_t P, int layout,
+                   void* stream);
+
+typedef struct {
+  float clip_low, clip_high;   /* 0 <= clip_low <= 1, clip_high >= 0: the ratio counts from 1 - clip_low to 1 + clip_high */
+  float kl;                    /* factor of the distance to the reference, >= 0; 0 without one */
+  float entropy;               /* factor of the entropy (a bonus), >= 0 */
+  int32_t per_image;           /* 1: advantage holds a value for each image; 0: for each row */
+  int32_t reserved;            /* 0 */
+} train_policy;
+
+/* Loss and gradient in one call, for labels that were taken with log-probability logp_old.  Of a row with advantage A and weight w:
+ *     r = exp(logp - logp_old)                       (1, with its gradient, where logp_old is NULL)
+ *     s = min(r A, clip(r, 1 - clip_low, 1 + clip_high) A)                       (0 for A = 0)
+ *     d = exp(q) - q - 1 with q = logp_ref - logp    (0 where logp_ref is NULL)
+ *     out[0] = sum w (-s + kl d - entropy H)      out[1] = sum w d      out[2] = sum w H      out[3] = sum of w where s is cut
+ * (H, the entropy, counts as 0 where its factor is 0, and d where kl is 0.)  s is cut where A > 0 and r > 1 + clip_high, or A < 0 and
+ * r < 1 - clip_low: it has no gradient there.
+ *     dlogits_j = w (G (1[j = label] - p_j) + entropy p_j (ln p_j + H)),      G = (cut ? 0 : -A r) + kl (1 - exp(q))
+ * weight: fp32 [N, P], or NULL for 1 / (N P); the caller's own normalisation and mask.  Left out too: rows of weight 0, and rows
+ * whose logits are all -infinity.  logp: fp32 [N, P] or NULL.  advantage: fp32 [N, P] or [N].  out: fp32 [4], sums in 64 bits.
+ * dlogits may be the logits themselves, but overlap nothing else; NULL where only the loss is wanted. */
+int train_policy_loss(const float* logits, const int32_t* labels, const float* advantage, const float* logp_old,
+                      const float* logp_ref, const float* weight, float* out, float* dlogits, float* logp, int N, int K,
+                      size_t P, int layout, const train_policy* options, void* ws, size_t ws_bytes, void* stream);
+/* bfloat16 twins: logits and dlogits as bfloat16, everything else fp32; arithmetic in fp32, results rounded once. */
+int train_logp_fwd_bf16(const uint16_t* logits, const int32_t* labels, float* logp, float* entropy, float* stat, int N,
+                        int K, size_t P, int layout, void* ws, size_t ws_bytes, void* stream);
+int train_logp_bwd_bf16(const uint16_t* logits, const int32_t* labels, const float* stat, const float* entropy,
+                        const float* dlogp, const float* dentropy, uint16_t* dlogits, int N, int K, size_t P, int layout,
+                        void* stream);
+int train_policy_loss_bf16(const uint16_t* logits, const int32_t* labels, const float* advantage, const float* logp_old,
+                           const float* logp_ref, const float* weight, float* out, uint16_t* dlogits, float* logp, int N,
+                           int K, size_t P, int layout, const train_policy* options, void* ws, size_t ws_bytes,
+                           void* stream);
 
 /* ---- many tensors at once -----------------------------------------------------------------------
  * A list names parameter tensors with their gradients.  It holds their addresses, not their values: the
@@ -137,6 +194,51 @@ typedef struct {
 } train_adamw;
 int train_adamw_step(const train_list* list, const train_adamw* options, void* m, void* v, uint8_t* m_scale,
                      uint8_t* v_scale, train_control* control, void* stream);
+
+/* ---- Muon: orthogonalised updates of many matrices ---------------------------------------------------
+ * Matrices with their gradients, as train_list names tensors.  A stack of `count` matrices of one shape lies in one piece,
+ * each row-major; a filter bank is a matrix of output channels x taps. */
+typedef struct {
+  float* param;            /* fp32 [count][rows][cols] */
+  const void* grad;        /* of the handle's gradient type */
+  uint16_t* copy;          /* NULL, or a bfloat16 copy of param that every step refreshes (rounded to nearest even) */
+  int32_t count, rows, cols;
+  float weight_decay;      /* >= 0 */
+  float scale;             /* factor of the orthogonal matrix beside the learning rate, finite */
+  int32_t reserved;        /* 0 */
+} train_matrix;
+
+typedef struct train_matrices train_matrices;
+
+/* As train_list_create.  Refused (ROTCONV_ERR_SHAPE): extents below 1, the shorter side of a matrix above 32768, the longer above 2^24,
+ * stacks of more than 2^40 elements, more matrices than 65535 or more work than 2^24 - 1 workgroups do. */
+int train_matrices_create(const train_matrix* matrices, int count, int grad_dtype, train_matrices** out);
+int train_matrices_destroy(train_matrices* matrices);
+/* Elements that the momentum spans: stack k's start at the sum of the sizes before it, each size rounded up to a
+ * multiple of 32. */
+uint64_t train_matrices_elements(const train_matrices* matrices);
+size_t train_matrices_workspace_bytes(const train_matrices* matrices);
+
+/* One step of every matrix.  With g = control->coef * grad:
+ *     momentum = mu * momentum + g
+ *     u = g + mu * momentum (nesterov), or momentum      X = u / (|u| + eps), |u| the root of the sum of u's squares
+ *     `steps` times: A = X X^T, X = a X + (b A + c A^2) X with a = 3.4445, b = -4.7750, c = 2.0315 (transposed where rows > cols)
+ *     param -= lr * weight_decay * param + lr * scale * X
+ * five steps bring every singular value of u that is not vanishing beside the others to between 0.7 and 1.2.
+ * momentum: fp32, train_matrices_elements(), zero before the first step.  Products multiply fp16 values (all of them bounded: see
+ * the kernels) and add in fp32; X is held in 22 bits between them, and the diagonals of A and of the polynomial in 32: X's result is off by
+ * some 4e-4 of its norm.  A NaN or an infinity makes its own matrix NaN.
+ * Then the control block is advanced as by train_adamw_step, unless `keep` is set: a further step that shares the block (AdamW over the
+ * network's other tensors) does it.  With control->nonfinite set nothing else is changed. */
+typedef struct {
+  float momentum;          /* 0 <= momentum < 1 */
+  float eps;               /* a normal number > 0 */
+  int32_t nesterov, steps; /* steps: 1 to 16 */
+  int32_t keep;            /* 1: leaves the control block as it is */
+  int32_t reserved;        /* 0 */
+} train_muon;
+int train_muon_step(const train_matrices* matrices, const train_muon* options, float* momentum, train_control* control,
+                    void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

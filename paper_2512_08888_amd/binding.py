@@ -46,6 +46,10 @@ TRAIN_EXPORTS = [
     "train_groupnorm_bwd_bf16", "train_diag_groupnorm_wait",
     "train_list_create", "train_list_destroy", "train_list_elements", "train_list_workspace_bytes",
     "train_control_init", "train_grad_norm", "train_adamw_step",
+    "train_logp_workspace_bytes", "train_logp_fwd", "train_logp_bwd", "train_policy_loss", "train_logp_fwd_bf16",
+    "train_logp_bwd_bf16", "train_policy_loss_bf16",
+    "train_matrices_create", "train_matrices_destroy", "train_matrices_elements", "train_matrices_workspace_bytes",
+    "train_muon_step",
 ]
 ACTS = {"none": 0, "relu": 1, "silu": 2}
 NCHW, NHWC = 0, 1
@@ -86,6 +90,31 @@ class TrainAdamW(ctypes.Structure):
     _fields_ = [
         ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_float), ("state", ctypes.c_int32),
         ("seed", ctypes.c_uint32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class TrainPolicy(ctypes.Structure):
+    """train_policy: the clipped policy loss's constants."""
+    _fields_ = [
+        ("clip_low", ctypes.c_float), ("clip_high", ctypes.c_float), ("kl", ctypes.c_float), ("entropy", ctypes.c_float),
+        ("per_image", ctypes.c_int32), ("reserved", ctypes.c_int32),
+    ]
+
+
+class TrainMatrix(ctypes.Structure):
+    """train_matrix: a stack of matrices of one shape with their gradients."""
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("count", ctypes.c_int32),
+        ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float),
+        ("reserved", ctypes.c_int32),
+    ]
+
+
+class TrainMuon(ctypes.Structure):
+    """train_muon: what Muon's step keeps from step to step."""
+    _fields_ = [
+        ("momentum", ctypes.c_float), ("eps", ctypes.c_float), ("nesterov", ctypes.c_int32), ("steps", ctypes.c_int32),
+        ("keep", ctypes.c_int32), ("reserved", ctypes.c_int32),
     ]
 
 
@@ -178,6 +207,20 @@ def lib():
         L.train_control_init.argtypes = [vp, ci, fp, vp]
         L.train_grad_norm.argtypes = [vp, fp, vp, vp, vp, sz, vp]
         L.train_adamw_step.argtypes = [vp, ctypes.POINTER(TrainAdamW), vp, vp, vp, vp, vp, vp]
+        L.train_logp_workspace_bytes.argtypes = [ci, ci, sz]
+        L.train_logp_workspace_bytes.restype = sz
+        L.train_logp_fwd.argtypes = [vp] * 5 + [ci, ci, sz, ci, vp, sz, vp]
+        L.train_logp_bwd.argtypes = [vp] * 7 + [ci, ci, sz, ci, vp]
+        L.train_policy_loss.argtypes = [vp] * 9 + [ci, ci, sz, ci, ctypes.POINTER(TrainPolicy), vp, sz, vp]
+        for name in ("train_logp_fwd", "train_logp_bwd", "train_policy_loss"):
+            getattr(L, name + "_bf16").argtypes = getattr(L, name).argtypes
+        L.train_matrices_create.argtypes = [ctypes.POINTER(TrainMatrix), ci, ci, ctypes.POINTER(vp)]
+        L.train_matrices_destroy.argtypes = [vp]
+        L.train_matrices_elements.argtypes = [vp]
+        L.train_matrices_elements.restype = ctypes.c_uint64
+        L.train_matrices_workspace_bytes.argtypes = [vp]
+        L.train_matrices_workspace_bytes.restype = sz
+        L.train_muon_step.argtypes = [vp, ctypes.POINTER(TrainMuon), vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -686,3 +729,140 @@ def train_adamw_step(tensors: TrainList, options: TrainAdamW, m, v, m_scale, v_s
                                   _room(what, "v", v, n * size, align), _room(what, "m_scale", m_scale, n // 32),
                                   _room(what, "v_scale", v_scale, n // 32), _room(what, "control", control, CONTROL_BYTES),
                                   _stream()), what)
+
+
+def train_logp_workspace_bytes(N, K, P):
+    _ints("train_logp_workspace_bytes", N, K)
+    return int(lib().train_logp_workspace_bytes(N, K, P))
+
+
+def _row_values(what, name, t, n, dtype=None):
+    """Address of a tensor of n values (fp32 unless dtype says otherwise), one for each row; None stays NULL."""
+    if t is None:
+        return None
+    if t.dtype != (dtype or _f32) or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+        raise ValueError(f"{what}: {name} must be {str(dtype or _f32)[6:]}, contiguous, on the GPU, with {n} elements")
+    return t.data_ptr()
+
+
+def _loss(what, logits, dlogits, labels, ws, scratch):
+    """What the calls on logits share: entry point, N, K, P, order of the logits, the labels' address, workspace."""
+    global _f32
+    import torch
+
+    if _f32 is None:
+        _f32 = torch.float32
+    layout = _map_layout(what, logits, () if dlogits is None else (dlogits,))
+    N, K = logits.shape[0], logits.shape[1]
+    _ints(what, N, K)
+    P = logits.numel() // (N * K) if N * K else 0
+    fn = _glue(what, logits)
+    at = _row_values(what, "labels", labels, N * P, torch.int32)
+    for name, t in (("labels", labels), ("dlogits", dlogits), ("ws", ws)):
+        if t is not None and t.device != logits.device:
+            raise ValueError(f"{what}: {name} must be on the logits' device")
+    if scratch:
+        if ws is None:
+            ws = torch.empty(max(256, train_logp_workspace_bytes(N, K, P)), dtype=torch.uint8, device=logits.device)
+        elif not ws.is_cuda:
+            raise ValueError(f"{what}: the workspace must be on the GPU")
+    return fn, N, K, P, layout, at, ws
+
+
+def train_logp_fwd(logits, labels, logp, entropy=None, stat=None, ws=None):
+    """logits [N, K, ...], contiguous or channels last (tokens: [N, K]); labels int32, logp, entropy: one value a row; stat:
+    two, for the backward call."""
+    what = "train_logp_fwd"
+    fn, N, K, P, layout, at, ws = _loss(what, logits, None, labels, ws, True)
+    n = N * P
+    _check(fn(logits.data_ptr(), at, _row_values(what, "logp", logp, n), _row_values(what, "entropy", entropy, n),
+              _row_values(what, "stat", stat, 2 * n), N, K, P, layout, _ptr(ws), _nbytes(ws), _stream()), what)
+
+
+def train_logp_bwd(logits, labels, stat, dlogp, dlogits, entropy=None, dentropy=None):
+    """The logits' gradient from those of log-probability and entropy (None: none); stat and entropy from the forward call.
+    dlogits, in the logits' order, may be the logits themselves."""
+    what = "train_logp_bwd"
+    fn, N, K, P, layout, at, _ = _loss(what, logits, dlogits, labels, None, False)
+    n = N * P
+    _check(fn(logits.data_ptr(), at, _row_values(what, "stat", stat, 2 * n), _row_values(what, "entropy", entropy, n),
+              _row_values(what, "dlogp", dlogp, n), _row_values(what, "dentropy", dentropy, n), dlogits.data_ptr(), N, K, P,
+              layout, _stream()), what)
+
+
+def train_policy_loss(logits, labels, advantage, out, dlogits=None, logp_old=None, logp_ref=None, weight=None, logp=None,
+                      clip=(0.2, 0.2), kl=0.0, entropy=0.0, ws=None):
+    """out [4]: loss, distance to the reference, entropy, share of cut rows (weighted sums).  advantage: a value for each row
+    or for each image; weight None: 1 / rows; the others: one value a row.  dlogits may be the logits themselves, or None."""
+    what = "train_policy_loss"
+    fn, N, K, P, layout, at, ws = _loss(what, logits, dlogits, labels, ws, True)
+    n = N * P
+    per_image = advantage.numel() == N and P != 1
+    o = TrainPolicy(clip[0], clip[1], kl, entropy, int(per_image), 0)
+    _check(fn(logits.data_ptr(), at, _row_values(what, "advantage", advantage, N if per_image else n),
+              _row_values(what, "logp_old", logp_old, n), _row_values(what, "logp_ref", logp_ref, n),
+              _row_values(what, "weight", weight, n), _row_values(what, "out", out, 4), None if dlogits is None else dlogits.data_ptr(),
+              _row_values(what, "logp", logp, n), N, K, P, layout, ctypes.byref(o), _ptr(ws), _nbytes(ws), _stream()), what)
+
+
+class TrainMatrices:
+    """Owns a train_matrices*: matrices [rows, cols] or stacks of them [count, rows, cols] with their gradients, optional
+    bf16 copies, and a weight decay and a scale of the update for each stack.  Keeps the tensors alive, as the handle
+    holds their addresses."""
+
+    def __init__(self, grads, params, scale, copies=None, weight_decay=0.0):
+        import torch
+
+        self._h = ctypes.c_void_p()
+        grads, params = list(grads), list(params)
+        k = len(grads)
+        copies = [None] * k if copies is None else list(copies)
+        each = lambda v: [float(v)] * k if isinstance(v, (int, float)) else [float(w) for w in v]  # noqa: E731
+        decay, scale = each(weight_decay), each(scale)
+        if not (len(params) == len(copies) == len(decay) == len(scale) == k):
+            raise ValueError("TrainMatrices: one parameter, gradient, copy, weight decay and scale for each stack")
+        kinds = {g.dtype for g in grads}
+        if len(kinds) > 1 or not kinds <= {torch.float32, torch.bfloat16}:
+            raise TypeError(f"TrainMatrices: gradients must be all float32 or all bfloat16, got {sorted(map(str, kinds))}")
+        for p, g, c in zip(params, grads, copies):
+            if p.dim() not in (2, 3):
+                raise ValueError("TrainMatrices: matrices are [rows, cols] or [count, rows, cols]")
+            if p.dtype != torch.float32 or p.shape != g.shape:
+                raise TypeError("TrainMatrices: parameters must be float32 in the shape of their gradients")
+            if c is not None and (c.dtype != torch.bfloat16 or c.shape != g.shape):
+                raise TypeError("TrainMatrices: copies must be bfloat16 in the shape of the gradients")
+            _ints("TrainMatrices", *p.shape)
+        devices = {t.device for ts in (params, grads, copies) for t in ts if t is not None}
+        if len(devices) > 1 or any(d.type != "cuda" for d in devices):
+            raise ValueError(f"TrainMatrices: tensors must be on one GPU, got {sorted(map(str, devices))}")
+        self.tensors = (params, grads, copies)
+        rows = (TrainMatrix * max(1, k))(*[
+            TrainMatrix(_ptr(p), _ptr(g), _ptr(c), 1 if p.dim() == 2 else p.shape[0], p.shape[-2], p.shape[-1], w, f, 0)
+            for p, g, c, w, f in zip(params, grads, copies, decay, scale)])
+        _check(lib().train_matrices_create(rows, k, BF16 if kinds == {torch.bfloat16} else F32, ctypes.byref(self._h)),
+               "train_matrices_create")
+        self.count = k
+        self.elements = int(lib().train_matrices_elements(self._h))
+        self.workspace_bytes = int(lib().train_matrices_workspace_bytes(self._h))
+
+    def close(self):
+        if self._h:
+            lib().train_matrices_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    @property
+    def handle(self):
+        return self._h
+
+
+def train_muon_step(matrices: TrainMatrices, options: TrainMuon, momentum, control, ws):
+    """momentum: matrices.elements fp32 values; control: 16 int32; ws: matrices.workspace_bytes."""
+    what = "train_muon_step"
+    _check(lib().train_muon_step(matrices.handle, ctypes.byref(options), _room(what, "momentum", momentum, 4 * matrices.elements, 16),
+                                 _room(what, "control", control, CONTROL_BYTES), _room(what, "ws", ws, 0), _nbytes(ws), _stream()), what)

@@ -18,6 +18,7 @@
 
 #include "glue_elt.h"
 #include "rotconv.h"
+#include "train_control.h"
 #include "unettrain.h"
 
 namespace {
@@ -309,11 +310,6 @@ __device__ __forceinline__ void round_up_or_down(float* q, const uint32_t* rando
   }
 }
 
-// The factor of a step's gradients: a clip factor that a step has used, and that nobody has written over, counts no more.
-__device__ __forceinline__ float factor(const train_control& c) {
-  return c.clip == 2 && __float_as_uint(c.coef) == __float_as_uint(c.spent) ? 1.f : c.coef;
-}
-
 struct Step {                          // what a step's elements share
   float b1, c1, b2, c2;                // beta, 1 - beta
   float eps, coef, root;               // root: 1 / sqrt(1 - beta2^t)
@@ -438,13 +434,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
     if (!ends || threadIdx.x != 0) return;             // (more launches of this step follow)
     const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
     if (!draw_last(tickets + 32 * (1 + mine), of) || !draw_last(tickets, min(gridDim.x, (uint32_t)kFan))) return;
-    if (s.skip) {
-      ctl->skipped += 1, ctl->nonfinite = 0;
-      ctl->coef = 1.f, ctl->clip = 0;                  // of a norm that was not finite
-      return;
-    }
-    ctl->step = s.t;
-    if (ctl->clip == 1) ctl->clip = 2, ctl->spent = ctl->coef;
+    end_step(ctl, s.skip, s.t);
   };
   if (s.skip || !inside) {             // (the first lane is inside)
     end();

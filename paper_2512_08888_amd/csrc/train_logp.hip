@@ -1,0 +1,687 @@
+// Log-probabilities of labels, forward and backward, and the clipped policy loss with its gradient (see
+// include/unettrain.h).
+//
+// A row is the K logits of a pixel or token.  With t its largest, y_j = z_j - t, s = sum exp(y_j) and h = sum exp(y_j) y_j,
+//     l = ln s      logp = y_label - l      entropy = l - h / s      p_j = exp(y_j) / s
+// and every gradient here has the form dz_j = c1 1[j = label] - p_j (base + c2 y_j), with base = c1 + c2 (entropy - l): c1 is the
+// gradient of the log-probability, c2 that of the entropy.  All of it is bound by memory: a row is read once, held in registers
+// (packed as it came) while its sums are formed, and its gradient written from there.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+#include <cmath>
+#include <cstdint>
+
+#include "glue_elt.h"
+#include "rotconv.h"
+#include "unettrain.h"
+
+namespace rotconv {
+namespace {
+
+enum Mode { kFwd, kBwd, kPolicy };
+constexpr int kMostBlocks = 4096;      // of a launch; a workgroup's four sums each in the workspace
+
+struct LossArgs {
+  const void* z;
+  const int32_t* labels;
+  const float *stat, *ent, *dlogp, *dent;                    // backward
+  const float *adv, *old, *ref, *w;                          // policy
+  float *logp, *ent_out, *stat_out;
+  void* dz;                                                  // may be z
+  double* part;
+  size_t rows, P;
+  int K, per_image;
+  int alike;                                                 // rows: dz's vectors start where z's do
+  float low, high, kl, entc, unit;                           // the clipping range's ends; unit: the weight where there are none
+};
+
+struct RowIn {                         // what a row brings beside its logits
+  int label;
+  float a, b, c, d;                    // backward: t, l, dlogp, dentropy; policy: advantage, logp_old, logp_ref, weight
+  float ent;                           // backward
+};
+struct RowGrad {
+  float t, inv, c1, base, c2;          // p_j = exp(z_j - t) inv
+  bool live;                           // false: the row's gradient is 0
+};
+
+template <int MODE>
+__device__ __forceinline__ RowIn row_in(const LossArgs& g, size_t row) {
+  RowIn r = {};
+  r.label = g.labels[row];
+  if constexpr (MODE == kBwd) {
+    r.a = g.stat[2 * row], r.b = g.stat[2 * row + 1];
+    r.c = g.dlogp[row];
+    if (g.dent) r.d = g.dent[row], r.ent = g.ent[row];
+  } else if constexpr (MODE == kPolicy) {
+    r.a = g.adv[g.per_image ? row / g.P : row];
+    if (g.old) r.b = g.old[row];
+    if (g.ref) r.c = g.ref[row];
+    r.d = g.w ? g.w[row] : g.unit;
+  }
+  return r;
+}
+__device__ __forceinline__ bool has_label(const LossArgs& g, const RowIn& r) { return r.label >= 0 && r.label < g.K; }
+
+// exp(q) - q - 1: by its series near 0, where the difference would lose its digits
+__device__ __forceinline__ float distance(float q, float e1) {
+  if (fabsf(q) < 0.25f) {
+    float s = 1.f / 40320;
+    s = fmaf(s, q, 1.f / 5040), s = fmaf(s, q, 1.f / 720), s = fmaf(s, q, 1.f / 120);
+    s = fmaf(s, q, 1.f / 24), s = fmaf(s, q, 1.f / 6), s = fmaf(s, q, 0.5f);
+    return s * q * q;
+  }
+  return e1 == INFINITY ? e1 : e1 - q;
+}
+
+// exp of a difference to the row's largest; what lies 10^30 below it (-infinity too) counts as that, so that 0 times it stays 0
+__device__ __forceinline__ float below(float z, float t) {
+  const float y = z - t;
+  return y < -1e30f ? -1e30f : y;      // (a NaN stays)
+}
+__device__ __forceinline__ void add_element(float y, float& s, float& h) {
+  const float e = __expf(y);
+  s += e;
+  h = fmaf(e, y, h);
+}
+
+// A row's results from its sums (t: -infinity where no logit is above that, and the sums are then those over z itself), written by one
+// lane; the sums over rows are added to acc.  Returns what the gradient needs.
+template <int MODE>
+__device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const RowIn& r, float t, float s, float h, float za, bool writes,
+                                           double* acc) {
+  RowGrad o = {};
+  if constexpr (MODE == kBwd) {
+    o.t = r.a;
+    o.inv = __expf(-r.b);
+    o.c1 = r.c, o.c2 = r.d;
+    o.base = r.c + r.d * (r.ent - r.b);
+    if (r.d == 0.f) o.base = r.c;
+    o.live = has_label(g, r) && r.a != -INFINITY && !(r.c == 0.f && r.d == 0.f);
+  } else {
+    const bool none = t == -INFINITY && s == 0.f;
+    bool live = has_label(g, r) && !none;
+    if constexpr (MODE == kPolicy) live = live && r.d != 0.f;
+    const float l = logf(s), logp = za - t - l, ent = l - h / s;
+    if (writes && g.logp) g.logp[row] = live ? logp : 0.f;
+    if constexpr (MODE == kFwd) {
+      if (writes && g.ent_out) g.ent_out[row] = live ? ent : 0.f;
+      if (writes && g.stat_out) {
+        const bool label = has_label(g, r);
+        g.stat_out[2 * row] = label ? t : 0.f, g.stat_out[2 * row + 1] = live ? l : 0.f;
+      }
+    } else {
+      const float A = r.a, w = r.d;
+      const float ratio = g.old ? expf(logp - r.b) : 1.f;
+      const bool cut = (A > 0.f && ratio > g.high) || (A < 0.f && ratio < g.low);
+      // (A = 0 counts as no advantage whatever the ratio; a NaN goes through)
+      const float kept = A == 0.f ? 0.f : ratio * A, gain = cut ? (A > 0.f ? g.high : g.low) * A : kept;
+      float loss = -gain, G = cut ? 0.f : -kept, d = 0.f, H = 0.f;
+      if (g.kl != 0.f && g.ref) {
+        const float q = r.c - logp, e1 = expm1f(q);
+        d = distance(q, e1);
+        loss += g.kl * d;
+        G -= g.kl * e1;
+      }
+      if (g.entc != 0.f) {
+        H = ent;
+        loss -= g.entc * H;
+      }
+      if (writes && live) {
+        acc[0] += (double)w * loss;
+        acc[1] += (double)w * d;
+        acc[2] += (double)w * H;
+        acc[3] += cut ? (double)w : 0.0;
+      }
+      o.t = t;
+      o.inv = 1.f / s;
+      o.c1 = w * G;
+      o.c2 = -g.entc * w;
+      o.base = g.entc != 0.f ? o.c1 + o.c2 * (ent - l) : o.c1;
+      o.live = live;
+    }
+  }
+  return o;
+}
+__device__ __forceinline__ float element(const RowGrad& o, float z, bool label) {
+  const float y = below(z, o.t), p = __expf(y) * o.inv;
+  return (label ? o.c1 : 0.f) - p * fmaf(o.c2, y, o.base);
+}
+
+// Waits for a loaded value.  Where gradients take the logits' place, other waves store behind the next barrier, and a barrier alone
+// does not wait for loads under way.
+__device__ __forceinline__ void arrived(float v) { asm volatile("" ::"v"(v)); }
+
+// max and sum over G neighbouring lanes
+template <int G> __device__ __forceinline__ float lanes_max(float v) {
+#pragma unroll
+  for (int k = G / 2; k > 0; k /= 2) v = fmaxf(v, __shfl_xor(v, k));
+  return v;
+}
+template <int G> __device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int k = G / 2; k > 0; k /= 2) v += __shfl_xor(v, k);
+  return v;
+}
+// the four sums of a workgroup, to its place in the workspace
+__device__ __forceinline__ void write_sums(const LossArgs& g, const double* acc) {
+  __shared__ double red[16][4];
+  const int wave = threadIdx.x / 64, waves = (blockDim.x + 63) / 64;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    double v = acc[k];
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) v += __shfl_xor(v, o);
+    if (threadIdx.x % 64 == 0) red[wave][k] = v;
+  }
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    double v = 0;
+    for (int w = 0; w < waves; ++w) v += red[w][threadIdx.x];
+    g.part[4 * (size_t)blockIdx.x + threadIdx.x] = v;
+  }
+}
+
+// Rows of few classes: G lanes to a row, E elements a lane, an element to a load (neighbouring rows lie side by side).
+template <typename T, int G, int E, int MODE>
+__global__ __launch_bounds__(256) void k_rows_small(LossArgs g) {
+  const int sub = threadIdx.x % G;
+  const size_t apart = (size_t)gridDim.x * (256 / G);
+  double acc[4] = {};
+  for (size_t row = (size_t)blockIdx.x * (256 / G) + threadIdx.x / G; row < g.rows; row += apart) {
+    const T* z = static_cast<const T*>(g.z) + row * g.K;
+    const RowIn r = row_in<MODE>(g, row);
+    float v[E], t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = sub + G * e < g.K ? Elt<T>::ld(z + sub + G * e) : -INFINITY;
+    if constexpr (MODE != kBwd) {
+      if (has_label(g, r)) za = Elt<T>::ld(z + r.label);
+#pragma unroll
+      for (int e = 0; e < E; ++e) t = fmaxf(t, v[e]);
+      t = lanes_max<G>(t);
+      const float from = t == -INFINITY ? 0.f : t;
+#pragma unroll
+      for (int e = 0; e < E; ++e) add_element(below(v[e], from), s, h);
+      s = lanes_sum<G>(s), h = lanes_sum<G>(h);
+    }
+    const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, sub == 0, acc);
+    if (MODE != kFwd && g.dz) {
+      T* d = static_cast<T*>(g.dz) + row * g.K;
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (sub + G * e < g.K) Elt<T>::st(d + sub + G * e, o.live ? element(o, v[e], sub + G * e == r.label) : 0.f);
+    }
+  }
+  if constexpr (MODE == kPolicy) write_sums(g, acc);
+}
+
+// A vector of 16 bytes as it lies in memory.  Rows start anywhere: vectors are those of the address space, and the first
+// and the last of a row may hold elements of its neighbours, which are neither read nor written.
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int V = 4;
+  static constexpr uint32_t kLowest = 0xff800000u;
+  static __device__ __forceinline__ float get(const u4& a, int k) { return __uint_as_float(a[k]); }
+  static __device__ __forceinline__ void set(u4& a, int k, float v) { a[k] = __float_as_uint(v); }
+};
+template <> struct Vec<uint16_t> {
+  static constexpr int V = 8;
+  static constexpr uint32_t kLowest = 0xff80ff80u;
+  static __device__ __forceinline__ float get(const u4& a, int k) {
+    return __uint_as_float(k % 2 ? a[k / 2] & 0xffff0000u : a[k / 2] << 16);
+  }
+  static __device__ __forceinline__ void set(u4& a, int k, float v) {
+    const uint32_t b = f32_to_bf16(v);
+    a[k / 2] = k % 2 ? (a[k / 2] & 0xffffu) | b << 16 : (a[k / 2] & 0xffff0000u) | b;
+  }
+};
+template <typename T>
+__device__ __forceinline__ u4 load_part(const T* z, int first, int K) {        // elements first .. of a row, -infinity outside it
+  constexpr int V = Vec<T>::V;
+  if (first >= 0 && first + V <= K) return *reinterpret_cast<const u4*>(z + first);
+  u4 a;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) a[k] = Vec<T>::kLowest;
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+    if (first + k >= 0 && first + k < K) Vec<T>::set(a, k, Elt<T>::ld(z + first + k));
+  return a;
+}
+template <typename T>
+__device__ __forceinline__ void store_part(T* d, const u4& a, int first, int K, bool alike) {
+  constexpr int V = Vec<T>::V;
+  if (alike && first >= 0 && first + V <= K) {
+    *reinterpret_cast<u4*>(d + first) = a;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k)
+    if (first + k >= 0 && first + k < K) Elt<T>::st(d + first + k, Vec<T>::get(a, k));
+}
+
+// over the workgroup's B threads, the same in all of them; red: a float a wave
+template <int B, bool MAX>
+__device__ __forceinline__ float block_join(float v, float* red) {
+  v = MAX ? lanes_max<64>(v) : lanes_sum<64>(v);
+  if constexpr (B == 64) return v;
+  __syncthreads();
+  if (threadIdx.x % 64 == 0) red[threadIdx.x / 64] = v;
+  __syncthreads();
+  v = red[threadIdx.x % (B / 64)];
+  return MAX ? lanes_max<B / 64>(v) : lanes_sum<B / 64>(v);
+}
+
+template <typename T>
+__device__ __forceinline__ u4 gradient(const RowGrad& o, const u4& a, int first, int label) {
+  constexpr int V = Vec<T>::V;
+  u4 d;
+#pragma unroll
+  for (int k = 0; k < V; ++k) Vec<T>::set(d, k, o.live ? element(o, Vec<T>::get(a, k), first + k == label) : 0.f);
+  return d;
+}
+
+// Rows of many classes: a workgroup of B threads to a row, up to E vectors a thread in registers.  E = 0: rows of any
+// length, read twice (their sums are then formed with a running maximum).
+template <typename T, int B, int E, int MODE>
+__global__ __launch_bounds__(B) void k_rows(LossArgs g) {
+  constexpr int V = Vec<T>::V;
+  __shared__ float red[16];
+  double acc[4] = {};
+  for (size_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
+    const T* z = static_cast<const T*>(g.z) + row * g.K;
+    T* dz = static_cast<T*>(g.dz) + row * g.K;
+    // elements between the last 16-byte border and the row's start
+    const int shift = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T));
+    const RowIn r = row_in<MODE>(g, row);
+    float t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
+    if (MODE != kBwd && has_label(g, r)) za = Elt<T>::ld(z + r.label);
+    arrived(za);
+    if constexpr (E > 0) {
+      u4 v[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = load_part(z, (int)(threadIdx.x + e * B) * V - shift, g.K);
+      if constexpr (MODE != kBwd) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int k = 0; k < V; ++k) t = fmaxf(t, Vec<T>::get(v[e], k));
+        t = block_join<B, true>(t, red);
+        const float from = t == -INFINITY ? 0.f : t;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int k = 0; k < V; ++k) add_element(below(Vec<T>::get(v[e], k), from), s, h);
+        s = block_join<B, false>(s, red), h = block_join<B, false>(h, red);
+      }
+      const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, threadIdx.x == 0, acc);
+      if (MODE != kFwd && g.dz) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int first = (int)(threadIdx.x + e * B) * V - shift;
+          store_part(dz, gradient<T>(o, v[e], first, r.label), first, g.K, g.alike);
+        }
+      }
+    } else {
+      if constexpr (MODE != kBwd) {
+        for (int first = (int)threadIdx.x * V - shift; first < g.K; first += B * V) {
+          const u4 v = load_part(z, first, g.K);
+          float top = t;
+#pragma unroll
+          for (int k = 0; k < V; ++k) top = fmaxf(top, Vec<T>::get(v, k));
+          if (top > t) {
+            const float y = below(t, top), f = __expf(y);
+            h = f * fmaf(y, s, h);
+            s = f * s;
+            t = top;
+          }
+          const float from = t == -INFINITY ? 0.f : t;
+#pragma unroll
+          for (int k = 0; k < V; ++k) add_element(below(Vec<T>::get(v, k), from), s, h);
+        }
+        const float top = block_join<B, true>(t, red);
+        const float y = top == -INFINITY ? 0.f : below(t, top), f = __expf(y);
+        h = f * fmaf(y, s, h);
+        s = f * s;
+        t = top;
+        s = block_join<B, false>(s, red), h = block_join<B, false>(h, red);
+      }
+      const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, threadIdx.x == 0, acc);
+      if (MODE != kFwd && g.dz)
+        for (int first = (int)threadIdx.x * V - shift; first < g.K; first += B * V)
+          store_part(dz, gradient<T>(o, load_part(z, first, g.K), first, r.label), first, g.K, g.alike);
+    }
+  }
+  if constexpr (MODE == kPolicy) write_sums(g, acc);
+}
+
+// Classes in planes: a lane holds V neighbouring pixels.  KM > 0: all K <= KM classes in registers; KM = 0: any number, read
+// twice, and blockDim.y waves share the classes of 64 lanes' pixels.
+template <typename T, int V>
+__device__ __forceinline__ void load_pixels(const T* p, float* v) {
+  if constexpr (V == 1) v[0] = Elt<T>::ld(p);
+  else if constexpr (sizeof(T) == 4) Elt<T>::ldv(p, v);
+  else Elt<T>::ldh(p, v);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_pixels(T* p, const float* v) {
+  if constexpr (V == 1) Elt<T>::st(p, v[0]);
+  else if constexpr (sizeof(T) == 4) Elt<T>::stv(p, v);
+  else Elt<T>::sth(p, v);
+}
+
+template <typename T, int V, int KM, int MODE>
+__global__ __launch_bounds__(256) void k_planes(LossArgs g) {
+  double acc[4] = {};
+  const size_t apart = (size_t)gridDim.x * 256 * V;
+  for (size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) * V; row < g.rows; row += apart) {
+    const size_t n = row / g.P, at = n * g.K * g.P + (row - n * g.P);
+    const T* z = static_cast<const T*>(g.z) + at;
+    T* dz = static_cast<T*>(g.dz) + at;
+    float v[KM][V];
+#pragma unroll
+    for (int k = 0; k < KM; ++k)
+      if (k < g.K) load_pixels<T, V>(z + k * g.P, v[k]);
+    RowGrad o[V];
+    int label[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const RowIn r = row_in<MODE>(g, row + i);
+      label[i] = r.label;
+      float t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
+      if constexpr (MODE != kBwd) {
+#pragma unroll
+        for (int k = 0; k < KM; ++k)
+          if (k < g.K) {
+            t = fmaxf(t, v[k][i]);
+            if (k == r.label) za = v[k][i];
+          }
+        const float from = t == -INFINITY ? 0.f : t;
+#pragma unroll
+        for (int k = 0; k < KM; ++k)
+          if (k < g.K) add_element(below(v[k][i], from), s, h);
+      }
+      o[i] = row_end<MODE>(g, row + i, r, t, s, h, za, true, acc);
+    }
+    if (MODE != kFwd && g.dz) {
+#pragma unroll
+      for (int k = 0; k < KM; ++k)
+        if (k < g.K) {
+          float d[V];
+#pragma unroll
+          for (int i = 0; i < V; ++i) d[i] = o[i].live ? element(o[i], v[k][i], k == label[i]) : 0.f;
+          store_pixels<T, V>(dz + k * g.P, d);
+        }
+    }
+  }
+  if constexpr (MODE == kPolicy) write_sums(g, acc);
+}
+
+template <typename T, int V, int MODE>
+__global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
+  __shared__ float shared[16][3][64 * V];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+  double acc[4] = {};
+  const size_t apart = (size_t)gridDim.x * 64 * V;
+  for (size_t first = (size_t)blockIdx.x * 64 * V; first < g.rows; first += apart) {
+    const size_t row = first + (size_t)lane * V;
+    const bool inside = row < g.rows;
+    const size_t n = row / g.P, at = n * g.K * g.P + (row - n * g.P);
+    const T* z = static_cast<const T*>(g.z) + at;
+    float t[V], s[V], h[V], za[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) t[i] = -INFINITY, s[i] = h[i] = za[i] = 0.f;
+    if constexpr (MODE != kBwd) {
+      if (inside) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int label = g.labels[row + i];
+          if (label >= 0 && label < g.K) za[i] = Elt<T>::ld(z + (size_t)label * g.P + i);
+          arrived(za[i]);
+        }
+        auto add = [&](const float* v) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            if (v[i] > t[i]) {
+              const float y = below(t[i], v[i]), f = __expf(y);
+              h[i] = f * fmaf(y, s[i], h[i]);
+              s[i] = f * s[i];
+              t[i] = v[i];
+            }
+            add_element(below(v[i], t[i] == -INFINITY ? 0.f : t[i]), s[i], h[i]);
+          }
+        };
+        int k = wave;
+        for (; k + 3 * waves < g.K; k += 4 * waves) {
+          float v[4][V];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) load_pixels<T, V>(z + (size_t)(k + u * waves) * g.P, v[u]);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) add(v[u]);
+        }
+        for (; k < g.K; k += waves) {
+          float v[V];
+          load_pixels<T, V>(z + (size_t)k * g.P, v);
+          add(v);
+        }
+      }
+      if (waves > 1) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) shared[wave][0][lane * V + i] = t[i], shared[wave][1][lane * V + i] = s[i], shared[wave][2][lane * V + i] = h[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          float top = -INFINITY;
+          for (int w = 0; w < waves; ++w) top = fmaxf(top, shared[w][0][lane * V + i]);
+          s[i] = h[i] = 0.f, t[i] = top;
+          for (int w = 0; w < waves; ++w) {
+            const float sw = shared[w][1][lane * V + i], hw = shared[w][2][lane * V + i];
+            const float y = top == -INFINITY ? 0.f : below(shared[w][0][lane * V + i], top), f = __expf(y);
+            h[i] += f * fmaf(y, sw, hw);
+            s[i] += f * sw;
+          }
+        }
+      }
+    }
+    if (!inside) continue;             // (every wave of the workgroup has the same lanes inside, and no barrier follows within the pass)
+    RowGrad o[V];
+    int label[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const RowIn r = row_in<MODE>(g, row + i);
+      label[i] = r.label;
+      o[i] = row_end<MODE>(g, row + i, r, t[i], s[i], h[i], za[i], wave == 0, acc);
+    }
+    if (MODE != kFwd && g.dz) {
+      T* dz = static_cast<T*>(g.dz) + at;
+      for (int k = wave; k < g.K; k += waves) {
+        float v[V];
+        load_pixels<T, V>(z + (size_t)k * g.P, v);
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = o[i].live ? element(o[i], v[i], k == label[i]) : 0.f;
+        store_pixels<T, V>(dz + (size_t)k * g.P, v);
+      }
+    }
+  }
+  if constexpr (MODE == kPolicy) write_sums(g, acc);
+}
+
+// out[k] = sum of the workgroups' k-th sums, each thread's in order and then a fixed tree
+__global__ __launch_bounds__(1024) void k_policy_end(const double* __restrict__ part, int count, float* __restrict__ out) {
+  __shared__ double red[16][4];
+  double acc[4] = {};
+  for (int i = threadIdx.x; i < count; i += 1024)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[k] += part[4 * (size_t)i + k];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+#pragma unroll
+    for (int o = 32; o > 0; o /= 2) acc[k] += __shfl_xor(acc[k], o);
+    if (threadIdx.x % 64 == 0) red[threadIdx.x / 64][k] = acc[k];
+  }
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    double v = 0;
+    for (int w = 0; w < 16; ++w) v += red[w][threadIdx.x];
+    out[threadIdx.x] = (float)v;
+  }
+}
+
+int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
+bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+unsigned blocks_for(size_t n) { return (unsigned)std::min<size_t>(n, kMostBlocks); }
+
+template <typename T, int B, int E, int MODE>
+void launch_rows(const LossArgs& g, unsigned* blocks, hipStream_t st) {
+  *blocks = blocks_for(g.rows);
+  k_rows<T, B, E, MODE><<<*blocks, B, 0, st>>>(g);
+}
+template <typename T, int G, int E, int MODE>
+void launch_small(const LossArgs& g, unsigned* blocks, hipStream_t st) {
+  *blocks = blocks_for((g.rows + 256 / G - 1) / (256 / G));
+  k_rows_small<T, G, E, MODE><<<*blocks, 256, 0, st>>>(g);
+}
+
+template <typename T, int MODE>
+void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st) {
+  constexpr int V = Vec<T>::V;
+  if (rows) {
+    // vectors of a row, counted as if it started one element past a border unless all of them start on one
+    const bool even = !misaligned(g.z, 16) && g.K % V == 0;
+    const int vecs = even ? g.K / V : (g.K + V - 2) / V + 1;
+    if (g.K <= 8) launch_small<T, 1, 8, MODE>(g, blocks, st);
+    else if (g.K <= 64) launch_small<T, 8, 8, MODE>(g, blocks, st);
+    else if (g.K <= 512) launch_small<T, 64, 8, MODE>(g, blocks, st);
+    else if (vecs <= 64 * 4) launch_rows<T, 64, 4, MODE>(g, blocks, st);
+    else if (vecs <= 256 * 4) launch_rows<T, 256, 4, MODE>(g, blocks, st);
+    else if (vecs <= 1024 * 4) launch_rows<T, 1024, 4, MODE>(g, blocks, st);
+    else if (vecs <= 1024 * 8) launch_rows<T, 1024, 8, MODE>(g, blocks, st);
+    else if (vecs <= 1024 * 16) launch_rows<T, 1024, 16, MODE>(g, blocks, st);
+    else launch_rows<T, 1024, 0, MODE>(g, blocks, st);
+    return;
+  }
+  const bool four = g.P % 4 == 0 && !misaligned(g.z, 4 * sizeof(T)) && !misaligned(g.dz, 4 * sizeof(T));
+  if (g.K <= 16) {
+    *blocks = blocks_for((g.rows + 256 * (four ? 4 : 1) - 1) / (256 * (four ? 4 : 1)));
+    auto kernel = four ? (g.K <= 8 ? k_planes<T, 4, 8, MODE> : k_planes<T, 4, 16, MODE>)
+                       : (g.K <= 8 ? k_planes<T, 1, 8, MODE> : k_planes<T, 1, 16, MODE>);
+    kernel<<<*blocks, 256, 0, st>>>(g);
+  } else {
+    const size_t strips = (g.rows + 64 * (four ? 4 : 1) - 1) / (64 * (four ? 4 : 1));
+    *blocks = blocks_for(strips);
+    int waves = 1;                     // until the chip has its fill of them, or a wave would have too few classes
+    while (waves < 16 && strips * waves < 4096 && g.K / waves >= 16) waves *= 2;
+    auto kernel = four ? k_planes_long<T, 4, MODE> : k_planes_long<T, 1, MODE>;
+    kernel<<<*blocks, 64 * waves, 0, st>>>(g);
+  }
+}
+
+bool refused(int N, int K, size_t P) {
+  return N < 1 || K < 1 || P < 1 || K > (1 << 24) || P > 0x7fffffffull || (uint64_t)N * P > 0x7fffffffull;
+}
+constexpr size_t kWorkspace = (size_t)kMostBlocks * 4 * sizeof(double);
+
+template <typename T>
+int check(const LossArgs& g, int N, int K, size_t P, int layout) {
+  if (refused(N, K, P)) return ROTCONV_ERR_SHAPE;
+  if (layout != TRAIN_NCHW && layout != TRAIN_NHWC) return ROTCONV_ERR_UNSUPPORTED;
+  if (misaligned(g.z, sizeof(T)) || misaligned(g.dz, sizeof(T)) || misaligned(g.labels, 4)) return ROTCONV_ERR_UNSUPPORTED;
+  for (const float* p : {g.stat, g.ent, g.dlogp, g.dent, g.adv, g.old, g.ref, g.w, (const float*)g.logp, (const float*)g.ent_out, (const float*)g.stat_out})
+    if (misaligned(p, 4)) return ROTCONV_ERR_UNSUPPORTED;
+  return ROTCONV_OK;
+}
+LossArgs arguments(const void* z, void* dz, const int32_t* labels, int N, int K, size_t P) {
+  LossArgs g = {};
+  g.z = z, g.dz = dz, g.labels = labels, g.K = K, g.P = P, g.rows = (size_t)N * P;
+  g.alike = (reinterpret_cast<uintptr_t>(z) - reinterpret_cast<uintptr_t>(dz)) % 16 == 0;
+  return g;
+}
+bool in_rows(int layout, size_t P) { return layout == TRAIN_NHWC || P == 1; }
+
+template <typename T>
+int logp_fwd_t(const T* z, const int32_t* labels, float* logp, float* entropy, float* stat, int N, int K, size_t P, int layout, void* ws,
+               size_t ws_bytes, void* stream) {
+  if (!z || !labels || !logp) return ROTCONV_ERR_NULL;
+  LossArgs g = arguments(z, nullptr, labels, N, K, P);
+  g.logp = logp, g.ent_out = entropy, g.stat_out = stat;
+  if (int e = check<T>(g, N, K, P, layout)) return e;
+  if (!ws || misaligned(ws, 8) || ws_bytes < kWorkspace) return ROTCONV_ERR_WORKSPACE;
+  unsigned blocks;
+  launch_loss<T, kFwd>(g, in_rows(layout, P), &blocks, static_cast<hipStream_t>(stream));
+  return finish();
+}
+template <typename T>
+int logp_bwd_t(const T* z, const int32_t* labels, const float* stat, const float* entropy, const float* dlogp, const float* dentropy, T* dz,
+               int N, int K, size_t P, int layout, void* stream) {
+  if (!z || !labels || !stat || !dlogp || !dz || (dentropy && !entropy)) return ROTCONV_ERR_NULL;
+  LossArgs g = arguments(z, dz, labels, N, K, P);
+  g.stat = stat, g.ent = entropy, g.dlogp = dlogp, g.dent = dentropy;
+  if (int e = check<T>(g, N, K, P, layout)) return e;
+  unsigned blocks;
+  launch_loss<T, kBwd>(g, in_rows(layout, P), &blocks, static_cast<hipStream_t>(stream));
+  return finish();
+}
+template <typename T>
+int policy_loss_t(const T* z, const int32_t* labels, const float* advantage, const float* logp_old, const float* logp_ref, const float* weight,
+                  float* out, T* dz, float* logp, int N, int K, size_t P, int layout, const train_policy* o, void* ws, size_t ws_bytes,
+                  void* stream) {
+  if (!z || !labels || !advantage || !out || !o || (o->kl != 0.f && !logp_ref)) return ROTCONV_ERR_NULL;
+  LossArgs g = arguments(z, dz, labels, N, K, P);
+  g.adv = advantage, g.old = logp_old, g.ref = logp_ref, g.w = weight, g.logp = logp;
+  if (int e = check<T>(g, N, K, P, layout)) return e;
+  if (!(o->clip_low >= 0.f && o->clip_low <= 1.f) || !(o->clip_high >= 0.f && o->clip_high <= FLT_MAX) || !(o->kl >= 0.f && o->kl <= FLT_MAX) ||
+      !(o->entropy >= 0.f && o->entropy <= FLT_MAX) || (o->per_image != 0 && o->per_image != 1) || o->reserved != 0 ||
+      misaligned(out, 4))
+    return ROTCONV_ERR_UNSUPPORTED;
+  if (!ws || misaligned(ws, 8) || ws_bytes < kWorkspace) return ROTCONV_ERR_WORKSPACE;
+  g.per_image = o->per_image, g.low = 1.f - o->clip_low, g.high = 1.f + o->clip_high, g.kl = o->kl, g.entc = o->entropy;
+  g.unit = (float)(1.0 / ((double)N * (double)P));
+  g.part = static_cast<double*>(ws);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  unsigned blocks;
+  launch_loss<T, kPolicy>(g, in_rows(layout, P), &blocks, st);
+  k_policy_end<<<1, 1024, 0, st>>>(g.part, (int)blocks, out);
+  return finish();
+}
+
+}  // namespace
+}  // namespace rotconv
+
+using namespace rotconv;
+
+extern "C" {
+
+size_t train_logp_workspace_bytes(int N, int K, size_t P) { return refused(N, K, P) ? 0 : kWorkspace; }
+
+int train_logp_fwd(const float* logits, const int32_t* labels, float* logp, float* entropy, float* stat, int N, int K, size_t P, int layout,
+                   void* ws, size_t ws_bytes, void* stream) {
+  return logp_fwd_t(logits, labels, logp, entropy, stat, N, K, P, layout, ws, ws_bytes, stream);
+}
+int train_logp_fwd_bf16(const uint16_t* logits, const int32_t* labels, float* logp, float* entropy, float* stat, int N, int K, size_t P,
+                        int layout, void* ws, size_t ws_bytes, void* stream) {
+  return logp_fwd_t(logits, labels, logp, entropy, stat, N, K, P, layout, ws, ws_bytes, stream);
+}
+int train_logp_bwd(const float* logits, const int32_t* labels, const float* stat, const float* entropy, const float* dlogp,
+                   const float* dentropy, float* dlogits, int N, int K, size_t P, int layout, void* stream) {
+  return logp_bwd_t(logits, labels, stat, entropy, dlogp, dentropy, dlogits, N, K, P, layout, stream);
+}
+int train_logp_bwd_bf16(const uint16_t* logits, const int32_t* labels, const float* stat, const float* entropy, const float* dlogp,
+                        const float* dentropy, uint16_t* dlogits, int N, int K, size_t P, int layout, void* stream) {
+  return logp_bwd_t(logits, labels, stat, entropy, dlogp, dentropy, dlogits, N, K, P, layout, stream);
+}
+int train_policy_loss(const float* logits, const int32_t* labels, const float* advantage, const float* logp_old, const float* logp_ref,
+                      const float* weight, float* out, float* dlogits, float* logp, int N, int K, size_t P, int layout,
+                      const train_policy* options, void* ws, size_t ws_bytes, void* stream) {
+  return policy_loss_t(logits, labels, advantage, logp_old, logp_ref, weight, out, dlogits, logp, N, K, P, layout, options, ws, ws_bytes,
+                       stream);
+}
+int train_policy_loss_bf16(const uint16_t* logits, const int32_t* labels, const float* advantage, const float* logp_old, const float* logp_ref,
+                           const float* weight, float* out, uint16_t* dlogits, float* logp, int N, int K, size_t P, int layout,
+                           const train_policy* options, void* ws, size_t ws_bytes, void* stream) {
+  return policy_loss_t(logits, labels, advantage, logp_old, logp_ref, weight, out, dlogits, logp, N, K, P, layout, options, ws, ws_bytes,
+                       stream);
+}
+
+}  // extern "C"

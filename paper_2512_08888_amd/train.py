@@ -1,8 +1,8 @@
-"""The optimiser's side of a training step: the norm and clip factor of all gradients, and AdamW over all parameters,
-through the C-ABI library (include/unettrain.h).  This module only owns the device buffers (torch tensors as plain
+"""The optimiser's side of a training step: the norm and clip factor of all gradients, AdamW over all parameters, and Muon
+over matrices (with AdamW for the rest), through the C-ABI library (include/unettrain.h).  This module only owns the device buffers (torch tensors as plain
 memory) and the order of the calls; no arithmetic of the method happens here.
 
-    python -m paper_2512_08888_amd.train [--steps 60] [--dtype bf16] [--state mx8] [--graph]
+    python -m paper_2512_08888_amd.train [--steps 60] [--dtype bf16] [--state mx8] [--method muon] [--loss policy] [--graph]
 
 trains a small stack with group norms (paper_2512_08888_amd/unet.py) on one synthetic batch and prints its loss.
 """
@@ -40,6 +40,23 @@ class GradNorm(_Control):
 
     def compute(self, max_norm=math.inf):
         rc.train_grad_norm(self.list, max_norm, self.norms, self.control, self.ws)
+
+
+def _load(optimizer, step, state):
+    """Copies a saved state into an optimizer's own buffers, or refuses all of it."""
+    import torch
+
+    mine, step = optimizer.state(), int(step)
+    if not 0 <= step < 2**31 - 1:
+        raise ValueError(f"load_state: a step number is from 0 to 2^31 - 2, got {step}")
+    if set(state) != set(mine):
+        raise ValueError(f"load_state: expected {sorted(mine)}, got {sorted(state)}")
+    for name, t in state.items():
+        if t.dtype != mine[name].dtype or t.numel() != mine[name].numel():
+            raise ValueError(f"load_state: {name} must be {mine[name].dtype} with {mine[name].numel()} elements")
+    for name, t in state.items():
+        mine[name].view(torch.uint8).copy_(t.reshape(-1).view(torch.uint8))
+    optimizer.step_count.fill_(step)
 
 
 class AdamW(_Control):
@@ -91,19 +108,62 @@ class AdamW(_Control):
     def load_state(self, step, **state):
         """Continues from a saved step number and state(), taken from a list of the same sizes in the same order.  A state
         that does not fit is refused as a whole."""
+        _load(self, step, state)
+
+
+class Muon(_Control):
+    """Muon over fp32 matrices [rows, cols], or stacks of them [count, rows, cols], whose gradients (fp32 or bf16) lie in
+    fixed buffers: the momentum's direction, orthogonalised, times lr and a scale.
+
+    scale "rms": 0.2 sqrt(max(rows, cols)), with which an update's elements are as large as AdamW's, so that one learning
+    rate and weight decay serve both; "spectral": sqrt(max(1, rows / cols)); or a number.  rest: an AdamW of the network's other
+    tensors, whose step follows in step() under this one's control block (its own lr, clip factor and step number are not
+    used).  Step number, learning rate, clip factor and the skip of a step live on the device as AdamW's do."""
+
+    def __init__(self, params, grads, lr=1e-3, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, scale="rms", eps=1e-12,
+                 copies=None, rest=None):
         import torch
 
-        mine, step = self.state(), int(step)
-        if not 0 <= step < 2**31 - 1:
-            raise ValueError(f"load_state: a step number is from 0 to 2^31 - 2, got {step}")
-        if set(state) != set(mine):
-            raise ValueError(f"load_state: expected {sorted(mine)}, got {sorted(state)}")
-        for name, t in state.items():
-            if t.dtype != mine[name].dtype or t.numel() != mine[name].numel():
-                raise ValueError(f"load_state: {name} must be {mine[name].dtype} with {mine[name].numel()} elements")
-        for name, t in state.items():
-            mine[name].view(torch.uint8).copy_(t.reshape(-1).view(torch.uint8))
-        self.step_count.fill_(step)
+        params, grads = list(params), list(grads)
+        if scale == "rms":
+            factors = [0.2 * math.sqrt(max(p.shape[-2:])) for p in params]
+        elif scale == "spectral":
+            factors = [math.sqrt(max(1.0, p.shape[-2] / p.shape[-1])) for p in params]
+        elif isinstance(scale, (int, float)):
+            factors = float(scale)
+        else:
+            raise ValueError(f"Muon: scale must be 'rms', 'spectral' or a number, got {scale!r}")
+        self.matrices = rc.TrainMatrices(grads, params, factors, copies, weight_decay)
+        dev = self.matrices.tensors[1][0].device
+        super().__init__(dev)
+        self.rest = rest
+        self.options = rc.TrainMuon(momentum, eps, int(bool(nesterov)), steps, int(rest is not None), 0)
+        self.m = torch.zeros(self.matrices.elements, device=dev)
+        self.work = torch.empty(self.matrices.workspace_bytes, dtype=torch.uint8, device=dev)
+        # the norm is that of all gradients, the rest's among them
+        self.list = rc.TrainList(grads + (rest.list.tensors[1] if rest is not None else []))
+        self.norms = torch.zeros(self.list.count, device=dev)
+        self.ws = torch.empty(self.list.workspace_bytes, dtype=torch.uint8, device=dev)
+        rc.train_control_init(self.control, 0, lr)
+
+    def clip(self, max_norm):
+        """As AdamW.clip, over the matrices' gradients and the rest's."""
+        rc.train_grad_norm(self.list, max_norm, self.norms, self.control, self.ws)
+
+    def step(self):
+        rc.train_muon_step(self.matrices, self.options, self.m, self.control, self.work)
+        if self.rest is not None:
+            r = self.rest
+            rc.train_adamw_step(r.list, r.options, r.m, r.v, r.m_scale, r.v_scale, self.control)
+
+    def state(self):
+        """The momentum's own buffer; with a rest, its states as rest_m and so on."""
+        more = {} if self.rest is None else {"rest_" + k: t for k, t in self.rest.state().items()}
+        return {"m": self.m, **more}
+
+    def load_state(self, step, **state):
+        """Continues from a saved step number and state().  A state that does not fit is refused as a whole."""
+        _load(self, step, state)
 
 
 def main(argv=None):
