@@ -45,7 +45,7 @@ struct Matrix {
   uint64_t pos;                        // of the momentum
   uint32_t rows, cols, n, m;           // n = min, m = max
   uint32_t ldn, ldm;                   // n, m up to a multiple of kDepth; what is between is 0
-  uint32_t tall, vec;                  // vec: gradient and momentum can be read four elements at a time
+  uint32_t tall, vec, even;            // vec: gradient and momentum can be read four elements at a time; even: the rows of p and copy
   float wd, scale;
   uint32_t first, chunks;              // in the momentum's pass
   // byte offsets in the workspace: X's upper parts before and after an iteration, its lower part, A, B; the diagonals
@@ -156,7 +156,7 @@ __device__ __forceinline__ void split(float v, half* upper, half* lower) {
 }
 __device__ __forceinline__ float joined(half upper, half lower) { return (float)upper + (float)lower * (1.f / kLow); }
 
-// X from u, tiles of 64 x 64 of the matrix as it lies in memory; the columns up to ldm are 0 in both of X's buffers
+// X from u, tiles of 64 x 64 of the matrix as it lies in memory; the columns up to ldm are 0 (and stay so: a product of zeros)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ mats, const Tile* __restrict__ tiles, train_muon opt,
                                                     const float* __restrict__ momentum, const train_control* __restrict__ ctl,
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
     turned[k][lane] = v;
   }
   __syncthreads();
-  half *upper = reinterpret_cast<half*>(ws + x.x[0]), *other = reinterpret_cast<half*>(ws + x.x[1]), *lower = reinterpret_cast<half*>(ws + x.low);
+  half *upper = reinterpret_cast<half*>(ws + x.x[0]), *lower = reinterpret_cast<half*>(ws + x.low);
   const uint32_t ti = x.tall ? t.j : t.i, tj = x.tall ? t.i : t.j;
   for (int k = wave; k < kTurn; k += 4) {
     const uint32_t i = ti * kTurn + k, j = tj * kTurn + lane;
@@ -188,20 +188,66 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
     half u, l;
     split(x.tall ? turned[lane][k] : turned[k][lane], &u, &l);
     upper[at] = u, lower[at] = l;
-    if (j >= x.m) other[at] = (half)0.f;
   }
 }
 
 enum Product { kGram, kPoly, kApply, kLast };
 
-// One tile of 128 x 128 of a product, four waves of 64 x 64.
+// A wave's lanes bring 16 bytes each from memory to 1 KB of LDS in a row.
+__device__ __forceinline__ void bring(const half* from, half* to) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+// Rows r0 .. r0 + R - 1 (the last row again behind it) and kDepth columns of a matrix, a row of 128 bytes in LDS; its eight pieces of
+// 16 bytes are exchanged by the row's number, so that the lanes of a fragment, a row each, meet all banks.
+template <int R, int T>
+__device__ __forceinline__ void bring_rows(const half* from, uint32_t ld, uint32_t r0, uint32_t rows, uint32_t k0, half* to) {
+  const int tid = threadIdx.x, wave = tid / 64;
+#pragma unroll
+  for (int u = 0; u < R * 8 / T; ++u) {
+    const int piece = u * T + tid, r = piece / 8, c = (piece % 8) ^ (r & 7);
+    bring(from + (uint64_t)min(r0 + r, rows - 1) * ld + k0 + 8 * c, to + (u * T + wave * 64) * 8);
+  }
+}
+__device__ __forceinline__ h8 fragment(const half* tile, int r, int c) { return *reinterpret_cast<const h8*>(tile + r * kDepth + (c ^ (r & 7)) * 8); }
+// kDepth rows (the last again behind it) and C columns; the pieces of four neighbouring rows are moved 64 bytes apart.
+template <int C, int T>
+__device__ __forceinline__ void bring_columns(const half* from, uint32_t ld, uint32_t j0, uint32_t rows, uint32_t k0, half* to) {
+  const int tid = threadIdx.x, wave = tid / 64;
+  constexpr int P = C / 8;
+#pragma unroll
+  for (int u = 0; u < kDepth * P / T; ++u) {
+    const int piece = u * T + tid, k = piece / P, c = (piece % P) ^ ((k & 3) << 2 & (P - 1));
+    bring(from + (uint64_t)min(k0 + k, rows - 1) * ld + min(j0 + 8 * c, ld - 8), to + (u * T + wave * 64) * 8);
+  }
+}
+// Eight rows k .. k + 7 of a column for each lane: columns j .. j + 31, the upper half of the lanes eight rows further.  The
+// instruction turns a block of 4 rows x 16 columns for sixteen lanes: lane 4 r + q gives the address of row r's columns 4 q .., and gets
+// column 4 r + q.
+template <int C>
+__device__ __forceinline__ h8 turned_fragment(const half* tile, int k, int j, int lane) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  constexpr int P = C / 8;
+  h8 v;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int row = k + 8 * (lane / 32) + 4 * e + lane % 16 / 4, col = j + lane % 32 / 16 * 16 + 4 * (lane % 4);
+    const half* at = tile + row * C + ((col / 8) ^ ((row & 3) << 2 & (P - 1))) * 8 + col % 8;
+    const h4 w = __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)at));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[4 * e + q] = w[q];
+  }
+  return v;
+}
+
+// One tile of TM x TN of a product, WM x WN waves.
 //   kGram   A = X X^T      kPoly   B = b A + c A^2      (tiles on and above the diagonal; the others are their mirror images)
 //   kApply  X <- a X + B X      kLast   the same, into the parameters
-template <int KIND>
-__global__ __launch_bounds__(kThreads) void k_product(const Matrix* __restrict__ mats, const Tile* __restrict__ tiles, char* ws, int from,
-                                                      const train_control* __restrict__ ctl) {
-  __shared__ __attribute__((aligned(16))) half sa[kTile * kDepth];
-  __shared__ __attribute__((aligned(16))) half sb[kTile * kDepth];
+template <int KIND, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restrict__ mats, const Tile* __restrict__ tiles, char* ws, int from,
+                                                          const train_control* __restrict__ ctl) {
+  constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
+  constexpr bool kSquare = KIND == kGram || KIND == kPoly;
+  __shared__ __attribute__((aligned(16))) half a0[TM * kDepth], b0[TN * kDepth], a1[TM * kDepth], b1[TN * kDepth];
   if (ctl->nonfinite) return;
   const Tile t = tiles[blockIdx.x];
   const Matrix& x = mats[t.matrix];
@@ -211,100 +257,187 @@ __global__ __launch_bounds__(kThreads) void k_product(const Matrix* __restrict__
   const half* left = KIND == kGram ? X : KIND == kPoly ? A : reinterpret_cast<const half*>(ws + x.b);
   const half* right = KIND == kPoly ? A : X;
   const uint32_t ldl = KIND == kGram ? ldm : ldn, ldr = KIND == kPoly ? ldn : ldm, depth = KIND == kGram ? ldm : ldn;
-  const int tid = threadIdx.x, lane = tid % 64, wr = tid / 128, wc = tid / 64 % 2;
-  f16v acc[2][2] = {};
-  for (uint32_t k0 = 0; k0 < depth; k0 += kDepth) {
-    h8 va[4], vb[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const uint32_t r = tid / 8 + 32 * u, c = tid % 8;
-      va[u] = *reinterpret_cast<const h8*>(left + (uint64_t)min(t.i * kTile + r, n - 1) * ldl + k0 + 8 * c);
-      if constexpr (KIND == kGram || KIND == kPoly) {
-        vb[u] = *reinterpret_cast<const h8*>(right + (uint64_t)min(t.j * kTile + r, n - 1) * ldr + k0 + 8 * c);
-      } else {
-        const uint32_t k = tid / 16 + 16 * u, j = min(t.j * kTile + 8 * (tid % 16), ldm - 8);
-        vb[u] = *reinterpret_cast<const h8*>(right + (uint64_t)min(k0 + k, n - 1) * ldr + j);
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int r = tid / 8 + 32 * u, c = tid % 8;
-      *reinterpret_cast<h8*>(sa + r * kDepth + (c ^ (r & 7)) * 8) = va[u];
-      if constexpr (KIND == kGram || KIND == kPoly) {
-        *reinterpret_cast<h8*>(sb + r * kDepth + (c ^ (r & 7)) * 8) = vb[u];
-      } else {
-        const int k = tid / 16 + 16 * u;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = 8 * (tid % 16) + e;
-          sb[j * kDepth + ((k / 8) ^ (j & 7)) * 8 + k % 8] = vb[u][e];
-        }
-      }
-    }
-    __syncthreads();
+  const int tid = threadIdx.x, lane = tid % 64, wr = tid / 64 / WN, wc = tid / 64 % WN;
+  f16v acc[FM][FN] = {};
+  auto load = [&](uint32_t k0, half* sa, half* sb) {
+    bring_rows<TM, T>(left, ldl, t.i * TM, n, k0, sa);
+    if constexpr (kSquare) bring_rows<TN, T>(right, ldr, t.j * TN, n, k0, sb);
+    else bring_columns<TN, T>(right, ldr, t.j * TN, n, k0, sb);
+  };
+  auto multiply = [&](const half* __restrict__ sa, const half* __restrict__ sb) {
 #pragma unroll
     for (int kk = 0; kk < kDepth / 16; ++kk) {
-      h8 fa[2], fb[2];
+      h8 fa[FM], fb[FN];
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const int ra = wr * 64 + q * 32 + lane % 32, rb = wc * 64 + q * 32 + lane % 32, c = kk * 2 + lane / 32;
-        fa[q] = *reinterpret_cast<const h8*>(sa + ra * kDepth + (c ^ (ra & 7)) * 8);
-        fb[q] = *reinterpret_cast<const h8*>(sb + rb * kDepth + (c ^ (rb & 7)) * 8);
-      }
+      for (int q = 0; q < FM; ++q) fa[q] = fragment(sa, (wr * FM + q) * 32 + lane % 32, kk * 2 + lane / 32);
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+      for (int q = 0; q < FN; ++q)
+        fb[q] = kSquare ? fragment(sb, (wc * FN + q) * 32 + lane % 32, kk * 2 + lane / 32)
+                        : turned_fragment<TN>(sb, kk * 16, (wc * FN + q) * 32, lane);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[p], fb[q], acc[p][q], 0, 0, 0);
+      for (int p = 0; p < FM; ++p)
+#pragma unroll
+        for (int q = 0; q < FN; ++q) acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[p], fb[q], acc[p][q], 0, 0, 0);
     }
+  };
+  auto arrived = [] {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  load(0, a0, b0);
+  arrived();
+  uint32_t k0 = 0;
+  for (; k0 + kDepth < depth; k0 += 2 * kDepth) {
+    load(k0 + kDepth, a1, b1);
+    multiply(a0, b0);
+    arrived();
+    if (k0 + 2 * kDepth < depth) load(k0 + 2 * kDepth, a0, b0);
+    multiply(a1, b1);
+    arrived();
   }
+  if (k0 < depth) {
+    multiply(a0, b0);
+    __syncthreads();
+  }
+  // What each wave holds, blocks of 32 x 32 one after the other, goes through 4 KB of its own in LDS, so that memory sees
+  // eight elements a lane, four lanes a row.
+  static_assert(TM * kDepth * sizeof(half) >= WM * WN * 4096, "a block of each wave");
+  float* block = reinterpret_cast<float*>(a0) + tid / 64 * 1024;
+  auto place = [](int r, int c) { return r * 32 + (((c / 4) ^ (r & 7)) * 4) + c % 4; };
+  auto settle = [] {                   // this wave's LDS accesses, in order
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  };
   float* da = reinterpret_cast<float*>(ws + x.da);
   float* db = reinterpret_cast<float*>(ws + x.db);
   const float lr = KIND == kLast ? ctl->lr : 0.f;
 #pragma unroll
-  for (int p = 0; p < 2; ++p)
+  for (int p = 0; p < FM; ++p)
 #pragma unroll
-    for (int q = 0; q < 2; ++q)
+    for (int q = 0; q < FN; ++q) {
+      const uint32_t i0 = t.i * TM + (wr * FM + p) * 32, j0 = t.j * TN + (wc * FN + q) * 32;
+      if (i0 >= n || j0 >= (kSquare ? ldn : ldm)) continue;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        const uint32_t i = t.i * kTile + wr * 64 + p * 32 + 8 * (e / 4) + 4 * (lane / 32) + e % 4;
-        const uint32_t j = t.j * kTile + wc * 64 + q * 32 + lane % 32;
         const float v = acc[p][q][e];
-        if constexpr (KIND == kGram || KIND == kPoly) {
-          half* out = reinterpret_cast<half*>(ws + (KIND == kGram ? x.a : x.b));
-          float w = 0.f;
-          if (i < n && j < n) {
-            if constexpr (KIND == kGram) {
-              w = v * (1.f / kHeld);
-              if (i == j) da[i] = v * (1.f / (kHeld * kHeld));
-            } else {
-              const float held = (float)A[(uint64_t)i * ldn + j], di = da[i], dj = da[j];
-              w = held * (0.5f * (kB + kC * (di + dj))) + v * (0.5f * kC / kHeld);
-              if (i == j) db[i] = kA + di * (kB + kC * di) + kC * (v * (1.f / (kHeld * kHeld)));
+        block[place(8 * (e / 4) + 4 * (lane / 32) + e % 4, lane % 32)] = v;
+      }
+      settle();
+      // eight elements of the block, along a row or along a column
+      auto along_row = [&](int r, int c, float* v) {
+        *reinterpret_cast<f4*>(v) = *reinterpret_cast<const f4*>(block + place(r, c));
+        *reinterpret_cast<f4*>(v + 4) = *reinterpret_cast<const f4*>(block + place(r, c + 4));
+      };
+      auto along_column = [&](int r, int c, float* v) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = block[place(r + e, c)];
+      };
+      if constexpr (kSquare) {
+        half* out = reinterpret_cast<half*>(ws + (KIND == kGram ? x.a : x.b));
+        // out[i][j ..], from the sums v
+        auto write = [&](uint32_t i, uint32_t j, const float* v) {
+          if (i >= n || j >= ldn) return;
+          h8 w;
+          if constexpr (KIND == kGram) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (i == j + e) da[i] = v[e] * (1.f / (kHeld * kHeld));
+              w[e] = i == j + e || j + e >= n ? (half)0.f : (half)(v[e] * (1.f / kHeld));
             }
-            if (i == j) w = 0.f;
-          }
-          if (i < n && j < ldn) out[(uint64_t)i * ldn + j] = (half)w;
-          if (t.i != t.j && j < n && i < ldn) out[(uint64_t)j * ldn + i] = (half)w;
-        } else {
-          if (i >= n || j >= x.m) continue;
-          const uint64_t at = (uint64_t)i * ldm + j;
-          half* low = reinterpret_cast<half*>(ws + x.low);
-          const float w = db[i] * joined(X[at], low[at]) + v * (2.f / kHeld);
-          if constexpr (KIND == kApply) {
-            half u, l;
-            split(w, &u, &l);
-            reinterpret_cast<half*>(ws + x.x[1 - from])[at] = u;
-            low[at] = l;
           } else {
-            const uint64_t to = x.tall ? (uint64_t)j * x.cols + i : (uint64_t)i * x.cols + j;
-            float r = x.p[to];
-            r = r - r * (x.wd * lr) - w * (x.scale * lr / kHeld);
-            x.p[to] = r;
-            if (x.copy) x.copy[to] = f32_to_bf16(r);
+            const h8 held = *reinterpret_cast<const h8*>(A + (uint64_t)i * ldn + j);
+            const float di = da[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float dj = da[min(j + e, n - 1)];
+              if (i == j + e) db[i] = kA + di * (kB + kC * di) + kC * (v[e] * (1.f / (kHeld * kHeld)));
+              w[e] = i == j + e || j + e >= n ? (half)0.f : (half)((float)held[e] * (0.5f * (kB + kC * (di + dj))) + v[e] * (0.5f * kC / kHeld));
+            }
+          }
+          *reinterpret_cast<h8*>(out + (uint64_t)i * ldn + j) = w;
+        };
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+          const int r = h + lane / 4, c = lane % 4 * 8;
+          float v[8];
+          along_row(r, c, v);
+          write(i0 + r, j0 + c, v);
+          if (t.i != t.j) {
+            along_column(c, r, v);
+            write(j0 + r, i0 + c, v);
+          }
+        }
+      } else {
+        half* low = reinterpret_cast<half*>(ws + x.low);
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+          const int r = h + lane / 4, c = lane % 4 * 8;
+          const uint32_t i = i0 + r, j = j0 + c;
+          if (i < n && j < ldm) {
+            const uint64_t at = (uint64_t)i * ldm + j;
+            float v[8];
+            along_row(r, c, v);
+            const h8 hi = *reinterpret_cast<const h8*>(X + at), lo = *reinterpret_cast<const h8*>(low + at);
+            const float d = db[i];
+            h8 u, l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              v[e] = d * joined(hi[e], lo[e]) + v[e] * (2.f / kHeld);
+              if constexpr (KIND == kApply) {
+                half ue, le;
+                split(v[e], &ue, &le);
+                u[e] = ue, l[e] = le;
+              }
+            }
+            if constexpr (KIND == kApply) {
+              *reinterpret_cast<h8*>(reinterpret_cast<half*>(ws + x.x[1 - from]) + at) = u;
+              *reinterpret_cast<h8*>(low + at) = l;
+            } else {
+              *reinterpret_cast<f4*>(block + place(r, c)) = *reinterpret_cast<f4*>(v);
+              *reinterpret_cast<f4*>(block + place(r, c + 4)) = *reinterpret_cast<f4*>(v + 4);
+            }
+          }
+        }
+        if constexpr (KIND == kLast) {
+          settle();
+          const float keep = x.wd * lr, move = x.scale * lr / kHeld;
+#pragma unroll
+          for (int h = 0; h < 32; h += 16) {
+            float v[8];
+            uint32_t row, col;
+            if (x.tall) {
+              along_column(lane % 4 * 8, h + lane / 4, v);
+              row = j0 + h + lane / 4, col = i0 + lane % 4 * 8;
+            } else {
+              along_row(h + lane / 4, lane % 4 * 8, v);
+              row = i0 + h + lane / 4, col = j0 + lane % 4 * 8;
+            }
+            if (row >= x.rows) continue;
+            const uint64_t at = (uint64_t)row * x.cols + col;
+            auto updated = [&](float r, float o) { return r - r * keep - o * move; };
+            if (x.even && col + 8 <= x.cols) {
+#pragma unroll
+              for (int e = 0; e < 8; e += 4) {
+                f4 r = *reinterpret_cast<const f4*>(x.p + at + e);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = updated(r[k], v[e + k]);
+                *reinterpret_cast<f4*>(x.p + at + e) = r;
+                if (x.copy) *reinterpret_cast<us4*>(x.copy + at + e) = us4{f32_to_bf16(r[0]), f32_to_bf16(r[1]), f32_to_bf16(r[2]), f32_to_bf16(r[3])};
+              }
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (col + e < x.cols) {
+                  const float r = updated(x.p[at + e], v[e]);
+                  x.p[at + e] = r;
+                  if (x.copy) x.copy[at + e] = f32_to_bf16(r);
+                }
+            }
           }
         }
       }
+      settle();
+    }
 }
 
 __global__ void k_step_end(train_control* ctl) { end_step(ctl, ctl->nonfinite, ctl->step + 1); }
@@ -366,6 +499,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
         x.n = std::min(t.rows, t.cols), x.m = std::max(t.rows, t.cols);
         x.ldn = (uint32_t)up(x.n, kDepth), x.ldm = (uint32_t)up(x.m, kDepth);
         x.vec = !misaligned(x.g, 4 * ge) && x.pos % 4 == 0;
+        x.even = !misaligned(x.p, 16) && !misaligned(x.copy, 8) && x.cols % 4 == 0;
         x.wd = t.weight_decay, x.scale = t.scale;
         x.first = (uint32_t)chunk.size(), x.chunks = (uint32_t)((size + kChunk - 1) / kChunk);
         const uint64_t wide_bytes = (uint64_t)x.n * x.ldm * sizeof(half), square_bytes = (uint64_t)x.n * x.ldn * sizeof(half);
@@ -449,10 +583,10 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
   auto start = l->bf16 ? k_start<uint16_t> : k_start<float>;
   start<<<l->nturn, kThreads, 0, st>>>(l->matrices, l->turn, *o, momentum, control, inverse, w);
   for (int k = 0; k < o->steps; ++k) {
-    k_product<kGram><<<l->nsquare, kThreads, 0, st>>>(l->matrices, l->square, w, k % 2, control);
-    k_product<kPoly><<<l->nsquare, kThreads, 0, st>>>(l->matrices, l->square, w, k % 2, control);
-    if (k + 1 < o->steps) k_product<kApply><<<l->nwide, kThreads, 0, st>>>(l->matrices, l->wide, w, k % 2, control);
-    else k_product<kLast><<<l->nwide, kThreads, 0, st>>>(l->matrices, l->wide, w, k % 2, control);
+    k_product<kGram, 128, 128, 2, 2><<<l->nsquare, kThreads, 0, st>>>(l->matrices, l->square, w, k % 2, control);
+    k_product<kPoly, 128, 128, 2, 2><<<l->nsquare, kThreads, 0, st>>>(l->matrices, l->square, w, k % 2, control);
+    if (k + 1 < o->steps) k_product<kApply, 128, 128, 2, 2><<<l->nwide, kThreads, 0, st>>>(l->matrices, l->wide, w, k % 2, control);
+    else k_product<kLast, 128, 128, 2, 2><<<l->nwide, kThreads, 0, st>>>(l->matrices, l->wide, w, k % 2, control);
   }
   if (!o->keep) k_step_end<<<1, 1, 0, st>>>(control);
   return finish();
