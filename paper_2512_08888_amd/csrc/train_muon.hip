@@ -21,6 +21,7 @@
 #include <cmath>
 #include <cstdint>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "glue_elt.h"
@@ -32,9 +33,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kPad = 32;               // elements: a stack's momentum starts on a multiple
-constexpr int kTile = 128;             // of the products
+constexpr int kTile = 128;             // edge of the products' tiles
+constexpr int kSmall = 64;             // of A^2's, where tiles of 128 would leave CUs idle
 constexpr int kDepth = 64;             // elements that a step of a product adds up
-constexpr uint32_t kChunk = 4096;      // elements of the momentum's pass, to a workgroup
+constexpr uint32_t kSlots = 512;       // workgroups of the products that the chip holds at a time
 constexpr int kTurn = 64;              // edge of the tiles by which X is first written
 constexpr uint32_t kMostWorkgroups = (1u << 24) - 1;
 
@@ -44,8 +46,8 @@ struct Matrix {
   uint16_t* copy;
   uint64_t pos;                        // of the momentum
   uint32_t rows, cols, n, m;           // n = min, m = max
-  uint32_t ldn, ldm;                   // n, m up to a multiple of kDepth; what is between is 0
-  uint32_t tall, vec, even;            // vec: gradient and momentum can be read four elements at a time; even: the rows of p and copy
+  uint32_t ldn, ldm;                   // elements from row to row (leading()); what a product reads behind n and m is 0
+  uint32_t tall, vec, even;            // vec: gradient and momentum can be read four elements at a time; even: the rows of p and copy, eight
   float wd, scale;
   uint32_t first, chunks;              // in the momentum's pass
   // byte offsets in the workspace: X's upper parts before and after an iteration, its lower part, A, B; the diagonals
@@ -54,17 +56,29 @@ struct Matrix {
 struct Tile {
   uint32_t matrix, i, j;
 };
+// A tile, or steps k0 .. k1 - 1 of its product: their sums then go to a place of their own in the workspace.
+struct Unit {
+  uint32_t matrix, i, j, k0, k1, place;
+};
+constexpr uint32_t kWhole = ~0u;
+struct Join {                          // a tile whose sums lie in `count` places
+  uint32_t matrix, i, j, first, count;
+};
 
 }  // namespace
 
 struct train_matrices {
   int device = -1, bf16 = 0;
   uint64_t elements = 0;
-  size_t workspace = 0, inverse = 0, sums = 0;         // byte offsets: 1 / |u| of every matrix, the chunks' sums
+  size_t workspace = 0, sums = 0, parts = 0;           // byte offsets: the chunks' sums, the units'
+  uint32_t size = 0;                                   // elements of a chunk
+  int small = 0;                                       // A^2 by tiles of 64
   void* memory = nullptr;
   Matrix* matrices = nullptr;
-  Tile *chunk = nullptr, *turn = nullptr, *square = nullptr, *wide = nullptr;
-  uint32_t count = 0, nchunk = 0, nturn = 0, nsquare = 0, nwide = 0;
+  Tile *chunk = nullptr, *turn = nullptr;
+  Unit *gram = nullptr, *poly = nullptr, *apply = nullptr;
+  Join* join = nullptr;
+  uint32_t nchunk = 0, nturn = 0, ngram = 0, npoly = 0, napply = 0, njoin = 0;
 };
 
 namespace rotconv {
@@ -100,13 +114,14 @@ __device__ __forceinline__ float direction(float m, float g, float mu, int neste
 // momentum <- mu momentum + g, and the sum of u's squares of every chunk, in 64 bits
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_momentum(const Matrix* __restrict__ mats, const Tile* __restrict__ chunks, train_muon opt,
-                                                       float* __restrict__ momentum, const train_control* __restrict__ ctl, double* sums) {
+                                                       uint32_t chunk, float* __restrict__ momentum, const train_control* __restrict__ ctl,
+                                                       double* sums) {
   __shared__ double red[kThreads / 64];
   if (ctl->nonfinite) return;
   const Tile c = chunks[blockIdx.x];
-  const Matrix& x = mats[c.matrix];
-  const uint64_t from = (uint64_t)c.i * kChunk, size = (uint64_t)x.rows * x.cols;
-  const uint32_t n = (uint32_t)min((uint64_t)kChunk, size - from);
+  const Matrix x = mats[c.matrix];
+  const uint64_t from = (uint64_t)c.i * chunk, size = (uint64_t)x.rows * x.cols;
+  const uint32_t n = (uint32_t)min((uint64_t)chunk, size - from);
   const T* g = static_cast<const T*>(x.g) + from;
   float* m = momentum + x.pos + from;
   const float coef = factor(*ctl), mu = opt.momentum;
@@ -138,16 +153,6 @@ __global__ __launch_bounds__(kThreads) void k_momentum(const Matrix* __restrict_
   if (threadIdx.x == 0) sums[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
 
-// 1 / (|u| + eps) of every matrix, a wave each
-__global__ __launch_bounds__(64) void k_inverse_norm(const Matrix* __restrict__ mats, float eps, const double* __restrict__ sums,
-                                                     float* __restrict__ inverse) {
-  const Matrix& x = mats[blockIdx.x];
-  double s = 0;
-  for (uint32_t c = threadIdx.x; c < x.chunks; c += 64) s += sums[x.first + c];
-  s = lanes_sum(s);
-  if (threadIdx.x == 0) inverse[blockIdx.x] = (float)(1.0 / (sqrt(s) + (double)eps));
-}
-
 // v = X times 2^15, as two fp16 numbers
 __device__ __forceinline__ void split(float v, half* upper, half* lower) {
   const half u = (half)v;
@@ -160,62 +165,106 @@ __device__ __forceinline__ float joined(half upper, half lower) { return (float)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ mats, const Tile* __restrict__ tiles, train_muon opt,
                                                     const float* __restrict__ momentum, const train_control* __restrict__ ctl,
-                                                    const float* __restrict__ inverse, char* ws) {
+                                                    const double* __restrict__ sums, char* ws) {
   __shared__ float turned[kTurn][kTurn + 1];
+  __shared__ double red[kThreads / 64];
   if (ctl->nonfinite) return;
   const Tile t = tiles[blockIdx.x];
-  const Matrix& x = mats[t.matrix];
-  const float coef = factor(*ctl), mu = opt.momentum, scale = inverse[t.matrix] * kHeld;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const Matrix x = mats[t.matrix];
+  const int tid = threadIdx.x;
+  const float coef = factor(*ctl), mu = opt.momentum;
   const T* g = static_cast<const T*>(x.g);
   const float* m = momentum + x.pos;
-  for (int k = wave; k < kTurn; k += 4) {
-    const uint32_t r = t.i * kTurn + k, c = t.j * kTurn + lane;
-    float v = 0.f;
+  const bool pieces = x.vec && x.cols % 8 == 0;
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t r = t.i * kTurn + tid / 8 + 32 * h, c = t.j * kTurn + tid % 8 * 8;
+    const uint64_t at = (uint64_t)r * x.cols + c;
+    float gv[8] = {}, mv[8] = {};
     if (r < x.rows && c < x.cols) {
-      const uint64_t at = (uint64_t)r * x.cols + c;
-      v = direction(m[at], Elt<T>::ld(g + at) * coef, mu, opt.nesterov) * scale;
+      if (pieces) {
+        Elt<float>::ldv(m + at, mv), Elt<float>::ldv(m + at + 4, mv + 4);
+        Elt<T>::ldv(g + at, gv);
+        if constexpr (sizeof(T) == 4) Elt<T>::ldv(g + at + 4, gv + 4);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < x.cols) mv[e] = m[at + e], gv[e] = Elt<T>::ld(g + at + e);
+      }
     }
-    turned[k][lane] = v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[h][e] = direction(mv[e], gv[e] * coef, mu, opt.nesterov);
   }
+  // 1 / (|u| + eps), by every workgroup for itself while its loads are under way
+  double s = 0;
+  for (uint32_t c = tid; c < x.chunks; c += kThreads) s += sums[x.first + c];
+  s = lanes_sum(s);
+  if (tid % 64 == 0) red[tid / 64] = s;
   __syncthreads();
-  half *upper = reinterpret_cast<half*>(ws + x.x[0]), *lower = reinterpret_cast<half*>(ws + x.low);
+  const float scale = (float)(1.0 / (sqrt((red[0] + red[1]) + (red[2] + red[3])) + (double)opt.eps)) * kHeld;
+  if (x.tall) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) turned[tid / 8 + 32 * h][tid % 8 * 8 + e] = v[h][e];
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[h][e] = turned[tid % 8 * 8 + e][tid / 8 + 32 * h];
+  }
   const uint32_t ti = x.tall ? t.j : t.i, tj = x.tall ? t.i : t.j;
-  for (int k = wave; k < kTurn; k += 4) {
-    const uint32_t i = ti * kTurn + k, j = tj * kTurn + lane;
-    if (i >= x.n || j >= x.ldm) continue;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t i = ti * kTurn + tid / 8 + 32 * h, j = tj * kTurn + tid % 8 * 8;
+    if (i >= x.n) continue;
+    h8 u, l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      half ue, le;
+      split(v[h][e] * scale, &ue, &le);
+      u[e] = ue, l[e] = le;
+    }
     const uint64_t at = (uint64_t)i * x.ldm + j;
-    half u, l;
-    split(x.tall ? turned[lane][k] : turned[k][lane], &u, &l);
-    upper[at] = u, lower[at] = l;
+    *reinterpret_cast<h8*>(reinterpret_cast<half*>(ws + x.x[0]) + at) = u;
+    *reinterpret_cast<h8*>(reinterpret_cast<half*>(ws + x.low) + at) = l;
   }
 }
 
 enum Product { kGram, kPoly, kApply, kLast };
 
-// A wave's lanes bring 16 bytes each from memory to 1 KB of LDS in a row.
+// A wave's lanes bring 16 bytes each from memory to 1 KB of LDS in a row.  In assembler, without an output register, so that the
+// products alone say when it has to have arrived (step() below): the compiler would wait for all loads under way before reading
+// an LDS array that a loop fills.
 __device__ __forceinline__ void bring(const half* from, half* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+  const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
 }
 // Rows r0 .. r0 + R - 1 (the last row again behind it) and kDepth columns of a matrix, a row of 128 bytes in LDS; its eight pieces of
-// 16 bytes are exchanged by the row's number, so that the lanes of a fragment, a row each, meet all banks.
-template <int R, int T>
+// 16 bytes are exchanged by the row's number, two rows alike, so that sixteen lanes of a fragment, a row each, meet all 64 banks.
+template <int R, int D, int T>
 __device__ __forceinline__ void bring_rows(const half* from, uint32_t ld, uint32_t r0, uint32_t rows, uint32_t k0, half* to) {
   const int tid = threadIdx.x, wave = tid / 64;
+  constexpr int P = D / 8;
 #pragma unroll
-  for (int u = 0; u < R * 8 / T; ++u) {
-    const int piece = u * T + tid, r = piece / 8, c = (piece % 8) ^ (r & 7);
+  for (int u = 0; u < R * P / T; ++u) {
+    const int piece = u * T + tid, r = piece / P, c = (piece % P) ^ (r / (16 / P) & (P - 1));
     bring(from + (uint64_t)min(r0 + r, rows - 1) * ld + k0 + 8 * c, to + (u * T + wave * 64) * 8);
   }
 }
-__device__ __forceinline__ h8 fragment(const half* tile, int r, int c) { return *reinterpret_cast<const h8*>(tile + r * kDepth + (c ^ (r & 7)) * 8); }
+template <int D>
+__device__ __forceinline__ h8 fragment(const half* tile, int r, int c) {
+  constexpr int P = D / 8;
+  return *reinterpret_cast<const h8*>(tile + r * D + (c ^ (r / (16 / P) & (P - 1))) * 8);
+}
 // kDepth rows (the last again behind it) and C columns; the pieces of four neighbouring rows are moved 64 bytes apart.
-template <int C, int T>
+template <int C, int D, int T>
 __device__ __forceinline__ void bring_columns(const half* from, uint32_t ld, uint32_t j0, uint32_t rows, uint32_t k0, half* to) {
   const int tid = threadIdx.x, wave = tid / 64;
   constexpr int P = C / 8;
 #pragma unroll
-  for (int u = 0; u < kDepth * P / T; ++u) {
+  for (int u = 0; u < D * P / T; ++u) {
     const int piece = u * T + tid, k = piece / P, c = (piece % P) ^ ((k & 3) << 2 & (P - 1));
     bring(from + (uint64_t)min(k0 + k, rows - 1) * ld + min(j0 + 8 * c, ld - 8), to + (u * T + wave * 64) * 8);
   }
@@ -239,40 +288,243 @@ __device__ __forceinline__ h8 turned_fragment(const half* tile, int k, int j, in
   return v;
 }
 
-// One tile of TM x TN of a product, WM x WN waves.
+// What becomes of a tile's sums.
 //   kGram   A = X X^T      kPoly   B = b A + c A^2      (tiles on and above the diagonal; the others are their mirror images)
 //   kApply  X <- a X + B X      kLast   the same, into the parameters
+// A wave's blocks of up to 64 x 64 go one after the other through LDS of its own, so that memory sees eight elements a lane and whole
+// lines a row, and what they are joined with is loaded all at once before.
 template <int KIND, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restrict__ mats, const Tile* __restrict__ tiles, char* ws, int from,
-                                                          const train_control* __restrict__ ctl) {
+struct Finish {
+  static constexpr int kRows = TM / WM < 64 ? TM / WM : 64, kCols = TN / WN < 64 ? TN / WN : 64;       // of a block
+  static constexpr int kBytes = WM * WN * kRows * kCols * sizeof(float);
+  static constexpr bool kSquare = KIND == kGram || KIND == kPoly;
+  // eight elements a lane: along the rows kAcross lanes a row, along the columns kDown lanes a column
+  static constexpr int kAcross = kCols / 8, kDown = kRows / 8, kPass = kRows * kAcross / 64, kTurnPass = kCols * kDown / 64;
+
+  // pieces of four elements exchanged so that neither direction's lanes meet in a bank
+  static __device__ __forceinline__ int place(int r, int c) { return r * kCols + (((c / 4) ^ ((r ^ r / 8) & (kCols / 4 - 1))) * 4) + c % 4; }
+  static __device__ __forceinline__ void settle() {              // this wave's LDS accesses, in order
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+  static __device__ __forceinline__ void along_row(const float* block, int r, int c, float* v) {
+    *reinterpret_cast<f4*>(v) = *reinterpret_cast<const f4*>(block + place(r, c));
+    *reinterpret_cast<f4*>(v + 4) = *reinterpret_cast<const f4*>(block + place(r, c + 4));
+  }
+  static __device__ __forceinline__ void along_column(const float* block, int r, int c, float* v) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = block[place(r + e, c)];
+  }
+
+  // out[i][j .. j + 7] of a symmetric product, from its sums v; held: A's elements there, di, dj: its diagonal's.  The diagonal itself
+  // is left 0.
+  static __device__ __forceinline__ void symmetric(const Matrix& x, half* out, uint32_t i, uint32_t j, const float* v, const h8& held, float di,
+                                                   const float* dj) {
+    h8 w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float r;
+      if constexpr (KIND == kGram) r = v[e] * (1.f / kHeld);
+      else r = (float)held[e] * (0.5f * (kB + kC * (di + dj[e]))) + v[e] * (0.5f * kC / kHeld);
+      w[e] = i == j + e || j + e >= x.n ? (half)0.f : (half)r;
+    }
+    if (i < x.n && j < x.ldn) *reinterpret_cast<h8*>(out + (uint64_t)i * x.ldn + j) = w;
+  }
+
+  static __device__ __forceinline__ void tile(const Matrix& x, uint32_t ti, uint32_t tj, const f16v (&acc)[TM / WM / 32][TN / WN / 32], float* lds,
+                                              char* ws, int from, const train_control* ctl) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wr = wave / WN, wc = wave % WN;
+    const uint32_t n = x.n, ldn = x.ldn, ldm = x.ldm;
+    float* block = lds + wave * kRows * kCols;
+    const float lr = KIND == kLast ? ctl->lr : 0.f;
+#pragma unroll
+    for (int bp = 0; bp < TM / WM / kRows; ++bp)
+#pragma unroll
+      for (int bq = 0; bq < TN / WN / kCols; ++bq) {
+        const uint32_t i0 = ti * TM + wr * (TM / WM) + bp * kRows, j0 = tj * TN + wc * (TN / WN) + bq * kCols;
+        if (i0 >= n || j0 >= (kSquare ? ldn : ldm)) continue;
+        const int r0 = lane / kAcross, c0 = lane % kAcross * 8, rt = lane % kDown * 8, ct = lane / kDown;
+        auto hold = [&] {
+#pragma unroll
+          for (int p = 0; p < kRows / 32; ++p)
+#pragma unroll
+            for (int q = 0; q < kCols / 32; ++q)
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float v = acc[bp * (kRows / 32) + p][bq * (kCols / 32) + q][e];
+                block[place(p * 32 + 8 * (e / 4) + 4 * (lane / 32) + e % 4, q * 32 + lane % 32)] = v;
+              }
+          settle();
+        };
+        if constexpr (kSquare) {
+          const half* A = reinterpret_cast<const half*>(ws + x.a);
+          half* out = reinterpret_cast<half*>(ws + (KIND == kGram ? x.a : x.b));
+          float *da = reinterpret_cast<float*>(ws + x.da), *db = reinterpret_cast<float*>(ws + x.db);
+          const bool mirror = ti != tj;
+          // a lane's columns are the same in all passes, its rows are not
+          auto pass = [&](uint32_t i, uint32_t j, auto passes, int step, auto read) {
+            constexpr int P = decltype(passes)::value;
+            h8 held[P] = {};
+            float di[P] = {}, dj[8] = {};
+            if constexpr (KIND == kPoly) {
+              const uint32_t at = min(j, ldn - 8);
+#pragma unroll
+              for (int h = 0; h < P; ++h) {
+                const uint32_t row = min(i + h * step, n - 1);
+                held[h] = *reinterpret_cast<const h8*>(A + (uint64_t)row * ldn + at);
+                di[h] = da[row];
+              }
+              Elt<float>::ldv(da + at, dj), Elt<float>::ldv(da + at + 4, dj + 4);  // (ldn of them: what is behind the last is not used)
+            }
+#pragma unroll
+            for (int h = 0; h < P; ++h) {
+              float v[8];
+              read(h * step, v);
+              symmetric(x, out, i + h * step, j, v, held[h], di[h], dj);
+            }
+          };
+          hold();
+          if (i0 == j0 && lane < kRows && i0 + lane < n) {
+            const float v = block[place(lane, lane)] * (1.f / (kHeld * kHeld));
+            if constexpr (KIND == kGram) da[i0 + lane] = v;
+            else db[i0 + lane] = kA + da[i0 + lane] * (kB + kC * da[i0 + lane]) + kC * v;
+          }
+          pass(i0 + r0, j0 + c0, std::integral_constant<int, kPass>{}, 64 / kAcross, [&](int h, float* v) { along_row(block, r0 + h, c0, v); });
+          if (mirror)
+            pass(j0 + ct, i0 + rt, std::integral_constant<int, kTurnPass>{}, 64 / kDown, [&](int h, float* v) { along_column(block, rt, ct + h, v); });
+        } else {
+          const half* X = reinterpret_cast<const half*>(ws + (from ? x.x[1] : x.x[0]));
+          half* low = reinterpret_cast<half*>(ws + x.low);
+          const float* db = reinterpret_cast<const float*>(ws + x.db);
+          h8 hi[kPass], lo[kPass];
+          float d[kPass];
+#pragma unroll
+          for (int h = 0; h < kPass; ++h) {
+            const uint32_t i = min(i0 + r0 + h * (64 / kAcross), n - 1);
+            const uint64_t at = (uint64_t)i * ldm + min(j0 + c0, ldm - 8);
+            hi[h] = *reinterpret_cast<const h8*>(X + at), lo[h] = *reinterpret_cast<const h8*>(low + at);
+            d[h] = db[i];
+          }
+          hold();
+#pragma unroll
+          for (int h = 0; h < kPass; ++h) {
+            const int r = r0 + h * (64 / kAcross);
+            const uint32_t i = i0 + r, j = j0 + c0;
+            float v[8];
+            along_row(block, r, c0, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = d[h] * joined(hi[h][e], lo[h][e]) + v[e] * (2.f / kHeld);
+            if constexpr (KIND == kApply) {
+              h8 u, l;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                half ue, le;
+                split(v[e], &ue, &le);
+                u[e] = ue, l[e] = le;
+              }
+              if (i < n && j < ldm) {
+                const uint64_t at = (uint64_t)i * ldm + j;
+                *reinterpret_cast<h8*>(reinterpret_cast<half*>(ws + (from ? x.x[0] : x.x[1])) + at) = u;
+                *reinterpret_cast<h8*>(low + at) = l;
+              }
+            } else {
+              *reinterpret_cast<f4*>(block + place(r, c0)) = f4{v[0], v[1], v[2], v[3]};
+              *reinterpret_cast<f4*>(block + place(r, c0 + 4)) = f4{v[4], v[5], v[6], v[7]};
+            }
+          }
+          if constexpr (KIND == kLast) {
+            settle();
+            if (x.tall) update<kTurnPass, true>(x, block, j0 + ct, i0 + rt, rt, ct, lr);
+            else update<kPass, false>(x, block, i0 + r0, j0 + c0, r0, c0, lr);
+          }
+        }
+        settle();
+      }
+  }
+  // the parameters from a block of X, by rows of the matrix as it lies in memory (TALL: the block's columns)
+  template <int PASSES, bool TALL>
+  static __device__ __forceinline__ void update(const Matrix& x, const float* block, uint32_t row0, uint32_t col, int r0, int c0, float lr) {
+    constexpr int kStep = 64 / (TALL ? kDown : kAcross);
+    const float keep = x.wd * lr, move = x.scale * lr / kHeld;
+    auto updated = [&](float r, float o) { return r - r * keep - o * move; };
+    auto read = [&](int h, float* v) {
+      if constexpr (TALL) along_column(block, r0, c0 + h * kStep, v);
+      else along_row(block, r0 + h * kStep, c0, v);
+    };
+    if (x.even) {
+      if (col >= x.cols) return;
+      f4 old[PASSES][2];
+#pragma unroll
+      for (int h = 0; h < PASSES; ++h)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) old[h][e] = *reinterpret_cast<const f4*>(x.p + (uint64_t)min(row0 + h * kStep, x.rows - 1) * x.cols + col + 4 * e);
+#pragma unroll
+      for (int h = 0; h < PASSES; ++h) {
+        float v[8];
+        read(h, v);
+        if (row0 + h * kStep >= x.rows) continue;
+        const uint64_t at = (uint64_t)(row0 + h * kStep) * x.cols + col;
+        float r[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = updated(old[h][e / 4][e % 4], v[e]);
+        *reinterpret_cast<f4*>(x.p + at) = f4{r[0], r[1], r[2], r[3]};
+        *reinterpret_cast<f4*>(x.p + at + 4) = f4{r[4], r[5], r[6], r[7]};
+        if (x.copy) Elt<uint16_t>::stv(x.copy + at, r);
+      }
+      return;
+    }
+#pragma unroll 1
+    for (int h = 0; h < PASSES; ++h) {
+      float v[8];
+      read(h, v);
+      if (row0 + h * kStep >= x.rows) continue;
+      const uint64_t at = (uint64_t)(row0 + h * kStep) * x.cols + col;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < x.cols) {
+          const float r = updated(x.p[at + e], v[e]);
+          x.p[at + e] = r;
+          if (x.copy) x.copy[at + e] = f32_to_bf16(r);
+        }
+    }
+  }
+};
+
+// One tile of TM x TN of a product, or some of its steps, WM x WN waves.
+template <int KIND, int TM, int TN, int WM, int WN, int D, int NS>
+__global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restrict__ mats, const Unit* __restrict__ units, char* ws, int from,
+                                                          f4* parts, const train_control* __restrict__ ctl) {
   constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr bool kSquare = KIND == kGram || KIND == kPoly;
-  __shared__ __attribute__((aligned(16))) half a0[TM * kDepth], b0[TN * kDepth], a1[TM * kDepth], b1[TN * kDepth];
+  __shared__ __attribute__((aligned(16))) half stages[NS][(TM + TN) * D];
   if (ctl->nonfinite) return;
-  const Tile t = tiles[blockIdx.x];
-  const Matrix& x = mats[t.matrix];
+  const Unit t = units[blockIdx.x];
+  if (t.k0 == t.k1) return;
+  const Matrix x = mats[t.matrix];
   const uint32_t n = x.n, ldn = x.ldn, ldm = x.ldm;
-  const half* X = reinterpret_cast<const half*>(ws + x.x[from]);
+  const half* X = reinterpret_cast<const half*>(ws + (from ? x.x[1] : x.x[0]));
   const half* A = reinterpret_cast<const half*>(ws + x.a);
   const half* left = KIND == kGram ? X : KIND == kPoly ? A : reinterpret_cast<const half*>(ws + x.b);
   const half* right = KIND == kPoly ? A : X;
-  const uint32_t ldl = KIND == kGram ? ldm : ldn, ldr = KIND == kPoly ? ldn : ldm, depth = KIND == kGram ? ldm : ldn;
+  const uint32_t ldl = KIND == kGram ? ldm : ldn, ldr = KIND == kPoly ? ldn : ldm;
   const int tid = threadIdx.x, lane = tid % 64, wr = tid / 64 / WN, wc = tid / 64 % WN;
   f16v acc[FM][FN] = {};
-  auto load = [&](uint32_t k0, half* sa, half* sb) {
-    bring_rows<TM, T>(left, ldl, t.i * TM, n, k0, sa);
-    if constexpr (kSquare) bring_rows<TN, T>(right, ldr, t.j * TN, n, k0, sb);
-    else bring_columns<TN, T>(right, ldr, t.j * TN, n, k0, sb);
+  auto load = [&](uint32_t k0, half* sa) {
+    half* sb = sa + TM * D;
+    bring_rows<TM, D, T>(left, ldl, t.i * TM, n, k0, sa);
+    if constexpr (kSquare) bring_rows<TN, D, T>(right, ldr, t.j * TN, n, k0, sb);
+    else bring_columns<TN, D, T>(right, ldr, t.j * TN, n, k0, sb);
   };
-  auto multiply = [&](const half* __restrict__ sa, const half* __restrict__ sb) {
+  auto multiply = [&](const half* sa) {
+    const half* sb = sa + TM * D;
 #pragma unroll
-    for (int kk = 0; kk < kDepth / 16; ++kk) {
+    for (int kk = 0; kk < D / 16; ++kk) {
       h8 fa[FM], fb[FN];
 #pragma unroll
-      for (int q = 0; q < FM; ++q) fa[q] = fragment(sa, (wr * FM + q) * 32 + lane % 32, kk * 2 + lane / 32);
+      for (int q = 0; q < FM; ++q) fa[q] = fragment<D>(sa, (wr * FM + q) * 32 + lane % 32, kk * 2 + lane / 32);
 #pragma unroll
       for (int q = 0; q < FN; ++q)
-        fb[q] = kSquare ? fragment(sb, (wc * FN + q) * 32 + lane % 32, kk * 2 + lane / 32)
+        fb[q] = kSquare ? fragment<D>(sb, (wc * FN + q) * 32 + lane % 32, kk * 2 + lane / 32)
                         : turned_fragment<TN>(sb, kk * 16, (wc * FN + q) * 32, lane);
 #pragma unroll
       for (int p = 0; p < FM; ++p)
@@ -280,171 +532,99 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restri
         for (int q = 0; q < FN; ++q) acc[p][q] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[p], fb[q], acc[p][q], 0, 0, 0);
     }
   };
-  auto arrived = [] {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-  };
-  load(0, a0, b0);
-  arrived();
-  uint32_t k0 = 0;
-  for (; k0 + kDepth < depth; k0 += 2 * kDepth) {
-    load(k0 + kDepth, a1, b1);
-    multiply(a0, b0);
-    arrived();
-    if (k0 + 2 * kDepth < depth) load(k0 + 2 * kDepth, a0, b0);
-    multiply(a1, b1);
-    arrived();
+  // Before step k, what it needs has arrived (later steps' loads stay on their way) and everybody is done with step k - 1, whose
+  // place step k + NS - 1 takes.  The last steps load the last columns again, into places that nobody reads any more.
+  constexpr int kLoads = (TM + TN) * (D / 8) / T;
+  const uint32_t last = t.k1 - 1;
+#pragma unroll
+  for (int u = 0; u < NS - 1; ++u) load(min(t.k0 + u, last) * D, stages[u]);
+  uint32_t here = 0, next = NS - 1;
+  for (uint32_t k = t.k0; k <= last; ++k) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((NS - 2) * kLoads) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    load(min(k + NS - 1, last) * D, stages[next]);
+    multiply(stages[here]);
+    here = here + 1 == NS ? 0 : here + 1;
+    next = next + 1 == NS ? 0 : next + 1;
   }
-  if (k0 < depth) {
-    multiply(a0, b0);
-    __syncthreads();
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (t.place != kWhole) {             // as the lanes hold them
+    f4* to = parts + (uint64_t)t.place * (TM * TN / 4) + tid;
+#pragma unroll
+    for (int p = 0; p < FM; ++p)
+#pragma unroll
+      for (int q = 0; q < FN; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          to[((p * FN + q) * 4 + e) * T] = f4{acc[p][q][4 * e], acc[p][q][4 * e + 1], acc[p][q][4 * e + 2], acc[p][q][4 * e + 3]};
+    return;
   }
-  // What each wave holds, blocks of 32 x 32 one after the other, goes through 4 KB of its own in LDS, so that memory sees
-  // eight elements a lane, four lanes a row.
-  static_assert(TM * kDepth * sizeof(half) >= WM * WN * 4096, "a block of each wave");
-  float* block = reinterpret_cast<float*>(a0) + tid / 64 * 1024;
-  auto place = [](int r, int c) { return r * 32 + (((c / 4) ^ (r & 7)) * 4) + c % 4; };
-  auto settle = [] {                   // this wave's LDS accesses, in order
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-  };
-  float* da = reinterpret_cast<float*>(ws + x.da);
-  float* db = reinterpret_cast<float*>(ws + x.db);
-  const float lr = KIND == kLast ? ctl->lr : 0.f;
+  using F = Finish<KIND, TM, TN, WM, WN>;
+  static_assert(sizeof(stages) >= F::kBytes, "a block of each wave");
+  F::tile(x, t.i, t.j, acc, reinterpret_cast<float*>(stages), ws, from, ctl);
+}
+
+// The tiles whose sums units have left in places of their own: added in the places' order, and finished.
+template <int KIND, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_join(const Matrix* __restrict__ mats, const Join* __restrict__ joins, char* ws, const f4* __restrict__ parts,
+                                                       const train_control* __restrict__ ctl) {
+  constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
+  using F = Finish<KIND, TM, TN, WM, WN>;
+  __shared__ __attribute__((aligned(16))) float blocks[F::kBytes / sizeof(float)];
+  if (ctl->nonfinite) return;
+  const Join t = joins[blockIdx.x];
+  const Matrix x = mats[t.matrix];
+  f16v acc[FM][FN] = {};
+  for (uint32_t c = 0; c < t.count; ++c) {
+    const f4* from = parts + (uint64_t)(t.first + c) * (TM * TN / 4) + threadIdx.x;
 #pragma unroll
-  for (int p = 0; p < FM; ++p)
+    for (int p = 0; p < FM; ++p)
 #pragma unroll
-    for (int q = 0; q < FN; ++q) {
-      const uint32_t i0 = t.i * TM + (wr * FM + p) * 32, j0 = t.j * TN + (wc * FN + q) * 32;
-      if (i0 >= n || j0 >= (kSquare ? ldn : ldm)) continue;
+      for (int q = 0; q < FN; ++q)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float v = acc[p][q][e];
-        block[place(8 * (e / 4) + 4 * (lane / 32) + e % 4, lane % 32)] = v;
-      }
-      settle();
-      // eight elements of the block, along a row or along a column
-      auto along_row = [&](int r, int c, float* v) {
-        *reinterpret_cast<f4*>(v) = *reinterpret_cast<const f4*>(block + place(r, c));
-        *reinterpret_cast<f4*>(v + 4) = *reinterpret_cast<const f4*>(block + place(r, c + 4));
-      };
-      auto along_column = [&](int r, int c, float* v) {
+        for (int e = 0; e < 4; ++e) {
+          const f4 v = from[((p * FN + q) * 4 + e) * T];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = block[place(r + e, c)];
-      };
-      if constexpr (kSquare) {
-        half* out = reinterpret_cast<half*>(ws + (KIND == kGram ? x.a : x.b));
-        // out[i][j ..], from the sums v
-        auto write = [&](uint32_t i, uint32_t j, const float* v) {
-          if (i >= n || j >= ldn) return;
-          h8 w;
-          if constexpr (KIND == kGram) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (i == j + e) da[i] = v[e] * (1.f / (kHeld * kHeld));
-              w[e] = i == j + e || j + e >= n ? (half)0.f : (half)(v[e] * (1.f / kHeld));
-            }
-          } else {
-            const h8 held = *reinterpret_cast<const h8*>(A + (uint64_t)i * ldn + j);
-            const float di = da[i];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float dj = da[min(j + e, n - 1)];
-              if (i == j + e) db[i] = kA + di * (kB + kC * di) + kC * (v[e] * (1.f / (kHeld * kHeld)));
-              w[e] = i == j + e || j + e >= n ? (half)0.f : (half)((float)held[e] * (0.5f * (kB + kC * (di + dj))) + v[e] * (0.5f * kC / kHeld));
-            }
-          }
-          *reinterpret_cast<h8*>(out + (uint64_t)i * ldn + j) = w;
-        };
-#pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-          const int r = h + lane / 4, c = lane % 4 * 8;
-          float v[8];
-          along_row(r, c, v);
-          write(i0 + r, j0 + c, v);
-          if (t.i != t.j) {
-            along_column(c, r, v);
-            write(j0 + r, i0 + c, v);
-          }
+          for (int k = 0; k < 4; ++k) acc[p][q][4 * e + k] += v[k];
         }
-      } else {
-        half* low = reinterpret_cast<half*>(ws + x.low);
-#pragma unroll
-        for (int h = 0; h < 32; h += 16) {
-          const int r = h + lane / 4, c = lane % 4 * 8;
-          const uint32_t i = i0 + r, j = j0 + c;
-          if (i < n && j < ldm) {
-            const uint64_t at = (uint64_t)i * ldm + j;
-            float v[8];
-            along_row(r, c, v);
-            const h8 hi = *reinterpret_cast<const h8*>(X + at), lo = *reinterpret_cast<const h8*>(low + at);
-            const float d = db[i];
-            h8 u, l;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              v[e] = d * joined(hi[e], lo[e]) + v[e] * (2.f / kHeld);
-              if constexpr (KIND == kApply) {
-                half ue, le;
-                split(v[e], &ue, &le);
-                u[e] = ue, l[e] = le;
-              }
-            }
-            if constexpr (KIND == kApply) {
-              *reinterpret_cast<h8*>(reinterpret_cast<half*>(ws + x.x[1 - from]) + at) = u;
-              *reinterpret_cast<h8*>(low + at) = l;
-            } else {
-              *reinterpret_cast<f4*>(block + place(r, c)) = *reinterpret_cast<f4*>(v);
-              *reinterpret_cast<f4*>(block + place(r, c + 4)) = *reinterpret_cast<f4*>(v + 4);
-            }
-          }
-        }
-        if constexpr (KIND == kLast) {
-          settle();
-          const float keep = x.wd * lr, move = x.scale * lr / kHeld;
-#pragma unroll
-          for (int h = 0; h < 32; h += 16) {
-            float v[8];
-            uint32_t row, col;
-            if (x.tall) {
-              along_column(lane % 4 * 8, h + lane / 4, v);
-              row = j0 + h + lane / 4, col = i0 + lane % 4 * 8;
-            } else {
-              along_row(h + lane / 4, lane % 4 * 8, v);
-              row = i0 + h + lane / 4, col = j0 + lane % 4 * 8;
-            }
-            if (row >= x.rows) continue;
-            const uint64_t at = (uint64_t)row * x.cols + col;
-            auto updated = [&](float r, float o) { return r - r * keep - o * move; };
-            if (x.even && col + 8 <= x.cols) {
-#pragma unroll
-              for (int e = 0; e < 8; e += 4) {
-                f4 r = *reinterpret_cast<const f4*>(x.p + at + e);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) r[k] = updated(r[k], v[e + k]);
-                *reinterpret_cast<f4*>(x.p + at + e) = r;
-                if (x.copy) *reinterpret_cast<us4*>(x.copy + at + e) = us4{f32_to_bf16(r[0]), f32_to_bf16(r[1]), f32_to_bf16(r[2]), f32_to_bf16(r[3])};
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (col + e < x.cols) {
-                  const float r = updated(x.p[at + e], v[e]);
-                  x.p[at + e] = r;
-                  if (x.copy) x.copy[at + e] = f32_to_bf16(r);
-                }
-            }
-          }
-        }
-      }
-      settle();
-    }
+  }
+  F::tile(x, t.i, t.j, acc, blocks, ws, 0, ctl);
 }
 
 __global__ void k_step_end(train_control* ctl) { end_step(ctl, ctl->nonfinite, ctl->step + 1); }
 
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+// Workgroups go to the eight dies in turn, and each die has a cache of its own.  So the units, listed in an order in which neighbours share
+// operands, are cut into eight runs of like work; a die's deepest units come first, so that none starts when the others end, and where a run
+// is shorter than another, units without steps stand in.  (Matrices of 2048 x 2048 and 2048 x 5632, A: 590 MB through the caches where every
+// die works on every matrix.)
+std::vector<Unit> by_die(const std::vector<Unit>& in) {
+  constexpr uint64_t kDies = 8, kEnds = 8;             // kEnds: what a unit takes beside its steps, in steps
+  uint64_t work = 0, done = 0;
+  for (const Unit& u : in) work += u.k1 - u.k0 + kEnds;
+  std::vector<Unit> runs[kDies];
+  for (const Unit& u : in) {
+    runs[std::min(kDies - 1, done * kDies / work)].push_back(u);
+    done += u.k1 - u.k0 + kEnds;
+  }
+  size_t most = 0;
+  for (auto& r : runs) {
+    std::stable_sort(r.begin(), r.end(), [](const Unit& p, const Unit& q) { return p.k1 - p.k0 > q.k1 - q.k0; });
+    most = std::max(most, r.size());
+  }
+  std::vector<Unit> out;
+  out.reserve(most * kDies);
+  for (size_t k = 0; k < most; ++k)
+    for (auto& r : runs) out.push_back(k < r.size() ? r[k] : Unit{});
+  return out;
+}
 uint64_t up(uint64_t n, uint64_t to) { return (n + to - 1) / to * to; }
+// Elements from row to row: an odd number of lines of 128 bytes, so that the rows of a tile lie in different channels of the caches.
+// (Rows of 2048 elements without that: XXX)
+uint32_t leading(uint32_t n) { return (uint32_t)((up(n, kDepth) / kDepth | 1) * kDepth); }
 
 }  // namespace
 }  // namespace rotconv
@@ -458,7 +638,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
   if (count < 1) return ROTCONV_ERR_SHAPE;
   if (grad_dtype != ROTCONV_F32 && grad_dtype != ROTCONV_BF16) return ROTCONV_ERR_UNSUPPORTED;
   const uintptr_t ge = grad_dtype == ROTCONV_BF16 ? 2 : 4;
-  uint64_t nchunk = 0, nturn = 0, nsquare = 0, nwide = 0, all = 0;
+  uint64_t total = 0, nturn = 0, nsquare = 0, nsmall = 0, nwide = 0, all = 0, depth = 0;
   for (int k = 0; k < count; ++k) {
     const train_matrix& t = matrices[k];
     if (!t.param || !t.grad) return ROTCONV_ERR_NULL;
@@ -468,19 +648,27 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     if (!(t.weight_decay >= 0.f && t.weight_decay <= FLT_MAX) || !(std::fabs(t.scale) <= FLT_MAX) || t.reserved != 0 || misaligned(t.param, 4) ||
         misaligned(t.grad, ge) || misaligned(t.copy, 2))
       return ROTCONV_ERR_UNSUPPORTED;
-    const uint64_t tn = (n + kTile - 1) / kTile, tm = (m + kTile - 1) / kTile;
-    nchunk += c * ((n * m + kChunk - 1) / kChunk), nturn += c * (up(n, kTurn) / kTurn) * (up(m, kTurn) / kTurn);
-    nsquare += c * tn * (tn + 1) / 2, nwide += c * tn * tm, all += c;
-    if (all > 65535 || std::max(std::max(nchunk, nturn), std::max(nsquare, nwide)) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
+    const uint64_t tn = (n + kTile - 1) / kTile, tm = (m + kTile - 1) / kTile, ts = (n + kSmall - 1) / kSmall;
+    nturn += c * (up(n, kTurn) / kTurn) * (up(m, kTurn) / kTurn);
+    nsquare += c * tn * (tn + 1) / 2, nsmall += c * ts * (ts + 1) / 2, nwide += c * tn * tm;
+    depth += c * tn * (tn + 1) / 2 * (up(m, kDepth) / kDepth);
+    all += c, total += c * n * m;
+    if (all > 65535 || std::max(std::max(nturn, nsmall), nwide) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
   }
+  // The momentum's chunks: from 1024 elements (fewer leave lanes idle) to 16384 where there are many.
+  uint32_t size = 1024;
+  while (size < 16384 && total / size > 2048) size *= 2;
+  // Steps of a unit of A: so that all units together fill the chip evenly, but no fewer than pay for the sums' way through memory.
+  const uint64_t most = std::max<uint64_t>(8, (depth + kSlots - 1) / kSlots);
+  const bool small = nsquare < kSlots;
   train_matrices* l = nullptr;
   try {
     std::vector<Matrix> mats;
-    std::vector<Tile> chunk, turn, square, wide;
-    mats.reserve(all), chunk.reserve(nchunk), turn.reserve(nturn), square.reserve(nsquare), wide.reserve(nwide);
-    uint64_t base = 0, at = up(all * sizeof(float), 256);
-    const uint64_t sums = at;
-    at = up(at + nchunk * sizeof(double), 256);
+    std::vector<Tile> chunk, turn;
+    std::vector<Unit> gram, poly, apply;
+    std::vector<Join> join;
+    mats.reserve(all), turn.reserve(nturn), apply.reserve(nwide);
+    uint64_t base = 0, at = 0;
     auto room = [&](uint64_t bytes) {
       const uint64_t here = at;
       at = up(at + bytes, 256);
@@ -488,58 +676,87 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     };
     for (int k = 0; k < count; ++k) {
       const train_matrix& t = matrices[k];
-      const uint64_t size = (uint64_t)t.rows * t.cols;
+      const uint64_t each = (uint64_t)t.rows * t.cols;
       for (int i = 0; i < t.count; ++i) {
         Matrix x = {};
-        x.p = t.param + i * size;
-        x.g = static_cast<const char*>(t.grad) + i * size * ge;
-        x.copy = t.copy ? t.copy + i * size : nullptr;
-        x.pos = base + i * size;
+        x.p = t.param + i * each;
+        x.g = static_cast<const char*>(t.grad) + i * each * ge;
+        x.copy = t.copy ? t.copy + i * each : nullptr;
+        x.pos = base + i * each;
         x.rows = t.rows, x.cols = t.cols, x.tall = t.rows > t.cols;
         x.n = std::min(t.rows, t.cols), x.m = std::max(t.rows, t.cols);
-        x.ldn = (uint32_t)up(x.n, kDepth), x.ldm = (uint32_t)up(x.m, kDepth);
+        x.ldn = leading(x.n), x.ldm = leading(x.m);
         x.vec = !misaligned(x.g, 4 * ge) && x.pos % 4 == 0;
-        x.even = !misaligned(x.p, 16) && !misaligned(x.copy, 8) && x.cols % 4 == 0;
+        x.even = !misaligned(x.p, 16) && !misaligned(x.copy, 16) && x.cols % 8 == 0;
         x.wd = t.weight_decay, x.scale = t.scale;
-        x.first = (uint32_t)chunk.size(), x.chunks = (uint32_t)((size + kChunk - 1) / kChunk);
+        x.first = (uint32_t)chunk.size(), x.chunks = (uint32_t)((each + size - 1) / size);
         const uint64_t wide_bytes = (uint64_t)x.n * x.ldm * sizeof(half), square_bytes = (uint64_t)x.n * x.ldn * sizeof(half);
         x.x[0] = room(wide_bytes), x.x[1] = room(wide_bytes), x.low = room(wide_bytes);
         x.a = room(square_bytes), x.b = room(square_bytes);
-        x.da = room(x.n * sizeof(float)), x.db = room(x.n * sizeof(float));
+        x.da = room(x.ldn * sizeof(float)), x.db = room(x.ldn * sizeof(float));
         const uint32_t id = (uint32_t)mats.size();
         for (uint32_t c = 0; c < x.chunks; ++c) chunk.push_back(Tile{id, c, 0});
         for (uint32_t r = 0; r * kTurn < x.rows; ++r)
           for (uint32_t c = 0; c * kTurn < x.cols; ++c) turn.push_back(Tile{id, r, c});
-        for (uint32_t r = 0; r * kTile < x.n; ++r) {
-          for (uint32_t c = r; c * kTile < x.n; ++c) square.push_back(Tile{id, r, c});
-          for (uint32_t c = 0; c * kTile < x.m; ++c) wide.push_back(Tile{id, r, c});
-        }
         mats.push_back(x);
       }
-      base += up(size * t.count, kPad);
+      base += up(each * t.count, kPad);
     }
+    // Units of the products, neighbours with operands in common; the parts of A's tiles by their columns of X.
+    std::vector<uint32_t> order(mats.size());
+    for (uint32_t k = 0; k < order.size(); ++k) order[k] = k;
+    std::stable_sort(order.begin(), order.end(), [&](uint32_t p, uint32_t q) { return mats[p].n > mats[q].n; });
+    uint32_t places = 0;
+    for (uint32_t id : order) {
+      const Matrix& x = mats[id];
+      const uint32_t tiles = (x.n + kTile - 1) / kTile, deep = (uint32_t)(up(x.m, kDepth) / kDepth), parts = (uint32_t)((deep + most - 1) / most);
+      const uint32_t first = places;
+      for (uint32_t q = 0; q < parts; ++q) {
+        uint32_t tile = 0;
+        for (uint32_t r = 0; r < tiles; ++r)
+          for (uint32_t c = r; c < tiles; ++c, ++tile)
+            gram.push_back(Unit{id, r, c, (uint32_t)((uint64_t)deep * q / parts), (uint32_t)((uint64_t)deep * (q + 1) / parts),
+                                parts > 1 ? first + tile * parts + q : kWhole});
+      }
+      if (parts > 1) {
+        for (uint32_t r = 0; r < tiles; ++r)
+          for (uint32_t c = r; c < tiles; ++c, places += parts) join.push_back(Join{id, r, c, places, parts});
+      }
+      const uint32_t steps = (uint32_t)(up(x.n, kDepth) / kDepth), edge = small ? kSmall : kTile;
+      for (uint32_t r = 0; r * edge < x.n; ++r)
+        for (uint32_t c = r; c * edge < x.n; ++c) poly.push_back(Unit{id, r, c, 0, steps, kWhole});
+      for (uint32_t c = 0; c * kTile < x.m; ++c)
+        for (uint32_t r = 0; r < tiles; ++r) apply.push_back(Unit{id, r, c, 0, steps, kWhole});
+    }
+    gram = by_die(gram), poly = by_die(poly), apply = by_die(apply);
+    if (std::max(std::max(gram.size(), poly.size()), std::max(apply.size(), chunk.size())) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
+    const uint64_t sums = room(chunk.size() * sizeof(double)), part_bytes = room((uint64_t)places * kTile * kTile * sizeof(float));
     l = new train_matrices;
     l->bf16 = grad_dtype == ROTCONV_BF16;
     l->elements = base;
-    l->sums = sums, l->workspace = at;
-    l->count = (uint32_t)mats.size(), l->nchunk = (uint32_t)chunk.size(), l->nturn = (uint32_t)turn.size();
-    l->nsquare = (uint32_t)square.size(), l->nwide = (uint32_t)wide.size();
-    const size_t tiles = (size_t)l->nchunk + l->nturn + l->nsquare + l->nwide;
+    l->sums = sums, l->parts = part_bytes, l->workspace = at;
+    l->size = size, l->small = small;
+    l->nchunk = (uint32_t)chunk.size(), l->nturn = (uint32_t)turn.size(), l->ngram = (uint32_t)gram.size();
+    l->npoly = (uint32_t)poly.size(), l->napply = (uint32_t)apply.size(), l->njoin = (uint32_t)join.size();
+    const size_t tables = mats.size() * sizeof(Matrix) + (chunk.size() + turn.size()) * sizeof(Tile) +
+                          (gram.size() + poly.size() + apply.size()) * sizeof(Unit) + join.size() * sizeof(Join);
     bool ok = hipGetDevice(&l->device) == hipSuccess &&
-              hipMalloc(&l->memory, mats.size() * sizeof(Matrix) + tiles * sizeof(Tile)) == hipSuccess;
+              hipMalloc(&l->memory, tables) == hipSuccess;
     if (ok) {
       char* p = static_cast<char*>(l->memory);
       auto put = [&](const void* from, size_t bytes) {
         void* to = p;
-        ok = ok && hipMemcpy(to, from, bytes, hipMemcpyHostToDevice) == hipSuccess;
+        ok = ok && (bytes == 0 || hipMemcpy(to, from, bytes, hipMemcpyHostToDevice) == hipSuccess);
         p += bytes;
         return to;
       };
       l->matrices = static_cast<Matrix*>(put(mats.data(), mats.size() * sizeof(Matrix)));
       l->chunk = static_cast<Tile*>(put(chunk.data(), chunk.size() * sizeof(Tile)));
       l->turn = static_cast<Tile*>(put(turn.data(), turn.size() * sizeof(Tile)));
-      l->square = static_cast<Tile*>(put(square.data(), square.size() * sizeof(Tile)));
-      l->wide = static_cast<Tile*>(put(wide.data(), wide.size() * sizeof(Tile)));
+      l->gram = static_cast<Unit*>(put(gram.data(), gram.size() * sizeof(Unit)));
+      l->poly = static_cast<Unit*>(put(poly.data(), poly.size() * sizeof(Unit)));
+      l->apply = static_cast<Unit*>(put(apply.data(), apply.size() * sizeof(Unit)));
+      l->join = static_cast<Join*>(put(join.data(), join.size() * sizeof(Join)));
     }
     if (!ok) {
       (void)hipGetLastError();
@@ -575,18 +792,19 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
   if (!ws || misaligned(ws, 16) || ws_bytes < l->workspace) return ROTCONV_ERR_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   char* w = static_cast<char*>(ws);
-  float* inverse = reinterpret_cast<float*>(w + l->inverse);
   double* sums = reinterpret_cast<double*>(w + l->sums);
+  f4* parts = reinterpret_cast<f4*>(w + l->parts);
   auto first = l->bf16 ? k_momentum<uint16_t> : k_momentum<float>;
-  first<<<l->nchunk, kThreads, 0, st>>>(l->matrices, l->chunk, *o, momentum, control, sums);
-  k_inverse_norm<<<l->count, 64, 0, st>>>(l->matrices, o->eps, sums, inverse);
+  first<<<l->nchunk, kThreads, 0, st>>>(l->matrices, l->chunk, *o, l->size, momentum, control, sums);
   auto start = l->bf16 ? k_start<uint16_t> : k_start<float>;
-  start<<<l->nturn, kThreads, 0, st>>>(l->matrices, l->turn, *o, momentum, control, inverse, w);
+  start<<<l->nturn, kThreads, 0, st>>>(l->matrices, l->turn, *o, momentum, control, sums, w);
+  auto poly = l->small ? k_product<kPoly, 64, 64, 2, 2, kDepth, 2> : k_product<kPoly, 128, 128, 2, 2, kDepth, 2>;
   for (int k = 0; k < o->steps; ++k) {
-    k_product<kGram, 128, 128, 2, 2><<<l->nsquare, kThreads, 0, st>>>(l->matrices, l->square, w, k % 2, control);
-    k_product<kPoly, 128, 128, 2, 2><<<l->nsquare, kThreads, 0, st>>>(l->matrices, l->square, w, k % 2, control);
-    if (k + 1 < o->steps) k_product<kApply, 128, 128, 2, 2><<<l->nwide, kThreads, 0, st>>>(l->matrices, l->wide, w, k % 2, control);
-    else k_product<kLast, 128, 128, 2, 2><<<l->nwide, kThreads, 0, st>>>(l->matrices, l->wide, w, k % 2, control);
+    k_product<kGram, 128, 128, 2, 2, kDepth, 2><<<l->ngram, kThreads, 0, st>>>(l->matrices, l->gram, w, k % 2, parts, control);
+    if (l->njoin) k_join<kGram, 128, 128, 2, 2><<<l->njoin, kThreads, 0, st>>>(l->matrices, l->join, w, parts, control);
+    poly<<<l->npoly, kThreads, 0, st>>>(l->matrices, l->poly, w, k % 2, parts, control);
+    auto apply = k + 1 < o->steps ? k_product<kApply, 128, 128, 2, 2, kDepth, 2> : k_product<kLast, 128, 128, 2, 2, kDepth, 2>;
+    apply<<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control);
   }
   if (!o->keep) k_step_end<<<1, 1, 0, st>>>(control);
   return finish();
