@@ -4,8 +4,9 @@
 // A row is the K logits of a pixel or token.  With t its largest, y_j = z_j - t, s = sum exp(y_j) and h = sum exp(y_j) y_j,
 //     l = ln s      logp = y_label - l      entropy = l - h / s      p_j = exp(y_j) / s
 // and every gradient here has the form dz_j = c1 1[j = label] - p_j (base + c2 y_j), with base = c1 + c2 (entropy - l): c1 is the
-// gradient of the log-probability, c2 that of the entropy.  All of it is bound by memory: a row is read once, held in registers
-// (packed as it came) while its sums are formed, and its gradient written from there.
+// gradient of the log-probability, c2 that of the entropy.  All of it is bound by memory, but only just: a row is read once, held in
+// registers (packed as it came) while its sums are formed, and its gradient written from there.
+// Exponentials are the instruction's, of base 2, of x_j = y_j log2 e.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -43,9 +44,19 @@ struct RowIn {                         // what a row brings beside its logits
   float ent;                           // backward
 };
 struct RowGrad {
-  float t, inv, c1, base, c2;          // p_j = exp(z_j - t) inv
+  float t, inv, c1, base, c2;          // p_j = exp2(x_j) inv, dz_j = c1 1[j = label] - p_j (base + c2 x_j)
   bool live;                           // false: the row's gradient is 0
 };
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+// what a row's logits are taken from: the largest, or 0 where that is -infinity
+__device__ __forceinline__ float origin(float t) { return t == -INFINITY ? 0.f : t; }
+__device__ __forceinline__ float exponent(float z, float from) { return (z - from) * kLog2e; }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+// x as a factor: what lies 10^30 below a row's largest (-infinity too) counts as that, so that 0 times it stays 0; a NaN's exponential is a
+// factor beside it
+__device__ __forceinline__ float bounded(float x) { return fmaxf(x, -1e30f); }
 
 template <int MODE>
 __device__ __forceinline__ RowIn row_in(const LossArgs& g, size_t row) {
@@ -56,7 +67,7 @@ __device__ __forceinline__ RowIn row_in(const LossArgs& g, size_t row) {
     r.c = g.dlogp[row];
     if (g.dent) r.d = g.dent[row], r.ent = g.ent[row];
   } else if constexpr (MODE == kPolicy) {
-    r.a = g.adv[g.per_image ? row / g.P : row];
+    r.a = g.adv[g.per_image ? (uint32_t)row / (uint32_t)g.P : row];
     if (g.old) r.b = g.old[row];
     if (g.ref) r.c = g.ref[row];
     r.d = g.w ? g.w[row] : g.unit;
@@ -65,46 +76,43 @@ __device__ __forceinline__ RowIn row_in(const LossArgs& g, size_t row) {
 }
 __device__ __forceinline__ bool has_label(const LossArgs& g, const RowIn& r) { return r.label >= 0 && r.label < g.K; }
 
-// exp(q) - q - 1: by its series near 0, where the difference would lose its digits
-__device__ __forceinline__ float distance(float q, float e1) {
+// exp(q) - 1 and exp(q) - q - 1: by series near 0, where the differences would lose their digits
+__device__ __forceinline__ void distance(float q, float* e1, float* d) {
   if (fabsf(q) < 0.25f) {
     float s = 1.f / 40320;
     s = fmaf(s, q, 1.f / 5040), s = fmaf(s, q, 1.f / 720), s = fmaf(s, q, 1.f / 120);
     s = fmaf(s, q, 1.f / 24), s = fmaf(s, q, 1.f / 6), s = fmaf(s, q, 0.5f);
-    return s * q * q;
+    *d = s * q * q;
+    *e1 = q + *d;
+  } else {
+    *e1 = expf(q) - 1.f;
+    *d = *e1 == INFINITY ? INFINITY : *e1 - q;
   }
-  return e1 == INFINITY ? e1 : e1 - q;
 }
 
-// exp of a difference to the row's largest; what lies 10^30 below it (-infinity too) counts as that, so that 0 times it stays 0
-__device__ __forceinline__ float below(float z, float t) {
-  const float y = z - t;
-  return y < -1e30f ? -1e30f : y;      // (a NaN stays)
-}
-__device__ __forceinline__ void add_element(float y, float& s, float& h) {
-  const float e = __expf(y);
+__device__ __forceinline__ void add_element(float z, float from, float& s, float& h) {
+  const float x = exponent(z, from), e = exp2_of(x);
   s += e;
-  h = fmaf(e, y, h);
+  h = fmaf(e, bounded(x), h);
 }
 
-// A row's results from its sums (t: -infinity where no logit is above that, and the sums are then those over z itself), written by one
-// lane; the sums over rows are added to acc.  Returns what the gradient needs.
+// A row's results from its sums (s, h: over exp2(x) and exp2(x) x), written by one lane; the sums over rows are added to acc.  Returns
+// what the gradient needs.
 template <int MODE>
 __device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const RowIn& r, float t, float s, float h, float za, bool writes,
                                            double* acc) {
   RowGrad o = {};
   if constexpr (MODE == kBwd) {
     o.t = r.a;
-    o.inv = __expf(-r.b);
-    o.c1 = r.c, o.c2 = r.d;
-    o.base = r.c + r.d * (r.ent - r.b);
-    if (r.d == 0.f) o.base = r.c;
+    o.inv = exp2_of(-r.b * kLog2e);
+    o.c1 = r.c, o.c2 = r.d * kLn2;
+    o.base = r.d == 0.f ? r.c : r.c + r.d * (r.ent - r.b);
     o.live = has_label(g, r) && r.a != -INFINITY && !(r.c == 0.f && r.d == 0.f);
   } else {
     const bool none = t == -INFINITY && s == 0.f;
     bool live = has_label(g, r) && !none;
     if constexpr (MODE == kPolicy) live = live && r.d != 0.f;
-    const float l = logf(s), logp = za - t - l, ent = l - h / s;
+    const float l = __logf(s), inv = __builtin_amdgcn_rcpf(s), logp = za - t - l, ent = l - kLn2 * (h * inv);
     if (writes && g.logp) g.logp[row] = live ? logp : 0.f;
     if constexpr (MODE == kFwd) {
       if (writes && g.ent_out) g.ent_out[row] = live ? ent : 0.f;
@@ -114,14 +122,14 @@ __device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const 
       }
     } else {
       const float A = r.a, w = r.d;
-      const float ratio = g.old ? expf(logp - r.b) : 1.f;
+      const float ratio = g.old ? exp2_of((logp - r.b) * kLog2e) : 1.f;
       const bool cut = (A > 0.f && ratio > g.high) || (A < 0.f && ratio < g.low);
       // (A = 0 counts as no advantage whatever the ratio; a NaN goes through)
       const float kept = A == 0.f ? 0.f : ratio * A, gain = cut ? (A > 0.f ? g.high : g.low) * A : kept;
       float loss = -gain, G = cut ? 0.f : -kept, d = 0.f, H = 0.f;
       if (g.kl != 0.f && g.ref) {
-        const float q = r.c - logp, e1 = expm1f(q);
-        d = distance(q, e1);
+        float e1;
+        distance(r.c - logp, &e1, &d);
         loss += g.kl * d;
         G -= g.kl * e1;
       }
@@ -136,23 +144,41 @@ __device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const 
         acc[3] += cut ? (double)w : 0.0;
       }
       o.t = t;
-      o.inv = 1.f / s;
+      o.inv = inv;
       o.c1 = w * G;
-      o.c2 = -g.entc * w;
-      o.base = g.entc != 0.f ? o.c1 + o.c2 * (ent - l) : o.c1;
+      const float c2 = -g.entc * w;
+      o.c2 = c2 * kLn2;
+      o.base = g.entc != 0.f ? o.c1 + c2 * (ent - l) : o.c1;
       o.live = live;
     }
   }
   return o;
 }
 __device__ __forceinline__ float element(const RowGrad& o, float z, bool label) {
-  const float y = below(z, o.t), p = __expf(y) * o.inv;
-  return (label ? o.c1 : 0.f) - p * fmaf(o.c2, y, o.base);
+  const float x = exponent(z, o.t), p = exp2_of(x) * o.inv;
+  return (label ? o.c1 : 0.f) - p * fmaf(o.c2, bounded(x), o.base);
 }
 
 // Waits for a loaded value.  Where gradients take the logits' place, other waves store behind the next barrier, and a barrier alone
 // does not wait for loads under way.
 __device__ __forceinline__ void arrived(float v) { asm volatile("" ::"v"(v)); }
+
+// Sums that were formed below the maximum t, for a larger one
+__device__ __forceinline__ void moved_to(float top, float& t, float& s, float& h) {
+  if (!(top > t) || s == 0.f) {
+    t = fmaxf(t, top);
+    return;
+  }
+  const float by = bounded(exponent(t, top)), f = exp2_of(by);
+  h = f * fmaf(by, s, h);
+  s = f * s;
+  t = top;
+}
+// A vector's elements are taken from it anew, one vector after the other: the compiler would keep them all, in twice the registers for bf16.
+__device__ __forceinline__ void packed(u4& v) {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" : "+v"(v));
+}
 
 // max and sum over G neighbouring lanes
 template <int G> __device__ __forceinline__ float lanes_max(float v) {
@@ -201,9 +227,9 @@ __global__ __launch_bounds__(256) void k_rows_small(LossArgs g) {
 #pragma unroll
       for (int e = 0; e < E; ++e) t = fmaxf(t, v[e]);
       t = lanes_max<G>(t);
-      const float from = t == -INFINITY ? 0.f : t;
+      const float from = origin(t);
 #pragma unroll
-      for (int e = 0; e < E; ++e) add_element(below(v[e], from), s, h);
+      for (int e = 0; e < E; ++e) add_element(v[e], from, s, h);
       s = lanes_sum<G>(s), h = lanes_sum<G>(h);
     }
     const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, sub == 0, acc);
@@ -225,6 +251,9 @@ template <> struct Vec<float> {
   static constexpr uint32_t kLowest = 0xff800000u;
   static __device__ __forceinline__ float get(const u4& a, int k) { return __uint_as_float(a[k]); }
   static __device__ __forceinline__ void set(u4& a, int k, float v) { a[k] = __float_as_uint(v); }
+  static __device__ __forceinline__ u4 pack(const float* v) {
+    return u4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
 };
 template <> struct Vec<uint16_t> {
   static constexpr int V = 8;
@@ -235,6 +264,14 @@ template <> struct Vec<uint16_t> {
   static __device__ __forceinline__ void set(u4& a, int k, float v) {
     const uint32_t b = f32_to_bf16(v);
     a[k / 2] = k % 2 ? (a[k / 2] & 0xffffu) | b << 16 : (a[k / 2] & 0xffff0000u) | b;
+  }
+  static __device__ __forceinline__ u4 pack(const float* v) {    // rounded to nearest even by the instruction
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    u4 a;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) a[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[2 * k], v[2 * k + 1]}, b2));
+    return a;
   }
 };
 template <typename T>
@@ -273,22 +310,32 @@ __device__ __forceinline__ float block_join(float v, float* red) {
   return MAX ? lanes_max<B / 64>(v) : lanes_sum<B / 64>(v);
 }
 
-template <typename T>
+// ENT: the gradient has a part of the entropy's.  The label's own part is added where it lies.
+template <typename T, bool ENT>
 __device__ __forceinline__ u4 gradient(const RowGrad& o, const u4& a, int first, int label) {
   constexpr int V = Vec<T>::V;
-  u4 d;
+  float d[V];
+  const float factor = -o.inv * o.base;
 #pragma unroll
-  for (int k = 0; k < V; ++k) Vec<T>::set(d, k, o.live ? element(o, Vec<T>::get(a, k), first + k == label) : 0.f);
-  return d;
+  for (int k = 0; k < V; ++k) {
+    const float x = exponent(Vec<T>::get(a, k), o.t), e = exp2_of(x);
+    d[k] = ENT ? -(e * o.inv) * fmaf(o.c2, bounded(x), o.base) : e * factor;
+  }
+  if (label >= first && label < first + V) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) d[k] += first + k == label ? o.c1 : 0.f;
+  }
+  return Vec<T>::pack(d);
 }
 
 // Rows of many classes: a workgroup of B threads to a row, up to E vectors a thread in registers.  E = 0: rows of any
-// length, read twice (their sums are then formed with a running maximum).
-template <typename T, int B, int E, int MODE>
-__global__ __launch_bounds__(B) void k_rows(LossArgs g) {
+// length, read twice (their sums are then formed with a running maximum).  ENT: somebody wants the entropy or its gradient.
+template <typename T, int B, int E, int MODE, bool ENT>
+__global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 : 8))) void k_rows(LossArgs g) {
   constexpr int V = Vec<T>::V;
   __shared__ float red[16];
-  double acc[4] = {};
+  __shared__ double acc[4];            // the first thread's
+  if (MODE == kPolicy && threadIdx.x == 0) acc[0] = acc[1] = acc[2] = acc[3] = 0;
   for (size_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
     const T* z = static_cast<const T*>(g.z) + row * g.K;
     T* dz = static_cast<T*>(g.dz) + row * g.K;
@@ -298,6 +345,7 @@ __global__ __launch_bounds__(B) void k_rows(LossArgs g) {
     float t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
     if (MODE != kBwd && has_label(g, r)) za = Elt<T>::ld(z + r.label);
     arrived(za);
+    const u4 zero = {};
     if constexpr (E > 0) {
       u4 v[E];
 #pragma unroll
@@ -308,19 +356,29 @@ __global__ __launch_bounds__(B) void k_rows(LossArgs g) {
 #pragma unroll
           for (int k = 0; k < V; ++k) t = fmaxf(t, Vec<T>::get(v[e], k));
         t = block_join<B, true>(t, red);
-        const float from = t == -INFINITY ? 0.f : t;
+        const float from = origin(t);
 #pragma unroll
-        for (int e = 0; e < E; ++e)
+        for (int e = 0; e < E; ++e) {
+          packed(v[e]);
 #pragma unroll
-          for (int k = 0; k < V; ++k) add_element(below(Vec<T>::get(v[e], k), from), s, h);
-        s = block_join<B, false>(s, red), h = block_join<B, false>(h, red);
+          for (int k = 0; k < V; ++k) {
+            if constexpr (ENT) add_element(Vec<T>::get(v[e], k), from, s, h);
+            else s += exp2_of(exponent(Vec<T>::get(v[e], k), from));
+          }
+          asm volatile("" : "+v"(s), "+v"(h));         // (both sums now: the compiler would put one off, and keep its terms)
+        }
+        s = block_join<B, false>(s, red);
+        if constexpr (ENT) h = block_join<B, false>(h, red);
       }
       const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, threadIdx.x == 0, acc);
       if (MODE != kFwd && g.dz) {
+        int from = (int)threadIdx.x * V - shift;
+        asm volatile("" : "+v"(from));                 // (places are formed anew, not kept from the loads)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const int first = (int)(threadIdx.x + e * B) * V - shift;
-          store_part(dz, gradient<T>(o, v[e], first, r.label), first, g.K, g.alike);
+          const int first = from + e * B * V;
+          packed(v[e]);
+          store_part(dz, o.live ? gradient<T, ENT>(o, v[e], first, r.label) : zero, first, g.K, g.alike);
         }
       }
     } else {
@@ -330,30 +388,23 @@ __global__ __launch_bounds__(B) void k_rows(LossArgs g) {
           float top = t;
 #pragma unroll
           for (int k = 0; k < V; ++k) top = fmaxf(top, Vec<T>::get(v, k));
-          if (top > t) {
-            const float y = below(t, top), f = __expf(y);
-            h = f * fmaf(y, s, h);
-            s = f * s;
-            t = top;
-          }
-          const float from = t == -INFINITY ? 0.f : t;
+          moved_to(top, t, s, h);
 #pragma unroll
-          for (int k = 0; k < V; ++k) add_element(below(Vec<T>::get(v, k), from), s, h);
+          for (int k = 0; k < V; ++k) add_element(Vec<T>::get(v, k), origin(t), s, h);
         }
-        const float top = block_join<B, true>(t, red);
-        const float y = top == -INFINITY ? 0.f : below(t, top), f = __expf(y);
-        h = f * fmaf(y, s, h);
-        s = f * s;
-        t = top;
+        moved_to(block_join<B, true>(t, red), t, s, h);
         s = block_join<B, false>(s, red), h = block_join<B, false>(h, red);
       }
       const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, threadIdx.x == 0, acc);
       if (MODE != kFwd && g.dz)
         for (int first = (int)threadIdx.x * V - shift; first < g.K; first += B * V)
-          store_part(dz, gradient<T>(o, load_part(z, first, g.K), first, r.label), first, g.K, g.alike);
+          store_part(dz, o.live ? gradient<T, ENT>(o, load_part(z, first, g.K), first, r.label) : zero, first, g.K, g.alike);
     }
   }
-  if constexpr (MODE == kPolicy) write_sums(g, acc);
+  if (MODE == kPolicy && threadIdx.x == 0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) g.part[4 * (size_t)blockIdx.x + k] = acc[k];
+  }
 }
 
 // Classes in planes: a lane holds V neighbouring pixels.  KM > 0: all K <= KM classes in registers; KM = 0: any number, read
@@ -371,12 +422,53 @@ __device__ __forceinline__ void store_pixels(T* p, const float* v) {
   else Elt<T>::sth(p, v);
 }
 
+// V rows' values at a time: the caller has checked that vectors of them lie on their borders
+template <int V>
+__device__ __forceinline__ void load_rows(const float* p, size_t row, float* v) {
+  if constexpr (V == 1) v[0] = p[row];
+  else Elt<float>::ldv(p + row, v);
+}
+template <int MODE, int V>
+__device__ __forceinline__ void rows_in(const LossArgs& g, size_t row, RowIn* r) {
+  if constexpr (V == 1) {
+    r[0] = row_in<MODE>(g, row);
+  } else {
+    float v[5][V] = {}, second[V] = {};
+    load_rows<V>(reinterpret_cast<const float*>(g.labels), row, v[0]);
+    if constexpr (MODE == kBwd) {
+      load_rows<V>(g.stat, 2 * row, v[1]), load_rows<V>(g.stat, 2 * row + V, second);
+      load_rows<V>(g.dlogp, row, v[2]);
+      if (g.dent) load_rows<V>(g.dent, row, v[3]), load_rows<V>(g.ent, row, v[4]);
+    } else if constexpr (MODE == kPolicy) {
+      if (g.per_image) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[1][i] = g.adv[(uint32_t)row / (uint32_t)g.P];      // (P is a multiple of V)
+      } else {
+        load_rows<V>(g.adv, row, v[1]);
+      }
+      if (g.old) load_rows<V>(g.old, row, v[2]);
+      if (g.ref) load_rows<V>(g.ref, row, v[3]);
+      if (g.w) load_rows<V>(g.w, row, v[4]);
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      r[i].label = __float_as_int(v[0][i]);
+      if constexpr (MODE == kBwd) {
+        r[i].a = i < V / 2 ? v[1][2 * i] : second[2 * i - V], r[i].b = i < V / 2 ? v[1][2 * i + 1] : second[2 * i + 1 - V];
+        r[i].c = v[2][i], r[i].d = v[3][i], r[i].ent = v[4][i];
+      } else {
+        r[i].a = v[1][i], r[i].b = v[2][i], r[i].c = v[3][i], r[i].d = g.w ? v[4][i] : g.unit, r[i].ent = 0.f;
+      }
+    }
+  }
+}
+
 template <typename T, int V, int KM, int MODE>
 __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
   double acc[4] = {};
   const size_t apart = (size_t)gridDim.x * 256 * V;
   for (size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) * V; row < g.rows; row += apart) {
-    const size_t n = row / g.P, at = n * g.K * g.P + (row - n * g.P);
+    const size_t n = (uint32_t)row / (uint32_t)g.P, at = n * g.K * g.P + (row - n * g.P);      // (fewer than 2^31 rows)
     const T* z = static_cast<const T*>(g.z) + at;
     T* dz = static_cast<T*>(g.dz) + at;
     float v[KM][V];
@@ -384,25 +476,24 @@ __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
     for (int k = 0; k < KM; ++k)
       if (k < g.K) load_pixels<T, V>(z + k * g.P, v[k]);
     RowGrad o[V];
-    int label[V];
+    RowIn r[V];
+    rows_in<MODE, V>(g, row, r);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const RowIn r = row_in<MODE>(g, row + i);
-      label[i] = r.label;
       float t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
       if constexpr (MODE != kBwd) {
 #pragma unroll
         for (int k = 0; k < KM; ++k)
           if (k < g.K) {
             t = fmaxf(t, v[k][i]);
-            if (k == r.label) za = v[k][i];
+            if (k == r[i].label) za = v[k][i];
           }
-        const float from = t == -INFINITY ? 0.f : t;
+        const float from = origin(t);
 #pragma unroll
         for (int k = 0; k < KM; ++k)
-          if (k < g.K) add_element(below(v[k][i], from), s, h);
+          if (k < g.K) add_element(v[k][i], from, s, h);
       }
-      o[i] = row_end<MODE>(g, row + i, r, t, s, h, za, true, acc);
+      o[i] = row_end<MODE>(g, row + i, r[i], t, s, h, za, true, acc);
     }
     if (MODE != kFwd && g.dz) {
 #pragma unroll
@@ -410,7 +501,7 @@ __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
         if (k < g.K) {
           float d[V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) d[i] = o[i].live ? element(o[i], v[k][i], k == label[i]) : 0.f;
+          for (int i = 0; i < V; ++i) d[i] = o[i].live ? element(o[i], v[k][i], k == r[i].label) : 0.f;
           store_pixels<T, V>(dz + k * g.P, d);
         }
     }
@@ -427,7 +518,7 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
   for (size_t first = (size_t)blockIdx.x * 64 * V; first < g.rows; first += apart) {
     const size_t row = first + (size_t)lane * V;
     const bool inside = row < g.rows;
-    const size_t n = row / g.P, at = n * g.K * g.P + (row - n * g.P);
+    const size_t n = (uint32_t)row / (uint32_t)g.P, at = n * g.K * g.P + (row - n * g.P);
     const T* z = static_cast<const T*>(g.z) + at;
     float t[V], s[V], h[V], za[V];
 #pragma unroll
@@ -443,13 +534,8 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
         auto add = [&](const float* v) {
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            if (v[i] > t[i]) {
-              const float y = below(t[i], v[i]), f = __expf(y);
-              h[i] = f * fmaf(y, s[i], h[i]);
-              s[i] = f * s[i];
-              t[i] = v[i];
-            }
-            add_element(below(v[i], t[i] == -INFINITY ? 0.f : t[i]), s[i], h[i]);
+            moved_to(v[i], t[i], s[i], h[i]);
+            add_element(v[i], origin(t[i]), s[i], h[i]);
           }
         };
         int k = wave;
@@ -477,30 +563,26 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
           for (int w = 0; w < waves; ++w) top = fmaxf(top, shared[w][0][lane * V + i]);
           s[i] = h[i] = 0.f, t[i] = top;
           for (int w = 0; w < waves; ++w) {
-            const float sw = shared[w][1][lane * V + i], hw = shared[w][2][lane * V + i];
-            const float y = top == -INFINITY ? 0.f : below(shared[w][0][lane * V + i], top), f = __expf(y);
-            h[i] += f * fmaf(y, sw, hw);
-            s[i] += f * sw;
+            float tw = shared[w][0][lane * V + i], sw = shared[w][1][lane * V + i], hw = shared[w][2][lane * V + i];
+            moved_to(top, tw, sw, hw);
+            s[i] += sw, h[i] += hw;
           }
         }
       }
     }
     if (!inside) continue;             // (every wave of the workgroup has the same lanes inside, and no barrier follows within the pass)
     RowGrad o[V];
-    int label[V];
+    RowIn r[V];
+    rows_in<MODE, V>(g, row, r);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const RowIn r = row_in<MODE>(g, row + i);
-      label[i] = r.label;
-      o[i] = row_end<MODE>(g, row + i, r, t[i], s[i], h[i], za[i], wave == 0, acc);
-    }
+    for (int i = 0; i < V; ++i) o[i] = row_end<MODE>(g, row + i, r[i], t[i], s[i], h[i], za[i], wave == 0, acc);
     if (MODE != kFwd && g.dz) {
       T* dz = static_cast<T*>(g.dz) + at;
       for (int k = wave; k < g.K; k += waves) {
         float v[V];
         load_pixels<T, V>(z + (size_t)k * g.P, v);
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = o[i].live ? element(o[i], v[i], k == label[i]) : 0.f;
+        for (int i = 0; i < V; ++i) v[i] = o[i].live ? element(o[i], v[i], k == r[i].label) : 0.f;
         store_pixels<T, V>(dz + (size_t)k * g.P, v);
       }
     }
@@ -536,7 +618,8 @@ unsigned blocks_for(size_t n) { return (unsigned)std::min<size_t>(n, kMostBlocks
 template <typename T, int B, int E, int MODE>
 void launch_rows(const LossArgs& g, unsigned* blocks, hipStream_t st) {
   *blocks = blocks_for(g.rows);
-  k_rows<T, B, E, MODE><<<*blocks, B, 0, st>>>(g);
+  const bool entropy = MODE == kFwd ? g.ent_out != nullptr : MODE == kBwd ? g.dent != nullptr : g.entc != 0.f;
+  (entropy ? k_rows<T, B, E, MODE, true> : k_rows<T, B, E, MODE, false>)<<<*blocks, B, 0, st>>>(g);
 }
 template <typename T, int G, int E, int MODE>
 void launch_small(const LossArgs& g, unsigned* blocks, hipStream_t st) {
@@ -562,7 +645,11 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
     else launch_rows<T, 1024, 0, MODE>(g, blocks, st);
     return;
   }
-  const bool four = g.P % 4 == 0 && !misaligned(g.z, 4 * sizeof(T)) && !misaligned(g.dz, 4 * sizeof(T));
+  // four pixels a lane where all that is read of them lies on its borders (and where that leaves the chip enough lanes)
+  bool four = g.P % 4 == 0 && !misaligned(g.z, 4 * sizeof(T)) && !misaligned(g.dz, 4 * sizeof(T)) && g.rows >= 4 * 65536;
+  for (const void* p : {(const void*)g.labels, (const void*)g.stat, (const void*)g.ent, (const void*)g.dlogp, (const void*)g.dent, (const void*)g.old, (const void*)g.ref, (const void*)g.w})
+    four = four && !misaligned(p, 16);
+  four = four && (g.per_image || !misaligned(g.adv, 16));
   if (g.K <= 16) {
     *blocks = blocks_for((g.rows + 256 * (four ? 4 : 1) - 1) / (256 * (four ? 4 : 1)));
     auto kernel = four ? (g.K <= 8 ? k_planes<T, 4, 8, MODE> : k_planes<T, 4, 16, MODE>)
