@@ -736,37 +736,45 @@ def train_logp_workspace_bytes(N, K, P):
     return int(lib().train_logp_workspace_bytes(N, K, P))
 
 
+_i32 = _bf16 = None
+
+
 def _row_values(what, name, t, n, dtype=None):
     """Address of a tensor of n values (fp32 unless dtype says otherwise), one for each row; None stays NULL."""
     if t is None:
         return None
-    if t.dtype != (dtype or _f32) or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
+    if t.dtype is not (dtype or _f32) or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{what}: {name} must be {str(dtype or _f32)[6:]}, contiguous, on the GPU, with {n} elements")
     return t.data_ptr()
 
 
 def _loss(what, logits, dlogits, labels, ws, scratch):
     """What the calls on logits share: entry point, N, K, P, order of the logits, the labels' address, workspace."""
-    global _f32
-    import torch
+    global _f32, _i32, _bf16
+    if _i32 is None:
+        import torch
 
-    if _f32 is None:
-        _f32 = torch.float32
+        lib()
+        _f32, _i32, _bf16 = torch.float32, torch.int32, torch.bfloat16
     layout = _map_layout(what, logits, () if dlogits is None else (dlogits,))
-    N, K = logits.shape[0], logits.shape[1]
+    shape, kind = logits.shape, logits.dtype
+    N, K = shape[0], shape[1]
     _ints(what, N, K)
     P = logits.numel() // (N * K) if N * K else 0
-    fn = _glue(what, logits)
-    at = _row_values(what, "labels", labels, N * P, torch.int32)
-    for name, t in (("labels", labels), ("dlogits", dlogits), ("ws", ws)):
-        if t is not None and t.device != logits.device:
-            raise ValueError(f"{what}: {name} must be on the logits' device")
+    if kind is not _f32 and kind is not _bf16:
+        raise TypeError(f"{what}: logits must be float32 or bfloat16, got {kind}")
+    at = _row_values(what, "labels", labels, N * P, _i32)
+    home = logits.get_device()
+    if labels.get_device() != home or (dlogits is not None and dlogits.get_device() != home):
+        raise ValueError(f"{what}: labels and dlogits must be on the logits' device")
     if scratch:
         if ws is None:
+            import torch
+
             ws = torch.empty(max(256, train_logp_workspace_bytes(N, K, P)), dtype=torch.uint8, device=logits.device)
-        elif not ws.is_cuda:
-            raise ValueError(f"{what}: the workspace must be on the GPU")
-    return fn, N, K, P, layout, at, ws
+        elif ws.get_device() != home:
+            raise ValueError(f"{what}: the workspace must be on the logits' device")
+    return getattr(_lib, what if kind is _f32 else what + "_bf16"), N, K, P, layout, at, ws
 
 
 def train_logp_fwd(logits, labels, logp, entropy=None, stat=None, ws=None):

@@ -35,6 +35,8 @@ struct LossArgs {
   size_t rows, P;
   int K, per_image;
   int alike;                                                 // rows: dz's vectors start where z's do
+  float4* shares;                                            // few long rows: t, s, h of every part of a row ..
+  float* taken;                                              // .. and the label's logit of every row
   float low, high, kl, entc, unit;                           // the clipping range's ends; unit: the weight where there are none
 };
 
@@ -85,7 +87,7 @@ __device__ __forceinline__ void distance(float q, float* e1, float* d) {
     *d = s * q * q;
     *e1 = q + *d;
   } else {
-    *e1 = expf(q) - 1.f;
+    *e1 = exp2_of(q * kLog2e) - 1.f;
     *d = *e1 == INFINITY ? INFINITY : *e1 - q;
   }
 }
@@ -96,11 +98,14 @@ __device__ __forceinline__ void add_element(float z, float from, float& s, float
   h = fmaf(e, bounded(x), h);
 }
 
-// A row's results from its sums (s, h: over exp2(x) and exp2(x) x), written by one lane; the sums over rows are added to acc.  Returns
-// what the gradient needs.
-template <int MODE>
-__device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const RowIn& r, float t, float s, float h, float za, bool writes,
-                                           double* acc) {
+struct RowOut {
+  float logp, ent, t, l;
+};
+
+// A row's results from its sums (s, h: over exp2(x) and exp2(x) x), for memory (out) and for the gradient; adds: its part of the sums
+// over rows goes to acc.
+template <int MODE, typename A>
+__device__ __forceinline__ RowGrad row_end(const LossArgs& g, const RowIn& r, float t, float s, float h, float za, RowOut* out, bool adds, A* acc) {
   RowGrad o = {};
   if constexpr (MODE == kBwd) {
     o.t = r.a;
@@ -113,19 +118,13 @@ __device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const 
     bool live = has_label(g, r) && !none;
     if constexpr (MODE == kPolicy) live = live && r.d != 0.f;
     const float l = __logf(s), inv = __builtin_amdgcn_rcpf(s), logp = za - t - l, ent = l - kLn2 * (h * inv);
-    if (writes && g.logp) g.logp[row] = live ? logp : 0.f;
-    if constexpr (MODE == kFwd) {
-      if (writes && g.ent_out) g.ent_out[row] = live ? ent : 0.f;
-      if (writes && g.stat_out) {
-        const bool label = has_label(g, r);
-        g.stat_out[2 * row] = label ? t : 0.f, g.stat_out[2 * row + 1] = live ? l : 0.f;
-      }
-    } else {
-      const float A = r.a, w = r.d;
+    *out = RowOut{live ? logp : 0.f, live ? ent : 0.f, has_label(g, r) ? t : 0.f, live ? l : 0.f};
+    if constexpr (MODE == kPolicy) {
+      const float a = r.a, w = r.d;
       const float ratio = g.old ? exp2_of((logp - r.b) * kLog2e) : 1.f;
-      const bool cut = (A > 0.f && ratio > g.high) || (A < 0.f && ratio < g.low);
-      // (A = 0 counts as no advantage whatever the ratio; a NaN goes through)
-      const float kept = A == 0.f ? 0.f : ratio * A, gain = cut ? (A > 0.f ? g.high : g.low) * A : kept;
+      const bool cut = (a > 0.f && ratio > g.high) || (a < 0.f && ratio < g.low);
+      // (a = 0 counts as no advantage whatever the ratio; a NaN goes through)
+      const float kept = a == 0.f ? 0.f : ratio * a, gain = cut ? (a > 0.f ? g.high : g.low) * a : kept;
       float loss = -gain, G = cut ? 0.f : -kept, d = 0.f, H = 0.f;
       if (g.kl != 0.f && g.ref) {
         float e1;
@@ -137,11 +136,11 @@ __device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const 
         H = ent;
         loss -= g.entc * H;
       }
-      if (writes && live) {
-        acc[0] += (double)w * loss;
-        acc[1] += (double)w * d;
-        acc[2] += (double)w * H;
-        acc[3] += cut ? (double)w : 0.0;
+      if (adds && live) {
+        acc[0] += (A)w * loss;
+        acc[1] += (A)w * d;
+        acc[2] += (A)w * H;
+        acc[3] += cut ? w : 0.f;
       }
       o.t = t;
       o.inv = inv;
@@ -153,6 +152,12 @@ __device__ __forceinline__ RowGrad row_end(const LossArgs& g, size_t row, const 
     }
   }
   return o;
+}
+template <int MODE>
+__device__ __forceinline__ void write_row(const LossArgs& g, size_t row, const RowOut& out) {
+  if (MODE != kBwd && g.logp) g.logp[row] = out.logp;
+  if (MODE == kFwd && g.ent_out) g.ent_out[row] = out.ent;
+  if (MODE == kFwd && g.stat_out) g.stat_out[2 * row] = out.t, g.stat_out[2 * row + 1] = out.l;
 }
 __device__ __forceinline__ float element(const RowGrad& o, float z, bool label) {
   const float x = exponent(z, o.t), p = exp2_of(x) * o.inv;
@@ -232,7 +237,9 @@ __global__ __launch_bounds__(256) void k_rows_small(LossArgs g) {
       for (int e = 0; e < E; ++e) add_element(v[e], from, s, h);
       s = lanes_sum<G>(s), h = lanes_sum<G>(h);
     }
-    const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, sub == 0, acc);
+    RowOut out;
+    const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, sub == 0, acc);
+    if (sub == 0) write_row<MODE>(g, row, out);
     if (MODE != kFwd && g.dz) {
       T* d = static_cast<T*>(g.dz) + row * g.K;
 #pragma unroll
@@ -241,6 +248,13 @@ __global__ __launch_bounds__(256) void k_rows_small(LossArgs g) {
     }
   }
   if constexpr (MODE == kPolicy) write_sums(g, acc);
+}
+
+// two values rounded to nearest even by the instruction
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{a, b}, b2));
 }
 
 // A vector of 16 bytes as it lies in memory.  Rows start anywhere: vectors are those of the address space, and the first
@@ -265,13 +279,8 @@ template <> struct Vec<uint16_t> {
     const uint32_t b = f32_to_bf16(v);
     a[k / 2] = k % 2 ? (a[k / 2] & 0xffffu) | b << 16 : (a[k / 2] & 0xffff0000u) | b;
   }
-  static __device__ __forceinline__ u4 pack(const float* v) {    // rounded to nearest even by the instruction
-    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    u4 a;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[2 * k], v[2 * k + 1]}, b2));
-    return a;
+  static __device__ __forceinline__ u4 pack(const float* v) {
+    return u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
   }
 };
 template <typename T>
@@ -370,7 +379,9 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
         s = block_join<B, false>(s, red);
         if constexpr (ENT) h = block_join<B, false>(h, red);
       }
-      const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, threadIdx.x == 0, acc);
+      RowOut out;
+      const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, threadIdx.x == 0, acc);
+      if (threadIdx.x == 0) write_row<MODE>(g, row, out);
       if (MODE != kFwd && g.dz) {
         int from = (int)threadIdx.x * V - shift;
         asm volatile("" : "+v"(from));                 // (places are formed anew, not kept from the loads)
@@ -395,7 +406,9 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
         moved_to(block_join<B, true>(t, red), t, s, h);
         s = block_join<B, false>(s, red), h = block_join<B, false>(h, red);
       }
-      const RowGrad o = row_end<MODE>(g, row, r, t, s, h, za, threadIdx.x == 0, acc);
+      RowOut out;
+      const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, threadIdx.x == 0, acc);
+      if (threadIdx.x == 0) write_row<MODE>(g, row, out);
       if (MODE != kFwd && g.dz)
         for (int first = (int)threadIdx.x * V - shift; first < g.K; first += B * V)
           store_part(dz, o.live ? gradient<T, ENT>(o, load_part(z, first, g.K), first, r.label) : zero, first, g.K, g.alike);
@@ -404,6 +417,82 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
   if (MODE == kPolicy && threadIdx.x == 0) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) g.part[4 * (size_t)blockIdx.x + k] = acc[k];
+  }
+}
+
+// Few long rows: a row's parts of kPart vectors go to workgroups of their own, since one CU forms 16 exponentials a clock (one row of 131072
+// bf16 logits: 12.7 us by one workgroup).  k_share forms the parts' sums; k_rest, a launch behind it, joins a row's, each workgroup for
+// itself, and writes the part's gradient.  The label's logit is passed on, since a gradient may take its place.
+constexpr int kPartThreads = 256, kPartVecs = 4, kPart = kPartThreads * kPartVecs;
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_share(LossArgs g) {
+  constexpr int V = Vec<T>::V;
+  __shared__ float red[16];
+  const size_t row = blockIdx.y;
+  const T* z = static_cast<const T*>(g.z) + row * g.K;
+  const int shift = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T)), from = ((int)blockIdx.x * kPart + (int)threadIdx.x) * V - shift;
+  u4 v[kPartVecs];
+#pragma unroll
+  for (int e = 0; e < kPartVecs; ++e) v[e] = load_part(z, from + e * kPartThreads * V, g.K);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    const int label = g.labels[row];
+    if (label >= 0 && label < g.K) g.taken[row] = Elt<T>::ld(z + label);
+  }
+  float t = -INFINITY, s = 0.f, h = 0.f;
+#pragma unroll
+  for (int e = 0; e < kPartVecs; ++e)
+#pragma unroll
+    for (int k = 0; k < V; ++k) t = fmaxf(t, Vec<T>::get(v[e], k));
+  t = block_join<kPartThreads, true>(t, red);
+#pragma unroll
+  for (int e = 0; e < kPartVecs; ++e)
+#pragma unroll
+    for (int k = 0; k < V; ++k) add_element(Vec<T>::get(v[e], k), origin(t), s, h);
+  s = block_join<kPartThreads, false>(s, red), h = block_join<kPartThreads, false>(h, red);
+  if (threadIdx.x == 0) g.shares[row * gridDim.x + blockIdx.x] = make_float4(t, s, h, 0.f);
+}
+
+// parts: of a row; the grid has one workgroup for each, or (without a gradient) for each row
+template <typename T, int MODE>
+__global__ __launch_bounds__(kPartThreads) void k_rest(LossArgs g, int parts) {
+  constexpr int V = Vec<T>::V;
+  const size_t row = blockIdx.y;
+  const T* z = static_cast<const T*>(g.z) + row * g.K;
+  T* dz = static_cast<T*>(g.dz) + row * g.K;
+  const bool writes = blockIdx.x == 0 && threadIdx.x == 0;
+  const RowIn r = row_in<MODE>(g, row);
+  float t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
+  if constexpr (MODE != kBwd) {
+    if (has_label(g, r)) za = g.taken[row];
+    for (int c = threadIdx.x % 64; c < parts; c += 64) t = fmaxf(t, g.shares[row * parts + c].x);
+    t = lanes_max<64>(t);
+    for (int c = threadIdx.x % 64; c < parts; c += 64) {
+      const float4 p = g.shares[row * parts + c];
+      float pt = p.x, ps = p.y, ph = p.z;
+      moved_to(t, pt, ps, ph);
+      s += ps, h += ph;
+    }
+    s = lanes_sum<64>(s), h = lanes_sum<64>(h);
+  }
+  RowOut out;
+  double acc[4] = {};
+  const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, writes, acc);
+  if (writes) {
+    write_row<MODE>(g, row, out);
+    if constexpr (MODE == kPolicy) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) g.part[4 * row + k] = acc[k];
+    }
+  }
+  if (MODE != kFwd && g.dz) {
+    const int shift = (int)(reinterpret_cast<uintptr_t>(z) % 16 / sizeof(T)), from = ((int)blockIdx.x * kPart + (int)threadIdx.x) * V - shift;
+    const u4 zero = {};
+#pragma unroll
+    for (int e = 0; e < kPartVecs; ++e) {
+      const int first = from + e * kPartThreads * V;
+      store_part(dz, o.live ? gradient<T, true>(o, load_part(z, first, g.K), first, r.label) : zero, first, g.K, g.alike);
+    }
   }
 }
 
@@ -419,7 +508,7 @@ template <typename T, int V>
 __device__ __forceinline__ void store_pixels(T* p, const float* v) {
   if constexpr (V == 1) Elt<T>::st(p, v[0]);
   else if constexpr (sizeof(T) == 4) Elt<T>::stv(p, v);
-  else Elt<T>::sth(p, v);
+  else *reinterpret_cast<uint2*>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
 }
 
 // V rows' values at a time: the caller has checked that vectors of them lie on their borders
@@ -463,46 +552,92 @@ __device__ __forceinline__ void rows_in(const LossArgs& g, size_t row, RowIn* r)
   }
 }
 
+template <int V>
+__device__ __forceinline__ void store_rows(float* p, size_t row, const float* v) {
+  if constexpr (V == 1) p[row] = v[0];
+  else Elt<float>::stv(p + row, v);
+}
+// Classes behind the last are -infinity, so that nothing but their loads and stores asks for K; x and its exponential are kept from the
+// sums for the gradient (the 4 x 6 x 512 x 512 logits of a stack, bf16, with a reference and weights: 19.3 us where both were formed again and every
+// class asked, bound by instructions).
 template <typename T, int V, int KM, int MODE>
 __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
   double acc[4] = {};
   const size_t apart = (size_t)gridDim.x * 256 * V;
   for (size_t row = ((size_t)blockIdx.x * 256 + threadIdx.x) * V; row < g.rows; row += apart) {
     const size_t n = (uint32_t)row / (uint32_t)g.P, at = n * g.K * g.P + (row - n * g.P);      // (fewer than 2^31 rows)
+    float v[KM][V], p[KM][V];
     const T* z = static_cast<const T*>(g.z) + at;
-    T* dz = static_cast<T*>(g.dz) + at;
-    float v[KM][V];
 #pragma unroll
-    for (int k = 0; k < KM; ++k)
-      if (k < g.K) load_pixels<T, V>(z + k * g.P, v[k]);
+    for (int k = 0; k < KM; ++k, z += g.P) {
+      if (k < g.K) {
+        load_pixels<T, V>(z, v[k]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[k][i] = -INFINITY;
+      }
+    }
     RowGrad o[V];
     RowIn r[V];
+    RowOut out[V];
+    float part[4] = {};
     rows_in<MODE, V>(g, row, r);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float t = -INFINITY, s = 0.f, h = 0.f, za = 0.f;
       if constexpr (MODE != kBwd) {
 #pragma unroll
-        for (int k = 0; k < KM; ++k)
-          if (k < g.K) {
-            t = fmaxf(t, v[k][i]);
-            if (k == r[i].label) za = v[k][i];
-          }
-        const float from = origin(t);
+        for (int k = 0; k < KM; ++k) t = fmaxf(t, v[k][i]);
 #pragma unroll
-        for (int k = 0; k < KM; ++k)
-          if (k < g.K) add_element(v[k][i], from, s, h);
+        for (int k = 0; k < KM; ++k) za = k == r[i].label ? v[k][i] : za;
+      } else {
+        t = r[i].a;
       }
-      o[i] = row_end<MODE>(g, row + i, r[i], t, s, h, za, true, acc);
+      const float from = origin(t);
+#pragma unroll
+      for (int k = 0; k < KM; ++k) {
+        const float x = exponent(v[k][i], from), e = exp2_of(x);
+        v[k][i] = bounded(x), p[k][i] = e;
+        s += e;
+        h = fmaf(e, v[k][i], h);
+      }
+      o[i] = row_end<MODE>(g, r[i], t, s, h, za, &out[i], true, part);
+    }
+    if constexpr (MODE == kPolicy) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[k] += part[k];
+    }
+    if constexpr (MODE != kBwd) {
+      float w[2 * V];
+      if (g.logp) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = out[i].logp;
+        store_rows<V>(g.logp, row, w);
+      }
+      if (MODE == kFwd && g.ent_out) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = out[i].ent;
+        store_rows<V>(g.ent_out, row, w);
+      }
+      if (MODE == kFwd && g.stat_out) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[2 * i] = out[i].t, w[2 * i + 1] = out[i].l;
+        store_rows<V>(g.stat_out, 2 * row, w);
+        store_rows<V>(g.stat_out, 2 * row + V, w + V);
+      }
     }
     if (MODE != kFwd && g.dz) {
+      T* dz = static_cast<T*>(g.dz) + at;
 #pragma unroll
-      for (int k = 0; k < KM; ++k)
+      for (int k = 0; k < KM; ++k, dz += g.P)
         if (k < g.K) {
           float d[V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) d[i] = o[i].live ? element(o[i], v[k][i], k == r[i].label) : 0.f;
-          store_pixels<T, V>(dz + k * g.P, d);
+          for (int i = 0; i < V; ++i) {
+            const float c1 = k == r[i].label ? o[i].c1 : 0.f;
+            d[i] = o[i].live ? c1 - p[k][i] * o[i].inv * fmaf(o[i].c2, v[k][i], o[i].base) : 0.f;
+          }
+          store_pixels<T, V>(dz, d);
         }
     }
   }
@@ -575,7 +710,11 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
     RowIn r[V];
     rows_in<MODE, V>(g, row, r);
 #pragma unroll
-    for (int i = 0; i < V; ++i) o[i] = row_end<MODE>(g, row + i, r[i], t[i], s[i], h[i], za[i], wave == 0, acc);
+    for (int i = 0; i < V; ++i) {
+      RowOut out;
+      o[i] = row_end<MODE>(g, r[i], t[i], s[i], h[i], za[i], &out, wave == 0, acc);
+      if (wave == 0) write_row<MODE>(g, row + i, out);
+    }
     if (MODE != kFwd && g.dz) {
       T* dz = static_cast<T*>(g.dz) + at;
       for (int k = wave; k < g.K; k += waves) {
@@ -627,6 +766,13 @@ void launch_small(const LossArgs& g, unsigned* blocks, hipStream_t st) {
   k_rows_small<T, G, E, MODE><<<*blocks, 256, 0, st>>>(g);
 }
 
+// Parts of a row where few long ones are shared, 1 otherwise.  Calls one after the other, shared and by a workgroup to a row: 131072 bf16
+// logits forward 9.6 and 10.8 us (1 row), 9.7 and 11.5 (128), loss 13.3 and 21.6, 24.3 and 27.8; fp32 9.5 and 15.4, 15.1 and 20.9, 13.3 and
+// 31.4, 38.0 and 45.4.  With more rows every CU has one, and up to 8192 vectors a row (65536 bf16 logits) a second launch costs more than
+// it gives: 32768 bf16 logits forward 9.5 and 7.0, loss 13.3 and 10.8.
+constexpr size_t kFewRows = 128;
+int parts_of(size_t rows, int vecs) { return rows <= kFewRows && vecs > 8 * kPart ? (vecs + kPart - 1) / kPart : 1; }
+
 template <typename T, int MODE>
 void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st) {
   constexpr int V = Vec<T>::V;
@@ -634,6 +780,12 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
     // vectors of a row, counted as if it started one element past a border unless all of them start on one
     const bool even = !misaligned(g.z, 16) && g.K % V == 0;
     const int vecs = even ? g.K / V : (g.K + V - 2) / V + 1;
+    if (const int parts = parts_of(g.rows, vecs); parts > 1) {
+      *blocks = (unsigned)g.rows;
+      if (MODE != kBwd) k_share<T><<<dim3(parts, *blocks), kPartThreads, 0, st>>>(g);
+      k_rest<T, MODE><<<dim3(MODE == kFwd || !g.dz ? 1 : parts, *blocks), kPartThreads, 0, st>>>(g, parts);
+      return;
+    }
     if (g.K <= 8) launch_small<T, 1, 8, MODE>(g, blocks, st);
     else if (g.K <= 64) launch_small<T, 8, 8, MODE>(g, blocks, st);
     else if (g.K <= 512) launch_small<T, 64, 8, MODE>(g, blocks, st);
@@ -647,12 +799,14 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
   }
   // four pixels a lane where all that is read of them lies on its borders (and where that leaves the chip enough lanes)
   bool four = g.P % 4 == 0 && !misaligned(g.z, 4 * sizeof(T)) && !misaligned(g.dz, 4 * sizeof(T)) && g.rows >= 4 * 65536;
-  for (const void* p : {(const void*)g.labels, (const void*)g.stat, (const void*)g.ent, (const void*)g.dlogp, (const void*)g.dent, (const void*)g.old, (const void*)g.ref, (const void*)g.w})
+  for (const void* p : {(const void*)g.labels, (const void*)g.stat, (const void*)g.ent, (const void*)g.dlogp, (const void*)g.dent, (const void*)g.old, (const void*)g.ref, (const void*)g.w,
+                        (const void*)g.logp, (const void*)g.ent_out, (const void*)g.stat_out})
     four = four && !misaligned(p, 16);
   four = four && (g.per_image || !misaligned(g.adv, 16));
   if (g.K <= 16) {
     *blocks = blocks_for((g.rows + 256 * (four ? 4 : 1) - 1) / (256 * (four ? 4 : 1)));
-    auto kernel = four ? (g.K <= 8 ? k_planes<T, 4, 8, MODE> : k_planes<T, 4, 16, MODE>)
+    auto kernel = four ? (g.K <= 4 ? k_planes<T, 4, 4, MODE> : g.K <= 6 ? k_planes<T, 4, 6, MODE> : g.K <= 8 ? k_planes<T, 4, 8, MODE>
+                                                             : g.K <= 12 ? k_planes<T, 4, 12, MODE> : k_planes<T, 4, 16, MODE>)
                        : (g.K <= 8 ? k_planes<T, 1, 8, MODE> : k_planes<T, 1, 16, MODE>);
     kernel<<<*blocks, 256, 0, st>>>(g);
   } else {
@@ -668,7 +822,18 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
 bool refused(int N, int K, size_t P) {
   return N < 1 || K < 1 || P < 1 || K > (1 << 24) || P > 0x7fffffffull || (uint64_t)N * P > 0x7fffffffull;
 }
-constexpr size_t kWorkspace = (size_t)kMostBlocks * 4 * sizeof(double);
+// The sums of a launch's workgroups; behind them the shares of few long rows (fp32 rows have the most parts) and their labels' logits.
+constexpr size_t kSums = (size_t)kMostBlocks * 4 * sizeof(double);
+size_t workspace(size_t rows, int K) {
+  const int parts = parts_of(rows, K / Vec<float>::V + 2);
+  return kSums + (parts > 1 ? rows * parts * sizeof(float4) + kFewRows * sizeof(float) : 0);
+}
+void place(LossArgs& g, void* ws) {
+  char* w = static_cast<char*>(ws);
+  g.part = reinterpret_cast<double*>(w);
+  g.taken = reinterpret_cast<float*>(w + kSums);
+  g.shares = reinterpret_cast<float4*>(w + kSums + kFewRows * sizeof(float));
+}
 
 template <typename T>
 int check(const LossArgs& g, int N, int K, size_t P, int layout) {
@@ -694,7 +859,8 @@ int logp_fwd_t(const T* z, const int32_t* labels, float* logp, float* entropy, f
   LossArgs g = arguments(z, nullptr, labels, N, K, P);
   g.logp = logp, g.ent_out = entropy, g.stat_out = stat;
   if (int e = check<T>(g, N, K, P, layout)) return e;
-  if (!ws || misaligned(ws, 8) || ws_bytes < kWorkspace) return ROTCONV_ERR_WORKSPACE;
+  if (!ws || misaligned(ws, 16) || ws_bytes < workspace(g.rows, K)) return ROTCONV_ERR_WORKSPACE;
+  place(g, ws);
   unsigned blocks;
   launch_loss<T, kFwd>(g, in_rows(layout, P), &blocks, static_cast<hipStream_t>(stream));
   return finish();
@@ -722,10 +888,10 @@ int policy_loss_t(const T* z, const int32_t* labels, const float* advantage, con
       !(o->entropy >= 0.f && o->entropy <= FLT_MAX) || (o->per_image != 0 && o->per_image != 1) || o->reserved != 0 ||
       misaligned(out, 4))
     return ROTCONV_ERR_UNSUPPORTED;
-  if (!ws || misaligned(ws, 8) || ws_bytes < kWorkspace) return ROTCONV_ERR_WORKSPACE;
+  if (!ws || misaligned(ws, 16) || ws_bytes < workspace(g.rows, K)) return ROTCONV_ERR_WORKSPACE;
   g.per_image = o->per_image, g.low = 1.f - o->clip_low, g.high = 1.f + o->clip_high, g.kl = o->kl, g.entc = o->entropy;
   g.unit = (float)(1.0 / ((double)N * (double)P));
-  g.part = static_cast<double*>(ws);
+  place(g, ws);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   unsigned blocks;
   launch_loss<T, kPolicy>(g, in_rows(layout, P), &blocks, st);
@@ -740,7 +906,7 @@ using namespace rotconv;
 
 extern "C" {
 
-size_t train_logp_workspace_bytes(int N, int K, size_t P) { return refused(N, K, P) ? 0 : kWorkspace; }
+size_t train_logp_workspace_bytes(int N, int K, size_t P) { return refused(N, K, P) ? 0 : workspace((size_t)N * P, K); }
 
 int train_logp_fwd(const float* logits, const int32_t* labels, float* logp, float* entropy, float* stat, int N, int K, size_t P, int layout,
                    void* ws, size_t ws_bytes, void* stream) {
