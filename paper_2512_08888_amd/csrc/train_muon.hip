@@ -73,6 +73,8 @@ struct train_matrices {
   size_t workspace = 0, sums = 0, parts = 0;           // byte offsets: the chunks' sums, the units'
   uint32_t size = 0;                                   // elements of a chunk
   int small = 0;                                       // A^2 by tiles of 64
+  uint32_t least = 0;                                  // matrices, where all of them are small enough for a workgroup; blocks of the widest
+  uint32_t widest = 0;
   void* memory = nullptr;
   Matrix* matrices = nullptr;
   Tile *chunk = nullptr, *turn = nullptr;
@@ -593,6 +595,233 @@ __global__ __launch_bounds__(64 * WM * WN) void k_join(const Matrix* __restrict_
   F::tile(x, t.i, t.j, acc, blocks, ws, 0, ctl);
 }
 
+// Four elements at any element's address
+template <typename T> struct Any4;
+template <> struct Any4<float> {
+  typedef float f4a __attribute__((ext_vector_type(4), aligned(4)));
+  static __device__ __forceinline__ void ld(const float* p, float* v) {
+    const f4a a = *reinterpret_cast<const f4a*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = a[k];
+  }
+  static __device__ __forceinline__ void st(float* p, const float* v) { *reinterpret_cast<f4a*>(p) = f4a{v[0], v[1], v[2], v[3]}; }
+};
+template <> struct Any4<uint16_t> {
+  typedef uint16_t us4a __attribute__((ext_vector_type(4), aligned(2)));
+  static __device__ __forceinline__ void ld(const uint16_t* p, float* v) {
+    const us4a a = *reinterpret_cast<const us4a*>(p);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint16_t b = a[k];
+      v[k] = bf16_to_f32(b);
+    }
+  }
+  static __device__ __forceinline__ void st(uint16_t* p, const float* v) {
+    *reinterpret_cast<us4a*>(p) = us4a{f32_to_bf16(v[0]), f32_to_bf16(v[1]), f32_to_bf16(v[2]), f32_to_bf16(v[3])};
+  }
+};
+
+// The whole step of a matrix with at most 64 rows (or columns) and 1024 columns (or rows), by one workgroup of sixteen waves: X stays in
+// registers in 32 bits, blocks of 32 x 32 as the matrix instructions leave them, up to NT a wave, and its upper part in LDS for the products.
+// For lists of such matrices alone: a step is two launches instead of nineteen (nine of a stack of widths 16, 32, 64: XXX us).
+constexpr uint32_t kLeastRows = 64, kLeastCols = 1024;
+constexpr int kLeastThreads = 1024, kAcross = kLeastCols + 40, kAside = 72;      // elements from row to row in LDS: rows in banks of their own
+template <typename T, int NT>
+__global__ __launch_bounds__(kLeastThreads) void k_least(const Matrix* __restrict__ mats, train_muon opt, float* __restrict__ momentum,
+                                                         const train_control* __restrict__ ctl) {
+  constexpr int kWaves = kLeastThreads / 64;
+  __shared__ __attribute__((aligned(16))) half X[kLeastRows * kAcross];
+  __shared__ __attribute__((aligned(16))) half A[kLeastRows * kAside];
+  __shared__ __attribute__((aligned(16))) half B[kLeastRows * kAside];             // (as it is: its elements meet those of the diagonal, of order 1)
+  __shared__ __attribute__((aligned(16))) float da[kLeastRows], db[kLeastRows];
+  __shared__ double red[kWaves];
+  if (ctl->nonfinite) return;
+  const Matrix x = mats[blockIdx.x];
+  const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+  const int high = x.n > 32 ? 2 : 1, wide = (int)((x.m + 31) / 32), blocks = high * wide, K = high * 32;
+  const float coef = factor(*ctl), mu = opt.momentum, lr = ctl->lr;
+  const T* g = static_cast<const T*>(x.g);
+  float* m = momentum + x.pos;
+  // element e of a lane in a block: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
+  auto row_of = [&](int block, int e) { return (block % high) * 32 + 8 * (e / 4) + 4 * (lane / 32) + e % 4; };
+  auto col_of = [&](int block) { return (block / high) * 32 + lane % 32; };
+  // Calls use(e, place in memory, inside) for a lane's elements.  Blocks inside the matrix: a lane's place and what all lanes add to it.  Others:
+  // outside the matrix the place is that of its last row or column, so that loads go without questions.
+  auto each = [&](int block, auto use) {
+    const uint32_t i0 = (block % high) * 32, j0 = (block / high) * 32;
+    if (i0 + 32 <= x.n && j0 + 32 <= x.m) {
+      const uint32_t across = x.tall ? 1 : x.cols, down = x.tall ? x.cols : 1, own = 4 * (lane / 32) * across + (lane % 32) * down;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) use(e, own + ((i0 + 8 * (e / 4) + e % 4) * across + j0 * down), true);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const uint32_t i = row_of(block, e), j = col_of(block), ic = min(i, x.n - 1), jc = min(j, x.m - 1);
+        use(e, x.tall ? jc * x.cols + ic : ic * x.cols + jc, i < x.n && j < x.m);
+      }
+    }
+  };
+  // Four elements side by side in memory, where a tall matrix holds a lane's: their places
+  auto fours = [&](int block) { return x.tall && (uint32_t)(block % high) * 32 + 32 <= x.n && (uint32_t)(block / high) * 32 + 32 <= x.m; };
+  auto place_of = [&](int block, int q) { return ((uint32_t)(block / high) * 32 + lane % 32) * x.cols + (uint32_t)(block % high) * 32 + 8 * q + 4 * (lane / 32); };
+  f16v v[NT];
+  double square = 0;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int block = wave + t * kWaves;
+    v[t] = f16v{};
+    if (block >= blocks) continue;
+    float gv[16], mv[16];
+    if (fours(block)) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) Any4<T>::ld(g + place_of(block, q), gv + 4 * q), Any4<float>::ld(m + place_of(block, q), mv + 4 * q);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float gk = gv[e] * coef;
+        mv[e] = next_momentum(mv[e], gk, mu);
+        v[t][e] = direction(mv[e], gk, mu, opt.nesterov);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) Any4<float>::st(m + place_of(block, q), mv + 4 * q);
+    } else {
+      each(block, [&](int e, uint32_t at, bool) { gv[e] = Elt<T>::ld(g + at), mv[e] = m[at]; });
+      each(block,  [&](int e, uint32_t at, bool inside) {
+        const float gk = gv[e] * coef, mk = next_momentum(mv[e], gk, mu);
+        if (inside) {
+          m[at] = mk;
+          v[t][e] = direction(mk, gk, mu, opt.nesterov);
+        }
+      });
+    }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const double u = v[t][e];
+      square += u * u;
+    }
+  }
+  square = lanes_sum(square);
+  if (lane == 0) red[wave] = square;
+  __syncthreads();
+  double all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) all += red[w];
+  const float scale = (float)(1.0 / (sqrt(all) + (double)opt.eps)) * kHeld;
+#pragma unroll
+  for (int t = 0; t < NT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[t][e] = v[t][e] * scale;
+
+  // The symmetric products by blocks of 16 x 16, one a wave: row and column of its four elements a lane
+  const int edge = 2 * high, bi = wave / edge, bj = wave % edge, sj = bj * 16 + lane % 16, si = bi * 16 + 4 * (lane / 16);
+  const bool works = wave < edge * edge;
+  auto product = [&](const half* from, int across, int depth) {
+    f4 sum = {};
+    for (int k = 0; k < depth; k += 32) {
+      const h8 fa = *reinterpret_cast<const h8*>(from + (bi * 16 + lane % 16) * across + k + 8 * (lane / 16));
+      const h8 fb = *reinterpret_cast<const h8*>(from + (bj * 16 + lane % 16) * across + k + 8 * (lane / 16));
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa, fb, sum, 0, 0, 0);
+    }
+    return sum;
+  };
+  for (int step = 0; step < opt.steps; ++step) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int block = wave + t * kWaves;
+      if (block < blocks) {
+        half* to = X + row_of(block, 0) * kAcross + col_of(block);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const float r = v[t][e];
+          to[(8 * (e / 4) + e % 4) * kAcross] = (half)r;
+        }
+      }
+    }
+    __syncthreads();
+    float a[4] = {};
+    if (works) {
+      const f4 sum = product(X, kAcross, wide * 32);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float r = sum[e];
+        a[e] = si + e == sj ? 0.f : (float)(half)(r * (1.f / kHeld));
+        A[(si + e) * kAside + sj] = (half)a[e];
+        if (si + e == sj) da[sj] = r * (1.f / (kHeld * kHeld));
+      }
+    }
+    __syncthreads();
+    if (works) {
+      const f4 sum = product(A, kAside, K);
+      const float dj = da[sj];
+      const f4 di = *reinterpret_cast<const f4*>(da + si);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float s = sum[e] * (kC / (kHeld * kHeld)), d = di[e];
+        B[(si + e) * kAside + sj] = si + e == sj ? (half)0.f : (half)(a[e] * ((kB + kC * (d + dj)) / kHeld) + s);
+        if (si + e == sj) db[sj] = kA + d * (kB + kC * d) + s;
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int own = wave + t * kWaves;
+      if (own < blocks) {
+        // a X + B X in the same registers
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const f4 d = *reinterpret_cast<const f4*>(db + row_of(own, e));
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[t][e + k] = v[t][e + k] * d[k];
+        }
+        const half* rows = B + ((own % high) * 32 + lane % 32) * kAside + 8 * (lane / 32);
+        const half* cols = X + (8 * (lane / 32) + lane % 16 / 4) * kAcross + (own / high) * 32 + lane % 32 / 16 * 16 + 4 * (lane % 4);
+        for (int k = 0; k < K; k += 16) {
+          const h8 fa = *reinterpret_cast<const h8*>(rows + k);
+          h8 fb;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            typedef short s4 __attribute__((ext_vector_type(4)));
+            const h4 w = __builtin_bit_cast(h4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)(cols + (k + 4 * e) * kAcross)));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) fb[4 * e + q] = w[q];
+          }
+          v[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa, fb, v[t], 0, 0, 0);
+        }
+      }
+    }
+    __syncthreads();
+  }
+  const float keep = x.wd * lr, move = x.scale * lr / kHeld;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int block = wave + t * kWaves;
+    if (block >= blocks) continue;
+    float old[16];
+    if (fours(block)) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) Any4<float>::ld(x.p + place_of(block, q), old + 4 * q);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float o = v[t][e];
+        old[e] = old[e] - old[e] * keep - o * move;
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        Any4<float>::st(x.p + place_of(block, q), old + 4 * q);
+        if (x.copy) Any4<uint16_t>::st(x.copy + place_of(block, q), old + 4 * q);
+      }
+      continue;
+    }
+    each(block, [&](int e, uint32_t at, bool) { old[e] = x.p[at]; });
+    each(block, [&](int e, uint32_t at, bool inside) {
+      const float o = v[t][e], r = old[e] - old[e] * keep - o * move;
+      if (inside) {
+        x.p[at] = r;
+        if (x.copy) x.copy[at] = f32_to_bf16(r);
+      }
+    });
+  }
+}
+
 __global__ void k_step_end(train_control* ctl) { end_step(ctl, ctl->nonfinite, ctl->step + 1); }
 
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
@@ -661,6 +890,13 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
   // Steps of a unit of A: so that all units together fill the chip evenly, but no fewer than pay for the sums' way through memory.
   const uint64_t most = std::max<uint64_t>(8, (depth + kSlots - 1) / kSlots);
   const bool small = nsquare < kSlots;
+  bool least = true;
+  uint32_t widest = 0;
+  for (int k = 0; k < count; ++k) {
+    const uint32_t n = std::min(matrices[k].rows, matrices[k].cols), m = std::max(matrices[k].rows, matrices[k].cols);
+    least = least && n <= kLeastRows && m <= kLeastCols;
+    widest = std::max(widest, (n > 32 ? 2 : 1) * ((m + 31) / 32));
+  }
   train_matrices* l = nullptr;
   try {
     std::vector<Matrix> mats;
@@ -736,6 +972,9 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     l->elements = base;
     l->sums = sums, l->parts = part_bytes, l->workspace = at;
     l->size = size, l->small = small;
+    if (least) {
+      l->least = (uint32_t)mats.size(), l->widest = widest, l->workspace = 256;          // (nothing of it is used)
+    }
     l->nchunk = (uint32_t)chunk.size(), l->nturn = (uint32_t)turn.size(), l->ngram = (uint32_t)gram.size();
     l->npoly = (uint32_t)poly.size(), l->napply = (uint32_t)apply.size(), l->njoin = (uint32_t)join.size();
     const size_t tables = mats.size() * sizeof(Matrix) + (chunk.size() + turn.size()) * sizeof(Tile) +
@@ -791,6 +1030,13 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
     return ROTCONV_ERR_UNSUPPORTED;
   if (!ws || misaligned(ws, 16) || ws_bytes < l->workspace) return ROTCONV_ERR_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(stream);
+  if (l->least) {
+    auto kernel = l->widest <= 16 ? (l->bf16 ? k_least<uint16_t, 1> : k_least<float, 1>)
+                  : l->widest <= 32 ? (l->bf16 ? k_least<uint16_t, 2> : k_least<float, 2>) : (l->bf16 ? k_least<uint16_t, 4> : k_least<float, 4>);
+    kernel<<<l->least, kLeastThreads, 0, st>>>(l->matrices, *o, momentum, control);
+    if (!o->keep) k_step_end<<<1, 1, 0, st>>>(control);
+    return finish();
+  }
   char* w = static_cast<char*>(ws);
   double* sums = reinterpret_cast<double*>(w + l->sums);
   f4* parts = reinterpret_cast<f4*>(w + l->parts);
