@@ -27,7 +27,6 @@ constexpr int kBlock = 32;             // elements that share a scale; a tensor'
 constexpr int kThreads = 256;
 constexpr uint32_t kStepChunk = 4 * kThreads;          // elements of a step's chunk: four a lane
 constexpr int kStaged = 2048;          // sums of chunks that the end of the norm holds in LDS
-constexpr int kFan = 64;               // ticket counters of a launch, a cache line each
 constexpr uint32_t kMostWorkgroups = (1u << 24) - 1;   // of a launch: fewer than 2^32 threads
 
 // The chunks of a list: what a workgroup needs to know, in one read
@@ -55,7 +54,7 @@ struct train_list {
   bool trains = true;                  // every tensor has a param
   void* memory = nullptr;              // device: the tables below
   uint32_t nnorm = 0, nstep = 0;
-  uint32_t* tickets = nullptr;         // kFan + 1 counters, 32 words apart, 0 between calls
+  uint32_t* tickets = nullptr;         // 0 between calls
   StepChunk* step = nullptr;
   NormChunk* norm = nullptr;
   Row* rows = nullptr;
@@ -84,24 +83,14 @@ __device__ __forceinline__ void load_g4(const uint16_t* g, float* v) {
 template <typename T> __device__ __forceinline__ T stream_load(const T* p) { return __builtin_nontemporal_load(p); }
 template <typename T> __device__ __forceinline__ void stream_store(T* p, T v) { __builtin_nontemporal_store(v, p); }
 
-// Whether this workgroup is the last of its launch to come here.  Every workgroup of the grid calls it exactly once; the
-// tickets are 0 again afterwards.  Atomics on one counter take 12 ns each, one after the other (23 us for 1934 workgroups,
-// half of the norm of 31 M gradients), so a workgroup draws from one of 64 counters, and the last of each from a further
-// one.  No fence: a release at device scope writes back an XCD's whole L2 (the same norm: 153 us).  What the last workgroup
+// Whether this workgroup is the last of its launch to come here.  Every workgroup of the grid calls it exactly once.  (On one counter
+// the tickets take 23 us for 1934 workgroups, half of the norm of 31 M gradients.)  No fence: a release at device scope writes back an XCD's whole L2 (the same norm: 153 us).  What the last workgroup
 // reads of the others has to go through memory by itself (store_shared, load_shared).
-__device__ __forceinline__ bool draw_last(uint32_t* ticket, uint32_t of) {
-  const bool last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
-  if (last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return last;
-}
 __device__ __forceinline__ bool last_of_grid(uint32_t* tickets) {
   __shared__ int last;
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // this wave's stores have arrived
   __syncthreads();
-  if (threadIdx.x == 0) {
-    const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
-    last = draw_last(tickets + 32 * (1 + mine), of) && draw_last(tickets, min(gridDim.x, (uint32_t)kFan));
-  }
+  if (threadIdx.x == 0) last = last_to_come(tickets);
   __syncthreads();
   return last;
 }
@@ -432,9 +421,7 @@ __global__ __launch_bounds__(kThreads) void k_adamw(const StepChunk* __restrict_
   // The first lane alone reads the control block, and has done so: who draws the last ticket knows that nobody will again.
   auto end = [&] {
     if (!ends || threadIdx.x != 0) return;             // (more launches of this step follow)
-    const uint32_t mine = blockIdx.x % kFan, of = (gridDim.x - mine + kFan - 1) / kFan;
-    if (!draw_last(tickets + 32 * (1 + mine), of) || !draw_last(tickets, min(gridDim.x, (uint32_t)kFan))) return;
-    end_step(ctl, s.skip, s.t);
+    if (last_to_come(tickets)) end_step(ctl, s.skip, s.t);
   };
   if (s.skip || !inside) {             // (the first lane is inside)
     end();
@@ -578,7 +565,7 @@ int train_list_create(const train_tensor* tensors, int count, int grad_dtype, tr
     l->trains = tensors[0].param != nullptr;
     l->nnorm = (uint32_t)norm.size();
     l->nstep = (uint32_t)step.size();
-    const std::vector<uint32_t> tickets((kFan + 1) * 32, 0);
+    const std::vector<uint32_t> tickets(kTicketWords, 0);
     const size_t ticket_bytes = tickets.size() * sizeof(uint32_t), step_bytes = step.size() * sizeof(StepChunk);
     const size_t norm_bytes = norm.size() * sizeof(NormChunk), row_bytes = rows.size() * sizeof(Row);
     bool ok = hipGetDevice(&l->device) == hipSuccess &&

@@ -76,6 +76,7 @@ struct train_matrices {
   uint32_t least = 0;                                  // matrices, where all of them are small enough for a workgroup; blocks of the widest
   uint32_t widest = 0;
   void* memory = nullptr;
+  uint32_t* tickets = nullptr;                         // 0 between calls
   Matrix* matrices = nullptr;
   Tile *chunk = nullptr, *turn = nullptr;
   Unit *gram = nullptr, *poly = nullptr, *apply = nullptr;
@@ -234,6 +235,14 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
   }
 }
 
+// By every workgroup of a step's last launch, when all its waves have what they want of the control block (skip, and two more values): the
+// last of them advances it.  (A barrier alone does not wait for loads under way.)
+__device__ __forceinline__ void end_of_step(train_control* ctl, int skip, float one, float two, uint32_t* tickets) {
+  asm volatile("" ::"v"(skip), "v"(one), "v"(two));
+  __syncthreads();
+  if (threadIdx.x == 0 && last_to_come(tickets)) end_step(ctl, skip, ctl->step + 1);
+}
+
 enum Product { kGram, kPoly, kApply, kLast };
 
 // A wave's lanes bring 16 bytes each from memory to 1 KB of LDS in a row.  In assembler, without an output register, so that the
@@ -333,12 +342,10 @@ struct Finish {
     if (i < x.n && j < x.ldn) *reinterpret_cast<h8*>(out + (uint64_t)i * x.ldn + j) = w;
   }
 
-  static __device__ __forceinline__ void tile(const Matrix& x, uint32_t ti, uint32_t tj, const f16v (&acc)[TM / WM / 32][TN / WN / 32], float* lds,
-                                              char* ws, int from, const train_control* ctl) {
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, wr = wave / WN, wc = wave % WN;
+  static __device__ __forceinline__ void tile(const Matrix& x, uint32_t ti, uint32_t tj, const f16v (&acc)[TM / WM / 32][TN / WN / 32], int wave, float* block,
+                                              char* ws, int from, float lr) {
+    const int lane = threadIdx.x % 64, wr = wave / WN, wc = wave % WN;
     const uint32_t n = x.n, ldn = x.ldn, ldm = x.ldm;
-    float* block = lds + wave * kRows * kCols;
-    const float lr = KIND == kLast ? ctl->lr : 0.f;
 #pragma unroll
     for (int bp = 0; bp < TM / WM / kRows; ++bp)
 #pragma unroll
@@ -495,11 +502,14 @@ struct Finish {
 // One tile of TM x TN of a product, or some of its steps, WM x WN waves.
 template <int KIND, int TM, int TN, int WM, int WN, int D, int NS>
 __global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restrict__ mats, const Unit* __restrict__ units, char* ws, int from,
-                                                          f4* parts, const train_control* __restrict__ ctl) {
+                                                          f4* parts, train_control* ctl, uint32_t* tickets) {
   constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr bool kSquare = KIND == kGram || KIND == kPoly;
   __shared__ __attribute__((aligned(16))) half stages[NS][(TM + TN) * D];
-  if (ctl->nonfinite) return;
+  const int skip = ctl->nonfinite;
+  const float lr = KIND == kLast ? ctl->lr : 0.f;
+  if (KIND == kLast && tickets) end_of_step(ctl, skip, lr, lr, tickets);
+  if (skip) return;
   const Unit t = units[blockIdx.x];
   if (t.k0 == t.k1) return;
   const Matrix x = mats[t.matrix];
@@ -565,34 +575,33 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restri
   }
   using F = Finish<KIND, TM, TN, WM, WN>;
   static_assert(sizeof(stages) >= F::kBytes, "a block of each wave");
-  F::tile(x, t.i, t.j, acc, reinterpret_cast<float*>(stages), ws, from, ctl);
+  F::tile(x, t.i, t.j, acc, tid / 64, reinterpret_cast<float*>(stages) + tid / 64 * (F::kBytes / (WM * WN) / sizeof(float)), ws, from, lr);
 }
 
-// The tiles whose sums units have left in places of their own: added in the places' order, and finished.
-template <int KIND, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_join(const Matrix* __restrict__ mats, const Join* __restrict__ joins, char* ws, const f4* __restrict__ parts,
-                                                       const train_control* __restrict__ ctl) {
-  constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
-  using F = Finish<KIND, TM, TN, WM, WN>;
-  __shared__ __attribute__((aligned(16))) float blocks[F::kBytes / sizeof(float)];
+// The tiles of A whose sums units have left in places of their own: added in the places' order, and finished, a block of 32 x 32 a wave (and a
+// workgroup: the places' sums are then on their way all at once; 31 M parameters of a stack, 158 tiles in up to 6 places: XXX us).
+__global__ __launch_bounds__(64) void k_join(const Matrix* __restrict__ mats, const Join* __restrict__ joins, char* ws, const f4* __restrict__ parts,
+                                             const train_control* __restrict__ ctl) {
+  constexpr int kEdge = kTile / 32;    // blocks of a tile
+  using F = Finish<kGram, kTile, kTile, kEdge, kEdge>;
+  __shared__ __attribute__((aligned(16))) float block[32 * 32];
   if (ctl->nonfinite) return;
-  const Join t = joins[blockIdx.x];
+  const Join t = joins[blockIdx.x / (kEdge * kEdge)];
   const Matrix x = mats[t.matrix];
-  f16v acc[FM][FN] = {};
-  for (uint32_t c = 0; c < t.count; ++c) {
-    const f4* from = parts + (uint64_t)(t.first + c) * (TM * TN / 4) + threadIdx.x;
+  // the units' four waves hold 2 x 2 blocks each
+  const int mine = blockIdx.x % (kEdge * kEdge), r = mine / kEdge, c = mine % kEdge;
+  const f4* from = parts + (uint64_t)t.first * (kTile * kTile / 4) + ((r % 2) * 2 + c % 2) * 4 * kThreads + (r / 2 * 2 + c / 2) * 64 + threadIdx.x;
+  f16v acc[1][1] = {};
+#pragma unroll 4
+  for (uint32_t q = 0; q < t.count; ++q, from += kTile * kTile / 4) {
 #pragma unroll
-    for (int p = 0; p < FM; ++p)
+    for (int e = 0; e < 4; ++e) {
+      const f4 v = from[e * kThreads];
 #pragma unroll
-      for (int q = 0; q < FN; ++q)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const f4 v = from[((p * FN + q) * 4 + e) * T];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) acc[p][q][4 * e + k] += v[k];
-        }
+      for (int k = 0; k < 4; ++k) acc[0][0][4 * e + k] += v[k];
+    }
   }
-  F::tile(x, t.i, t.j, acc, blocks, ws, 0, ctl);
+  F::tile(x, t.i, t.j, acc, mine, block, ws, 0, 0.f);
 }
 
 // Four elements at any element's address
@@ -628,18 +637,20 @@ constexpr uint32_t kLeastRows = 64, kLeastCols = 1024;
 constexpr int kLeastThreads = 1024, kAcross = kLeastCols + 40, kAside = 72;      // elements from row to row in LDS: rows in banks of their own
 template <typename T, int NT>
 __global__ __launch_bounds__(kLeastThreads) void k_least(const Matrix* __restrict__ mats, train_muon opt, float* __restrict__ momentum,
-                                                         const train_control* __restrict__ ctl) {
+                                                         train_control* ctl, uint32_t* tickets) {
   constexpr int kWaves = kLeastThreads / 64;
   __shared__ __attribute__((aligned(16))) half X[kLeastRows * kAcross];
   __shared__ __attribute__((aligned(16))) half A[kLeastRows * kAside];
   __shared__ __attribute__((aligned(16))) half B[kLeastRows * kAside];             // (as it is: its elements meet those of the diagonal, of order 1)
   __shared__ __attribute__((aligned(16))) float da[kLeastRows], db[kLeastRows];
   __shared__ double red[kWaves];
-  if (ctl->nonfinite) return;
+  const int skip = ctl->nonfinite;
+  const float coef = factor(*ctl), mu = opt.momentum, lr = ctl->lr;
+  if (tickets) end_of_step(ctl, skip, lr, coef, tickets);
+  if (skip) return;
   const Matrix x = mats[blockIdx.x];
   const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int high = x.n > 32 ? 2 : 1, wide = (int)((x.m + 31) / 32), blocks = high * wide, K = high * 32;
-  const float coef = factor(*ctl), mu = opt.momentum, lr = ctl->lr;
   const T* g = static_cast<const T*>(x.g);
   float* m = momentum + x.pos;
   // element e of a lane in a block: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
@@ -822,8 +833,6 @@ __global__ __launch_bounds__(kLeastThreads) void k_least(const Matrix* __restric
   }
 }
 
-__global__ void k_step_end(train_control* ctl) { end_step(ctl, ctl->nonfinite, ctl->step + 1); }
-
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 // Workgroups go to the eight dies in turn, and each die has a cache of its own.  So the units, listed in an order in which neighbours share
@@ -882,13 +891,13 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     nsquare += c * tn * (tn + 1) / 2, nsmall += c * ts * (ts + 1) / 2, nwide += c * tn * tm;
     depth += c * tn * (tn + 1) / 2 * (up(m, kDepth) / kDepth);
     all += c, total += c * n * m;
-    if (all > 65535 || std::max(std::max(nturn, nsmall), nwide) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
+    if (all > 65535 || std::max(std::max(nturn, 16 * nsquare), std::max(nsmall, nwide)) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
   }
   // The momentum's chunks: from 1024 elements (fewer leave lanes idle) to 16384 where there are many.
   uint32_t size = 1024;
   while (size < 16384 && total / size > 2048) size *= 2;
   // Steps of a unit of A: so that all units together fill the chip evenly, but no fewer than pay for the sums' way through memory.
-  const uint64_t most = std::max<uint64_t>(8, (depth + kSlots - 1) / kSlots);
+  const uint64_t most = std::max<uint64_t>(12, (depth + kSlots - 1) / kSlots);
   const bool small = nsquare < kSlots;
   bool least = true;
   uint32_t widest = 0;
@@ -977,7 +986,8 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     }
     l->nchunk = (uint32_t)chunk.size(), l->nturn = (uint32_t)turn.size(), l->ngram = (uint32_t)gram.size();
     l->npoly = (uint32_t)poly.size(), l->napply = (uint32_t)apply.size(), l->njoin = (uint32_t)join.size();
-    const size_t tables = mats.size() * sizeof(Matrix) + (chunk.size() + turn.size()) * sizeof(Tile) +
+    const std::vector<uint32_t> tickets(kTicketWords, 0);
+    const size_t tables = tickets.size() * sizeof(uint32_t) + mats.size() * sizeof(Matrix) + (chunk.size() + turn.size()) * sizeof(Tile) +
                           (gram.size() + poly.size() + apply.size()) * sizeof(Unit) + join.size() * sizeof(Join);
     bool ok = hipGetDevice(&l->device) == hipSuccess &&
               hipMalloc(&l->memory, tables) == hipSuccess;
@@ -989,6 +999,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
         p += bytes;
         return to;
       };
+      l->tickets = static_cast<uint32_t*>(put(tickets.data(), tickets.size() * sizeof(uint32_t)));
       l->matrices = static_cast<Matrix*>(put(mats.data(), mats.size() * sizeof(Matrix)));
       l->chunk = static_cast<Tile*>(put(chunk.data(), chunk.size() * sizeof(Tile)));
       l->turn = static_cast<Tile*>(put(turn.data(), turn.size() * sizeof(Tile)));
@@ -1030,11 +1041,11 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
     return ROTCONV_ERR_UNSUPPORTED;
   if (!ws || misaligned(ws, 16) || ws_bytes < l->workspace) return ROTCONV_ERR_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(stream);
+  uint32_t* tickets = o->keep ? nullptr : l->tickets;
   if (l->least) {
     auto kernel = l->widest <= 16 ? (l->bf16 ? k_least<uint16_t, 1> : k_least<float, 1>)
                   : l->widest <= 32 ? (l->bf16 ? k_least<uint16_t, 2> : k_least<float, 2>) : (l->bf16 ? k_least<uint16_t, 4> : k_least<float, 4>);
-    kernel<<<l->least, kLeastThreads, 0, st>>>(l->matrices, *o, momentum, control);
-    if (!o->keep) k_step_end<<<1, 1, 0, st>>>(control);
+    kernel<<<l->least, kLeastThreads, 0, st>>>(l->matrices, *o, momentum, control, tickets);
     return finish();
   }
   char* w = static_cast<char*>(ws);
@@ -1046,13 +1057,12 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
   start<<<l->nturn, kThreads, 0, st>>>(l->matrices, l->turn, *o, momentum, control, sums, w);
   auto poly = l->small ? k_product<kPoly, 64, 64, 2, 2, kDepth, 2> : k_product<kPoly, 128, 128, 2, 2, kDepth, 2>;
   for (int k = 0; k < o->steps; ++k) {
-    k_product<kGram, 128, 128, 2, 2, kDepth, 2><<<l->ngram, kThreads, 0, st>>>(l->matrices, l->gram, w, k % 2, parts, control);
-    if (l->njoin) k_join<kGram, 128, 128, 2, 2><<<l->njoin, kThreads, 0, st>>>(l->matrices, l->join, w, parts, control);
-    poly<<<l->npoly, kThreads, 0, st>>>(l->matrices, l->poly, w, k % 2, parts, control);
+    k_product<kGram, 128, 128, 2, 2, kDepth, 2><<<l->ngram, kThreads, 0, st>>>(l->matrices, l->gram, w, k % 2, parts, control, tickets);
+    if (l->njoin) k_join<<<16 * l->njoin, 64, 0, st>>>(l->matrices, l->join, w, parts, control);
+    poly<<<l->npoly, kThreads, 0, st>>>(l->matrices, l->poly, w, k % 2, parts, control, tickets);
     auto apply = k + 1 < o->steps ? k_product<kApply, 128, 128, 2, 2, kDepth, 2> : k_product<kLast, 128, 128, 2, 2, kDepth, 2>;
-    apply<<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control);
+    apply<<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control, tickets);
   }
-  if (!o->keep) k_step_end<<<1, 1, 0, st>>>(control);
   return finish();
 }
 
