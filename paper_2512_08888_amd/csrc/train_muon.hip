@@ -79,9 +79,9 @@ struct train_matrices {
   uint32_t* tickets = nullptr;                         // 0 between calls
   Matrix* matrices = nullptr;
   Tile *chunk = nullptr, *turn = nullptr;
-  Unit *gram = nullptr, *poly = nullptr, *apply = nullptr;
+  Unit *gram = nullptr, *poly = nullptr, *apply = nullptr, *last = nullptr;
   Join* join = nullptr;
-  uint32_t nchunk = 0, nturn = 0, ngram = 0, npoly = 0, napply = 0, njoin = 0;
+  uint32_t nchunk = 0, nturn = 0, ngram = 0, npoly = 0, napply = 0, nlast = 0, njoin = 0;
 };
 
 namespace rotconv {
@@ -306,7 +306,8 @@ __device__ __forceinline__ h8 turned_fragment(const half* tile, int k, int j, in
 // lines a row, and what they are joined with is loaded all at once before.
 template <int KIND, int TM, int TN, int WM, int WN>
 struct Finish {
-  static constexpr int kRows = TM / WM < 64 ? TM / WM : 64, kCols = TN / WN < 64 ? TN / WN : 64;       // of a block
+  static constexpr int kMost = KIND == kApply ? 32 : 64;         // (three workgroups of kApply share a CU: see k_product)
+  static constexpr int kRows = TM / WM < kMost ? TM / WM : kMost, kCols = TN / WN < 64 ? TN / WN : 64;       // of a block
   static constexpr int kBytes = WM * WN * kRows * kCols * sizeof(float);
   static constexpr bool kSquare = KIND == kGram || KIND == kPoly;
   // eight elements a lane: along the rows kAcross lanes a row, along the columns kDown lanes a column
@@ -501,7 +502,7 @@ struct Finish {
 
 // One tile of TM x TN of a product, or some of its steps, WM x WN waves.
 template <int KIND, int TM, int TN, int WM, int WN, int D, int NS>
-__global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restrict__ mats, const Unit* __restrict__ units, char* ws, int from,
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(KIND == kApply ? 3 : 2))) void k_product(const Matrix* __restrict__ mats, const Unit* __restrict__ units, char* ws, int from,
                                                           f4* parts, train_control* ctl, uint32_t* tickets) {
   constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr bool kSquare = KIND == kGram || KIND == kPoly;
@@ -547,11 +548,11 @@ __global__ __launch_bounds__(64 * WM * WN) void k_product(const Matrix* __restri
   // Before step k, what it needs has arrived (later steps' loads stay on their way) and everybody is done with step k - 1, whose
   // place step k + NS - 1 takes.  The last steps load the last columns again, into places that nobody reads any more.
   constexpr int kLoads = (TM + TN) * (D / 8) / T;
-  const uint32_t last = t.k1 - 1;
+  const uint32_t begin = t.k0 * (kDepth / D), last = t.k1 * (kDepth / D) - 1;
 #pragma unroll
-  for (int u = 0; u < NS - 1; ++u) load(min(t.k0 + u, last) * D, stages[u]);
+  for (int u = 0; u < NS - 1; ++u) load(min(begin + u, last) * D, stages[u]);
   uint32_t here = 0, next = NS - 1;
-  for (uint32_t k = t.k0; k <= last; ++k) {
+  for (uint32_t k = begin; k <= last; ++k) {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"((NS - 2) * kLoads) : "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
@@ -838,15 +839,16 @@ bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t
 // Workgroups go to the eight dies in turn, and each die has a cache of its own.  So the units, listed in an order in which neighbours share
 // operands, are cut into eight runs of like work; a die's deepest units come first, so that none starts when the others end, and where a run
 // is shorter than another, units without steps stand in.  (Matrices of 2048 x 2048 and 2048 x 5632, A: 590 MB through the caches where every
-// die works on every matrix.)
-std::vector<Unit> by_die(const std::vector<Unit>& in) {
-  constexpr uint64_t kDies = 8, kEnds = 8;             // kEnds: what a unit takes beside its steps, in steps
+// die works on every matrix.)  ends: what a unit takes beside its steps, in steps, as measured: 32 for A (113 us for those matrices, 120 with
+// 4), 4 for X (78 us for the 31 M parameters of a stack, 87 with 16 or 32, 91 not dealt).
+std::vector<Unit> by_die(const std::vector<Unit>& in, uint64_t ends) {
+  constexpr uint64_t kDies = 8;
   uint64_t work = 0, done = 0;
-  for (const Unit& u : in) work += u.k1 - u.k0 + kEnds;
+  for (const Unit& u : in) work += u.k1 - u.k0 + ends;
   std::vector<Unit> runs[kDies];
   for (const Unit& u : in) {
     runs[std::min(kDies - 1, done * kDies / work)].push_back(u);
-    done += u.k1 - u.k0 + kEnds;
+    done += u.k1 - u.k0 + ends;
   }
   size_t most = 0;
   for (auto& r : runs) {
@@ -973,7 +975,9 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
       for (uint32_t c = 0; c * kTile < x.m; ++c)
         for (uint32_t r = 0; r < tiles; ++r) apply.push_back(Unit{id, r, c, 0, steps, kWhole});
     }
-    gram = by_die(gram), poly = by_die(poly), apply = by_die(apply);
+    // (the last product, which waits for the parameters, takes X's units as they are listed: 130 us for the stack, 140 and more dealt)
+    const std::vector<Unit> last = apply;
+    gram = by_die(gram, 32), poly = by_die(poly, 8), apply = by_die(apply, 4);
     if (std::max(std::max(gram.size(), poly.size()), std::max(apply.size(), chunk.size())) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
     const uint64_t sums = room(chunk.size() * sizeof(double)), part_bytes = room((uint64_t)places * kTile * kTile * sizeof(float));
     l = new train_matrices;
@@ -985,10 +989,11 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
       l->least = (uint32_t)mats.size(), l->widest = widest, l->workspace = 256;          // (nothing of it is used)
     }
     l->nchunk = (uint32_t)chunk.size(), l->nturn = (uint32_t)turn.size(), l->ngram = (uint32_t)gram.size();
-    l->npoly = (uint32_t)poly.size(), l->napply = (uint32_t)apply.size(), l->njoin = (uint32_t)join.size();
+    l->npoly = (uint32_t)poly.size(), l->napply = (uint32_t)apply.size(), l->nlast = (uint32_t)last.size();
+    l->njoin = (uint32_t)join.size();
     const std::vector<uint32_t> tickets(kTicketWords, 0);
     const size_t tables = tickets.size() * sizeof(uint32_t) + mats.size() * sizeof(Matrix) + (chunk.size() + turn.size()) * sizeof(Tile) +
-                          (gram.size() + poly.size() + apply.size()) * sizeof(Unit) + join.size() * sizeof(Join);
+                          (gram.size() + poly.size() + apply.size() + last.size()) * sizeof(Unit) + join.size() * sizeof(Join);
     bool ok = hipGetDevice(&l->device) == hipSuccess &&
               hipMalloc(&l->memory, tables) == hipSuccess;
     if (ok) {
@@ -1006,6 +1011,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
       l->gram = static_cast<Unit*>(put(gram.data(), gram.size() * sizeof(Unit)));
       l->poly = static_cast<Unit*>(put(poly.data(), poly.size() * sizeof(Unit)));
       l->apply = static_cast<Unit*>(put(apply.data(), apply.size() * sizeof(Unit)));
+      l->last = static_cast<Unit*>(put(last.data(), last.size() * sizeof(Unit)));
       l->join = static_cast<Join*>(put(join.data(), join.size() * sizeof(Join)));
     }
     if (!ok) {
@@ -1060,8 +1066,10 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
     k_product<kGram, 128, 128, 2, 2, kDepth, 2><<<l->ngram, kThreads, 0, st>>>(l->matrices, l->gram, w, k % 2, parts, control, tickets);
     if (l->njoin) k_join<<<16 * l->njoin, 64, 0, st>>>(l->matrices, l->join, w, parts, control);
     poly<<<l->npoly, kThreads, 0, st>>>(l->matrices, l->poly, w, k % 2, parts, control, tickets);
-    auto apply = k + 1 < o->steps ? k_product<kApply, 128, 128, 2, 2, kDepth, 2> : k_product<kLast, 128, 128, 2, 2, kDepth, 2>;
-    apply<<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control, tickets);
+    if (k + 1 < o->steps)
+      k_product<kApply, 128, 128, 2, 2, 32, 3><<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control, tickets);
+    else
+      k_product<kLast, 128, 128, 2, 2, kDepth, 2><<<l->nlast, kThreads, 0, st>>>(l->matrices, l->last, w, k % 2, parts, control, tickets);
   }
   return finish();
 }
