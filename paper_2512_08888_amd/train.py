@@ -68,6 +68,8 @@ class AdamW(_Control):
     and the skip of a step with a non-finite gradient live on the device, so that step() can be recorded into a HIP
     graph: write a schedule's rate with `lr.fill_()`."""
 
+    call = "train_adamw_step"            # what step() issues
+
     def __init__(self, params, grads, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, state="f32", copies=None,
                  seed=0):
         import torch
@@ -120,6 +122,8 @@ class Muon(_Control):
     tensors, whose step follows in step() under this one's control block (its own lr, clip factor and step number are not
     used).  Step number, learning rate, clip factor and the skip of a step live on the device as AdamW's do."""
 
+    call = "train_muon_step"             # what step() issues (and train_adamw_step for the rest)
+
     def __init__(self, params, grads, lr=1e-3, momentum=0.95, nesterov=True, weight_decay=0.0, steps=5, scale="rms", eps=1e-12,
                  copies=None, rest=None):
         import torch
@@ -166,9 +170,16 @@ class Muon(_Control):
         _load(self, step, state)
 
 
+def sampled(logits, uniform):
+    """A label for each pixel of logits [N, K, H, W], drawn by its class probabilities with uniform numbers [N, H, W]."""
+    p = logits.float().softmax(1).cumsum(1)
+    return (uniform.unsqueeze(1) * p[:, -1:] > p).sum(1).clamp(max=logits.shape[1] - 1).int()
+
+
 def main(argv=None):
     """A stack of two levels learns to tell the quadrants of its images apart (labels by pixel position and brightness):
-    group norm, clipping and AdamW as a training program uses them.  Returns the losses."""
+    group norm, clipping and AdamW or Muon as a training program uses them.  With --loss policy the stack samples its labels
+    itself and is told only which of them were right.  Returns the losses."""
     import argparse
 
     import numpy as np
@@ -180,6 +191,8 @@ def main(argv=None):
     ap.add_argument("--steps", type=int, default=60)
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="f32")
     ap.add_argument("--state", choices=sorted(rc.STATES), default="f32")
+    ap.add_argument("--method", choices=("adamw", "muon"), default="adamw")
+    ap.add_argument("--loss", choices=("ce", "policy"), default="ce")
     ap.add_argument("--lr", type=float, default=3e-3)
     ap.add_argument("--graph", action="store_true", help="record the step into a HIP graph and replay it")
     a = ap.parse_args(argv)
@@ -188,15 +201,30 @@ def main(argv=None):
     images, _ = unet.make_batch(cfg)
     labels = (images.mean(1) > 0.5).astype(np.int32) + 2 * (np.arange(cfg.W) >= cfg.W // 2).astype(np.int32)
     net.load_batch(images, labels)
-    opt = net.optimizer(lr=a.lr, weight_decay=0.01, state=a.state)
+    opt = net.optimizer(lr=a.lr, weight_decay=0.01, state=a.state, method=a.method)
+    right = net.labels.clone()
+    draws = torch.Generator(device=net.dev).manual_seed(cfg.seed)
+
+    def roll_out():
+        """Samples labels and puts the loss of what they earned in place; the share of right ones."""
+        taken = sampled(net.forward_logits(), torch.rand(right.shape, generator=draws, device=net.dev))
+        earned = (taken == right).float()
+        old = net.label_logp(taken)
+        net.load_policy(taken, earned - earned.mean(), logp_old=old, entropy=0.01)
+        return earned.mean()
+
+    if a.loss == "policy":
+        roll_out()
     if a.graph:
         net.capture(opt, max_norm=1.0)
     losses = []
     for k in range(a.steps):
+        earned = roll_out() if a.loss == "policy" else None
         loss = net.replay() if a.graph else net.train_step(opt, max_norm=1.0)
         if k % 10 == 0 or k == a.steps - 1:
             losses.append(float(loss.cpu()[0]))
-            print(f"step {k:4d}  loss {losses[-1]:.4f}  gradient norm {opt.norm.item():.4f}  clipped by {opt.coef.item():.3f}", flush=True)
+            more = "" if earned is None else f"  right {earned.item():.3f}"
+            print(f"step {k:4d}  loss {losses[-1]:.4f}  gradient norm {opt.norm.item():.4f}  clipped by {opt.coef.item():.3f}{more}", flush=True)
     torch.cuda.synchronize()
     return losses
 

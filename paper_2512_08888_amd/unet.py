@@ -8,8 +8,9 @@ plain memory), the per-layer plans and the order of the calls.
     encoder: Block, 2x2 max-pool per level; bottleneck Block; decoder per level: 2x2 stride-2
     transposed convolution, concat [skip, up], Block; 1x1 head; mean soft-max cross-entropy.
 
-UNet.optimizer() and UNet.train_step() close the step: the gradients' norm, clipping and AdamW over all parameters
-(paper_2512_08888_amd/train.py).  No arithmetic happens here and nothing falls back to torch ops.
+UNet.optimizer() and UNet.train_step() close the step: the gradients' norm, clipping and AdamW over all parameters, or Muon
+over the filters with AdamW for the rest (paper_2512_08888_amd/train.py).  UNet.load_policy() puts the clipped policy loss over sampled
+labels in the soft-max cross-entropy's place, and UNet.label_logp() gives the log-probabilities that it starts from.  No arithmetic happens here and nothing falls back to torch ops.
 """
 from __future__ import annotations
 
@@ -208,9 +209,13 @@ class UNet:
             h, w = h // 2, w // 2
         P = cfg.H * cfg.W
         self.act["head"] = dict(y=buf(N, cfg.classes, cfg.H, cfg.W), g=buf(N, cfg.classes, cfg.H, cfg.W))
-        ws_bytes = max(ws_bytes, rc.glue_conv1x1_workspace_bytes(N, cfg.widths[0], cfg.classes, P), N * P * 4)
+        ws_bytes = max(ws_bytes, rc.glue_conv1x1_workspace_bytes(N, cfg.widths[0], cfg.classes, P), N * P * 4,
+                       rc.train_logp_workspace_bytes(N, cfg.classes, P))
         self.ws = torch.empty(ws_bytes, dtype=u8, device=device)
-        self.loss = buf(1, dtype=f32)
+        self.parts = buf(4, dtype=f32)    # the loss; of the policy loss also its distance, entropy and share of cut pixels
+        self.loss = self.parts[:1]
+        self.policy = None                # what load_policy() has put in the cross-entropy's place
+        self._policy = {}                 # its buffers
         self.trace = None         # a list turns on per-call event timing
         self._where = ""
         self.images = buf(N, cfg.Cin, cfg.H, cfg.W)
@@ -247,6 +252,43 @@ class UNet:
     def load_batch(self, images, labels):
         self.images.copy_(self.torch.from_numpy(np.ascontiguousarray(images, dtype=np.float32)))
         self.labels.copy_(self.torch.from_numpy(np.ascontiguousarray(labels, dtype=np.int32)))
+        self.policy = None
+
+    def load_policy(self, labels, advantage, logp_old=None, logp_ref=None, weight=None, clip=(0.2, 0.2), kl=0.0, entropy=0.0):
+        """From now on, until load_batch(), the loss is the clipped policy loss (binding.train_policy_loss) of the images held
+        now: labels sampled for them [N, H, W] (int32; outside the classes: left out), an advantage for each image [N] or
+        pixel [N, H, W], the labels' log-probabilities when they were sampled and in a reference, weights (None: 1 / pixels).
+        Tensors or arrays; their values are copied into buffers of the network, which a recorded step reads again: what is
+        given or None, the advantage's extent and the constants are part of the recording."""
+        torch, n, pixels = self.torch, self.cfg.N, self.labels.numel()
+
+        def hold(name, v, sizes, dtype=torch.float32):
+            if v is None:
+                return None
+            v = v if torch.is_tensor(v) else torch.from_numpy(np.ascontiguousarray(v))
+            if v.numel() not in sizes:
+                raise ValueError(f"load_policy: {name} must have {' or '.join(map(str, sizes))} values, got {v.numel()}")
+            key = (name, v.numel())
+            if key not in self._policy:
+                self._policy[key] = torch.empty(v.numel(), dtype=dtype, device=self.dev)
+            self._policy[key].copy_(v.reshape(-1))
+            return self._policy[key]
+
+        hold_labels = hold("labels", labels, (pixels,), torch.int32)
+        held = dict(advantage=hold("advantage", advantage, (n, pixels)), logp_old=hold("logp_old", logp_old, (pixels,)),
+                    logp_ref=hold("logp_ref", logp_ref, (pixels,)), weight=hold("weight", weight, (pixels,)))
+        self.labels.view(-1).copy_(hold_labels)
+        self.policy = dict(held, clip=clip, kl=kl, entropy=entropy)
+
+    def label_logp(self, labels=None):
+        """Log-probability of every pixel's label [N, H, W] (None: those held now) under the present parameters, for the images
+        held now: a forward pass without the loss.  A new tensor; 0 where the label is none of the classes."""
+        torch = self.torch
+        labels = self.labels if labels is None else torch.as_tensor(labels, dtype=torch.int32, device=self.dev).contiguous()
+        logp = torch.empty(self.labels.shape, dtype=torch.float32, device=self.dev)
+        logits = self.forward_logits()
+        self._c("train_logp_fwd", rc.train_logp_fwd, logits, labels, logp, ws=self.ws)
+        return logp
 
     # ---- the step -----------------------------------------------------------------------------
     def _c(self, what, fn, *args, **kw):
@@ -294,7 +336,7 @@ class UNet:
             self._c("rotconv_pool_bwd_data", rc.rotconv_pool_bwd_data, self.plans[name], g, a["idx"],
                     self.params[name], a["gx"], self.ws)
 
-    def forward(self):
+    def forward_logits(self):
         cfg, act = self.cfg, self.act
         x = self.images
         for lvl in range(cfg.depth):
@@ -318,7 +360,17 @@ class UNet:
         hd["x"] = x
         self._where = "head"
         self._c("glue_conv1x1_fwd", rc.glue_conv1x1_fwd, x, self.params["head"], hd["y"])
-        self._c("glue_softmax_ce", rc.glue_softmax_ce, hd["y"], self.labels, self.loss, hd["g"], self.ws)
+        return hd["y"]
+
+    def forward(self):
+        logits, hd = self.forward_logits(), self.act["head"]
+        if self.policy is None:
+            self._c("glue_softmax_ce", rc.glue_softmax_ce, logits, self.labels, self.loss, hd["g"], self.ws)
+        else:
+            p = self.policy
+            self._c("train_policy_loss", rc.train_policy_loss, logits, self.labels, p["advantage"], self.parts, hd["g"],
+                    logp_old=p["logp_old"], logp_ref=p["logp_ref"], weight=p["weight"], clip=p["clip"], kl=p["kl"],
+                    entropy=p["entropy"], ws=self.ws)
         return self.loss
 
     def backward(self):
@@ -364,19 +416,37 @@ class UNet:
         return self.loss
 
     # ---- training -----------------------------------------------------------------------------
-    def optimizer(self, weight_decay=0.0, **options):
-        """train.AdamW over all parameters and this network's gradient buffers; options: lr, betas, eps, state, seed.
-        Filters decay, a norm's scale and shift do not.  dtype "bf16": the optimizer updates fp32 copies (kept from the
-        parameters loaded from now on, or the rounded ones held now), and every step rounds them into the network's own."""
+    def optimizer(self, weight_decay=0.0, method="adamw", **options):
+        """method "adamw": train.AdamW over all parameters and this network's gradient buffers; options: lr, betas, eps, state,
+        seed.  "muon": train.Muon over the filters behind the first layer (each bank a matrix of output channels x taps, an
+        up-sampling one of input channels x taps), with further options momentum, nesterov, steps and scale, and AdamW for the
+        first layer, the head and the norms.  Filters decay, a norm's scale and shift do not.  dtype "bf16": the optimizer
+        updates fp32 copies (kept from the parameters loaded from now on, or the rounded ones held now), and every step
+        rounds them into the network's own."""
         from . import train
 
+        if method not in ("adamw", "muon"):
+            raise ValueError("optimizer: method must be 'adamw' or 'muon'")
         names = list(self.params)
         half = [n for n in names if self.params[n].dtype == self.torch.bfloat16]
         if half and self.masters is self.params:
             self.masters = {n: self.params[n].float() if n in half else self.params[n] for n in names}
-        return train.AdamW([self.masters[n] for n in names], [self.grads[n] for n in names],
-                           weight_decay=[0.0 if _is_norm(n) else weight_decay for n in names],
-                           copies=[self.params[n] if n in half else None for n in names], **options)
+        muon = {k: options.pop(k) for k in ("momentum", "nesterov", "steps", "scale") if method == "muon" and k in options}
+        matrices = [n for n in names if method == "muon" and not _is_norm(n) and n not in ("head", self.specs[0]["name"])]
+
+        def tensors(of):
+            return ([self.masters[n] for n in of], [self.grads[n] for n in of],
+                    [self.params[n] if n in half else None for n in of])
+
+        params, grads, copies = tensors([n for n in names if n not in matrices])
+        rest = train.AdamW(params, grads, copies=copies, weight_decay=[0.0 if _is_norm(n) else weight_decay for n in names
+                                                                       if n not in matrices], **options)
+        if method == "adamw":
+            return rest
+        # filters [B, Cout, Cin, 3, 3] are B matrices, an up-sampling's [Cin, Cout, 2, 2] one
+        flat = [[None if t is None else t.flatten(2) if t.dim() == 5 else t.flatten(1) for t in ts] for ts in tensors(matrices)]
+        lr = {k: options[k] for k in ("lr",) if k in options}
+        return train.Muon(flat[0], flat[1], copies=flat[2], weight_decay=weight_decay, rest=rest, **lr, **muon)
 
     def train_step(self, optimizer, max_norm=None):
         """Forward, backward, with max_norm the gradients' norm (clipping, and no update where it is not finite), update."""
@@ -385,7 +455,7 @@ class UNet:
             self._where = "clip"
             self._c("train_grad_norm", optimizer.clip, max_norm)
         self._where = "optimizer"
-        self._c("train_adamw_step", optimizer.step)
+        self._c(getattr(optimizer, "call", "train_adamw_step"), optimizer.step)
         return self.loss
 
     def capture(self, optimizer=None, max_norm=None):
