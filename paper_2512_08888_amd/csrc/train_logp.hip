@@ -22,7 +22,8 @@ namespace rotconv {
 namespace {
 
 enum Mode { kFwd, kBwd, kPolicy };
-constexpr int kMostBlocks = 4096;      // of a launch; a workgroup's four sums each in the workspace
+constexpr int kMostBlocks = 8192;      // of a launch whose workgroups have four sums each in the workspace; others: kMostOthers
+constexpr int kMostOthers = 65536;
 
 struct LossArgs {
   const void* z;
@@ -168,12 +169,9 @@ __device__ __forceinline__ float element(const RowGrad& o, float z, bool label) 
 // does not wait for loads under way.
 __device__ __forceinline__ void arrived(float v) { asm volatile("" ::"v"(v)); }
 
-// Sums that were formed below the maximum t, for a larger one
+// Sums that were formed below the maximum t, for the larger of t and top.  (Sums of nothing, at -infinity, stay 0; a NaN stays.)
 __device__ __forceinline__ void moved_to(float top, float& t, float& s, float& h) {
-  if (!(top > t) || s == 0.f) {
-    t = fmaxf(t, top);
-    return;
-  }
+  top = fmaxf(t, top);
   const float by = bounded(exponent(t, top)), f = exp2_of(by);
   h = f * fmaf(by, s, h);
   s = f * s;
@@ -215,7 +213,7 @@ __device__ __forceinline__ void write_sums(const LossArgs& g, const double* acc)
   }
 }
 
-// Rows of few classes: G lanes to a row, E elements a lane, an element to a load (neighbouring rows lie side by side).
+// Rows of few classes: G lanes to a row, up to E elements a lane, an element to a load (neighbouring rows lie side by side).
 template <typename T, int G, int E, int MODE>
 __global__ __launch_bounds__(256) void k_rows_small(LossArgs g) {
   const int sub = threadIdx.x % G;
@@ -264,7 +262,7 @@ template <> struct Vec<float> {
   static constexpr int V = 4;
   static constexpr uint32_t kLowest = 0xff800000u;
   static __device__ __forceinline__ float get(const u4& a, int k) { return __uint_as_float(a[k]); }
-  static __device__ __forceinline__ void set(u4& a, int k, float v) { a[k] = __float_as_uint(v); }
+  static __device__ __forceinline__ void put(u4& a, int k, float v) { a[k] = __float_as_uint(v); }
   static __device__ __forceinline__ u4 pack(const float* v) {
     return u4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
   }
@@ -275,9 +273,9 @@ template <> struct Vec<uint16_t> {
   static __device__ __forceinline__ float get(const u4& a, int k) {
     return __uint_as_float(k % 2 ? a[k / 2] & 0xffff0000u : a[k / 2] << 16);
   }
-  static __device__ __forceinline__ void set(u4& a, int k, float v) {
-    const uint32_t b = f32_to_bf16(v);
-    a[k / 2] = k % 2 ? (a[k / 2] & 0xffffu) | b << 16 : (a[k / 2] & 0xffff0000u) | b;
+  static __device__ __forceinline__ void put(u4& a, int k, float v) {        // (a value that a bf16 number holds)
+    const uint32_t b = __float_as_uint(v);
+    a[k / 2] = k % 2 ? (a[k / 2] & 0xffffu) | (b & 0xffff0000u) : (a[k / 2] & 0xffff0000u) | b >> 16;
   }
   static __device__ __forceinline__ u4 pack(const float* v) {
     return u4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
@@ -290,9 +288,12 @@ __device__ __forceinline__ u4 load_part(const T* z, int first, int K) {        /
   u4 a;
 #pragma unroll
   for (int k = 0; k < 4; ++k) a[k] = Vec<T>::kLowest;
+  if (first + V <= 0 || first >= K) return a;
+  float v[V];                          // all of them under way at once, from inside the row
 #pragma unroll
-  for (int k = 0; k < V; ++k)
-    if (first + k >= 0 && first + k < K) Vec<T>::set(a, k, Elt<T>::ld(z + first + k));
+  for (int k = 0; k < V; ++k) v[k] = Elt<T>::ld(z + min(max(first + k, 0), K - 1));
+#pragma unroll
+  for (int k = 0; k < V; ++k) Vec<T>::put(a, k, first + k >= 0 && first + k < K ? v[k] : -INFINITY);
   return a;
 }
 template <typename T>
@@ -337,15 +338,18 @@ __device__ __forceinline__ u4 gradient(const RowGrad& o, const u4& a, int first,
   return Vec<T>::pack(d);
 }
 
-// Rows of many classes: a workgroup of B threads to a row, up to E vectors a thread in registers.  E = 0: rows of any
-// length, read twice (their sums are then formed with a running maximum).  ENT: somebody wants the entropy or its gradient.
+// Rows of many classes: B threads to a row, up to E vectors a thread in registers (those that no thread has are passed over).  64
+// threads: four rows to a workgroup.  E = 0: rows of any length, read twice (their sums are then formed with a running maximum).
+// ENT: somebody wants the entropy or its gradient.
 template <typename T, int B, int E, int MODE, bool ENT>
-__global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 : 8))) void k_rows(LossArgs g) {
-  constexpr int V = Vec<T>::V;
+__global__ __launch_bounds__(B == 64 ? 256 : B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 : 8))) void k_rows(LossArgs g) {
+  constexpr int V = Vec<T>::V, kRows = B == 64 ? 4 : 1;
+  const int tid = threadIdx.x % B, which = kRows == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / B);
   __shared__ float red[16];
-  __shared__ double acc[4];            // the first thread's
-  if (MODE == kPolicy && threadIdx.x == 0) acc[0] = acc[1] = acc[2] = acc[3] = 0;
-  for (size_t row = blockIdx.x; row < g.rows; row += gridDim.x) {
+  __shared__ double sums[kRows][4];    // the rows' first threads'
+  double* acc = sums[which];
+  if (MODE == kPolicy && tid == 0) acc[0] = acc[1] = acc[2] = acc[3] = 0;
+  for (size_t row = (size_t)blockIdx.x * kRows + which; row < g.rows; row += (size_t)gridDim.x * kRows) {
     const T* z = static_cast<const T*>(g.z) + row * g.K;
     T* dz = static_cast<T*>(g.dz) + row * g.K;
     // elements between the last 16-byte border and the row's start
@@ -358,16 +362,20 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
     if constexpr (E > 0) {
       u4 v[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = load_part(z, (int)(threadIdx.x + e * B) * V - shift, g.K);
+      for (int e = 0; e < E; ++e)
+        if (e * B * V < g.K + V - 1) v[e] = load_part(z, (tid + e * B) * V - shift, g.K);
       if constexpr (MODE != kBwd) {
 #pragma unroll
-        for (int e = 0; e < E; ++e)
+        for (int e = 0; e < E; ++e) {
+          if (e * B * V >= g.K + V - 1) continue;
 #pragma unroll
           for (int k = 0; k < V; ++k) t = fmaxf(t, Vec<T>::get(v[e], k));
+        }
         t = block_join<B, true>(t, red);
         const float from = origin(t);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
+          if (e * B * V >= g.K + V - 1) continue;
           packed(v[e]);
 #pragma unroll
           for (int k = 0; k < V; ++k) {
@@ -380,13 +388,14 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
         if constexpr (ENT) h = block_join<B, false>(h, red);
       }
       RowOut out;
-      const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, threadIdx.x == 0, acc);
-      if (threadIdx.x == 0) write_row<MODE>(g, row, out);
+      const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, tid == 0, acc);
+      if (tid == 0) write_row<MODE>(g, row, out);
       if (MODE != kFwd && g.dz) {
-        int from = (int)threadIdx.x * V - shift;
+        int from = tid * V - shift;
         asm volatile("" : "+v"(from));                 // (places are formed anew, not kept from the loads)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
+          if (e * B * V >= g.K + V - 1) continue;
           const int first = from + e * B * V;
           packed(v[e]);
           store_part(dz, o.live ? gradient<T, ENT>(o, v[e], first, r.label) : zero, first, g.K, g.alike);
@@ -394,7 +403,7 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
       }
     } else {
       if constexpr (MODE != kBwd) {
-        for (int first = (int)threadIdx.x * V - shift; first < g.K; first += B * V) {
+        for (int first = tid * V - shift; first < g.K; first += B * V) {
           const u4 v = load_part(z, first, g.K);
           float top = t;
 #pragma unroll
@@ -407,16 +416,20 @@ __global__ __launch_bounds__(B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 :
         s = block_join<B, false>(s, red), h = block_join<B, false>(h, red);
       }
       RowOut out;
-      const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, threadIdx.x == 0, acc);
-      if (threadIdx.x == 0) write_row<MODE>(g, row, out);
+      const RowGrad o = row_end<MODE>(g, r, t, s, h, za, &out, tid == 0, acc);
+      if (tid == 0) write_row<MODE>(g, row, out);
       if (MODE != kFwd && g.dz)
-        for (int first = (int)threadIdx.x * V - shift; first < g.K; first += B * V)
+        for (int first = tid * V - shift; first < g.K; first += B * V)
           store_part(dz, o.live ? gradient<T, ENT>(o, load_part(z, first, g.K), first, r.label) : zero, first, g.K, g.alike);
     }
   }
-  if (MODE == kPolicy && threadIdx.x == 0) {
-#pragma unroll
-    for (int k = 0; k < 4; ++k) g.part[4 * (size_t)blockIdx.x + k] = acc[k];
+  if constexpr (MODE == kPolicy) {
+    __syncthreads();
+    if (threadIdx.x < 4) {
+      double v = sums[0][threadIdx.x];
+      for (int r = 1; r < kRows; ++r) v += sums[r][threadIdx.x];
+      g.part[4 * (size_t)blockIdx.x + threadIdx.x] = v;
+    }
   }
 }
 
@@ -646,7 +659,8 @@ __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
 
 template <typename T, int V, int MODE>
 __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
-  __shared__ float shared[16][3][64 * V];
+  extern __shared__ float joined[];    // of several waves: t, s, h of each
+  auto shared = [&](int wave, int what, int at) -> float& { return joined[(wave * 3 + what) * 64 * V + at]; };
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
   double acc[4] = {};
   const size_t apart = (size_t)gridDim.x * 64 * V;
@@ -666,39 +680,43 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
           if (label >= 0 && label < g.K) za[i] = Elt<T>::ld(z + (size_t)label * g.P + i);
           arrived(za[i]);
         }
-        auto add = [&](const float* v) {
+        // eight classes at a time: their largest first, so that the sums move to it once
+        constexpr int U = 8;
+        for (int k = wave; k < g.K; k += U * waves) {
+          float v[U][V];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            if (k + u * waves < g.K) {
+              load_pixels<T, V>(z + (size_t)(k + u * waves) * g.P, v[u]);
+            } else {
+#pragma unroll
+              for (int i = 0; i < V; ++i) v[u][i] = -INFINITY;
+            }
+          }
 #pragma unroll
           for (int i = 0; i < V; ++i) {
-            moved_to(v[i], t[i], s[i], h[i]);
-            add_element(v[i], origin(t[i]), s[i], h[i]);
+            float top = v[0][i];
+#pragma unroll
+            for (int u = 1; u < U; ++u) top = fmaxf(top, v[u][i]);
+            moved_to(top, t[i], s[i], h[i]);
+            const float from = origin(t[i]);
+#pragma unroll
+            for (int u = 0; u < U; ++u) add_element(v[u][i], from, s[i], h[i]);
           }
-        };
-        int k = wave;
-        for (; k + 3 * waves < g.K; k += 4 * waves) {
-          float v[4][V];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) load_pixels<T, V>(z + (size_t)(k + u * waves) * g.P, v[u]);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) add(v[u]);
-        }
-        for (; k < g.K; k += waves) {
-          float v[V];
-          load_pixels<T, V>(z + (size_t)k * g.P, v);
-          add(v);
         }
       }
       if (waves > 1) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < V; ++i) shared[wave][0][lane * V + i] = t[i], shared[wave][1][lane * V + i] = s[i], shared[wave][2][lane * V + i] = h[i];
+        for (int i = 0; i < V; ++i) shared(wave, 0, lane * V + i) = t[i], shared(wave, 1, lane * V + i) = s[i], shared(wave, 2, lane * V + i) = h[i];
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < V; ++i) {
           float top = -INFINITY;
-          for (int w = 0; w < waves; ++w) top = fmaxf(top, shared[w][0][lane * V + i]);
+          for (int w = 0; w < waves; ++w) top = fmaxf(top, shared(w, 0, lane * V + i));
           s[i] = h[i] = 0.f, t[i] = top;
           for (int w = 0; w < waves; ++w) {
-            float tw = shared[w][0][lane * V + i], sw = shared[w][1][lane * V + i], hw = shared[w][2][lane * V + i];
+            float tw = shared(w, 0, lane * V + i), sw = shared(w, 1, lane * V + i), hw = shared(w, 2, lane * V + i);
             moved_to(top, tw, sw, hw);
             s[i] += sw, h[i] += hw;
           }
@@ -717,12 +735,20 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
     }
     if (MODE != kFwd && g.dz) {
       T* dz = static_cast<T*>(g.dz) + at;
-      for (int k = wave; k < g.K; k += waves) {
-        float v[V];
-        load_pixels<T, V>(z + (size_t)k * g.P, v);
+      constexpr int U = 4;
+      for (int k = wave; k < g.K; k += U * waves) {
+        float v[U][V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = o[i].live ? element(o[i], v[i], k == r[i].label) : 0.f;
-        store_pixels<T, V>(dz + (size_t)k * g.P, v);
+        for (int u = 0; u < U; ++u)
+          if (k + u * waves < g.K) load_pixels<T, V>(z + (size_t)(k + u * waves) * g.P, v[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int at = k + u * waves;
+          if (at >= g.K) continue;
+#pragma unroll
+          for (int i = 0; i < V; ++i) v[u][i] = o[i].live ? element(o[i], v[u][i], at == r[i].label) : 0.f;
+          store_pixels<T, V>(dz + (size_t)at * g.P, v[u]);
+        }
       }
     }
   }
@@ -752,17 +778,18 @@ __global__ __launch_bounds__(1024) void k_policy_end(const double* __restrict__ 
 
 int finish() { return hipGetLastError() == hipSuccess ? ROTCONV_OK : ROTCONV_ERR_LAUNCH; }
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-unsigned blocks_for(size_t n) { return (unsigned)std::min<size_t>(n, kMostBlocks); }
+template <int MODE> unsigned blocks_for(size_t n) { return (unsigned)std::min<size_t>(n, MODE == kPolicy ? kMostBlocks : kMostOthers); }
 
 template <typename T, int B, int E, int MODE>
 void launch_rows(const LossArgs& g, unsigned* blocks, hipStream_t st) {
-  *blocks = blocks_for(g.rows);
+  constexpr int kRows = B == 64 ? 4 : 1;
+  *blocks = blocks_for<MODE>((g.rows + kRows - 1) / kRows);
   const bool entropy = MODE == kFwd ? g.ent_out != nullptr : MODE == kBwd ? g.dent != nullptr : g.entc != 0.f;
-  (entropy ? k_rows<T, B, E, MODE, true> : k_rows<T, B, E, MODE, false>)<<<*blocks, B, 0, st>>>(g);
+  (entropy ? k_rows<T, B, E, MODE, true> : k_rows<T, B, E, MODE, false>)<<<*blocks, B * kRows, 0, st>>>(g);
 }
 template <typename T, int G, int E, int MODE>
 void launch_small(const LossArgs& g, unsigned* blocks, hipStream_t st) {
-  *blocks = blocks_for((g.rows + 256 / G - 1) / (256 / G));
+  *blocks = blocks_for<MODE>((g.rows + 256 / G - 1) / (256 / G));
   k_rows_small<T, G, E, MODE><<<*blocks, 256, 0, st>>>(g);
 }
 
@@ -787,11 +814,13 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
       return;
     }
     if (g.K <= 8) launch_small<T, 1, 8, MODE>(g, blocks, st);
+    else if (g.K <= 32) launch_small<T, 8, 4, MODE>(g, blocks, st);
     else if (g.K <= 64) launch_small<T, 8, 8, MODE>(g, blocks, st);
-    else if (g.K <= 512) launch_small<T, 64, 8, MODE>(g, blocks, st);
-    else if (vecs <= 64 * 4) launch_rows<T, 64, 4, MODE>(g, blocks, st);
-    else if (vecs <= 256 * 4) launch_rows<T, 256, 4, MODE>(g, blocks, st);
-    else if (vecs <= 1024 * 4) launch_rows<T, 1024, 4, MODE>(g, blocks, st);
+    else if (g.K <= 128) launch_small<T, 16, 8, MODE>(g, blocks, st);
+    else if (g.K <= 256) launch_small<T, 32, 8, MODE>(g, blocks, st);
+    else if (g.K <= 384) launch_small<T, 64, 8, MODE>(g, blocks, st);
+    else if (vecs <= 64 * 8) launch_rows<T, 64, 8, MODE>(g, blocks, st);
+    else if (vecs <= 256 * 8) launch_rows<T, 256, 8, MODE>(g, blocks, st);
     else if (vecs <= 1024 * 8) launch_rows<T, 1024, 8, MODE>(g, blocks, st);
     else if (vecs <= 1024 * 16) launch_rows<T, 1024, 16, MODE>(g, blocks, st);
     else launch_rows<T, 1024, 0, MODE>(g, blocks, st);
@@ -804,18 +833,18 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
     four = four && !misaligned(p, 16);
   four = four && (g.per_image || !misaligned(g.adv, 16));
   if (g.K <= 16) {
-    *blocks = blocks_for((g.rows + 256 * (four ? 4 : 1) - 1) / (256 * (four ? 4 : 1)));
+    *blocks = blocks_for<MODE>((g.rows + 256 * (four ? 4 : 1) - 1) / (256 * (four ? 4 : 1)));
     auto kernel = four ? (g.K <= 4 ? k_planes<T, 4, 4, MODE> : g.K <= 6 ? k_planes<T, 4, 6, MODE> : g.K <= 8 ? k_planes<T, 4, 8, MODE>
                                                              : g.K <= 12 ? k_planes<T, 4, 12, MODE> : k_planes<T, 4, 16, MODE>)
                        : (g.K <= 8 ? k_planes<T, 1, 8, MODE> : k_planes<T, 1, 16, MODE>);
     kernel<<<*blocks, 256, 0, st>>>(g);
   } else {
     const size_t strips = (g.rows + 64 * (four ? 4 : 1) - 1) / (64 * (four ? 4 : 1));
-    *blocks = blocks_for(strips);
+    *blocks = blocks_for<MODE>(strips);
     int waves = 1;                     // until the chip has its fill of them, or a wave would have too few classes
     while (waves < 16 && strips * waves < 4096 && g.K / waves >= 16) waves *= 2;
     auto kernel = four ? k_planes_long<T, 4, MODE> : k_planes_long<T, 1, MODE>;
-    kernel<<<*blocks, 64 * waves, 0, st>>>(g);
+    kernel<<<*blocks, 64 * waves, waves > 1 ? waves * 3 * 64 * (four ? 4 : 1) * sizeof(float) : 0, st>>>(g);
   }
 }
 
