@@ -74,7 +74,8 @@ int train_diag_groupnorm_wait(int ticks);
  * name the further ones.  A NaN or a +infinity makes its own row's results NaN.
  * Refused (ROTCONV_ERR_SHAPE): N or K below 1, P of 0, K above 2^24, N * P of 2^31 or more. */
 
-/* scratch that train_logp_fwd and train_policy_loss need, whatever the layout and storage type; 0 for extents that are refused */
+/* scratch that train_logp_fwd and train_policy_loss need, whatever the layout and storage type; 0 for extents that are refused.  One serves
+ * calls of one stream at a time. */
 size_t train_logp_workspace_bytes(int N, int K, size_t P);
 /* logp, entropy: fp32 [N, P]; stat: fp32 [N, P, 2], t and l, which the backward call reads.  entropy and stat may be NULL.
  * Left out beside those without a label: rows whose logits are all -infinity (their t is kept as it is, -infinity). */
@@ -210,8 +211,10 @@ typedef struct {
 
 typedef struct train_matrices train_matrices;
 
-/* As train_list_create.  Refused (ROTCONV_ERR_SHAPE): extents below 1, the shorter side of a matrix above 32768, the longer above 2^24,
- * stacks of more than 2^40 elements, more matrices than 65535 or more work than 2^24 - 1 workgroups do. */
+/* As train_list_create; one handle and one workspace serve calls of one stream at a time.  Refused (ROTCONV_ERR_UNSUPPORTED): params and
+ * copies that overlap one another.  Refused (ROTCONV_ERR_SHAPE): extents below 1, the shorter side of a matrix above 32768, the longer above 2^24,
+ * stacks of more than 2^40 elements, more matrices than 65535 or more work than 2^24 - 1 workgroups do (of 128 x 128 elements; sixteen
+ * to each of A's). */
 int train_matrices_create(const train_matrix* matrices, int count, int grad_dtype, train_matrices** out);
 int train_matrices_destroy(train_matrices* matrices);
 /* Elements that the momentum spans: stack k's start at the sum of the sizes before it, each size rounded up to a

@@ -743,9 +743,19 @@ def _row_values(what, name, t, n, dtype=None):
     """Address of a tensor of n values (fp32 unless dtype says otherwise), one for each row; None stays NULL."""
     if t is None:
         return None
-    if t.dtype is not (dtype or _f32) or t.numel() != n or not t.is_contiguous() or not t.is_cuda:
-        raise ValueError(f"{what}: {name} must be {str(dtype or _f32)[6:]}, contiguous, on the GPU, with {n} elements")
+    if t.dtype is not (dtype or _f32) or t.numel() != n or not t.is_contiguous() or t.get_device() != _device():
+        raise ValueError(f"{what}: {name} must be {str(dtype or _f32)[6:]}, contiguous, on the current GPU, with {n} elements")
     return t.data_ptr()
+
+
+def _device() -> int:
+    """Number of the current device."""
+    import torch
+
+    try:
+        return torch._C._cuda_getDevice()
+    except AttributeError:
+        return torch.cuda.current_device()
 
 
 def _loss(what, logits, dlogits, labels, ws, scratch):
@@ -763,10 +773,12 @@ def _loss(what, logits, dlogits, labels, ws, scratch):
     P = logits.numel() // (N * K) if N * K else 0
     if kind is not _f32 and kind is not _bf16:
         raise TypeError(f"{what}: logits must be float32 or bfloat16, got {kind}")
-    at = _row_values(what, "labels", labels, N * P, _i32)
     home = logits.get_device()
-    if labels.get_device() != home or (dlogits is not None and dlogits.get_device() != home):
-        raise ValueError(f"{what}: labels and dlogits must be on the logits' device")
+    if home != _device():
+        raise ValueError(f"{what}: logits must be on the current device")
+    at = _row_values(what, "labels", labels, N * P, _i32)
+    if dlogits is not None and dlogits.get_device() != home:
+        raise ValueError(f"{what}: dlogits must be on the logits' device")
     if scratch:
         if ws is None:
             import torch

@@ -22,6 +22,7 @@
 #include <cstdint>
 #include <new>
 #include <type_traits>
+#include <utility>
 #include <vector>
 
 #include "glue_elt.h"
@@ -910,6 +911,17 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
   }
   train_matrices* l = nullptr;
   try {
+    // Nothing that a step writes may be there twice: two workgroups would write it.
+    std::vector<std::pair<uintptr_t, uintptr_t>> written;
+    for (int k = 0; k < count; ++k) {
+      const train_matrix& t = matrices[k];
+      const uintptr_t n = (uintptr_t)t.count * (uintptr_t)t.rows * (uintptr_t)t.cols, p = reinterpret_cast<uintptr_t>(t.param);
+      written.emplace_back(p, p + n * sizeof(float));
+      if (t.copy) written.emplace_back(reinterpret_cast<uintptr_t>(t.copy), reinterpret_cast<uintptr_t>(t.copy) + n * sizeof(uint16_t));
+    }
+    std::sort(written.begin(), written.end());
+    for (size_t k = 1; k < written.size(); ++k)
+      if (written[k].first < written[k - 1].second) return ROTCONV_ERR_UNSUPPORTED;
     std::vector<Matrix> mats;
     std::vector<Tile> chunk, turn;
     std::vector<Unit> gram, poly, apply;

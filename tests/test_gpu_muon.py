@@ -17,8 +17,11 @@ from paper_2512_08888_amd import train
 pytestmark = pytest.mark.gpu
 U = 2.0 ** -24
 # (count, rows, cols)
-STACKS = [(1, 64, 576), (2, 16, 144), (1, 6, 64), (1, 1, 1), (1, 1, 70), (1, 70, 1), (3, 5, 3), (1, 64, 27), (1, 130, 129), (1, 128, 256),
-          (1, 33, 65), (2, 65, 33), (1, 200, 300)]
+SMALL = [(1, 64, 576), (2, 16, 144), (1, 6, 64), (1, 1, 1), (1, 1, 70), (1, 70, 1), (3, 5, 3), (1, 64, 27), (1, 33, 65), (2, 65, 33)]
+# a workgroup keeps a matrix (16, 32 and 64 blocks of 32 x 32), or launches of products serve all of them
+LISTS = {"block": [(1, 20, 500), (1, 500, 20), (2, 30, 40)], "two": [(1, 64, 512), (1, 480, 50), (1, 33, 64)],
+         "least": SMALL + [(1, 64, 1024), (1, 1024, 64), (1, 1000, 63), (1, 40, 1001)],
+         "all": SMALL + [(1, 130, 129), (1, 128, 256), (1, 200, 300), (1, 65, 64), (1, 64, 1025)]}
 
 
 class Net:
@@ -84,8 +87,10 @@ def rms(stacks):
 
 @pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("shift,nesterov,steps", [(0, True, 5), (1, False, 5), (3, True, 1), (0, False, 2)])
-def test_steps(grad, shift, nesterov, steps):
-    net = Net(STACKS, grad, copy=True, shift=shift, seed=1)
+@pytest.mark.parametrize("stacks", LISTS)
+def test_steps(grad, shift, nesterov, steps, stacks):
+    stacks = LISTS[stacks]
+    net = Net(stacks, grad, copy=True, shift=shift, seed=1)
     lr, mu, wd = (float(np.float32(v)) for v in (0.05, 0.9, 0.1))
     opt = train.Muon(net.params, net.grads, lr=lr, momentum=mu, nesterov=nesterov, weight_decay=wd, steps=steps, copies=net.copies)
     opt.work.fill_(0xff)                                        # whatever the workspace held: fp16 NaN here
@@ -93,9 +98,9 @@ def test_steps(grad, shift, nesterov, steps):
         net.new_grads()
         coef = float(np.float32(0.7)) if k == 1 else 1.0
         opt.coef.fill_(coef)
-        before, m0 = net.read(net.params), cut(opt.m, STACKS)
+        before, m0 = net.read(net.params), cut(opt.m, stacks)
         opt.step()
-        check_step(net, before, m0, net.read(net.params), cut(opt.m, STACKS), lr, mu, nesterov, wd, rms(STACKS), coef, steps)
+        check_step(net, before, m0, net.read(net.params), cut(opt.m, stacks), lr, mu, nesterov, wd, rms(stacks), coef, steps)
         for p, c in zip(net.params, net.copies):
             assert torch.equal(c, p.to(torch.bfloat16))
         assert net.intact() and opt.step_count.item() == k + 1
@@ -163,8 +168,8 @@ def test_zero_gradients_decay_only():
     assert (opt.m == 0).all()
 
 
-def test_nan_stays_in_its_matrix_and_a_bad_norm_skips_the_step():
-    stacks = [(3, 20, 50), (1, 60, 30)]
+@pytest.mark.parametrize("stacks", [[(3, 20, 50), (1, 60, 30)], [(3, 20, 50), (1, 60, 30), (1, 140, 200)]])
+def test_nan_stays_in_its_matrix_and_a_bad_norm_skips_the_step(stacks):
     net = Net(stacks, seed=7)
     net.grads[0][1, 3, 4] = float("nan")
     opt = train.Muon(net.params, net.grads, lr=0.1)
@@ -178,10 +183,11 @@ def test_nan_stays_in_its_matrix_and_a_bad_norm_skips_the_step():
     assert all(t.all() for t in ok) and torch.isnan(net.params[0][1]).all() and opt.step_count.item() == 1
 
 
-def test_the_rest_shares_the_control_block():
+@pytest.mark.parametrize("stacks", [[(1, 24, 40), (2, 10, 7)], [(1, 24, 40), (1, 200, 65)]])
+def test_the_rest_shares_the_control_block(stacks):
     """Clipping over all gradients, Muon for the matrices and AdamW for the rest, as each alone with that factor."""
     def build():
-        net, other = Net([(1, 24, 40), (2, 10, 7)], seed=8), Net([(1, 1, 50), (1, 1, 9)], seed=9)
+        net, other = Net(stacks, seed=8), Net([(1, 1, 50), (1, 1, 9)], seed=9)
         return net, other, [p.view(-1) for p in other.params], [g.view(-1) for g in other.grads]
 
     net, other, ps, gs = build()
@@ -247,8 +253,8 @@ def test_a_matrix_alone_and_among_others():
     assert max(lengths) <= 5.0 ** 5 * 2.0 ** -21
 
 
-def test_graph_and_streams():
-    stacks = [(1, 64, 200), (1, 150, 40)]
+@pytest.mark.parametrize("stacks", [[(1, 64, 200), (1, 150, 40)], [(1, 64, 200), (1, 150, 2000), (1, 300, 70)]])
+def test_graph_and_streams(stacks):
     net, twin = Net(stacks, seed=13), Net(stacks, seed=13)
     opt, eager = train.Muon(net.params, net.grads, lr=0.1), train.Muon(twin.params, twin.grads, lr=0.1)
     side = torch.cuda.Stream()

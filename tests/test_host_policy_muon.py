@@ -88,6 +88,10 @@ def test_matrices_refusals():
                 (16, 32, None, 1, 5, 7, 0.0, NAN, 0), (16, 32, None, 1, 5, 7, 0.0, 1.0, 1), (18, 32, None, 1, 5, 7, 0.0, 1.0, 0),
                 (16, 34, None, 1, 5, 7, 0.0, 1.0, 0), (16, 32, 33, 1, 5, 7, 0.0, 1.0, 0)):
         assert matrices([bad]) == rc.ERR_UNSUPPORTED, bad
+    # what a step writes, named twice: the same matrix, one inside a stack, a copy over another's parameters
+    for pair in ((good, good), ((4096, 32, None, 3, 4, 4, 0.0, 1.0, 0), (4096 + 64, 32, None, 1, 4, 4, 0.0, 1.0, 0)),
+                 ((4096, 32, None, 1, 4, 4, 0.0, 1.0, 0), (8192, 32, 4096 + 32, 1, 4, 4, 0.0, 1.0, 0))):
+        assert matrices(list(pair)) == rc.ERR_UNSUPPORTED, pair
     assert L.train_matrices_destroy(None) == rc.OK
     assert L.train_matrices_elements(None) == 0 and L.train_matrices_workspace_bytes(None) == 0
     o = rc.TrainMuon(0.9, 1e-12, 1, 5, 0, 0)
@@ -111,6 +115,38 @@ def test_binding_refusals():
                     (torch.zeros(3, 4), torch.zeros(3, 4), torch.zeros(3, 4)), (torch.zeros(3, 4).half(), torch.zeros(3, 4), None)):
         with pytest.raises(TypeError):
             rc.TrainMatrices([g], [p], 1.0, None if c is None else [c])
+
+
+class Elsewhere:
+    """What the bindings ask of a tensor, for one on a device that is not the current one."""
+
+    def __init__(self, t, device):
+        self.t, self.device_number, self.is_cuda = t, device, True
+        self.shape, self.dtype = t.shape, t.dtype
+
+    def get_device(self):
+        return self.device_number
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_binding_refuses_other_devices(monkeypatch):
+    import torch
+
+    monkeypatch.setattr(rc, "_device", lambda: 0)
+    z, labels, one = torch.zeros(4, 6), torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    here = lambda t: Elsewhere(t, 0)  # noqa: E731
+    with pytest.raises(ValueError, match="current device"):
+        rc.train_logp_fwd(Elsewhere(z, 1), Elsewhere(labels, 1), Elsewhere(one, 1))
+    with pytest.raises(ValueError, match="labels"):
+        rc.train_logp_fwd(here(z), Elsewhere(labels, 1), here(one), ws=here(torch.zeros(1 << 19, dtype=torch.uint8)))
+    with pytest.raises(ValueError, match="logp"):
+        rc.train_logp_fwd(here(z), here(labels), Elsewhere(one, 1), ws=here(torch.zeros(1 << 19, dtype=torch.uint8)))
+    with pytest.raises(ValueError, match="dlogits"):
+        rc.train_policy_loss(here(z), here(labels), here(one), here(one), Elsewhere(z, 1))
+    with pytest.raises(ValueError, match="workspace"):
+        rc.train_policy_loss(here(z), here(labels), here(one), here(one), ws=Elsewhere(torch.zeros(1 << 19, dtype=torch.uint8), 1))
 
 
 def differences(f, x, h=1e-6):
