@@ -750,12 +750,15 @@ def _row_values(what, name, t, n, dtype=None):
 
 def _device() -> int:
     """Number of the current device."""
-    import torch
+    global _current
+    if _current is None:
+        import torch
 
-    try:
-        return torch._C._cuda_getDevice()
-    except AttributeError:
-        return torch.cuda.current_device()
+        _current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _current()
+
+
+_current = None
 
 
 def _loss(what, logits, dlogits, labels, ws, scratch):
