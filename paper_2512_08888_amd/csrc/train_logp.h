@@ -293,7 +293,7 @@ template <> struct Vec<uint16_t> {
 };
 // The vector of a row at `border` (the same for all lanes, so that addresses take no registers) + `off` elements; its first element is the
 // row's number `first`.  -infinity outside the row.  EVEN: rows start on borders and are whole vectors; nothing is asked of an end then,
-// and no registers are kept for it (4096 x 65536 bf16 logits, loss: XXX us, and 240 with the ends' code and addresses beside).
+// and no registers are kept for it (4096 x 65536 bf16 logits, loss: 201 us, and 240 with the ends' code and addresses beside).
 template <typename T, bool EVEN = false>
 __device__ __forceinline__ u4 load_part(const T* border, uint32_t off, int first, int K) {
   constexpr int V = Vec<T>::V;
@@ -841,6 +841,9 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
       k_rest<T, MODE><<<dim3(MODE == kFwd || !g.dz ? 1 : parts, *blocks), kPartThreads, 0, st>>>(g, parts);
       return;
     }
+    // The fewest threads whose eight vectors are a row: loads under way and workgroups at other stages are many then.  (Rows of half a
+    // workgroup's vectors in one of twice the threads: 4096 x 32768 bf16 forward 67 us, so 54; loss 138 and 116; 8192 x 9000 fp32 84 and 50,
+    // 151 and 124.)  Rows of up to 384 classes go to a part of a wave, element by element: vectors of so short rows are mostly ends.
     if (g.K <= 8) launch_small<T, 1, 8, MODE>(g, blocks, st);
     else if (g.K <= 32) launch_small<T, 8, 4, MODE>(g, blocks, st);
     else if (g.K <= 64) launch_small<T, 8, 8, MODE>(g, blocks, st);
@@ -848,7 +851,9 @@ void launch_loss(const LossArgs& g, bool rows, unsigned* blocks, hipStream_t st)
     else if (g.K <= 256) launch_small<T, 32, 8, MODE>(g, blocks, st);
     else if (g.K <= 384) launch_small<T, 64, 8, MODE>(g, blocks, st);
     else if (vecs <= 64 * 8) launch_rows<T, 64, 8, MODE>(g, blocks, st);
+    else if (vecs <= 128 * 8) launch_rows<T, 128, 8, MODE>(g, blocks, st);
     else if (vecs <= 256 * 8) launch_rows<T, 256, 8, MODE>(g, blocks, st);
+    else if (vecs <= 512 * 8) launch_rows<T, 512, 8, MODE>(g, blocks, st);
     else if (vecs <= 1024 * 8) launch_rows<T, 1024, 8, MODE>(g, blocks, st);
     else if (vecs <= 1024 * 16) launch_rows<T, 1024, 16, MODE>(g, blocks, st);
     else launch_rows<T, 1024, 0, MODE>(g, blocks, st);
