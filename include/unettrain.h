@@ -72,6 +72,8 @@ int train_diag_groupnorm_wait(int ticks);
  * Logits of -infinity are classes that cannot be taken: p_j = 0, and p_j ln p_j counts as 0.  A row is left out (its outputs 0,
  * its logits' gradient 0, nothing in any sum, whatever it holds) where its label lies outside 0..K-1; the notes at the calls
  * name the further ones.  A NaN or a +infinity makes its own row's results NaN.
+ * What a call writes (its scratch too) overlaps nothing that it reads and nothing else that it writes, but for gradients in the place of
+ * their logits, at the same address: anything else is refused (ROTCONV_ERR_UNSUPPORTED).
  * Refused (ROTCONV_ERR_SHAPE): N or K below 1, P of 0, K above 2^24, N * P of 2^31 or more. */
 
 /* scratch that train_logp_fwd and train_policy_loss need, whatever the layout and storage type; 0 for extents that are refused.  One serves
@@ -83,7 +85,7 @@ int train_logp_fwd(const float* logits, const int32_t* labels, float* logp, floa
                    size_t P, int layout, void* ws, size_t ws_bytes, void* stream);
 /* dlogits_j = dlogp (1[j = label] - p_j) - dentropy p_j (ln p_j + entropy)
  * stat, entropy: what the forward call wrote.  dentropy may be NULL (none), and entropy is read only beside it.
- * dlogits may be the logits themselves (same address), but overlap nothing else.  Left out too: rows whose t is -infinity, and
+ * dlogits may be the logits themselves (same address).  Left out too: rows whose t is -infinity, and
  * rows whose dlogp and dentropy are 0. */
 int train_logp_bwd(const float* logits, const int32_t* labels, const float* stat, const float* entropy,
                    const float* dlogp, const float* dentropy, float* dlogits, int N, int K, size_t P, int layout,
@@ -107,7 +109,7 @@ typedef struct {
  *     dlogits_j = w (G (1[j = label] - p_j) + entropy p_j (ln p_j + H)),      G = (cut ? 0 : -A r) + kl (1 - exp(q))
  * weight: fp32 [N, P], or NULL for 1 / (N P); the caller's own normalisation and mask.  Left out too: rows of weight 0, and rows
  * whose logits are all -infinity.  logp: fp32 [N, P] or NULL.  advantage: fp32 [N, P] or [N].  out: fp32 [4], sums in 64 bits.
- * dlogits may be the logits themselves, but overlap nothing else; NULL where only the loss is wanted. */
+ * dlogits may be the logits themselves; NULL where only the loss is wanted. */
 int train_policy_loss(const float* logits, const int32_t* labels, const float* advantage, const float* logp_old,
                       const float* logp_ref, const float* weight, float* out, float* dlogits, float* logp, int N, int K,
                       size_t P, int layout, const train_policy* options, void* ws, size_t ws_bytes, void* stream);

@@ -1,5 +1,7 @@
 // Log-probabilities of labels, forward and backward: their launches, and the entry points of these and of the policy loss (see
 // include/unettrain.h).  The kernels are train_logp.h's.
+#include <initializer_list>
+
 #include "train_logp.h"
 
 namespace rotconv {
@@ -31,6 +33,24 @@ int check(const LossArgs& g, int N, int K, size_t P, int layout) {
     if (misaligned(p, 4)) return ROTCONV_ERR_UNSUPPORTED;
   return ROTCONV_OK;
 }
+struct Span {
+  const void* p;                       // NULL: none
+  size_t bytes;
+};
+// Whether something that a call writes lies in what it reads, or in another thing that it writes.
+bool overlapping(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t p = reinterpret_cast<uintptr_t>(a.p), q = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && p < q + b.bytes && q < p + a.bytes;
+  };
+  for (const Span* a = written.begin(); a != written.end(); ++a) {
+    for (const Span* b = written.begin(); b != a; ++b)
+      if (meet(*a, *b)) return true;
+    for (const Span& b : read)
+      if (meet(*a, b)) return true;
+  }
+  return false;
+}
 LossArgs arguments(const void* z, void* dz, const int32_t* labels, int N, int K, size_t P) {
   LossArgs g = {};
   g.z = z, g.dz = dz, g.labels = labels, g.K = K, g.P = P, g.rows = (size_t)N * P;
@@ -47,6 +67,9 @@ int logp_fwd_t(const T* z, const int32_t* labels, float* logp, float* entropy, f
   g.logp = logp, g.ent_out = entropy, g.stat_out = stat;
   if (int e = check<T>(g, N, K, P, layout)) return e;
   if (!ws || misaligned(ws, 16) || ws_bytes < workspace(g.rows, K)) return ROTCONV_ERR_WORKSPACE;
+  const size_t row = g.rows * 4, all = g.rows * K * sizeof(T);
+  if (overlapping({{logp, row}, {entropy, row}, {stat, 2 * row}, {ws, workspace(g.rows, K)}}, {{z, all}, {labels, row}}))
+    return ROTCONV_ERR_UNSUPPORTED;
   place(g, ws);
   unsigned blocks;
   launch_loss<T, kFwd>(g, in_rows(layout, P), &blocks, static_cast<hipStream_t>(stream));
@@ -59,6 +82,10 @@ int logp_bwd_t(const T* z, const int32_t* labels, const float* stat, const float
   LossArgs g = arguments(z, dz, labels, N, K, P);
   g.stat = stat, g.ent = entropy, g.dlogp = dlogp, g.dent = dentropy;
   if (int e = check<T>(g, N, K, P, layout)) return e;
+  const size_t row = g.rows * 4, all = g.rows * K * sizeof(T);
+  if (overlapping({{dz, all}}, {{z == dz ? nullptr : z, all}, {labels, row}, {stat, 2 * row}, {dlogp, row}, {dentropy, row},
+                                {dentropy ? entropy : nullptr, row}}))
+    return ROTCONV_ERR_UNSUPPORTED;
   unsigned blocks;
   launch_loss<T, kBwd>(g, in_rows(layout, P), &blocks, static_cast<hipStream_t>(stream));
   return finish();
@@ -76,6 +103,11 @@ int policy_loss_t(const T* z, const int32_t* labels, const float* advantage, con
       misaligned(out, 4))
     return ROTCONV_ERR_UNSUPPORTED;
   if (!ws || misaligned(ws, 16) || ws_bytes < workspace(g.rows, K)) return ROTCONV_ERR_WORKSPACE;
+  const size_t row = g.rows * 4, all = g.rows * K * sizeof(T);
+  if (overlapping({{dz, all}, {logp, row}, {out, 4 * sizeof(float)}, {ws, workspace(g.rows, K)}},
+                  {{z == dz ? nullptr : z, all}, {labels, row}, {advantage, o->per_image ? (size_t)N * 4 : row}, {logp_old, row}, {logp_ref, row},
+                   {weight, row}}))
+    return ROTCONV_ERR_UNSUPPORTED;
   g.per_image = o->per_image, g.low = 1.f - o->clip_low, g.high = 1.f + o->clip_high, g.kl = o->kl, g.entc = o->entropy;
   g.unit = (float)(1.0 / ((double)N * (double)P));
   place(g, ws);

@@ -4,6 +4,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import train_oracle as to
 from paper_2512_08888_amd import binding as rc
@@ -33,6 +34,29 @@ def loss(z=16, labels=16, adv=16, old=None, ref=None, w=None, out=16, dz=None, l
 
 
 SHAPES = [dict(N=0), dict(N=-1), dict(K=0), dict(K=-3), dict(P=0), dict(K=(1 << 24) + 1), dict(P=1 << 31), dict(N=1 << 16, P=1 << 15), dict(P=1 << 63)]
+
+
+@pytest.mark.parametrize("bf16", (False, True))
+def test_outputs_in_each_others_place_are_refused(bf16):
+    """2 images of 4 classes, 4 pixels: 32 logits, 8 rows (nothing is read or written: a call is refused, or there is no device)."""
+    z, labels, adv, logp, stat, ent, out, dz = (1 << 20 | k << 10 for k in range(8))
+    ws, size = 1 << 30, 1 << 22
+    ok = lambda code: code != rc.ERR_UNSUPPORTED
+    if not torch.cuda.is_available():                      # (addresses of nothing: no launch may get them)
+        assert ok(fwd(z, labels, logp, ent, stat, ws=ws, size=size, bf16=bf16))
+        assert ok(bwd(z, labels, stat, ent, adv, adv, dz, bf16=bf16)) and ok(bwd(z, labels, stat, None, adv, None, z, bf16=bf16))
+        assert ok(loss(z, labels, adv, logp, logp, adv, out, dz, ent, ws=ws, size=size, bf16=bf16))
+        assert ok(loss(z, labels, adv, out=out, dz=z, ws=ws, size=size, bf16=bf16))
+    end = 32 * (2 if bf16 else 4)
+    bad = [lambda: fwd(z, labels, z + end - 4, ws=ws, size=size, bf16=bf16), lambda: fwd(z, labels, logp, logp + 28, ws=ws, size=size, bf16=bf16),
+           lambda: fwd(z, labels, logp, None, labels - 60, ws=ws, size=size, bf16=bf16), lambda: fwd(z, labels, ws, ws=ws, size=size, bf16=bf16),
+           lambda: bwd(z, labels, stat, None, adv, None, z + 4, bf16=bf16), lambda: bwd(z, labels, stat, None, adv, None, labels, bf16=bf16),
+           lambda: bwd(z, labels, stat, ent, adv, adv, ent, bf16=bf16),
+           lambda: loss(z, labels, adv, logp, out=out, logp=logp, ws=ws, size=size, bf16=bf16),
+           lambda: loss(z, labels, adv, out=out, dz=z - 4, ws=ws, size=size, bf16=bf16),
+           lambda: loss(z, labels, adv, out=z, dz=z, ws=ws, size=size, bf16=bf16),
+           lambda: loss(z, labels, adv, out=out, dz=dz, logp=out - 28, ws=ws, size=size, bf16=bf16)]
+    assert [call() for call in bad] == [rc.ERR_UNSUPPORTED] * len(bad)
 
 
 @pytest.mark.parametrize("bf16", [False, True])
