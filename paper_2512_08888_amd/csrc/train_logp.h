@@ -204,20 +204,21 @@ template <int G> __device__ __forceinline__ float lanes_sum(float v) {
   for (int k = G / 2; k > 0; k /= 2) v += __shfl_xor(v, k);
   return v;
 }
-// the four sums of a workgroup, to its place in the workspace
+// The four sums of a workgroup, to its place in the workspace.  Half of a wave's lanes take two of the sums, half of these one: 7 exchanges
+// instead of 24.
 __device__ __forceinline__ void write_sums(const LossArgs& g, const double* acc) {
   __shared__ double red[16][4];
-  const int wave = threadIdx.x / 64, waves = (blockDim.x + 63) / 64;
+  const int lane = threadIdx.x % 64, waves = (blockDim.x + 63) / 64;
+  const bool upper = lane & 32, odd = lane & 16;
+  const double a = (upper ? acc[2] : acc[0]) + __shfl_xor(upper ? acc[0] : acc[2], 32);
+  const double b = (upper ? acc[3] : acc[1]) + __shfl_xor(upper ? acc[1] : acc[3], 32);
+  double v = (odd ? b : a) + __shfl_xor(odd ? a : b, 16);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    double v = acc[k];
-#pragma unroll
-    for (int o = 32; o > 0; o /= 2) v += __shfl_xor(v, o);
-    if (threadIdx.x % 64 == 0) red[wave][k] = v;
-  }
+  for (int o = 8; o > 0; o /= 2) v += __shfl_xor(v, o);
+  if (lane % 16 == 0) red[threadIdx.x / 64][lane / 16] = v;
   __syncthreads();
   if (threadIdx.x < 4) {
-    double v = 0;
+    v = 0;
     for (int w = 0; w < waves; ++w) v += red[w][threadIdx.x];
     g.part[4 * (size_t)blockIdx.x + threadIdx.x] = v;
   }
@@ -616,7 +617,7 @@ __device__ __forceinline__ void store_rows(float* p, size_t row, const float* v)
 }
 // Classes behind the last are -infinity, so that nothing but their loads and stores asks for K; x and its exponential are kept from the
 // sums for the gradient (the 4 x 6 x 512 x 512 logits of a stack, bf16, with a reference and weights: 19.3 us where both were formed again and every
-// class asked, bound by instructions).
+// class asked, bound by instructions; 13.9 so).
 template <typename T, int V, int KM, int MODE>
 __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
   double acc[4] = {};
@@ -647,6 +648,7 @@ __global__ __launch_bounds__(256) void k_planes(LossArgs g) {
         for (int k = 0; k < KM; ++k) t = fmaxf(t, v[k][i]);
 #pragma unroll
         for (int k = 0; k < KM; ++k) za = k == r[i].label ? v[k][i] : za;
+        asm volatile("" : "+v"(r[i].label));           // (opaque: the gradient asks again, rather than that every answer is kept)
       } else {
         t = r[i].a;
       }

@@ -5,8 +5,8 @@ namespace rotconv {
 namespace {
 
 // out[k] = sum of the workgroups' k-th sums: a thread's, 16 at a time on their way, then a fixed tree over lanes and waves.  What it takes
-// is the way of its loads and its launch: one wave, where that has them all on their way at once (32 workgroups' sums 1.4 us, by sixteen
-// waves 3.3; 711 workgroups' by sixteen 3.4, 4096 workgroups' 5.4).
+// is the way of its loads and its launch: the fewest waves that have them all on their way at once (32 workgroups' sums by one wave 1.5 us,
+// by sixteen 3.3; 711 workgroups' by four 2.1, by sixteen 3.4; 4096 workgroups' by sixteen 5.4).
 constexpr int kEndThreads = 1024;
 __global__ __launch_bounds__(kEndThreads) void k_policy_end(const double* __restrict__ part, uint32_t values, float* __restrict__ out) {
   constexpr int kWaves = kEndThreads / 64, kAhead = 16;
@@ -38,7 +38,7 @@ void launch_policy(const LossArgs& g, bool bf16, bool rows, float* out, hipStrea
   unsigned blocks;
   if (bf16) launch_loss<uint16_t, kPolicy>(g, rows, &blocks, st);
   else launch_loss<float, kPolicy>(g, rows, &blocks, st);
-  k_policy_end<<<1, blocks <= 256 ? 64 : kEndThreads, 0, st>>>(g.part, 4 * blocks, out);
+  k_policy_end<<<1, blocks <= 256 ? 64 : blocks <= 1024 ? 256 : kEndThreads, 0, st>>>(g.part, 4 * blocks, out);
 }
 
 }  // namespace rotconv
