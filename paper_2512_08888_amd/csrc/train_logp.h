@@ -37,6 +37,7 @@ struct LossArgs {
   size_t rows, P;
   int K, per_image;
   int alike;                                                 // rows: dz's vectors start where z's do
+  int past;                                                  // rows of many classes: past the caches, 1: gradients, 2: logits too
   float4* shares;                                            // few long rows: t, s, h of every part of a row ..
   float* taken;                                              // .. and the label's logit of every row
   float low, high, kl, entc, unit;                           // the clipping range's ends; unit: the weight where there are none
@@ -319,16 +320,20 @@ __device__ __forceinline__ u4 load_part(const T* border, uint32_t off, int first
   return a;
 }
 template <typename T, bool EVEN = false>
-__device__ __forceinline__ void store_part(T* border, uint32_t off, const u4& a, int first, int K, bool alike) {
+__device__ __forceinline__ void store_part(T* border, uint32_t off, const u4& a, int first, int K, bool alike, bool past = false) {
   constexpr int V = Vec<T>::V;
-  if constexpr (EVEN) {
-    if (first < K) *reinterpret_cast<u4*>(border + off) = a;
+  if (EVEN ? first < K : alike && first >= 0 && first + V <= K) {
+    u4* to = reinterpret_cast<u4*>(border + off);
+    if (past) {
+      asm volatile("");                                // (before and behind: else the compiler makes one store of the two, through the caches)
+      __builtin_nontemporal_store(a, to);
+      asm volatile("");
+    } else {
+      *to = a;
+    }
     return;
   }
-  if (alike && first >= 0 && first + V <= K) {
-    *reinterpret_cast<u4*>(border + off) = a;
-    return;
-  }
+  if constexpr (EVEN) return;
   T* row = border + off - first;
 #pragma unroll
   for (int k = 0; k < V; ++k)
@@ -397,10 +402,22 @@ __global__ __launch_bounds__(B == 64 ? 256 : B) __attribute__((amdgpu_waves_per_
       int lane = tid;                  // (opaque: places are formed anew where they are asked for, and kept in no registers between)
       asm volatile("" : "+v"(lane));
       u4 v[E];
+      if constexpr (EVEN) {
+        const auto at = [&](int e) { return reinterpret_cast<const u4*>(z + min((uint32_t)(lane + e * B) * V, (uint32_t)g.K - V)); };
+        if (g.past == 2) {
+          asm volatile("");                            // (as in store_part)
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if constexpr (EVEN) v[e] = *reinterpret_cast<const u4*>(z + min((uint32_t)(lane + e * B) * V, (uint32_t)g.K - V));
-        else if (e * B * V < g.K + V - 1) v[e] = load_part(z - shift + e * B * V, lane * V, (lane + e * B) * V - shift, g.K);
+          for (int e = 0; e < E; ++e) v[e] = __builtin_nontemporal_load(at(e));
+          asm volatile("");
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) v[e] = *at(e);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (e * B * V < g.K + V - 1) v[e] = load_part(z - shift + e * B * V, lane * V, (lane + e * B) * V - shift, g.K);
+      }
       if constexpr (MODE != kBwd) {
         arrived(taken);
         za = has_label(g, r) ? Elt<T>::ld(&taken) : 0.f;
@@ -440,7 +457,8 @@ __global__ __launch_bounds__(B == 64 ? 256 : B) __attribute__((amdgpu_waves_per_
           asm volatile("" : "+v"(lane));
           const int first = (lane + e * B) * V - shift;
           packed(v[e]);
-          store_part<T, EVEN>(dz - shift + e * B * V, lane * V, o.live ? gradient<T, ENT>(o, v[e], first, r.label) : zero, first, g.K, g.alike);
+          store_part<T, EVEN>(dz - shift + e * B * V, lane * V, o.live ? gradient<T, ENT>(o, v[e], first, r.label) : zero, first, g.K, g.alike,
+                              g.past != 0);
         }
       }
     } else {
@@ -804,10 +822,19 @@ __global__ __launch_bounds__(1024) void k_planes_long(LossArgs g) {
 bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
 template <int MODE> unsigned blocks_for(size_t n) { return (unsigned)std::min<size_t>(n, MODE == kPolicy ? kMostBlocks : kMostOthers); }
 
+// What is larger than the caches' share of it passes them by, lest it drives out what the next calls read.  Made by a pass before, then the
+// call, then its gradient read by a pass behind; all through the caches, gradients past them, logits too: loss of bf16 8192 x 4096 (64 MiB)
+// 68.5, 71 and 71 us, of fp32 1237 x 20011 (94 MiB) 109.5, 105 and 106, of bf16 16384 x 4096 (128 MiB) 141, 134 and 135, of 4096 x 32768
+// (256 MiB) 285, 298 and 274, 4096 x 65536 546, 549 and 520; forward of the last three 63, 63 and 63, 147, 147 and 122, 272, 272 and 250;
+// forward of bf16 16384 x 4096 made longer ago 26.8 and 23.7.  Rows that are no whole vectors share lines: those are read through the caches.
+constexpr size_t kPastGradients = (size_t)80 << 20, kPastLogits = (size_t)128 << 20;
+
 template <typename T, int B, int E, int MODE>
-void launch_rows(const LossArgs& g, unsigned* blocks, hipStream_t st) {
+void launch_rows(LossArgs g, unsigned* blocks, hipStream_t st) {
   constexpr int kRows = B == 64 ? 4 : 1;
   *blocks = blocks_for<MODE>((g.rows + kRows - 1) / kRows);
+  const size_t bytes = g.rows * g.K * sizeof(T);
+  g.past = bytes >= kPastLogits ? 2 : bytes >= kPastGradients;
   const bool entropy = MODE == kFwd ? g.ent_out != nullptr : MODE == kBwd ? g.dent != nullptr : g.entc != 0.f;
   auto kernel = entropy ? k_rows<T, B, E, MODE, true, false> : k_rows<T, B, E, MODE, false, false>;
   if constexpr (E > 0) {
