@@ -378,3 +378,31 @@ def test_label_rows_of_a_map_and_of_tokens_agree():
     rc.train_logp_fwd(rows, c.labels, two)
     r = c.reference()
     assert (np.abs(one.cpu().numpy() - two.cpu().numpy()) <= 2 * bars(r, 40)["logp"]).all()
+
+
+@pytest.mark.parametrize("rows,K,dtype", [(1500, 15000, torch.float32), (1204, 20001, torch.float32), (2200, 16384, torch.float32),
+                                          (4400, 16384, torch.bfloat16), (4000, 20011, torch.bfloat16)])
+def test_large_logits_give_what_their_parts_do(rows, K, dtype):
+    """86 to 152 MiB, which pass the caches by, and 400 rows at a time, which do not: rows know nothing of each other."""
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    f = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    z = (f(rows, K) * 3).to(dtype)
+    labels = torch.randint(0, K, (rows,), generator=gen, device="cuda", dtype=torch.int32)
+    labels[7] = -1
+    adv, weight, d1, d2, old = f(rows), f(rows).abs(), f(rows), f(rows), f(rows) - 9.0
+    empty = lambda *s: torch.full(s, 7.0, device="cuda")  # noqa: E731
+
+    def run(i, j):
+        n = j - i
+        logp, ent, stat, lp, out = empty(n), empty(n), empty(n, 2), empty(n), empty(4)
+        dz, dp = torch.empty_like(z[i:j]), torch.empty_like(z[i:j])
+        rc.train_logp_fwd(z[i:j], labels[i:j], logp, entropy=ent, stat=stat)
+        rc.train_logp_bwd(z[i:j], labels[i:j], stat, d1[i:j], dz, entropy=ent, dentropy=d2[i:j])
+        rc.train_policy_loss(z[i:j], labels[i:j], adv[i:j], out, dp, logp_old=old[i:j], weight=weight[i:j], logp=lp, entropy=0.01)
+        return logp, ent, stat, lp, dz, dp
+
+    whole = run(0, rows)
+    for i in range(0, rows, 400):
+        j = min(i + 400, rows)
+        for k, (a, b) in enumerate(zip(whole, run(i, j))):
+            assert torch.equal(a[i:j], b), (k, i)
