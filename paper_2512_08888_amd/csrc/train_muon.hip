@@ -251,7 +251,7 @@ enum Product { kGram, kPoly, kApply, kLast };
 // an LDS array that a loop fills.
 __device__ __forceinline__ void bring(const half* from, half* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
 }
 // Rows r0 .. r0 + R - 1 (the last row again behind it) and kDepth columns of a matrix, a row of 128 bytes in LDS; its eight pieces of
 // 16 bytes are exchanged by the row's number, two rows alike, so that sixteen lanes of a fragment, a row each, meet all 64 banks.
@@ -635,7 +635,7 @@ template <> struct Any4<uint16_t> {
 
 // The whole step of a matrix with at most 64 rows (or columns) and 1024 columns (or rows), by one workgroup of sixteen waves: X stays in
 // registers in 32 bits, blocks of 32 x 32 as the matrix instructions leave them, up to NT a wave, and its upper part in LDS for the products.
-// For lists of such matrices alone: a step is one launch (the nine filters of a stack of widths 16, 32, 64: 36 us; by the products' launches 117).
+// For lists of such matrices alone: a step is one launch (eleven filters of a stack of widths 16, 32, 64: 36 us; by the products' launches 117).
 constexpr uint32_t kLeastRows = 64, kLeastCols = 1024;
 constexpr int kLeastThreads = 1024, kAcross = kLeastCols + 40, kAside = 72;      // elements from row to row in LDS: rows in banks of their own
 template <typename T, int NT>
