@@ -213,10 +213,10 @@ typedef struct {
 
 typedef struct train_matrices train_matrices;
 
-/* As train_list_create; one handle and one workspace serve calls of one stream at a time.  Refused (ROTCONV_ERR_UNSUPPORTED): params and
- * copies that overlap one another.  Refused (ROTCONV_ERR_SHAPE): extents below 1, the shorter side of a matrix above 32768, the longer above 2^24,
- * stacks of more than 2^40 elements, more matrices than 65535 or more work than 2^24 - 1 workgroups do (of 128 x 128 elements; sixteen
- * to each of A's). */
+/* As train_list_create; one handle and one workspace serve calls of one stream at a time.  Gradients, momentum and scratch lie apart from
+ * params and copies.  Refused (ROTCONV_ERR_UNSUPPORTED): params and copies that overlap one another.  Refused (ROTCONV_ERR_SHAPE): extents
+ * below 1, the shorter side of a matrix above 32768, the longer above 2^24, stacks of more than 2^40 elements, more matrices than 65535
+ * or more work than 2^24 - 1 workgroups do (of 128 x 128 elements; sixteen to each of A's). */
 int train_matrices_create(const train_matrix* matrices, int count, int grad_dtype, train_matrices** out);
 int train_matrices_destroy(train_matrices* matrices);
 /* Elements that the momentum spans: stack k's start at the sum of the sizes before it, each size rounded up to a

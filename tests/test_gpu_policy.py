@@ -406,3 +406,29 @@ def test_large_logits_give_what_their_parts_do(rows, K, dtype):
         j = min(i + 400, rows)
         for k, (a, b) in enumerate(zip(whole, run(i, j))):
             assert torch.equal(a[i:j], b), (k, i)
+
+
+@pytest.mark.parametrize("N,K,P,layout", [(33000, 65536, 1, "rows"), (2, 16, 8192 * 8192, "nchw"), (2, 16, 8192 * 8192, "nhwc"),
+                                          (2, 1100, 1024 * 1024, "nchw")])
+def test_offsets_past_32_bits(N, K, P, layout):
+    """More than 2^31 logits: the last rows (the last image) by themselves give the same bits."""
+    gen = torch.Generator(device="cuda").manual_seed(K)
+    side = int(P ** 0.5)
+    shape = (N, K) if P == 1 else (N, K, side, side) if layout == "nchw" else (N, side, side, K)
+    z = torch.randn(shape, generator=gen, device="cuda", dtype=torch.bfloat16)
+    z = z.permute(0, 3, 1, 2) if layout == "nhwc" else z
+    labels = torch.randint(0, K, (N, P), generator=gen, device="cuda", dtype=torch.int32)
+    adv, weight = (torch.rand(N, P, generator=gen, device="cuda") for _ in range(2))
+    first = N - 200 if P == 1 else 1
+    parts = []
+    for part in (slice(0, N), slice(first, N)):
+        x, at, w = z[part], labels[part], weight[part]
+        logp, lp, out = torch.empty_like(w), torch.empty_like(w), torch.empty(4, device="cuda")
+        stat = torch.empty(*w.shape, 2, device="cuda")
+        dz, dp = torch.empty_like(x), torch.empty_like(x)
+        rc.train_logp_fwd(x, at, logp, stat=stat)
+        rc.train_logp_bwd(x, at, stat, w, dz)
+        rc.train_policy_loss(x, at, adv[part], out, dp, weight=w, logp=lp, entropy=0.01)
+        parts.append((logp, lp, stat, dz, dp))
+    for a, b in zip(*parts):
+        assert torch.equal(a[first:], b)
