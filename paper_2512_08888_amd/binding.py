@@ -739,11 +739,11 @@ def train_logp_workspace_bytes(N, K, P):
 _i32 = _bf16 = None
 
 
-def _row_values(what, name, t, n, dtype=None):
-    """Address of a tensor of n values (fp32 unless dtype says otherwise), one for each row; None stays NULL."""
+def _row_values(what, name, t, n, home, dtype=None):
+    """Address of a tensor of n values on device `home` (fp32 unless dtype says otherwise), one for each row; None stays NULL."""
     if t is None:
         return None
-    if t.dtype is not (dtype or _f32) or t.numel() != n or not t.is_contiguous() or t.get_device() != _device():
+    if t.dtype is not (dtype or _f32) or t.numel() != n or not t.is_contiguous() or t.get_device() != home:
         raise ValueError(f"{what}: {name} must be {str(dtype or _f32)[6:]}, contiguous, on the current GPU, with {n} elements")
     return t.data_ptr()
 
@@ -762,7 +762,7 @@ _current = None
 
 
 def _loss(what, logits, dlogits, labels, ws, scratch):
-    """What the calls on logits share: entry point, N, K, P, order of the logits, the labels' address, workspace."""
+    """What the calls on logits share: entry point, N, K, P, order of the logits, the labels' address, workspace, device."""
     global _f32, _i32, _bf16
     if _i32 is None:
         import torch
@@ -779,7 +779,7 @@ def _loss(what, logits, dlogits, labels, ws, scratch):
     home = logits.get_device()
     if home != _device():
         raise ValueError(f"{what}: logits must be on the current device")
-    at = _row_values(what, "labels", labels, N * P, _i32)
+    at = _row_values(what, "labels", labels, N * P, home, _i32)
     if dlogits is not None and dlogits.get_device() != home:
         raise ValueError(f"{what}: dlogits must be on the logits' device")
     if scratch:
@@ -789,27 +789,27 @@ def _loss(what, logits, dlogits, labels, ws, scratch):
             ws = torch.empty(max(256, train_logp_workspace_bytes(N, K, P)), dtype=torch.uint8, device=logits.device)
         elif ws.get_device() != home:
             raise ValueError(f"{what}: the workspace must be on the logits' device")
-    return getattr(_lib, what if kind is _f32 else what + "_bf16"), N, K, P, layout, at, ws
+    return getattr(_lib, what if kind is _f32 else what + "_bf16"), N, K, P, layout, at, ws, home
 
 
 def train_logp_fwd(logits, labels, logp, entropy=None, stat=None, ws=None):
     """logits [N, K, ...], contiguous or channels last (tokens: [N, K]); labels int32, logp, entropy: one value a row; stat:
     two, for the backward call."""
     what = "train_logp_fwd"
-    fn, N, K, P, layout, at, ws = _loss(what, logits, None, labels, ws, True)
+    fn, N, K, P, layout, at, ws, home = _loss(what, logits, None, labels, ws, True)
     n = N * P
-    _check(fn(logits.data_ptr(), at, _row_values(what, "logp", logp, n), _row_values(what, "entropy", entropy, n),
-              _row_values(what, "stat", stat, 2 * n), N, K, P, layout, _ptr(ws), _nbytes(ws), _stream()), what)
+    _check(fn(logits.data_ptr(), at, _row_values(what, "logp", logp, n, home), _row_values(what, "entropy", entropy, n, home),
+              _row_values(what, "stat", stat, 2 * n, home), N, K, P, layout, _ptr(ws), _nbytes(ws), _stream()), what)
 
 
 def train_logp_bwd(logits, labels, stat, dlogp, dlogits, entropy=None, dentropy=None):
     """The logits' gradient from those of log-probability and entropy (None: none); stat and entropy from the forward call.
     dlogits, in the logits' order, may be the logits themselves."""
     what = "train_logp_bwd"
-    fn, N, K, P, layout, at, _ = _loss(what, logits, dlogits, labels, None, False)
+    fn, N, K, P, layout, at, _, home = _loss(what, logits, dlogits, labels, None, False)
     n = N * P
-    _check(fn(logits.data_ptr(), at, _row_values(what, "stat", stat, 2 * n), _row_values(what, "entropy", entropy, n),
-              _row_values(what, "dlogp", dlogp, n), _row_values(what, "dentropy", dentropy, n), dlogits.data_ptr(), N, K, P,
+    _check(fn(logits.data_ptr(), at, _row_values(what, "stat", stat, 2 * n, home), _row_values(what, "entropy", entropy, n, home),
+              _row_values(what, "dlogp", dlogp, n, home), _row_values(what, "dentropy", dentropy, n, home), dlogits.data_ptr(), N, K, P,
               layout, _stream()), what)
 
 
@@ -818,14 +818,14 @@ def train_policy_loss(logits, labels, advantage, out, dlogits=None, logp_old=Non
     """out [4]: loss, distance to the reference, entropy, share of cut rows (weighted sums).  advantage: a value for each row
     or for each image; weight None: 1 / rows; the others: one value a row.  dlogits may be the logits themselves, or None."""
     what = "train_policy_loss"
-    fn, N, K, P, layout, at, ws = _loss(what, logits, dlogits, labels, ws, True)
+    fn, N, K, P, layout, at, ws, home = _loss(what, logits, dlogits, labels, ws, True)
     n = N * P
     per_image = advantage.numel() == N and P != 1
     o = TrainPolicy(clip[0], clip[1], kl, entropy, int(per_image), 0)
-    _check(fn(logits.data_ptr(), at, _row_values(what, "advantage", advantage, N if per_image else n),
-              _row_values(what, "logp_old", logp_old, n), _row_values(what, "logp_ref", logp_ref, n),
-              _row_values(what, "weight", weight, n), _row_values(what, "out", out, 4), None if dlogits is None else dlogits.data_ptr(),
-              _row_values(what, "logp", logp, n), N, K, P, layout, ctypes.byref(o), _ptr(ws), _nbytes(ws), _stream()), what)
+    _check(fn(logits.data_ptr(), at, _row_values(what, "advantage", advantage, N if per_image else n, home),
+              _row_values(what, "logp_old", logp_old, n, home), _row_values(what, "logp_ref", logp_ref, n, home),
+              _row_values(what, "weight", weight, n, home), _row_values(what, "out", out, 4, home), None if dlogits is None else dlogits.data_ptr(),
+              _row_values(what, "logp", logp, n, home), N, K, P, layout, ctypes.byref(o), _ptr(ws), _nbytes(ws), _stream()), what)
 
 
 class TrainMatrices:

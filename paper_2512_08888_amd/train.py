@@ -1,6 +1,7 @@
 """The optimiser's side of a training step: the norm and clip factor of all gradients, AdamW over all parameters, and Muon
-over matrices (with AdamW for the rest), through the C-ABI library (include/unettrain.h).  This module only owns the device buffers (torch tensors as plain
-memory) and the order of the calls; no arithmetic of the method happens here.
+over matrices (with AdamW for the rest), through the C-ABI library (include/unettrain.h).  This module only owns the
+device buffers (torch tensors as plain memory) and the order of the calls; no arithmetic of the methods happens here, but for the
+draw of labels (sampled()) that the command's policy loss starts from.
 
     python -m paper_2512_08888_amd.train [--steps 60] [--dtype bf16] [--state mx8] [--method muon] [--loss policy] [--graph]
 
