@@ -37,6 +37,11 @@ constexpr int kPad = 32;               // elements: a stack's momentum starts on
 constexpr int kTile = 128;             // edge of the products' tiles
 constexpr int kSmall = 64;             // of A^2's, where tiles of 128 would leave CUs idle
 constexpr int kDepth = 64;             // elements that a step of a product adds up
+// Columns of X's tiles where its products add up kDeep steps or more on an average: fewer bytes through the caches, but fewer workgroups and
+// larger ends.  Steps over 8 matrices of 768 x 3200 by tiles of 128 x 128 610 us, by 128 x 256 654; of 1024 x 4096 1179 and 1188; 4 of
+// 1536 x 1536 and 2 of 1536 x 6144 1373 and 1370; 8 of 2048 x 8192 6935 and 6480; 4 of 4096 x 4096 7604 and 6970.
+constexpr int kWide = 256;
+constexpr uint32_t kDeep = 24;
 constexpr uint32_t kSlots = 512;       // workgroups of the products that the chip holds at a time
 constexpr int kTurn = 64;              // edge of the tiles by which X is first written
 constexpr uint32_t kMostWorkgroups = (1u << 24) - 1;
@@ -73,7 +78,7 @@ struct train_matrices {
   uint64_t elements = 0;
   size_t workspace = 0, sums = 0, parts = 0;           // byte offsets: the chunks' sums, the units'
   uint32_t size = 0;                                   // elements of a chunk
-  int small = 0;                                       // A^2 by tiles of 64
+  int small = 0, wide = 0;                             // A^2 by tiles of 64; X by tiles of kWide columns
   uint32_t least = 0;                                  // matrices, where all of them are small enough for a workgroup; blocks of the widest
   uint32_t widest = 0;
   void* memory = nullptr;
@@ -251,7 +256,7 @@ enum Product { kGram, kPoly, kApply, kLast };
 // an LDS array that a loop fills.
 __device__ __forceinline__ void bring(const half* from, half* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
 }
 // Rows r0 .. r0 + R - 1 (the last row again behind it) and kDepth columns of a matrix, a row of 128 bytes in LDS; its eight pieces of
 // 16 bytes are exchanged by the row's number, two rows alike, so that sixteen lanes of a fragment, a row each, meet all 64 banks.
@@ -503,7 +508,7 @@ struct Finish {
 
 // One tile of TM x TN of a product, or some of its steps, WM x WN waves.
 template <int KIND, int TM, int TN, int WM, int WN, int D, int NS>
-__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(KIND == kApply ? 3 : 2))) void k_product(const Matrix* __restrict__ mats, const Unit* __restrict__ units, char* ws, int from,
+__global__ __launch_bounds__(64 * WM * WN) __attribute__((amdgpu_waves_per_eu(KIND == kApply && TN == kTile ? 3 : 2))) void k_product(const Matrix* __restrict__ mats, const Unit* __restrict__ units, char* ws, int from,
                                                           f4* parts, train_control* ctl, uint32_t* tickets) {
   constexpr int T = 64 * WM * WN, FM = TM / WM / 32, FN = TN / WN / 32;
   constexpr bool kSquare = KIND == kGram || KIND == kPoly;
@@ -880,7 +885,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
   if (count < 1) return ROTCONV_ERR_SHAPE;
   if (grad_dtype != ROTCONV_F32 && grad_dtype != ROTCONV_BF16) return ROTCONV_ERR_UNSUPPORTED;
   const uintptr_t ge = grad_dtype == ROTCONV_BF16 ? 2 : 4;
-  uint64_t total = 0, nturn = 0, nsquare = 0, nsmall = 0, nwide = 0, all = 0, depth = 0;
+  uint64_t total = 0, nturn = 0, nsquare = 0, nsmall = 0, nwide = 0, all = 0, depth = 0, reach = 0;
   for (int k = 0; k < count; ++k) {
     const train_matrix& t = matrices[k];
     if (!t.param || !t.grad) return ROTCONV_ERR_NULL;
@@ -894,6 +899,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     nturn += c * (up(n, kTurn) / kTurn) * (up(m, kTurn) / kTurn);
     nsquare += c * tn * (tn + 1) / 2, nsmall += c * ts * (ts + 1) / 2, nwide += c * tn * tm;
     depth += c * tn * (tn + 1) / 2 * (up(m, kDepth) / kDepth);
+    reach += c * tn * tm * (up(n, kDepth) / kDepth);
     all += c, total += c * n * m;
     if (all > 65535 || std::max(std::max(nturn, 16 * nsquare), std::max(nsmall, nwide)) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
   }
@@ -902,7 +908,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
   while (size < 16384 && total / size > 2048) size *= 2;
   // Steps of a unit of A: so that all units together fill the chip evenly, but no fewer than pay for the sums' way through memory.
   const uint64_t most = std::max<uint64_t>(12, (depth + kSlots - 1) / kSlots);
-  const bool small = nsquare < kSlots;
+  const bool small = nsquare < kSlots, wide = reach >= nwide * kDeep;
   bool least = true;
   uint32_t widest = 0;
   for (int k = 0; k < count; ++k) {
@@ -925,7 +931,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
       if (written[k].first < written[k - 1].second) return ROTCONV_ERR_UNSUPPORTED;
     std::vector<Matrix> mats;
     std::vector<Tile> chunk, turn;
-    std::vector<Unit> gram, poly, apply;
+    std::vector<Unit> gram, poly, apply, last;
     std::vector<Join> join;
     mats.reserve(all), turn.reserve(nturn), apply.reserve(nwide);
     uint64_t base = 0, at = 0;
@@ -985,11 +991,13 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
       const uint32_t steps = (uint32_t)(up(x.n, kDepth) / kDepth), edge = small ? kSmall : kTile;
       for (uint32_t r = 0; r * edge < x.n; ++r)
         for (uint32_t c = r; c * edge < x.n; ++c) poly.push_back(Unit{id, r, c, 0, steps, kWhole});
-      for (uint32_t c = 0; c * kTile < x.m; ++c)
+      const uint32_t across = wide ? kWide : kTile;
+      for (uint32_t c = 0; c * across < x.m; ++c)
         for (uint32_t r = 0; r < tiles; ++r) apply.push_back(Unit{id, r, c, 0, steps, kWhole});
+      for (uint32_t c = 0; c * kTile < x.m; ++c)
+        for (uint32_t r = 0; r < tiles; ++r) last.push_back(Unit{id, r, c, 0, steps, kWhole});
     }
-    // (the last product, which waits for the parameters, takes X's units as they are listed: 130 us for the stack, 140 and more dealt)
-    const std::vector<Unit> last = apply;
+    // (the last product, which waits for the parameters, takes its units as they are listed: 130 us for the stack, 140 and more dealt)
     gram = by_die(gram, 32), poly = by_die(poly, 8), apply = by_die(apply, 4);
     if (std::max(std::max(gram.size(), poly.size()), std::max(apply.size(), chunk.size())) > kMostWorkgroups) return ROTCONV_ERR_SHAPE;
     const uint64_t sums = room(chunk.size() * sizeof(double)), part_bytes = room((uint64_t)places * kTile * kTile * sizeof(float));
@@ -997,7 +1005,7 @@ int train_matrices_create(const train_matrix* matrices, int count, int grad_dtyp
     l->bf16 = grad_dtype == ROTCONV_BF16;
     l->elements = base;
     l->sums = sums, l->parts = part_bytes, l->workspace = at;
-    l->size = size, l->small = small;
+    l->size = size, l->small = small, l->wide = wide;
     if (least) {
       l->least = (uint32_t)mats.size(), l->widest = widest, l->workspace = 256;          // (nothing of it is used)
     }
@@ -1075,12 +1083,13 @@ int train_muon_step(const train_matrices* l, const train_muon* o, float* momentu
   auto start = l->bf16 ? k_start<uint16_t> : k_start<float>;
   start<<<l->nturn, kThreads, 0, st>>>(l->matrices, l->turn, *o, momentum, control, sums, w);
   auto poly = l->small ? k_product<kPoly, 64, 64, 2, 2, kDepth, 2> : k_product<kPoly, 128, 128, 2, 2, kDepth, 2>;
+  auto apply = l->wide ? k_product<kApply, 128, kWide, 2, 2, 32, 3> : k_product<kApply, 128, 128, 2, 2, 32, 3>;
   for (int k = 0; k < o->steps; ++k) {
     k_product<kGram, 128, 128, 2, 2, kDepth, 2><<<l->ngram, kThreads, 0, st>>>(l->matrices, l->gram, w, k % 2, parts, control, tickets);
     if (l->njoin) k_join<<<16 * l->njoin, 64, 0, st>>>(l->matrices, l->join, w, parts, control);
     poly<<<l->npoly, kThreads, 0, st>>>(l->matrices, l->poly, w, k % 2, parts, control, tickets);
     if (k + 1 < o->steps)
-      k_product<kApply, 128, 128, 2, 2, 32, 3><<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control, tickets);
+      apply<<<l->napply, kThreads, 0, st>>>(l->matrices, l->apply, w, k % 2, parts, control, tickets);
     else
       k_product<kLast, 128, 128, 2, 2, kDepth, 2><<<l->nlast, kThreads, 0, st>>>(l->matrices, l->last, w, k % 2, parts, control, tickets);
   }

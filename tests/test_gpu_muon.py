@@ -315,3 +315,16 @@ def test_refusals():
         rc.train_muon_step(opt.matrices, o, opt.m[:5], opt.control, opt.work)
     with pytest.raises(ValueError):
         train.Muon(net.params, net.grads, scale="other")
+
+
+def test_deep_products_and_a_small_matrix_among_them():
+    """1600 rows: X's products go by tiles of 256 columns, a matrix of fewer columns than that among them."""
+    stacks = [(1, 1600, 1801), (1, 40, 300), (1, 130, 129)]
+    net = Net(stacks, seed=5)
+    opt = train.Muon(net.params, net.grads, lr=0.02, scale=1.0)
+    opt.work.fill_(0xff)
+    net.new_grads()
+    before, m0 = net.read(net.params), cut(opt.m, stacks)
+    opt.step()
+    check_step(net, before, m0, net.read(net.params), cut(opt.m, stacks), float(np.float32(0.02)), float(np.float32(0.95)), True, 0.0, [1.0] * 3, 1.0, 5)
+    assert net.intact()
