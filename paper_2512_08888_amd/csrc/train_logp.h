@@ -294,18 +294,10 @@ template <> struct Vec<uint16_t> {
   }
 };
 // The vector of a row at `border` (the same for all lanes, so that addresses take no registers) + `off` elements; its first element is the
-// row's number `first`.  -infinity outside the row.  EVEN: rows start on borders and are whole vectors; nothing is asked of an end then,
-// and no registers are kept for it (4096 x 65536 bf16 logits, loss: 201 us, and 240 with the ends' code and addresses beside).
-template <typename T, bool EVEN = false>
+// row's number `first`.  -infinity outside the row.
+template <typename T>
 __device__ __forceinline__ u4 load_part(const T* border, uint32_t off, int first, int K) {
   constexpr int V = Vec<T>::V;
-  if constexpr (EVEN) {
-    u4 a;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) a[k] = Vec<T>::kLowest;
-    if (first < K) a = *reinterpret_cast<const u4*>(border + off);
-    return a;
-  }
   if (first >= 0 && first + V <= K) return *reinterpret_cast<const u4*>(border + off);
   u4 a;
 #pragma unroll
@@ -319,7 +311,7 @@ __device__ __forceinline__ u4 load_part(const T* border, uint32_t off, int first
   for (int k = 0; k < V; ++k) Vec<T>::put(a, k, first + k >= 0 && first + k < K ? v[k] : -INFINITY);
   return a;
 }
-template <typename T, bool EVEN = false>
+template <typename T, bool EVEN = false>       // EVEN: as in k_rows
 __device__ __forceinline__ void store_part(T* border, uint32_t off, const u4& a, int first, int K, bool alike, bool past = false) {
   constexpr int V = Vec<T>::V;
   if (EVEN ? first < K : alike && first >= 0 && first + V <= K) {
@@ -378,7 +370,8 @@ __device__ __forceinline__ RowGrad row_wide(const RowGrad& o) {
 
 // Rows of many classes: B threads to a row, up to E vectors a thread in registers (those that no thread has are passed over).  64
 // threads: four rows to a workgroup.  E = 0: rows of any length, read twice (their sums are then formed with a running maximum).
-// ENT: somebody wants the entropy or its gradient.
+// ENT: somebody wants the entropy or its gradient.  EVEN: rows start on 16-byte borders and are whole vectors; nothing is asked of an end
+// then, and no registers are kept for it (4096 x 65536 bf16 logits, loss, through the caches: 201 us, and 240 with the ends' code beside).
 template <typename T, int B, int E, int MODE, bool ENT, bool EVEN>
 __global__ __launch_bounds__(B == 64 ? 256 : B) __attribute__((amdgpu_waves_per_eu(E == 16 ? 4 : 8))) void k_rows(LossArgs g) {
   constexpr int V = Vec<T>::V, kRows = B == 64 ? 4 : 1;
@@ -496,7 +489,7 @@ __global__ __launch_bounds__(B == 64 ? 256 : B) __attribute__((amdgpu_waves_per_
 }
 
 // Few long rows: a row's parts of kPart vectors go to workgroups of their own, since one CU forms 16 exponentials a clock (one row of 131072
-// bf16 logits: 12.7 us by one workgroup).  k_share forms the parts' sums; k_rest, a launch behind it, joins a row's, each workgroup for
+// bf16 logits: 10.8 us by one workgroup, 9.6 so).  k_share forms the parts' sums; k_rest, a launch behind it, joins a row's, each workgroup for
 // itself, and writes the part's gradient.  The label's logit is passed on, since a gradient may take its place.
 constexpr int kPartThreads = 256, kPartVecs = 4, kPart = kPartThreads * kPartVecs;
 
