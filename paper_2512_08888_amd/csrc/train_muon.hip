@@ -256,7 +256,9 @@ enum Product { kGram, kPoly, kApply, kLast };
 // an LDS array that a loop fills.
 __device__ __forceinline__ void bring(const half* from, half* to) {
   const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)to);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory", "m0");
+  // (m0, where the instruction takes the place in LDS from, is the compiler's to set, so that it keeps nothing else there; what reads it so has to
+  // wait for an instruction behind that)
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(at), "v"(from) : "memory");
 }
 // Rows r0 .. r0 + R - 1 (the last row again behind it) and kDepth columns of a matrix, a row of 128 bytes in LDS; its eight pieces of
 // 16 bytes are exchanged by the row's number, two rows alike, so that sixteen lanes of a fragment, a row each, meet all 64 banks.

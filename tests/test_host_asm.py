@@ -1,5 +1,5 @@
-"""CPU check of the kernels' inline assembler: a register that an instruction names by itself is named in the clobbers too, since the
-compiler may hold a value of its own there."""
+"""CPU check of the kernels' inline assembler: a scalar register that an instruction writes by name is named in the clobbers too, since the
+compiler may hold a value of its own there, and a load to LDS gets its place through m0 as an operand."""
 import glob
 import os
 import re
@@ -10,7 +10,7 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 
 
 def statements(text):
-    """(template, clobbers) of every asm statement."""
+    """(template, operands, clobbers) of every asm statement."""
     text = re.sub(r"//[^\n]*", "", text)
     for start in re.finditer(r"\basm\s*(?:volatile\s*)?\(", text):
         depth, parts, at, quoted = 1, [""], start.end(), False
@@ -26,24 +26,27 @@ def statements(text):
                     continue
             parts[-1] += c if depth else ""
             at += 1
-        yield parts[0], parts[3] if len(parts) > 3 else ""
+        yield parts[0], "".join(parts[1:3]), parts[3] if len(parts) > 3 else ""
 
 
-def missing(template, clobbers):
-    """Scalar registers that the template's instructions write and the clobbers do not name."""
-    written = re.findall(r"\bs_\w+\s+(m0|vcc|exec|s\d+)\b", template)
-    return [r for r in written if f'"{r}"' not in clobbers]
+def missing(template, operands, clobbers):
+    """Scalar registers that the template writes and the clobbers do not name, or that it reads without getting them."""
+    written = re.findall(r"(?:^|\W|\\[nt])s_(?!waitcnt|nop)\w+\s+(m0|vcc|exec|s\d+)\b", template)
+    reads = ["m0"] if "_load_lds" in template and "m0" not in written else []
+    return [r for r in written if f'"{r}"' not in clobbers] + [r for r in reads if f'"{{{r}}}"' not in operands]
 
 
 def test_the_check_itself():
     one = 'asm volatile("s_mov_b32 m0, %0\\n\\tnext" ::"s"(at(1)) : "memory");'
     two = 'asm volatile("s_mov_b32 m0, %0\\n\\tnext" ::"s"(at[1]) : "memory", "m0");  // asm("s_mov_b32 m0, 0")'
     assert [missing(*s) for s in statements(one + two)] == [["m0"], []]
+    three = 'asm volatile("s_nop 0\\n\\tglobal_load_lds_dword %1, off" ::"{m0}"(at), "v"(from) : "memory");'
+    assert [missing(*s) for s in statements(three + three.replace("{m0}", "s"))] == [[], ["m0"]]
     assert [missing(*s) for s in statements('asm("s_waitcnt vmcnt(0)" : "+v"(x)); asm volatile("");')] == [[], []]
 
 
 @pytest.mark.parametrize("path", sorted(glob.glob(os.path.join(CSRC, "*"))), ids=os.path.basename)
 def test_assembler_names_what_it_writes(path):
     with open(path) as f:
-        for template, clobbers in statements(f.read()):
-            assert not missing(template, clobbers), template
+        for statement in statements(f.read()):
+            assert not missing(*statement), statement[0]
