@@ -80,12 +80,13 @@ int train_diag_groupnorm_wait(int ticks);
  * calls of one stream at a time. */
 size_t train_logp_workspace_bytes(int N, int K, size_t P);
 /* logp, entropy: fp32 [N, P]; stat: fp32 [N, P, 2], t and l, which the backward call reads.  entropy and stat may be NULL.
- * Left out beside those without a label: rows whose logits are all -infinity (their t is kept as it is, -infinity). */
+ * Left out beside those without a label: rows whose logits are all -infinity (their t is kept as it is, -infinity, with l = 0; beside a NaN
+ * l is NaN). */
 int train_logp_fwd(const float* logits, const int32_t* labels, float* logp, float* entropy, float* stat, int N, int K,
                    size_t P, int layout, void* ws, size_t ws_bytes, void* stream);
 /* dlogits_j = dlogp (1[j = label] - p_j) - dentropy p_j (ln p_j + entropy)
  * stat, entropy: what the forward call wrote.  dentropy may be NULL (none), and entropy is read only beside it.
- * dlogits may be the logits themselves (same address).  Left out too: rows whose t is -infinity, and
+ * dlogits may be the logits themselves (same address).  Left out too: rows whose t is -infinity with l = 0, and
  * rows whose dlogp and dentropy are 0. */
 int train_logp_bwd(const float* logits, const int32_t* labels, const float* stat, const float* entropy,
                    const float* dlogp, const float* dentropy, float* dlogits, int N, int K, size_t P, int layout,

@@ -121,7 +121,8 @@ __device__ __forceinline__ RowGrad row_end(const LossArgs& g, const RowIn& r, fl
     o.inv = exp2_of(-r.b * kLog2e);
     o.c1 = r.c, o.c2 = r.d * kLn2;
     o.base = r.d == 0.f ? r.c : r.c + r.d * (r.ent - r.b);
-    o.live = has_label(g, r) && r.a != -INFINITY && !(r.c == 0.f && r.d == 0.f);
+    // (a row of NaN, or of NaN beside -infinity, has t at -infinity too, but l is NaN there)
+    o.live = has_label(g, r) && !(r.a == -INFINITY && r.b == 0.f) && !(r.c == 0.f && r.d == 0.f);
   } else {
     const bool none = t == -INFINITY && s == 0.f;
     bool live = has_label(g, r) && !none;

@@ -432,3 +432,36 @@ def test_offsets_past_32_bits(N, K, P, layout):
         parts.append((logp, lp, stat, dz, dp))
     for a, b in zip(*parts):
         assert torch.equal(a[first:], b)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layout,K", SPECIAL + [("nchw", 1), ("nhwc", 1), ("rows", 1)])
+def test_rows_of_nan_that_have_a_label(layout, K, dtype):
+    """NaN everywhere, or beside classes that cannot be taken: log-probability, entropy and gradient are NaN, and a row of -infinity
+    alone is left out as it is elsewhere."""
+    c = Case(2, K, 3, 4 if K < 10000 else 1, layout, dtype, seed=K + 4, ignored=False)
+    z = c.read(c.z).astype(np.float32)
+    z[1] = np.nan
+    z[2] = -np.inf
+    z[3], z[3, K // 2] = -np.inf, np.nan
+    z[4], z[4, 0] = -np.inf, np.nan
+    labels = c.labels.cpu().numpy().copy()
+    labels[4] = 0                                                # a label that is the NaN itself
+    labels[3] = K - 1
+    c.labels = torch.from_numpy(labels).cuda()
+    c.z.copy_((torch.from_numpy(z) if layout == "rows" else torch.from_numpy(np.moveaxis(z.reshape(2, *c.z.shape[2:], K), -1, 1).copy())).to(dtype))
+    logp, ent, stat = torch.empty(c.rows, device="cuda"), torch.empty(c.rows, device="cuda"), torch.empty(c.rows, 2, device="cuda")
+    rc.train_logp_fwd(c.z, c.labels, logp, entropy=ent, stat=stat)
+    nan, rest = [1, 3, 4], [0, 5]
+    assert all(torch.isnan(t[nan]).all() for t in (logp, ent, stat[:, 1])) and all(torch.isfinite(t[rest]).all() for t in (logp, ent, stat))
+    assert logp[2].item() == 0 and ent[2].item() == 0 and stat[2].tolist() == [-np.inf, 0.0]
+    d1, d2 = c.values(), c.values(0.3)
+    for kw in ({}, dict(entropy=ent, dentropy=d2)):
+        for dz in (torch.full_like(c.z, 7.0), c.z.clone(memory_format=torch.preserve_format)):
+            rc.train_logp_bwd(dz if (dz != 7.0).any() else c.z, c.labels, stat, d1, dz, **kw)
+            got = c.read(dz)
+            assert np.isnan(got[nan]).all() and np.isfinite(got[rest]).all() and (got[2] == 0).all()
+    out, dz = torch.empty(4, device="cuda"), torch.full_like(c.z, 7.0)
+    rc.train_policy_loss(c.z, c.labels, d1, out, dz, logp=logp, entropy=0.1)
+    got = c.read(dz)
+    assert np.isnan(got[nan]).all() and np.isfinite(got[rest]).all() and (got[2] == 0).all() and np.isnan(out[0].item())
