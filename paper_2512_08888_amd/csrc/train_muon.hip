@@ -162,6 +162,18 @@ __global__ __launch_bounds__(kThreads) void k_momentum(const Matrix* __restrict_
   if (threadIdx.x == 0) sums[blockIdx.x] = red[0] + red[1] + red[2] + red[3];
 }
 
+// 2^15 / (|u| + eps), from the sum of u's squares, as two factors that an element takes one after the other: together they need not be a
+// normal fp32 number (a matrix of zeros beside an eps below 9.6e-35, elements near 2^127), and lift, a power of two, is 1 where they are.
+// u's elements are no larger than |u|, so that none overflows between the two, and what falls below 2^-149 there is 0 in fp16.
+struct Factor {
+  float lift, scale;
+};
+__device__ __forceinline__ Factor factor_to_unit(double squares, float eps) {
+  const double f = (double)kHeld / (sqrt(squares) + (double)eps);
+  const bool large = f > 0x1p100, small = f < 0x1p-100;
+  return {large ? 0x1p100f : small ? 0x1p-100f : 1.f, (float)(f * (large ? 0x1p-100 : small ? 0x1p100 : 1.0))};
+}
+
 // v = X times 2^15, as two fp16 numbers
 __device__ __forceinline__ void split(float v, half* upper, half* lower) {
   const half u = (half)v;
@@ -205,13 +217,13 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[h][e] = direction(mv[e], gv[e] * coef, mu, opt.nesterov);
   }
-  // 1 / (|u| + eps), by every workgroup for itself while its loads are under way
+  // X's factor, by every workgroup for itself while its loads are under way
   double s = 0;
   for (uint32_t c = tid; c < x.chunks; c += kThreads) s += sums[x.first + c];
   s = lanes_sum(s);
   if (tid % 64 == 0) red[tid / 64] = s;
   __syncthreads();
-  const float scale = (float)(1.0 / (sqrt((red[0] + red[1]) + (red[2] + red[3])) + (double)opt.eps)) * kHeld;
+  const Factor unit = factor_to_unit((red[0] + red[1]) + (red[2] + red[3]), opt.eps);
   if (x.tall) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -232,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       half ue, le;
-      split(v[h][e] * scale, &ue, &le);
+      split(v[h][e] * unit.lift * unit.scale, &ue, &le);
       u[e] = ue, l[e] = le;
     }
     const uint64_t at = (uint64_t)i * x.ldm + j;
@@ -726,11 +738,11 @@ __global__ __launch_bounds__(kLeastThreads) void k_least(const Matrix* __restric
   double all = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) all += red[w];
-  const float scale = (float)(1.0 / (sqrt(all) + (double)opt.eps)) * kHeld;
+  const Factor unit = factor_to_unit(all, opt.eps);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[t][e] = v[t][e] * scale;
+    for (int e = 0; e < 16; ++e) v[t][e] = v[t][e] * unit.lift * unit.scale;
 
   // The symmetric products by blocks of 16 x 16, one a wave: row and column of its four elements a lane
   const int edge = 2 * high, bi = wave / edge, bj = wave % edge, sj = bj * 16 + lane % 16, si = bi * 16 + 4 * (lane / 16);

@@ -9,6 +9,7 @@ grows to less than (5 + 5^2 + .. + 5^steps) 2^-22 < 5^steps 2^-21.
 import numpy as np
 import pytest
 import torch
+from scipy.linalg import hadamard
 
 from oracle import train_oracle as to
 from paper_2512_08888_amd import binding as rc
@@ -328,3 +329,57 @@ def test_deep_products_and_a_small_matrix_among_them():
     opt.step()
     check_step(net, before, m0, net.read(net.params), cut(opt.m, stacks), float(np.float32(0.02)), float(np.float32(0.95)), True, 0.0, [1.0] * 3, 1.0, 5)
     assert net.intact()
+
+
+def moved_by(p, o, rough, steps):
+    """Whether parameters that were 0 moved by the oracle's o (lr and scale 1), within the bars above."""
+    return np.linalg.norm(-p - o) <= 3 * rough + 5.0 ** steps * 2.0 ** -21 * np.linalg.norm(o)
+
+
+LEAST_EPS = float(np.finfo(np.float32).tiny)
+
+
+@pytest.mark.parametrize("stacks", [[(1, 20, 30), (1, 30, 8)], [(1, 20, 30), (1, 70, 90), (1, 300, 90)]])
+@pytest.mark.parametrize("eps", [LEAST_EPS, 1e-36, 9e-35])
+def test_zero_gradients_beside_the_smallest_eps(stacks, eps):
+    """0 / eps is 0, also where fp32 holds no 2^15 / eps: decay alone."""
+    net = Net(stacks, copy=True, seed=6)
+    for g in net.grads:
+        g.zero_()
+    before = net.read(net.params)
+    opt = train.Muon(net.params, net.grads, lr=0.1, weight_decay=0.5, eps=eps, copies=net.copies)
+    opt.work.fill_(0xff)
+    opt.step()
+    for a, b in zip(before, net.read(net.params)):
+        assert (np.abs(b - a * 0.95) <= 4 * U * np.abs(a)).all()
+    assert (opt.m == 0).all() and all(torch.equal(c, p.to(torch.bfloat16)) for c, p in zip(net.copies, net.params))
+
+
+@pytest.mark.parametrize("shape", [(2, 40, 72), (1, 90, 200), (1, 200, 90)])
+@pytest.mark.parametrize("size", [1e-36, 1e-34, 1e37])
+def test_gradients_at_the_ends_of_fp32(shape, size):
+    net = Net([shape], seed=5)
+    net.new_grads(size)
+    net.params[0].zero_()
+    opt = train.Muon(net.params, net.grads, lr=1.0, nesterov=False, scale=1.0, eps=LEAST_EPS)
+    opt.step()
+    for u, p in zip(net.read(net.grads)[0], net.read(net.params)[0]):
+        o = to.newton_schulz(u, eps=LEAST_EPS)
+        assert moved_by(p, o, np.linalg.norm(to.newton_schulz_fp16(u, eps=LEAST_EPS) - o), 5)
+
+
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shape", [(1, 64, 1024), (1, 128, 2048), (1, 2048, 128)])
+def test_norms_whose_reciprocal_is_no_normal_number(shape, grad):
+    """Orthogonal rows of elements 1.9 2^127 and their negatives: X's are 2^-8 or 2^-9, which fp16 holds, and so is all that its products add
+    up, so that nothing but the norm's reciprocal and the last sums are rounded."""
+    net = Net([shape], grad, seed=5)
+    signs = hadamard(max(shape))[:shape[1], :shape[2]]
+    net.grads[0].copy_(torch.from_numpy(signs * (1.8984375 * 2.0 ** 127))[None])
+    net.params[0].zero_()
+    opt = train.Muon(net.params, net.grads, lr=1.0, nesterov=False, scale=1.0, steps=1)
+    opt.step()
+    u = net.read(net.grads)[0][0]
+    o = to.newton_schulz(u, 1)
+    rough = np.linalg.norm(to.newton_schulz_fp16(u, 1) - o)
+    assert rough <= 1e-9 * np.linalg.norm(o) and moved_by(net.read(net.params)[0][0], o, rough, 1)
