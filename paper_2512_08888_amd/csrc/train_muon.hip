@@ -196,7 +196,8 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
   const float coef = factor(*ctl), mu = opt.momentum;
   const T* g = static_cast<const T*>(x.g);
   const float* m = momentum + x.pos;
-  const bool pieces = x.vec && x.cols % 8 == 0;
+  // (four gradients of 16 bits are half a vector: a whole one needs a border of 16 bytes of its own)
+  const bool pieces = x.vec && x.cols % 8 == 0, whole = sizeof(T) == 4 || reinterpret_cast<uintptr_t>(g) % 16 == 0;
   float v[2][8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -206,8 +207,12 @@ __global__ __launch_bounds__(kThreads) void k_start(const Matrix* __restrict__ m
     if (r < x.rows && c < x.cols) {
       if (pieces) {
         Elt<float>::ldv(m + at, mv), Elt<float>::ldv(m + at + 4, mv + 4);
-        Elt<T>::ldv(g + at, gv);
-        if constexpr (sizeof(T) == 4) Elt<T>::ldv(g + at + 4, gv + 4);
+        if (whole) {
+          Elt<T>::ldv(g + at, gv);
+          if constexpr (sizeof(T) == 4) Elt<T>::ldv(g + at + 4, gv + 4);
+        } else if constexpr (sizeof(T) == 2) {
+          Elt<T>::ldh(g + at, gv), Elt<T>::ldh(g + at + 4, gv + 4);
+        }
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)

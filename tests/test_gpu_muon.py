@@ -383,3 +383,20 @@ def test_norms_whose_reciprocal_is_no_normal_number(shape, grad):
     o = to.newton_schulz(u, 1)
     rough = np.linalg.norm(to.newton_schulz_fp16(u, 1) - o)
     assert rough <= 1e-9 * np.linalg.norm(o) and moved_by(net.read(net.params)[0][0], o, rough, 1)
+
+
+@pytest.mark.parametrize("shift", [4, 8, 12])
+@pytest.mark.parametrize("grad", [torch.float32, torch.bfloat16])
+def test_rows_of_whole_vectors_between_borders(grad, shift):
+    """Gradients 4 and 12 elements past a border of 16 bytes, rows of a multiple of eight elements."""
+    stacks = [(1, 128, 256), (1, 200, 64), (2, 65, 72), (1, 16, 8)]
+    net = Net(stacks, grad, copy=True, shift=shift, seed=15)
+    lr, mu = (float(np.float32(v)) for v in (0.05, 0.9))
+    opt = train.Muon(net.params, net.grads, lr=lr, momentum=mu, scale=1.0, copies=net.copies)
+    opt.work.fill_(0xff)
+    for _ in range(2):
+        net.new_grads()
+        before, m0 = net.read(net.params), cut(opt.m, stacks)
+        opt.step()
+        check_step(net, before, m0, net.read(net.params), cut(opt.m, stacks), lr, mu, True, 0.0, [1.0] * len(stacks), 1.0, 5)
+        assert net.intact()
