@@ -145,6 +145,8 @@ def make_batch(cfg: UNetConfig):
 class UNet:
     """Device state of the stack: plans, parameters, activations, gradients, one shared workspace."""
 
+    policy = None                         # what load_policy() has put in the cross-entropy's place
+
     def __init__(self, cfg: UNetConfig, params: Optional[Dict[str, np.ndarray]] = None, device="cuda",
                  dtype: str = "f32", fuse_relu: bool = True):
         """dtype "f32": everything fp32.  "bf16": images, parameters, activations and activation gradients
@@ -214,8 +216,7 @@ class UNet:
         self.ws = torch.empty(ws_bytes, dtype=u8, device=device)
         self.parts = buf(4, dtype=f32)    # the loss; of the policy loss also its distance, entropy and share of cut pixels
         self.loss = self.parts[:1]
-        self.policy = None                # what load_policy() has put in the cross-entropy's place
-        self._policy = {}                 # its buffers
+        self._policy = {}                 # buffers of load_policy()
         self.trace = None         # a list turns on per-call event timing
         self._where = ""
         self.images = buf(N, cfg.Cin, cfg.H, cfg.W)
@@ -259,7 +260,7 @@ class UNet:
         now: labels sampled for them [N, H, W] (int32; outside the classes: left out), an advantage for each image [N] or
         pixel [N, H, W], the labels' log-probabilities when they were sampled and in a reference, weights (None: 1 / pixels).
         Tensors or arrays; their values are copied into buffers of the network, which a recorded step reads again: what is
-        given or None, the advantage's extent and the constants are part of the recording."""
+        given or None, the advantage's extent and the constants are part of the recording, and replay() refuses others."""
         torch, n, pixels = self.torch, self.cfg.N, self.labels.numel()
 
         def hold(name, v, sizes, dtype=torch.float32):
@@ -278,7 +279,9 @@ class UNet:
         held = dict(advantage=hold("advantage", advantage, (n, pixels)), logp_old=hold("logp_old", logp_old, (pixels,)),
                     logp_ref=hold("logp_ref", logp_ref, (pixels,)), weight=hold("weight", weight, (pixels,)))
         self.labels.view(-1).copy_(hold_labels)
-        self.policy = dict(held, clip=clip, kl=kl, entropy=entropy)
+        constants = tuple(float(np.float32(v)) for v in (*clip, kl, entropy))
+        self.policy = dict(held, clip=clip, kl=kl, entropy=entropy,
+                           form=(constants, *(None if v is None else v.numel() for v in held.values())))
 
     def label_logp(self, labels=None):
         """Log-probability of every pixel's label [N, H, W] (None: those held now) under the present parameters, for the images
@@ -415,6 +418,10 @@ class UNet:
         self.backward()
         return self.loss
 
+    def _loss_form(self):
+        """What a recording fixes of the loss in place: None for the cross-entropy."""
+        return self.policy and self.policy["form"]
+
     # ---- training -----------------------------------------------------------------------------
     def optimizer(self, weight_decay=0.0, method="adamw", **options):
         """method "adamw": train.AdamW over all parameters and this network's gradient buffers; options: lr, betas, eps, state,
@@ -464,8 +471,10 @@ class UNet:
         library call enqueues kernels only and every buffer of the step is preallocated, so the recorded step is
         the eager step.  With an optimizer the recorded step is train_step(optimizer, max_norm); its step number and
         learning rate live on the device, and the network keeps the optimizer until the next recording, since the
-        graph holds addresses of its memory.  (A graph that outlives the network needs both kept.)"""
+        graph holds addresses of its memory.  (A graph that outlives the network needs both kept.)  The recorded loss is the
+        one in place now: after load_batch() or load_policy() have put another there, replay() refuses."""
         assert self.trace is None
+        form = self._loss_form()
         self.step()
         self.torch.cuda.synchronize()
         graph = self.torch.cuda.CUDAGraph()
@@ -474,9 +483,12 @@ class UNet:
                 self.step()
             else:
                 self.train_step(optimizer, max_norm)
-        self._graph, self._graph_optimizer = graph, optimizer
+        self._graph, self._graph_optimizer, self._graph_loss = graph, optimizer, form
         return graph
 
     def replay(self):
+        if self._loss_form() != self._graph_loss:
+            raise RuntimeError("replay: the recorded step computes another loss than load_batch() or load_policy() have put in place since: "
+                               "record it again")
         self._graph.replay()
         return self.loss

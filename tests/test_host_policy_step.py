@@ -1,0 +1,88 @@
+"""CPU checks of the loss in place and the recorded one (paper_2512_08888_amd/unet.py): a network without kernels, whose recording is
+replaced."""
+import contextlib
+import types
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_08888_amd import unet
+
+SHAPE, PIXELS = (2, 4, 4), 32
+
+
+def network():
+    net = unet.UNet.__new__(unet.UNet)
+    graph = type("Graph", (), {"replays": 0, "replay": lambda self: setattr(self, "replays", self.replays + 1)})
+    cuda = types.SimpleNamespace(synchronize=lambda: None, CUDAGraph=graph, graph=lambda g: contextlib.nullcontext())
+    names = ("is_tensor", "from_numpy", "empty", "float32", "int32")
+    net.torch = types.SimpleNamespace(cuda=cuda, **{n: getattr(torch, n) for n in names})
+    net.cfg, net.dev, net.trace, net._policy = types.SimpleNamespace(N=2, H=4, W=4), "cpu", None, {}
+    net.images, net.labels, net.loss = torch.zeros(2, 3, 4, 4), torch.full(SHAPE, 3, dtype=torch.int32), torch.zeros(1)
+    net.step, net.train_step = lambda: None, lambda optimizer, max_norm: None
+    return net
+
+
+def given(**more):
+    return dict(dict(labels=np.ones(SHAPE, np.int32), advantage=np.ones(SHAPE, np.float32), logp_old=torch.zeros(SHAPE)), **more)
+
+
+def batch(net):
+    net.load_batch(np.zeros((2, 3, 4, 4)), np.zeros(SHAPE, np.int32))
+
+
+def test_a_recorded_cross_entropy_is_not_replayed_for_the_policy_loss():
+    net = network()
+    batch(net)
+    graph = net.capture()
+    net.replay()
+    net.load_policy(**given())
+    with pytest.raises(RuntimeError, match="another loss"):
+        net.replay()
+    assert graph.replays == 1
+    batch(net)
+    net.replay()
+    assert graph.replays == 2
+    net.load_policy(**given())
+    net.capture().replay()
+    net.replay()
+
+
+OTHERS = [dict(advantage=np.ones(2, np.float32)), dict(logp_old=None), dict(logp_ref=torch.zeros(SHAPE)), dict(weight=np.ones(SHAPE)),
+          dict(clip=(0.2, 0.3)), dict(clip=(0.1, 0.2)), dict(kl=0.1), dict(entropy=0.1)]
+
+
+@pytest.mark.parametrize("other", OTHERS, ids=lambda o: next(iter(o)))
+def test_a_recorded_policy_loss_is_not_replayed_for_another(other):
+    net = network()
+    net.load_policy(**given())
+    graph = net.capture()
+    net.load_policy(**given(advantage=np.zeros(SHAPE), logp_old=np.ones(SHAPE), clip=[np.float32(0.2), 0.2], kl=0, entropy=0))      # other values alone
+    net.replay()
+    for put in (lambda: net.load_policy(**given(**other)), lambda: batch(net)):
+        put()
+        with pytest.raises(RuntimeError, match="another loss"):
+            net.replay()
+    net.load_policy(**given())
+    net.replay()
+    assert graph.replays == 2
+
+
+def test_a_recording_that_fails_leaves_the_loss_of_the_one_before():
+    net = network()
+    net.load_policy(**given())
+    graph = net.capture()
+    batch(net)
+
+    def broken():
+        raise RuntimeError("not recorded")
+
+    net.step = broken
+    with pytest.raises(RuntimeError, match="not recorded"):
+        net.capture()
+    with pytest.raises(RuntimeError, match="another loss"):
+        net.replay()
+    net.load_policy(**given())
+    net.replay()
+    assert graph.replays == 1
