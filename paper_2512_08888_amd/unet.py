@@ -262,6 +262,9 @@ class UNet:
         Tensors or arrays; their values are copied into buffers of the network, which a recorded step reads again: what is
         given or None, the advantage's extent and the constants are part of the recording, and replay() refuses others."""
         torch, n, pixels = self.torch, self.cfg.N, self.labels.numel()
+        low, high = clip
+        constants = tuple(float(np.float32(float(v))) for v in (low, high, kl, entropy))
+        copies = []                       # (buffer, values), made when nothing is left to refuse
 
         def hold(name, v, sizes, dtype=torch.float32):
             if v is None:
@@ -272,14 +275,17 @@ class UNet:
             key = (name, v.numel())
             if key not in self._policy:
                 self._policy[key] = torch.empty(v.numel(), dtype=dtype, device=self.dev)
-            self._policy[key].copy_(v.reshape(-1))
+            copies.append((self._policy[key], v.reshape(-1)))
             return self._policy[key]
 
         hold_labels = hold("labels", labels, (pixels,), torch.int32)
         held = dict(advantage=hold("advantage", advantage, (n, pixels)), logp_old=hold("logp_old", logp_old, (pixels,)),
                     logp_ref=hold("logp_ref", logp_ref, (pixels,)), weight=hold("weight", weight, (pixels,)))
+        if hold_labels is None or held["advantage"] is None:
+            raise ValueError("load_policy: labels and advantage are needed")
+        for to, v in copies:
+            to.copy_(v)
         self.labels.view(-1).copy_(hold_labels)
-        constants = tuple(float(np.float32(v)) for v in (*clip, kl, entropy))
         self.policy = dict(held, clip=clip, kl=kl, entropy=entropy,
                            form=(constants, *(None if v is None else v.numel() for v in held.values())))
 

@@ -86,3 +86,30 @@ def test_a_recording_that_fails_leaves_the_loss_of_the_one_before():
     net.load_policy(**given())
     net.replay()
     assert graph.replays == 1
+
+
+class Broken:
+    """Neither a tensor nor an array of numbers."""
+
+
+REFUSED = [dict(labels=np.ones(31, np.int32)), dict(labels=None), dict(advantage=np.zeros(5)), dict(advantage=None), dict(logp_old=torch.zeros(1)),
+           dict(logp_ref=np.zeros((2, 4, 5))), dict(weight=torch.zeros(33)), dict(weight=Broken()), dict(clip=0.2), dict(clip=(0.2,)), dict(clip=("low", 0.2)), dict(kl=None)]
+
+
+@pytest.mark.parametrize("bad", REFUSED, ids=lambda o: next(iter(o)))
+def test_a_refused_call_leaves_the_loss_in_place(bad):
+    """Every earlier argument differs from what is in place, and none of it may arrive."""
+    net = network()
+    net.load_policy(**given(logp_ref=torch.full(SHAPE, -1.0), weight=np.ones(SHAPE)), kl=0.1)
+    graph, policy, buffers = net.capture(), net.policy, {k: v.clone() for k, v in net._policy.items()}
+    labels = net.labels.clone()
+    other = dict(labels=np.zeros(SHAPE, np.int32), advantage=np.full(SHAPE, 5.0), logp_old=torch.full(SHAPE, 6.0), logp_ref=torch.full(SHAPE, 7.0),
+                 weight=np.full(SHAPE, 8.0), kl=0.1)
+    with pytest.raises((ValueError, TypeError)):
+        net.load_policy(**{**other, **bad})
+    assert net.policy is policy and torch.equal(net.labels, labels)
+    assert all(torch.equal(net._policy[k], v) for k, v in buffers.items())
+    net.replay()
+    net.load_policy(**other)
+    net.replay()
+    assert graph.replays == 2 and (net.labels == 0).all() and (net.policy["advantage"] == 5).all() and (net.policy["weight"] == 8).all()
