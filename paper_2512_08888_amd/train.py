@@ -172,9 +172,12 @@ class Muon(_Control):
 
 
 def sampled(logits, uniform):
-    """A label for each pixel of logits [N, K, H, W], drawn by its class probabilities with uniform numbers [N, H, W]."""
+    """A label for each pixel of logits [N, K, H, W], drawn by its class probabilities with uniform numbers [N, H, W] from 0 to below 1.
+    No class without a probability is drawn."""
     p = logits.float().softmax(1).cumsum(1)
-    return (uniform.unsqueeze(1) * p[:, -1:] > p).sum(1).clamp(max=logits.shape[1] - 1).int()
+    at = uniform.unsqueeze(1) * p[:, -1:]
+    # the classes before the one in whose share `at` lies (a product that rounds up to the whole lies in the last share that is not empty)
+    return ((at >= p) & (p < p[:, -1:])).sum(1).int()
 
 
 def main(argv=None):

@@ -1,5 +1,5 @@
-"""CPU checks of the loss in place and the recorded one (paper_2512_08888_amd/unet.py): a network without kernels, whose recording is
-replaced."""
+"""CPU checks of the loss in place and the recorded one (paper_2512_08888_amd/unet.py), by a network without kernels whose recording is
+replaced, and of the draw of labels (paper_2512_08888_amd/train.py)."""
 import contextlib
 import types
 
@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2512_08888_amd import unet
+from paper_2512_08888_amd import train, unet
 
 SHAPE, PIXELS = (2, 4, 4), 32
 
@@ -113,3 +113,21 @@ def test_a_refused_call_leaves_the_loss_in_place(bad):
     net.load_policy(**other)
     net.replay()
     assert graph.replays == 2 and (net.labels == 0).all() and (net.policy["advantage"] == 5).all() and (net.policy["weight"] == 8).all()
+
+
+def test_sampled_labels_have_a_probability():
+    """Classes of -infinity at the start, in the middle and at the end; the smallest and the largest uniform numbers."""
+    inf = float("inf")
+    logits = torch.tensor([[-inf, 0.0, 1.0, 2.0], [0.0, -inf, -inf, 1.0], [1.0, 2.0, 0.5, -inf], [-inf, -200.0, 0.0, -inf], [-inf, -inf, 3.0, -inf]])
+    uniform = torch.tensor([0.0, 2.0 ** -24, 0.2, 0.25, 0.5, 0.75, 1 - 2.0 ** -24])
+    maps = logits.t().reshape(1, 4, 5, 1).expand(1, 4, 5, 7).contiguous()
+    got = train.sampled(maps, uniform.expand(1, 5, 7).contiguous())
+    assert got.shape == (1, 5, 7) and got.dtype == torch.int32
+    p = logits.softmax(1)
+    assert (p.gather(1, got[0].long()) > 0).all()
+    # shares in 64 bits, but for numbers within rounding of a border
+    ends = logits.double().softmax(1).cumsum(1)
+    for r in range(5):
+        for k, u in enumerate(uniform.double()):
+            if (ends[r] - u).abs().min() > 1e-6:
+                assert got[0, r, k].item() == (u > ends[r]).sum().item()
