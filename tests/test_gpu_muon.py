@@ -400,3 +400,15 @@ def test_rows_of_whole_vectors_between_borders(grad, shift):
         opt.step()
         check_step(net, before, m0, net.read(net.params), cut(opt.m, stacks), lr, mu, True, 0.0, [1.0] * len(stacks), 1.0, 5)
         assert net.intact()
+
+
+def test_many_products_of_middling_matrices():
+    """90 matrices of 300 x 300: A^2 goes by tiles of 128 from 512 of them on (here 540)."""
+    stacks = [(90, 300, 300)]
+    net = Net(stacks, seed=16)
+    opt = train.Muon(net.params, net.grads, lr=0.02, scale=1.0)
+    opt.work.fill_(0xff)
+    before, m0 = net.read(net.params), cut(opt.m, stacks)
+    opt.step()
+    check_step(net, before, m0, net.read(net.params), cut(opt.m, stacks), float(np.float32(0.02)), float(np.float32(0.95)), True, 0.0, [1.0], 1.0, 5)
+    assert net.intact()
