@@ -232,8 +232,9 @@ size_t train_matrices_workspace_bytes(const train_matrices* matrices);
  *     param -= lr * weight_decay * param + lr * scale * X
  * five steps bring every singular value of u that is not vanishing beside the others to between 0.7 and 1.2.
  * momentum: fp32, train_matrices_elements(), zero before the first step.  Products multiply fp16 values (all of them bounded: see
- * the kernels) and add in fp32; X is held in 22 bits between them, and the diagonals of A and of the polynomial in 32: X's result is off by
- * some 4e-4 of its norm.  A NaN or an infinity makes its own matrix NaN.
+ * the kernels) and add in fp32; X is held in 22 bits between them, and the diagonals of A and of the polynomial in 32.  X's result is off by
+ * 2e-4 to 8e-4 of its norm for gradients of full rank, by up to 6e-3 where a few singular values are all there is (rank 1, or noise a hundredth
+ * of the rest and below).  A NaN or an infinity makes its own matrix NaN.
  * Then the control block is advanced as by train_adamw_step, unless `keep` is set: a further step that shares the block (AdamW over the
  * network's other tensors) does it.  With control->nonfinite set nothing else is changed. */
 typedef struct {

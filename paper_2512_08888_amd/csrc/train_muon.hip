@@ -10,10 +10,10 @@
 // element is larger than the largest of them.  X and A are held times 2^15, B times 2^14.  Two things keep the digits that matter:
 //   - X is held as the sum of two fp16 numbers.  The products read the upper one; the term a X, by which small singular
 //     values grow 3.4-fold an iteration, takes both.  (Else the upper's rounding grows with them: momenta of rank 16 beside noise
-//     of a tenth come out 1e-2 off, with it 2e-4.)
+//     of a tenth come out 1e-2 off, with it 4e-4.)
 //   - The diagonals of A and of the polynomial are kept in fp32 and applied by themselves: rows of gradients are nearly
 //     orthogonal, so that the diagonals are most of them, and their rounding would shift all singular values together (random
-//     256 x 1024: 1.4e-3 off, without it 5e-4).
+//     256 x 1024: 1.7e-3 off, without it 5e-4).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -37,7 +37,7 @@ constexpr int kPad = 32;               // elements: a stack's momentum starts on
 constexpr int kTile = 128;             // edge of the products' tiles
 constexpr int kSmall = 64;             // of A^2's, where tiles of 128 would leave CUs idle
 constexpr int kDepth = 64;             // elements that a step of a product adds up
-// Columns of X's tiles where its products add up kDeep steps or more on an average: fewer bytes through the caches, but fewer workgroups and
+// Columns of X's tiles where a list's products add up kDeep steps or more on an average (all of its matrices take one kind of tile, since a launch serves them): fewer bytes through the caches, but fewer workgroups and
 // larger ends.  Steps over 8 matrices of 768 x 3200 by tiles of 128 x 128 610 us, by 128 x 256 654; of 1024 x 4096 1179 and 1188; 4 of
 // 1536 x 1536 and 2 of 1536 x 6144 1373 and 1370; 8 of 2048 x 8192 6935 and 6480; 4 of 4096 x 4096 7604 and 6970.
 constexpr int kWide = 256;
