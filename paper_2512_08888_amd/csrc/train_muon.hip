@@ -37,9 +37,10 @@ constexpr int kPad = 32;               // elements: a stack's momentum starts on
 constexpr int kTile = 128;             // edge of the products' tiles
 constexpr int kSmall = 64;             // of A^2's, where tiles of 128 would leave CUs idle
 constexpr int kDepth = 64;             // elements that a step of a product adds up
-// Columns of X's tiles where a list's products add up kDeep steps or more on an average (all of its matrices take one kind of tile, since a launch serves them): fewer bytes through the caches, but fewer workgroups and
-// larger ends.  Steps over 8 matrices of 768 x 3200 by tiles of 128 x 128 610 us, by 128 x 256 654; of 1024 x 4096 1179 and 1188; 4 of
-// 1536 x 1536 and 2 of 1536 x 6144 1373 and 1370; 8 of 2048 x 8192 6935 and 6480; 4 of 4096 x 4096 7604 and 6970.
+// Columns of X's tiles where a list's products add up kDeep steps or more on an average (one launch serves all of its matrices, by one kind of
+// tile): fewer bytes through the caches, but fewer workgroups and larger ends.  Steps over 8 matrices of 768 x 3200 by tiles of 128 x 128 610 us, by
+// 128 x 256 654; of 1024 x 4096 1179 and 1188; 4 of 1536 x 1536 and 2 of 1536 x 6144 1373 and 1370; 8 of 2048 x 8192 6935 and 6480; 4 of 4096 x 4096
+// 7604 and 6970.
 constexpr int kWide = 256;
 constexpr uint32_t kDeep = 24;
 constexpr uint32_t kSlots = 512;       // workgroups of the products that the chip holds at a time
